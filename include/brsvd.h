@@ -53,8 +53,8 @@ enum { BRSVD_ORTH_AUTO = 0, BRSVD_ORTH_CHOLQR2 = 1, BRSVD_ORTH_TSQR = 2 };
 enum { BRSVD_PASSES_SEPARATE = 0, BRSVD_PASSES_FUSED = 1 };
 /* Element type of A, Omega and the results.  F32: brsvd_run and everything else.  F64 (the precision
  * the paper measures in, Sec. 4 "Experiments"): the *_f64 entry points -- the same path on the fp64
- * matrix cores. */
-enum { BRSVD_DTYPE_F32 = 0, BRSVD_DTYPE_F64 = 1 };
+ * matrix cores.  BF16, F16: matrices of a model, in the calls at the end of this header only. */
+enum { BRSVD_DTYPE_F32 = 0, BRSVD_DTYPE_F64 = 1, BRSVD_DTYPE_BF16 = 2, BRSVD_DTYPE_F16 = 3 };
 
 /* Problem statement of Alg. 1 / Alg. 2 (inputs A, k, p, q and the partition), plus where A lives and
  * how much device memory may be used (Sec. 4 "Experiment environment and setup": the block size is
@@ -234,6 +234,98 @@ int brsvd_norm2_power_f64(brsvd_handle h, const double* A, int64_t lda, const do
 
 /* Frees everything the handle owns (never the caller's buffers or workspace).  NULL is allowed. */
 int brsvd_destroy(brsvd_handle h);
+
+/* ---- A model's matrices -------------------------------------------------------------------------
+ * What stands next to the factors of a weight matrix: the remainder kept in 8 bits and multiplied, and
+ * the losses that say what a factored or 8-bit output matrix costs and repair it.  All pointers are
+ * DEVICE pointers, leading dimensions count elements, and every call is asynchronous on `stream` (a
+ * hipStream_t or NULL): results are complete when the stream is.  No call allocates, clears or copies
+ * memory by itself, so all of them can be recorded into a HIP graph.  Scratch and workspace are the
+ * caller's, 256-byte aligned, need no initialisation, and belong to the call until the stream has
+ * passed it; one too small is BRSVD_ERR_BUDGET.  Sizes may be zero where nothing else is said: an
+ * output without elements is not touched, one that is a sum of nothing is zero.  Every result repeats
+ * itself bit for bit.  Rows of operands may begin at any element; 16-byte-aligned rows (address and
+ * leading dimension) are faster.  Leading dimensions are below 2^21. */
+
+/* Numbers of 8 bits: e4m3 (OCP: four bits of exponent, three of fraction, largest 448, no infinities)
+ * times a scale in fp32 for each block.  A block is 128 neighbouring numbers of a row (block_rows = 1:
+ * S is rows x ceil(cols/128), dense), or those of 128 rows (block_rows = 128: S is ceil(rows/128) x
+ * ceil(cols/128)); blocks at the ends are smaller.
+ *
+ * brsvd_quantize_e4m3: Q = round(X / S), S the least power of two >= 2^-126 for which no finite number
+ * of the block exceeds 448 S (1 for a block of zeros), rounding to nearest even; infinities and NaN
+ * become NaN.  X: rows x cols of dtype BRSVD_DTYPE_F32, _BF16 or _F16.  Qt, St (may be NULL; so may Q,
+ * S, but not both): the same of X^T, cols x rows, whose blocks run down the columns of X.  With
+ * block_rows = 128 they hold the same numbers as Q.
+ * brsvd_dequantize_e4m3: X = Q S, rounded to dtype. */
+int brsvd_quantize_e4m3(const void* X, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype,
+                        int32_t block_rows, uint8_t* Q, int64_t ldq, float* S, uint8_t* Qt,
+                        int64_t ldqt, float* St, void* stream);
+int brsvd_dequantize_e4m3(const uint8_t* Q, int64_t ldq, const float* S, int64_t rows, int64_t cols,
+                          int32_t block_rows, int32_t dtype, void* X, int64_t ldx, void* stream);
+
+/* C (m x n, dtype F32, BF16 or F16) = A B^T with A m x k and B n x k in 8 bits; SA has a scale per row
+ * and block of A, SB per row (block_rows = 1) or 128 rows (block_rows = 128) and block of B.  Scales are
+ * any fp32 numbers, they need not come from brsvd_quantize_e4m3.  Products of a block are added, then
+ * scaled and added to those of the other blocks in fp32; C is rounded once.  With an fp32 C, or up to 64
+ * rows of A and block_rows 128, all sums are those of exact products in fp32.  Otherwise the 8-bit matrix
+ * cores add the products of a block: of eight neighbouring products they drop what is below 2^-13 of the
+ * largest one's power of two, parts of 1e-5 of the sum of |products|.
+ * The three products of a linear layer Y = X W^T with weights W: Y from X and W (block_rows 128), dX from
+ * dY and W^T (128), dW from dY^T and X^T (1), each operand cast along the contraction. */
+int brsvd_gemm_e4m3(const uint8_t* A, int64_t lda, const float* SA, const uint8_t* B, int64_t ldb,
+                    const float* SB, int32_t block_rows, int64_t m, int64_t n, int64_t k, int32_t dtype,
+                    void* C, int64_t ldc, void* scratch, uint64_t scratch_bytes, void* stream);
+uint64_t brsvd_gemm_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t block_rows,
+                                       int32_t dtype);
+
+/* Y (m x n) = X W^T with X m x k of dtype F32, BF16 or F16 (Y has the same type) cast as by
+ * brsvd_quantize_e4m3 with block_rows = 1, and W n x k in 8 bits with a scale per 128 x 128 block. */
+int brsvd_linear_e4m3(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw,
+                      const float* SW, int64_t m, int64_t n, int64_t k, void* Y, int64_t ldy,
+                      void* scratch, uint64_t scratch_bytes, void* stream);
+uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t dtype);
+
+/* Softmax cross entropy of z = H W^T (H tokens x dim hidden states, W vocab x dim output matrix, both of
+ * dtype BF16 or F16), per token, without keeping z:
+ *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_{t, labels_t}
+ * A label outside [0, vocab) marks a token that does not count: its loss is 0.  loss, lse: fp32.
+ * Backward, for the gradient of sum_t grad_t loss_t, from the lse of the forward call:
+ *   G_tv = grad_t (exp(z_tv - lse_t) - [v = labels_t]),   dH = G W,   dW = G^T H      (of dtype)
+ * Rows of dH of tokens that do not count are 0, and what stands in those rows of H reaches nothing, NaN
+ * and infinities included.  grad_stride: 1, or 0 for one factor for all tokens.  dH or dW may be NULL.
+ * G is formed in 16 bits for `piece` rows of W at a time (0: so many that it takes up to 256 MiB of the
+ * workspace; otherwise rounded down to a multiple of 256, at least 256), dH is added up in fp32.
+ * With no tokens dW is 0.
+ * workspace: at least brsvd_head_workspace_bytes of the same sizes (forward: piece 0; top 0). */
+int brsvd_xent_forward(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,
+                       int64_t tokens, int64_t vocab, int64_t dim, int32_t dtype, float* loss, float* lse,
+                       void* workspace, uint64_t workspace_bytes, void* stream);
+int brsvd_xent_backward(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,
+                        const float* lse, const float* grad, int64_t grad_stride, int64_t tokens,
+                        int64_t vocab, int64_t dim, int64_t piece, int32_t dtype, void* dH, int64_t lddh,
+                        void* dW, int64_t lddw, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Distillation from the `top` logits that were kept of a teacher, temperature tau > 0:
+ *   q_t = softmax(logits_t / tau) over the listed entries,  lse_t = log sum_v exp(z_tv / tau)
+ *   loss_t = tau^2 sum_j q_tj (log q_tj - z_{t, ids_tj} / tau + lse_t)
+ *   G_tv = grad_t tau (exp(z_tv / tau - lse_t) - sum over j with ids_tj = v of q_tj)
+ * ids, logits (fp32): tokens x top, dense.  An entry with an id outside [0, vocab) or a logit of -inf or
+ * NaN is not listed; a token with nothing listed does not count.  z (fp32, tokens x top, OUT of the
+ * forward and input of the backward call): z_{t, ids_tj}, 0 where not listed.  The rest as above, with
+ * `top` in brsvd_head_workspace_bytes. */
+int brsvd_distill_forward(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* ids,
+                          const float* logits, int32_t top, float temperature, int64_t tokens,
+                          int64_t vocab, int64_t dim, int32_t dtype, float* loss, float* lse, float* z,
+                          void* workspace, uint64_t workspace_bytes, void* stream);
+int brsvd_distill_backward(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* ids,
+                           const float* logits, int32_t top, float temperature, const float* lse,
+                           const float* z, const float* grad, int64_t grad_stride, int64_t tokens,
+                           int64_t vocab, int64_t dim, int64_t piece, int32_t dtype, void* dH,
+                           int64_t lddh, void* dW, int64_t lddw, void* workspace,
+                           uint64_t workspace_bytes, void* stream);
+uint64_t brsvd_head_workspace_bytes(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece,
+                                    int32_t top, int32_t backward);
 
 /* Static, NUL-terminated description of a status code. */
 const char* brsvd_status_string(int status);

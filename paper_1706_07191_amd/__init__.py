@@ -30,6 +30,8 @@ BRSVD_PASSES_SEPARATE = 0
 BRSVD_PASSES_FUSED = 1
 BRSVD_DTYPE_F32 = 0
 BRSVD_DTYPE_F64 = 1
+BRSVD_DTYPE_BF16 = 2
+BRSVD_DTYPE_F16 = 3
 
 
 class brsvd_params(C.Structure):
@@ -63,6 +65,9 @@ class brsvd_stats(C.Structure):
 EXPORTS = ["brsvd_workspace_bytes", "brsvd_create", "brsvd_run", "brsvd_run_f64", "brsvd_rpca_ialm",
            "brsvd_rpca_ialm_tol", "brsvd_rpca_ialm_tol_f64", "brsvd_norm2_power", "brsvd_norm2_power_f64",
            "brsvd_run_alg2", "brsvd_run_alg2_f64", "brsvd_philox_normal", "brsvd_philox_normal_f64",
+           "brsvd_quantize_e4m3", "brsvd_dequantize_e4m3", "brsvd_gemm_e4m3", "brsvd_gemm_e4m3_scratch_bytes",
+           "brsvd_linear_e4m3", "brsvd_linear_e4m3_scratch_bytes", "brsvd_xent_forward", "brsvd_xent_backward",
+           "brsvd_distill_forward", "brsvd_distill_backward", "brsvd_head_workspace_bytes",
            "brsvd_destroy", "brsvd_status_string"]
 STEP_EXPORTS = ["brsvd_gemm_an", "brsvd_gemm_at", "brsvd_gemm_scratch_bytes", "brsvd_gemm_an_f64",
                 "brsvd_gemm_at_f64", "brsvd_gemm_scratch_bytes_f64", "brsvd_orth", "brsvd_orth_scratch_bytes",
@@ -122,8 +127,21 @@ def lib() -> C.CDLL:
     L.brsvd_small_svd.argtypes = [vp, i32, vp, vp, vp, C.POINTER(i32), vp, u64, vp]
     L.brsvd_small_svd_scratch_bytes.argtypes = [i32]
     L.brsvd_small_svd_static.argtypes = [vp, i32, vp, vp, vp, C.POINTER(i32), vp]
+    L.brsvd_quantize_e4m3.argtypes = [vp, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp]
+    L.brsvd_dequantize_e4m3.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, i64, vp]
+    L.brsvd_gemm_e4m3.argtypes = [vp, i64, vp, vp, i64, vp, i32, i64, i64, i64, i32, vp, i64, vp, u64, vp]
+    L.brsvd_gemm_e4m3_scratch_bytes.argtypes = [i64, i64, i64, i32, i32]
+    L.brsvd_linear_e4m3.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp, i64, vp, u64, vp]
+    L.brsvd_linear_e4m3_scratch_bytes.argtypes = [i64, i64, i64, i32]
+    L.brsvd_xent_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i32, vp, vp, vp, u64, vp]
+    L.brsvd_xent_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, i32, vp, i64, vp, i64, vp, u64, vp]
+    L.brsvd_distill_forward.argtypes = [vp, i64, vp, i64, vp, vp, i32, flt, i64, i64, i64, i32, vp, vp, vp, vp, u64, vp]
+    L.brsvd_distill_backward.argtypes = [vp, i64, vp, i64, vp, vp, i32, flt, vp, vp, vp, i64, i64, i64, i64, i64, i32, vp, i64,
+                                         vp, i64, vp, u64, vp]
+    L.brsvd_head_workspace_bytes.argtypes = [i64, i64, i64, i64, i32, i32]
     sizes = ("brsvd_gemm_scratch_bytes", "brsvd_gemm_scratch_bytes_f64", "brsvd_orth_scratch_bytes",
-             "brsvd_small_svd_scratch_bytes")
+             "brsvd_small_svd_scratch_bytes", "brsvd_gemm_e4m3_scratch_bytes", "brsvd_linear_e4m3_scratch_bytes",
+             "brsvd_head_workspace_bytes")
     for name in EXPORTS + STEP_EXPORTS:
         if name in sizes:
             getattr(L, name).restype = u64
@@ -410,6 +428,268 @@ def brsvd_small_svd(R, stream=None, out=None, static=False):
 
 def brsvd_small_svd_static(R, stream=None, out=None):
     return brsvd_small_svd(R, stream=stream, out=out, static=True)
+
+
+# ---- a model's matrices: 8-bit products and losses over a large vocabulary -----------------------------------------
+# Every call takes stream= (a torch stream or its address; default: torch's current stream), on which it runs and allocates.
+
+def _model_dtype(dtype, name, half=False):
+    import torch
+    types = {torch.bfloat16: BRSVD_DTYPE_BF16, torch.float16: BRSVD_DTYPE_F16}
+    if not half:
+        types[torch.float32] = BRSVD_DTYPE_F32
+    if dtype not in types:
+        raise TypeError(f"{name} must be of dtype {' or '.join(str(t) for t in types)}, not {dtype}")
+    return types[dtype]
+
+
+def _rows(t, dtype, shape, name):
+    """(address, leading dimension) of a CUDA matrix with neighbouring elements in a row; shape: None where any size will do."""
+    import torch
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2):
+        raise TypeError(f"{name} must be a 2-d CUDA tensor of dtype {dtype}")
+    if any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise TypeError(f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if s is None else s for s in shape)}")
+    rows, cols = t.shape
+    if rows and cols and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols)):
+        raise TypeError(f"{name} must have unit column stride and rows that do not overlap")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(cols, 1))
+
+
+def _scope(stream):
+    """Memory taken inside belongs to the stream that the call runs on: what a call frees at its end, or the caller later, is not handed out
+    to work of another stream before the call is through with it."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+def _scoped(call):
+    """Runs a binding with `stream` as torch's current stream."""
+    import functools
+
+    @functools.wraps(call)
+    def wrapped(*args, stream=None, **kw):
+        with _scope(stream):
+            return call(*args, **kw)
+    return wrapped
+
+
+def _blocks(n):
+    return -(-n // 128)
+
+
+def _scales(S, rows, cols, block_rows, name):
+    import torch
+    shape = (rows if block_rows == 1 else _blocks(rows), _blocks(cols))
+    if tuple(S.shape) != shape:
+        raise TypeError(f"{name} has shape {tuple(S.shape)}, expected {shape}")
+    return _dev(S, torch.float32, name)
+
+
+def _eight_bit(rows, cols, device):
+    """rows x cols numbers of 8 bits in rows of whole 16 bytes, which the products read fastest."""
+    import torch
+    return torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+
+
+@_scoped
+def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
+    """X (rows, cols) CUDA, fp32, bf16 or fp16, as e4m3 numbers Q (float8_e4m3fn, rows 16-byte aligned) and power-of-two
+    scales S, one for each 128 numbers of a row (block_rows=1) or each 128 x 128 block (block_rows=128).  Returns (Q, S), with
+    transpose=True (Q, S, Qt, St), the last two those of X^T."""
+    import torch
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    dt = _model_dtype(X.dtype, "X")
+    x, ldx = _rows(X, X.dtype, (None, None), "X")
+    rows, cols = X.shape
+    dev = X.device
+
+    def result(r, c):
+        return _eight_bit(r, c, dev), torch.empty(r if block_rows == 1 else _blocks(r), _blocks(c), device=dev)
+    Q, S = result(rows, cols)
+    Qt, St = result(cols, rows) if transpose else (None, None)
+    _check(lib().brsvd_quantize_e4m3(x, ldx, rows, cols, dt, block_rows, Q.data_ptr(), -(-cols // 16) * 16, S.data_ptr(),
+                                     Qt.data_ptr() if transpose else None, -(-rows // 16) * 16 if transpose else 0,
+                                     St.data_ptr() if transpose else None, _stream_ptr(None)), "brsvd_quantize_e4m3")
+    return (Q, S, Qt, St) if transpose else (Q, S)
+
+
+@_scoped
+def brsvd_dequantize_e4m3(Q, S, block_rows=1, dtype=None):
+    """What Q with its scales stands for, as fp32 (or bf16, fp16: dtype)."""
+    import torch
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    dtype = dtype or torch.float32
+    dt = _model_dtype(dtype, "the result")
+    q, ldq = _rows(Q, torch.float8_e4m3fn, (None, None), "Q")
+    rows, cols = Q.shape
+    X = torch.empty(rows, cols, dtype=dtype, device=Q.device)
+    _check(lib().brsvd_dequantize_e4m3(q, ldq, _scales(S, rows, cols, block_rows, "S"), rows, cols, block_rows, dt,
+                                       X.data_ptr(), max(cols, 1), _stream_ptr(None)), "brsvd_dequantize_e4m3")
+    return X
+
+
+@_scoped
+def brsvd_gemm_e4m3(A, SA, Bm, SB, block_rows=128, dtype=None, out=None):
+    """A Bm^T of 8-bit matrices A (m, k) with a scale per row and 128 numbers and Bm (n, k) with one per 128 x 128 block, or
+    with block_rows=1 like A's.  The result is bf16 unless dtype says fp32 or fp16; out: write it there."""
+    import torch
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
+    a, lda = _rows(A, torch.float8_e4m3fn, (None, None), "A")
+    m, k = A.shape
+    b, ldb = _rows(Bm, torch.float8_e4m3fn, (None, k), "Bm")
+    n = Bm.shape[0]
+    sa, sb = _scales(SA, m, k, 1, "SA"), _scales(SB, n, k, block_rows, "SB")
+    dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
+    dt = _model_dtype(dtype, "the result")
+    Cm = torch.empty(m, n, dtype=dtype, device=A.device) if out is None else out
+    c, ldc = _rows(Cm, dtype, (m, n), "out")
+    nbytes = lib().brsvd_gemm_e4m3_scratch_bytes(m, n, k, block_rows, dt)
+    scr = _byte_scratch(nbytes, A.device) if nbytes else None
+    _check(lib().brsvd_gemm_e4m3(a, lda, sa, b, ldb, sb, block_rows, m, n, k, dt, c, ldc,
+                                 scr.data_ptr() if nbytes else None, nbytes, _stream_ptr(None)), "brsvd_gemm_e4m3")
+    return Cm
+
+
+@_scoped
+def brsvd_linear_e4m3(X, W, SW, out=None):
+    """X W^T: X (m, k) fp32, bf16 or fp16 is cast into 8 bits by rows of 128 on the way, W (n, k) is in 8 bits with a scale
+    for each 128 x 128 block.  The result has X's type."""
+    import torch
+    dt = _model_dtype(X.dtype, "X")
+    x, ldx = _rows(X, X.dtype, (None, None), "X")
+    m, k = X.shape
+    w, ldw = _rows(W, torch.float8_e4m3fn, (None, k), "W")
+    n = W.shape[0]
+    sw = _scales(SW, n, k, 128, "SW")
+    Y = torch.empty(m, n, dtype=X.dtype, device=X.device) if out is None else out
+    y, ldy = _rows(Y, X.dtype, (m, n), "out")
+    nbytes = lib().brsvd_linear_e4m3_scratch_bytes(m, n, k, dt)
+    scr = _byte_scratch(nbytes, X.device) if nbytes else None
+    _check(lib().brsvd_linear_e4m3(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes,
+                                   _stream_ptr(None)), "brsvd_linear_e4m3")
+    return Y
+
+
+def _head(H, W):
+    dt = _model_dtype(H.dtype, "H", half=True)
+    h, ldh = _rows(H, H.dtype, (None, None), "H")
+    w, ldw = _rows(W, H.dtype, (None, H.shape[1]), "W")
+    return (h, ldh, w, ldw), (H.shape[0], W.shape[0], H.shape[1]), dt
+
+
+def _vector(t, dtype, n, name):
+    if tuple(t.shape) != (n,):
+        raise TypeError(f"{name} has shape {tuple(t.shape)}, expected {(n,)}")
+    return _dev(t, dtype, name)
+
+
+def _factors(grad, tokens):
+    """(tensor, address, stride) of a factor for each token: a number, a tensor with one for all (also expanded) or one for each."""
+    import torch
+    if not isinstance(grad, torch.Tensor):
+        raise TypeError("grad must be a CUDA tensor of dtype torch.float32")
+    if grad.dtype != torch.float32 or not grad.is_cuda:
+        raise TypeError("grad must be a CUDA tensor of dtype torch.float32")
+    if grad.numel() != 1 and tuple(grad.shape) != (tokens,):
+        raise TypeError(f"grad has shape {tuple(grad.shape)}, expected one number or {(tokens,)}")
+    if grad.numel() == 1:
+        return grad, grad.data_ptr(), 0
+    if grad.stride(0) < 0:
+        grad = grad.contiguous()
+    return grad, grad.data_ptr(), grad.stride(0)
+
+
+def _head_workspace(sizes, piece, top, backward, device):
+    nbytes = lib().brsvd_head_workspace_bytes(*sizes, piece, top, backward)
+    return _byte_scratch(nbytes, device), nbytes
+
+
+@_scoped
+def brsvd_xent_forward(H, W, labels):
+    """Softmax cross entropy of the logits H W^T (H (tokens, dim), W (vocab, dim), bf16 or fp16) per token, without the
+    logits: returns (loss, lse), fp32.  labels: int64, one outside [0, vocab) marks a token that does not count (loss 0)."""
+    import torch
+    ops, sizes, dt = _head(H, W)
+    y = _vector(labels, torch.int64, sizes[0], "labels")
+    loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
+    ws, nbytes = _head_workspace(sizes, 0, 0, 0, H.device)
+    _check(lib().brsvd_xent_forward(*ops, y, *sizes, dt, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes,
+                                    _stream_ptr(None)), "brsvd_xent_forward")
+    return loss, lse
+
+
+def _gradients(H, W, need_dH, need_dW):
+    import torch
+    if not (need_dH or need_dW):
+        raise ValueError("neither gradient is wanted")
+    dH = torch.empty(H.shape, dtype=H.dtype, device=H.device) if need_dH else None
+    dW = torch.empty(W.shape, dtype=W.dtype, device=W.device) if need_dW else None
+    d = max(H.shape[1], 1)
+    return dH, dW, (dH.data_ptr() if need_dH else None, d, dW.data_ptr() if need_dW else None, d)
+
+
+@_scoped
+def brsvd_xent_backward(H, W, labels, lse, grad, need_dH=True, need_dW=True, piece=0):
+    """Gradients (dH, dW) of sum_t grad_t loss_t, from the lse of the forward call; None for one that is not needed.  grad:
+    fp32 tensor with a factor for each token or one for all.  piece: rows of W taken at a time (0: by the memory they need)."""
+    import torch
+    ops, sizes, dt = _head(H, W)
+    y, l = _vector(labels, torch.int64, sizes[0], "labels"), _vector(lse, torch.float32, sizes[0], "lse")
+    keep, g, stride = _factors(grad, sizes[0])
+    dH, dW, outs = _gradients(H, W, need_dH, need_dW)
+    ws, nbytes = _head_workspace(sizes, piece, 0, 1, H.device)
+    _check(lib().brsvd_xent_backward(*ops, y, l, g, stride, *sizes, piece, dt, *outs, ws.data_ptr(), nbytes,
+                                     _stream_ptr(None)), "brsvd_xent_backward")
+    return dH, dW
+
+
+def _teacher(ids, logits, tokens):
+    import torch
+    if ids.dim() != 2 or ids.shape[0] != tokens or ids.shape[1] < 1 or ids.shape != logits.shape:
+        raise TypeError(f"ids and logits must have shape (tokens, top), not {tuple(ids.shape)} and {tuple(logits.shape)}")
+    return (_dev(ids, torch.int64, "ids"), _dev(logits, torch.float32, "logits"), ids.shape[1])
+
+
+@_scoped
+def brsvd_distill_forward(H, W, ids, logits, temperature=1.0):
+    """tau^2 KL(q || p) per token of the student's p = softmax(H W^T / tau) against the teacher's q, the softmax of its `top`
+    kept logits / tau: ids int64, logits fp32, both (tokens, top); an entry with an id outside [0, vocab) or a logit of -inf
+    does not count.  Returns (loss, lse, z), fp32: z (tokens, top) holds the student's logits of those words."""
+    import torch
+    ops, sizes, dt = _head(H, W)
+    te = _teacher(ids, logits, sizes[0])
+    loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
+    z = torch.empty(ids.shape, device=H.device)
+    ws, nbytes = _head_workspace(sizes, 0, te[2], 0, H.device)
+    _check(lib().brsvd_distill_forward(*ops, *te, temperature, *sizes, dt, loss.data_ptr(), lse.data_ptr(), z.data_ptr(),
+                                       ws.data_ptr(), nbytes, _stream_ptr(None)), "brsvd_distill_forward")
+    return loss, lse, z
+
+
+@_scoped
+def brsvd_distill_backward(H, W, ids, logits, temperature, lse, z, grad, need_dH=True, need_dW=True, piece=0):
+    """Gradients (dH, dW) of sum_t grad_t loss_t from the lse and z of the forward call; the rest as brsvd_xent_backward."""
+    import torch
+    ops, sizes, dt = _head(H, W)
+    te = _teacher(ids, logits, sizes[0])
+    l = _vector(lse, torch.float32, sizes[0], "lse")
+    if z.shape != ids.shape:
+        raise TypeError(f"z has shape {tuple(z.shape)}, expected {tuple(ids.shape)}")
+    keep, g, stride = _factors(grad, sizes[0])
+    dH, dW, outs = _gradients(H, W, need_dH, need_dW)
+    ws, nbytes = _head_workspace(sizes, piece, te[2], 1, H.device)
+    _check(lib().brsvd_distill_backward(*ops, *te, temperature, l, _dev(z, torch.float32, "z"), g, stride, *sizes, piece, dt,
+                                        *outs, ws.data_ptr(), nbytes, _stream_ptr(None)), "brsvd_distill_backward")
+    return dH, dW
 
 
 class PinnedMatrix:

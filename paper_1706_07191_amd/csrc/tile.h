@@ -1,0 +1,305 @@
+// Tile products on the 16-bit and 8-bit matrix cores (gfx950), shared by the 8-bit products and the losses over a vocabulary.
+//
+// A workgroup of WP x WQ waves works out D (BP x BQ) = P Q^T over a contraction of K numbers; a wave has NP x NQ tiles of 16 x 16.  In the
+// instruction's result a lane holds four consecutive rows (of P) of one column (of Q), so P is the side along which the output is
+// contiguous in memory: it is stored four numbers at a time.
+//
+// A step of the contraction takes 128 bytes of every row of P and Q (64 numbers of 16 bits, 128 of 8) into LDS, straight from memory
+// (global_load_lds, 16 bytes a lane) into one of two buffers while the other is multiplied; one barrier a step.  An operand is
+//   kRows: its rows hold the contraction, [rows][K].  A tile is [rows][128 bytes] in LDS, the 16-byte pieces of row r at piece ^ (r & 7): the 16
+//          rows that a fragment is read from then lie in different banks.
+//   kCols: the contraction runs down its rows, [K][cols] (16-bit numbers).  A tile is [64][cols]; fragments come out transposed
+//          (ds_read_b64_tr_b16), pieces of 32 bytes are exchanged by a function of the row for the same reason.
+// Rows and columns beyond the operand's end are read from inside it and dropped at the store; numbers of the contraction beyond K are zero on
+// both sides: a piece that straddles an end is put together number by number.  DIRECT = false: for operands whose rows do not begin at 16-byte
+// addresses; all pieces pass through registers.
+#pragma once
+#include "common.h"
+
+namespace brsvd {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Element types of the operands.
+struct Bf16 { static constexpr int kBytes = 2; };
+struct Fp16 { static constexpr int kBytes = 2; };
+struct E4m3 { static constexpr int kBytes = 1; };
+
+constexpr int kStepBytes = 128;          // of the contraction per step
+constexpr int64_t kMaxGrid = (int64_t)1 << 30;   // workgroups of a launch
+enum Order { kRows = 0, kCols = 1 };
+
+// One operand as a kernel gets it.
+struct Operand {
+  const char* base;
+  int64_t ld;       // bytes from one stored row to the next
+  int64_t n;        // rows (kRows) or columns (kCols) of the output that it spans
+};
+
+// Whether the pieces of 16 bytes that an operand's rows are read in lie at 16-byte addresses.
+inline bool aligned_pieces(const void* base, int64_t ld_bytes) { return (uintptr_t)base % 16 == 0 && ld_bytes % 16 == 0; }
+// Bytes between rows up to which a tile's pieces are addressed with 32 bits.
+constexpr int64_t kMaxPitch = (int64_t)1 << 22;
+
+struct __attribute__((packed, aligned(1))) Piece { uint32_t x[4]; };
+static __device__ const uint4 k_zero_piece = {0u, 0u, 0u, 0u};
+
+// 16 bytes per lane from `src` into LDS at `dst` (the same in all lanes) + 16 lane.  Written out so that the compiler does not hold back reads of the
+// other buffer until it is done: loads_done() before the barrier that hands the buffer over is the wait for it.
+__device__ __forceinline__ void load_to_lds(uint32_t dst, const char* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const lds_char*)p; }
+
+// 16 bytes from `src`, of which the first `valid` are there; the others are zero.
+template <int EB>
+__device__ __forceinline__ uint4 piece_of(const char* src, int64_t valid) {
+  if (valid >= 16) {
+    const Piece v = *(const Piece*)src;
+    return make_uint4(v.x[0], v.x[1], v.x[2], v.x[3]);
+  }
+  uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+  for (int at = 0; at < (int)valid; at += EB) {
+    const uint64_t e = EB == 1 ? (uint64_t) * (const uint8_t*)(src + at) : EB == 2 ? (uint64_t) * (const uint16_t*)(src + at) : (uint64_t) * (const uint32_t*)(src + at);
+    if (at < 8) lo |= e << (8 * at);
+    else hi |= e << (8 * at - 64);
+  }
+  return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+// The part of a workgroup that fills the LDS tile of one operand: N rows (columns) of the output, THREADS threads.
+template <class El, Order O, int N, int THREADS, bool DIRECT>
+struct Stager {
+  static constexpr int kPieces = N * (kStepBytes / 16), kLoads = kPieces / THREADS;
+  static constexpr int kPerRow = O == kRows ? kStepBytes / 16 : N * 2 / 16;      // pieces per row of the tile in LDS
+  static constexpr int kStepK = kStepBytes / El::kBytes;
+  static_assert(kPieces % THREADS == 0 && (O == kRows || El::kBytes == 2), "");
+  uint32_t off[kLoads];      // from `at`
+  const char* at;            // of this step, the same in all lanes
+  int64_t step;
+  int32_t valid[O == kRows ? 1 : kLoads];   // kCols: bytes of the piece inside the columns
+  bool ragged = false;                       // kCols: the columns end inside one of the tile's pieces
+  uint4 reg[DIRECT ? 1 : kLoads];
+
+  // first: the output row (column) that the tile begins with; k0: the number of the contraction that it begins with
+  __device__ __forceinline__ void init(const Operand& op, int64_t first, int64_t k0, int tid) {
+    const int64_t left = op.n - first;
+    if (O == kRows) {
+      at = op.base + first * op.ld + k0 * El::kBytes;
+      step = kStepBytes;
+    } else {
+      at = op.base + k0 * op.ld + first * 2;
+      step = (int64_t)kStepK * op.ld;
+      ragged = left < N && left % 8 != 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int slot = i * THREADS + tid, row = slot / kPerRow, pc = slot % kPerRow;
+      if (O == kRows) {
+        const int src = pc ^ (row & 7);
+        const int64_t r = row < left ? row : left - 1;
+        off[i] = (uint32_t)(r * op.ld + 16 * src);
+      } else {
+        const int src = ((pc >> 1) ^ (mix(row) & (kPerRow / 2 - 1))) * 2 + (pc & 1);
+        const int64_t c = 8 * src < left ? 8 * src : 0;      // a piece beyond the end: some other one, nothing of it is stored
+        off[i] = (uint32_t)((int64_t)row * op.ld + 2 * c);
+        valid[i] = (int32_t)(left - c >= 8 ? 16 : 2 * (left - c));
+      }
+    }
+  }
+  // rows of a kCols tile whose pieces of one column would lie in the same banks, told apart: a fragment is read from rows 8 g + i, g, i < 4
+  static __device__ __forceinline__ int mix(int row) { return (row & 3) | ((row >> 3) & 3) << 2; }
+
+  // left: numbers of the contraction from this step on
+  __device__ __forceinline__ void load(char* tile, int tid, int wave, int64_t left) {
+    const uint32_t dst = lds_address(tile);
+    if (DIRECT && left >= kStepK && !ragged) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load_to_lds(dst + 16 * (i * THREADS + 64 * wave), at + off[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int slot = i * THREADS + tid, kpos = O == kRows ? ((slot % kPerRow) ^ (slot / kPerRow & 7)) * 16 : slot / kPerRow;
+        const int64_t there = O == kRows ? left * El::kBytes - kpos : (kpos < left ? valid[O == kRows ? 0 : i] : 0);
+        if (!DIRECT) reg[i] = piece_of<El::kBytes>(at + off[i], there);
+        else if (there >= 16 || there <= 0) load_to_lds(dst + 16 * (i * THREADS + 64 * wave), there > 0 ? at + off[i] : (const char*)&k_zero_piece);
+        else *(uint4*)(tile + 16 * slot) = piece_of<El::kBytes>(at + off[i], there);
+      }
+    }
+    at += step;
+  }
+  __device__ __forceinline__ void store(char* tile, int tid) {
+    if (!DIRECT)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) *(uint4*)(tile + 16 * (i * THREADS + tid)) = reg[i];
+  }
+};
+
+// Fragments of 16 rows (columns) from `row` on: 16 bytes a lane of the half-step kk (kStepBytes / 2 of the contraction).
+template <Order O, int N>
+__device__ __forceinline__ int4v fragment(const char* tile, int row, int kk, int lane) {
+  if (O == kRows) {
+    const int r = row + (lane & 15), pc = (kk * 4 + (lane >> 4)) ^ (lane & 7);      // row is a multiple of 16
+    return *(const int4v*)(tile + r * kStepBytes + pc * 16);
+  } else {
+    const int g = lane >> 4, i = lane & 15, k = kk * 32 + 8 * g + (i >> 2);
+    const int pair = (row >> 4) ^ (((i >> 2) | g << 2) & (N / 16 - 1));
+    const char* at = tile + k * (N * 2) + pair * 32 + (i & 3) * 8;
+    typedef __attribute__((address_space(3))) short4v lds_short4;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)at);
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at + 4 * N * 2));
+    const short8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(int4v, both);
+  }
+}
+
+// Has a sum worked out here: left alone, the compiler puts the additions of a whole step behind its products and keeps all of them in registers.
+__device__ __forceinline__ void settle(floatx4& x) { asm volatile("" : "+v"(x)); }
+
+template <class El>
+__device__ __forceinline__ floatx4 mfma16(int4v p, int4v q, floatx4 c) {
+  if constexpr (__is_same(El, Bf16)) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p), __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, p), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
+}
+// 128 numbers of 8 bits; any order of them that both sides share will do
+__device__ __forceinline__ floatx4 mfma8(int4v p0, int4v p1, int4v q0, int4v q1, floatx4 c) {
+  const int8v p = {p0[0], p0[1], p0[2], p0[3], p1[0], p1[1], p1[2], p1[3]}, q = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 0, 0, 0, 0, 0, 0);
+}
+
+// The same through fp16, which holds every e4m3 number: products exact, sums in fp32.  mfma8 keeps less: of eight neighbouring products the instruction
+// cuts off what is below 2^-13 of the largest (measured; sums of different eights keep 24 bits).
+struct Wide8 { f16x8 x[4]; };
+__device__ __forceinline__ Wide8 widen(int4v p0, int4v p1) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  Wide8 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int a = i < 2 ? p0[2 * i] : p1[2 * i - 4], b = i < 2 ? p0[2 * i + 1] : p1[2 * i - 3];
+    const f16x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false), v1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true);
+    const f16x2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false), v3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true);
+    w.x[i] = f16x8{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+  }
+  return w;
+}
+__device__ __forceinline__ floatx4 mfma_wide(const Wide8& p, const Wide8& q) {
+  floatx4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(p.x[i], q.x[i], c, 0, 0, 0);
+  return c;
+}
+
+// What a tile product of 16-bit numbers is made of.  EXACT: every step's sum starts from zero and is added in rounded fp32 (the instruction truncates;
+// over a long contraction that is a bias); otherwise the sum runs through the instructions.
+template <class El, int NP_, int NQ_, int WP_, int WQ_, Order OP, Order OQ, bool DIRECT, bool EXACT>
+struct TileProduct {
+  static constexpr int NP = NP_, NQ = NQ_, WP = WP_, WQ = WQ_;
+  static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
+  static constexpr int kLds = 2 * (BP + BQ) * kStepBytes, kStepK = kStepBytes / El::kBytes;
+
+  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
+    constexpr int kHalf = (BP + BQ) * kStepBytes;
+    Stager<El, OP, BP, kThreads, DIRECT> sp;
+    Stager<El, OQ, BQ, kThreads, DIRECT> sq;
+    sp.init(P, p0, k0, tid);
+    sq.init(Q, q0, k0, tid);
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int steps = (int)((k1 - k0 + kStepK - 1) / kStepK);
+    sp.load(lds, tid, wave, k1 - k0);
+    sq.load(lds + BP * kStepBytes, tid, wave, k1 - k0);
+    sp.store(lds, tid);
+    sq.store(lds + BP * kStepBytes, tid);
+    loads_done();
+    __syncthreads();
+    for (int t = 0; t < steps; ++t) {
+      const int cur = (t & 1) * kHalf, nxt = kHalf - cur;
+      if (t + 1 < steps) {
+        const int64_t left = k1 - k0 - (int64_t)(t + 1) * kStepK;
+        sp.load(lds + nxt, tid, wave, left);
+        sq.load(lds + nxt + BP * kStepBytes, tid, wave, left);
+      }
+      const char *tp = lds + cur, *tq = tp + BP * kStepBytes;
+      int4v fq[2][NQ];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) fq[kk][q] = fragment<OQ, BQ>(tq, 16 * (wq * NQ + q), kk, lane);
+      int4v f0 = fragment<OP, BP>(tp, 16 * wp * NP, 0, lane), f1 = fragment<OP, BP>(tp, 16 * wp * NP, 1, lane);
+      floatx4 d[2][NQ];
+      // The fragments of the next tile row are on their way while this one is multiplied (and with EXACT a sum is added once the products of the next
+      // tile row are issued); the fences keep the compiler from fetching all rows at once, which it has no registers for.
+#pragma unroll
+      for (int p = 0; p < NP + (EXACT ? 1 : 0); ++p) {
+        if (p < NP) {
+          const int4v c0 = f0, c1 = f1;
+          if (p + 1 < NP) {
+            f0 = fragment<OP, BP>(tp, 16 * (wp * NP + p + 1), 0, lane);
+            f1 = fragment<OP, BP>(tp, 16 * (wp * NP + p + 1), 1, lane);
+          }
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            if (EXACT) d[p & 1][q] = mfma16<El>(c0, fq[0][q], floatx4{0.f, 0.f, 0.f, 0.f});
+            else acc[p][q] = mfma16<El>(c0, fq[0][q], acc[p][q]);
+          }
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            if (EXACT) d[p & 1][q] = mfma16<El>(c1, fq[1][q], d[p & 1][q]);
+            else acc[p][q] = mfma16<El>(c1, fq[1][q], acc[p][q]);
+          }
+        }
+        if (EXACT && p > 0) {
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[p - 1][q][r] += d[(p - 1) & 1][q][r];
+            settle(acc[p - 1][q]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!DIRECT && t + 1 < steps) {
+        sp.store(lds + nxt, tid);
+        sq.store(lds + nxt + BP * kStepBytes, tid);
+      }
+      loads_done();
+      __syncthreads();
+    }
+  }
+};
+
+// 16-bit numbers from fp32, to the nearest
+template <class El> __device__ __forceinline__ uint16_t to16(float x) {
+  if constexpr (__is_same(El, Bf16)) { const __bf16 h = (__bf16)x; return __builtin_bit_cast(uint16_t, h); }
+  else { const _Float16 h = (_Float16)x; return __builtin_bit_cast(uint16_t, h); }
+}
+template <class El> __device__ __forceinline__ float from16(uint16_t x) {
+  if constexpr (__is_same(El, Bf16)) return __builtin_bit_cast(float, (uint32_t)x << 16);
+  else return (float)__builtin_bit_cast(_Float16, x);
+}
+
+// Tiles of a np x nq grid (np along P) to workgroups: workgroups b, b + 8, b + 16 ... share an XCD and its L2, so each XCD gets a run of tiles, and a run
+// goes through `band` rows of the grid at a time.  Returns false for workgroups beyond the grid (the grid is rounded up to eight).
+__device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np, int64_t nq, int band, int64_t* tp, int64_t* tq) {
+  const int64_t all = np * nq, per = (all + 7) / 8, i = (int64_t)(b & 7) * per + (b >> 3);
+  if ((b >> 3) >= per || i >= all) return false;
+  const int64_t group = i / (band * nq), first = group * band, height = np - first < band ? np - first : band, in = i - group * band * nq;
+  *tp = first + in % height;
+  *tq = in / height;
+  return true;
+}
+inline unsigned tile_workgroups(int64_t np, int64_t nq) { return (unsigned)(8 * ((np * nq + 7) / 8)); }
+
+}  // namespace brsvd

@@ -1,0 +1,276 @@
+"""8-bit numbers with block scales: casting and back against the definition in 64 bits to the bit, products against the values that the
+numbers stand for, at the edges of blocks and tiles, for rows at any alignment and outputs of every type."""
+import itertools
+
+import pytest
+import torch
+
+import paper_1706_07191_amd as B
+from tests.gpu_util import need_gpu
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+# unit roundoff: half a step relative to the lower end of a binade
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def randn(seed, *shape):
+    g = torch.Generator(device="cpu")
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, dtype=torch.float64)
+
+
+def e4m3_values():
+    """The 256 numbers by their definition: sign, four bits of exponent with bias 7, three of fraction, NaN for all ones."""
+    v = []
+    for b in range(256):
+        e, m = b >> 3 & 15, b & 7
+        x = float("nan") if e == 15 and m == 7 else (m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7))
+        v.append(-x if b & 128 else x)
+    return torch.tensor(v, dtype=torch.float64)
+
+
+def cast_by_definition(x, block):
+    """x (fp64): the nearest of the 256 numbers (the even fraction where two are as near) of x / s, and s: loops over the blocks."""
+    rows, cols = x.shape
+    values = e4m3_values()[:127]                     # 0 ... 448
+    nr, nc = -(-rows // block), -(-cols // 128)
+    q, s = torch.zeros(rows, cols, dtype=torch.int64), torch.zeros(nr, nc, dtype=torch.float64)
+    for i, j in itertools.product(range(nr), range(nc)):
+        part = x[i * block:(i + 1) * block, j * 128:(j + 1) * 128]
+        finite = part[torch.isfinite(part)].abs()
+        top = float(finite.max()) if finite.numel() else 0.0
+        e = 0
+        if top > 0:
+            e = -126
+            while top > 448 * 2.0 ** e:
+                e += 1
+        s[i, j] = 2.0 ** e
+        u = (part / s[i, j]).abs()
+        d = (u.nan_to_num(0.0, 0.0)[..., None] - values).abs()
+        near = d.min(dim=-1, keepdim=True).values
+        tie = (d == near) * (2 - torch.arange(127) % 2)          # an even code counts more
+        code = tie.argmax(dim=-1)
+        code = torch.where(torch.isfinite(part), code + 128 * torch.signbit(part), 127)
+        q[i * block:(i + 1) * block, j * 128:(j + 1) * 128] = code
+    return q, s
+
+
+def codes(q):
+    c = q.contiguous().view(torch.uint8).long().cpu()
+    return torch.where((c & 127) == 127, 127, c)      # any NaN
+
+
+def placed(x, dtype, dev, pad, shift):
+    """x on the device with `pad` more elements a row than it has and the first one `shift` elements behind a 16-byte address."""
+    rows, cols = x.shape
+    flat = torch.full((rows * (cols + pad) + shift + 8,), 7.0, device=dev).to(dtype)
+    view = flat[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    view.copy_(x.to(dtype))
+    return view
+
+
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad,shift", [(1, 1, 0, 0), (1, 128, 0, 0), (3, 127, 1, 0), (128, 128, 0, 0), (129, 257, 0, 1), (127, 300, 4, 3),
+                                                 (260, 8, 8, 0), (2, 1000, 0, 0)])
+def test_cast_and_back(rows, cols, pad, shift, dtype, block):
+    dev = need_gpu()
+    x = randn(rows * 1000 + cols, rows, cols) * torch.exp2(torch.randint(-9, 9, (rows, cols), generator=torch.Generator().manual_seed(1)).double())
+    X = placed(x, dtype, dev, pad, shift)
+    Q, S, Qt, St = B.brsvd_quantize_e4m3(X, block_rows=block, transpose=True)
+    q, s = cast_by_definition(X.double().cpu(), block)
+    assert torch.equal(codes(Q), q) and torch.equal(S.double().cpu(), s)
+    qt, st = cast_by_definition(X.double().cpu().t().contiguous(), block)
+    assert torch.equal(codes(Qt), qt) and torch.equal(St.double().cpu(), st)
+    Q1, S1 = B.brsvd_quantize_e4m3(X, block_rows=block)
+    assert torch.equal(codes(Q1), q) and torch.equal(S1, S)
+    value = e4m3_values()[q] * s.repeat_interleave(block, 0)[:rows].repeat_interleave(128, 1)[:, :cols]
+    for out in TYPES:
+        assert torch.equal(B.brsvd_dequantize_e4m3(Q, S, block_rows=block, dtype=out).cpu(), value.to(out))
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_cast_of_every_pattern_of_16_bits(block):
+    """All bf16 numbers, infinities and NaN among them: what is not finite becomes NaN and leaves the scale alone."""
+    dev = need_gpu()
+    X = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(256, 256)
+    X = X[torch.randperm(256, generator=torch.Generator().manual_seed(2))]
+    Q, S, Qt, St = B.brsvd_quantize_e4m3(X.to(dev), block_rows=block, transpose=True)
+    q, s = cast_by_definition(X.double(), block)
+    assert torch.equal(codes(Q), q) and torch.equal(S.double().cpu(), s)
+    qt, st = cast_by_definition(X.double().t().contiguous(), block)
+    assert torch.equal(codes(Qt), qt) and torch.equal(St.double().cpu(), st)
+
+
+def test_cast_of_blocks_of_zeros_and_tiny_numbers():
+    dev = need_gpu()
+    X = torch.zeros(4, 256)
+    X[1, :128] = 1e-42
+    X[2, 130] = 3.4e38
+    X[3, 0], X[3, 1], X[3, 128] = float("inf"), 2.0, float("nan")
+    Q, S = B.brsvd_quantize_e4m3(X.to(dev))
+    q, s = cast_by_definition(X.double(), 1)
+    assert torch.equal(codes(Q), q) and torch.equal(S.double().cpu(), s)
+    assert S[0, 0] == 1 and S[3, 1] == 1
+
+
+def eight_bits(seed, rows, cols, block, dev, pad=0):
+    """Random 8-bit numbers in rows of cols + pad bytes with random scales, not powers of two, and the values they stand for."""
+    g = torch.Generator(device="cpu")
+    g.manual_seed(seed)
+    store = (torch.randn(rows, cols + pad, generator=g) * 20).to(torch.float8_e4m3fn).to(dev)
+    q = store[:, :cols]
+    s = torch.rand(rows if block == 1 else -(-rows // 128), -(-cols // 128), generator=g) + 0.1
+    value = q.float().double().cpu() * s.double().repeat_interleave(block, 0)[:rows].repeat_interleave(128, 1)[:, :cols]
+    return q, s.to(dev), value
+
+
+def check_product(got, a, b, dtype):
+    """Each result within a bound that holds for sums in any order: products of 8-bit numbers are exact in fp32, the 128 additions of a block and those
+    of the blocks lose at most a step each (not rounded but cut off), three scalings, and the rounding to the result's type.
+    A result of 16 bits may come from the 8-bit matrix cores: of eight products next to each other they keep 13 bits behind the largest one's power of two;
+    each of the other seven loses less than 2^-13 of the largest, which is no more than the sum of the eight."""
+    want, size = a @ b.t(), a.abs() @ b.abs().t()
+    k = a.shape[1]
+    bound = size * (2.0 ** -23 * (min(k, 128) + -(-k // 128) + 4) + (0.0 if dtype == torch.float32 else 7 * 2.0 ** -13))
+    bound = bound + ROUND[dtype] * (want.abs() + bound) + (2.0 ** -25 if dtype == torch.float16 else 0.0)
+    err = (got.double().cpu() - want).abs()
+    assert bool((err <= bound).all()), float((err / bound.clamp(min=1e-300)).max())
+
+
+@pytest.mark.parametrize("block", [128, 1])
+@pytest.mark.parametrize("m,n,k,pad_a,pad_b", [
+    (1, 1, 1, 0, 0), (1, 16, 16, 0, 0), (2, 3, 129, 0, 0), (15, 130, 128, 0, 0), (16, 300, 127, 1, 0), (17, 257, 300, 0, 4), (33, 64, 1000, 8, 8),
+    (64, 129, 2000, 0, 0), (65, 128, 256, 0, 0), (66, 257, 15, 1, 1), (100, 300, 4000, 0, 0), (128, 512, 144, 0, 0), (129, 256, 640, 0, 0),
+    (257, 513, 129, 0, 0), (300, 70, 1001, 7, 15), (513, 300, 1008, 8, 16)])
+def test_product(m, n, k, pad_a, pad_b, block):
+    dev = need_gpu()
+    qa, sa, a = eight_bits(m + 7 * k, m, k, 1, dev, pad_a)
+    qb, sb, b = eight_bits(n + 3 * k, n, k, block, dev, pad_b)
+    for dtype in TYPES:
+        check_product(B.brsvd_gemm_e4m3(qa, sa, qb, sb, block_rows=block, dtype=dtype), a, b, dtype)
+    wide = torch.full((m, n + 3), 5.0, device=dev)
+    out = B.brsvd_gemm_e4m3(qa, sa, qb, sb, block_rows=block, out=wide[:, 1:n + 1])
+    check_product(out, a, b, torch.float32)
+    assert bool((wide[:, 0] == 5).all() and (wide[:, n + 1:] == 5).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 200), (70, 260, 200), (300, 300, 520)])
+def test_product_of_whole_numbers_is_exact(m, n, k):
+    """Sums below 2^24 of whole numbers with scales of one have one answer, whatever the order: any index that is off shows."""
+    dev = need_gpu()
+    g = torch.Generator().manual_seed(m)
+    a, b = (torch.randint(-8, 9, (r, k), generator=g).float() for r in (m, n))
+    one = lambda r: torch.ones(r, -(-k // 128), device=dev)  # noqa: E731
+    qa, qb = a.to(dev).to(torch.float8_e4m3fn), b.to(dev).to(torch.float8_e4m3fn)
+    for block in (1, 128):
+        got = B.brsvd_gemm_e4m3(qa, one(m), qb, one(n if block == 1 else -(-n // 128)), block_rows=block, dtype=torch.float32)
+        assert torch.equal(got.cpu(), a @ b.t())
+
+
+def test_product_keeps_nan_in_its_row_and_column():
+    dev = need_gpu()
+    for m in (20, 100, 300):
+        qa, sa, _ = eight_bits(1, m, 300, 1, dev)
+        qb, sb, _ = eight_bits(2, 290, 300, 128, dev)
+        clean = B.brsvd_gemm_e4m3(qa, sa, qb, sb, dtype=torch.float32)
+        sa[m - 1, 2], bad = float("inf"), qb.clone()
+        bad[289, 299] = float("nan")
+        got = B.brsvd_gemm_e4m3(qa, sa, bad, sb, dtype=torch.float32)
+        assert torch.equal(got[:m - 1, :289], clean[:m - 1, :289])
+        assert not bool(torch.isfinite(got[m - 1]).any()) and bool(torch.isnan(got[:, 289]).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(1, 300, 500), (9, 64, 129), (40, 1000, 256), (64, 20, 4100), (65, 300, 500), (200, 260, 1000)])
+def test_linear_is_the_cast_and_the_product(m, n, k, dtype):
+    """Both ways give the same bits: a row is cast the same wherever it is done, and the product runs in the same order."""
+    dev = need_gpu()
+    X = placed(randn(m, m, k) * 3, dtype, dev, 3, 1)
+    W, SW = B.brsvd_quantize_e4m3(randn(n, n, k).float().to(dev), block_rows=128)
+    Q, S = B.brsvd_quantize_e4m3(X)
+    want = B.brsvd_gemm_e4m3(Q, S, W, SW, dtype=dtype)
+    assert torch.equal(B.brsvd_linear_e4m3(X, W, SW), want)
+    check_product(want, B.brsvd_dequantize_e4m3(Q, S).double().cpu(), B.brsvd_dequantize_e4m3(W, SW, block_rows=128).double().cpu(), dtype)
+
+
+def test_linear_with_numbers_that_are_not_finite():
+    dev = need_gpu()
+    W, SW = B.brsvd_quantize_e4m3(randn(5, 140, 300).float().to(dev), block_rows=128)
+    for m in (3, 90):
+        X = randn(4, m, 300).float().to(dev)
+        want = B.brsvd_linear_e4m3(X, W, SW)
+        X[1, 140], X[2, 7] = float("inf"), float("nan")
+        got = B.brsvd_linear_e4m3(X, W, SW)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[3:], want[3:]) and bool(torch.isnan(got[1:3]).all())
+
+
+def test_sizes_of_zero():
+    dev = need_gpu()
+    for rows, cols in ((0, 5), (5, 0)):
+        Q, S = B.brsvd_quantize_e4m3(torch.empty(rows, cols, device=dev))
+        assert tuple(Q.shape) == (rows, cols) and B.brsvd_dequantize_e4m3(Q, S).shape == Q.shape
+    q, s, _ = eight_bits(1, 4, 0, 1, dev)
+    for block, rows in ((128, 1), (1, 6)):
+        got = B.brsvd_gemm_e4m3(q, s, eight_bits(2, 6, 0, 1, dev)[0], torch.empty(rows, 0, device=dev), block_rows=block)
+        assert tuple(got.shape) == (4, 6) and not bool(got.any())
+    W, SW = B.brsvd_quantize_e4m3(torch.ones(6, 20, device=dev), block_rows=128)
+    assert tuple(B.brsvd_linear_e4m3(torch.empty(0, 20, device=dev), W, SW).shape) == (0, 6)
+
+
+def test_offsets_beyond_32_bits():
+    """A matrix of more than 2^32 bytes: the last rows are cast as they are alone, and multiplied."""
+    dev = need_gpu()
+    rows, cols = 70000, 65536
+    X = torch.zeros(rows, cols, dtype=torch.bfloat16, device=dev)
+    tail = randn(3, 300, cols).to(torch.bfloat16).to(dev)
+    X[-300:] = tail
+    Q, S = B.brsvd_quantize_e4m3(X)
+    del X
+    q, s = B.brsvd_quantize_e4m3(tail)
+    assert torch.equal(codes(Q[-300:]), codes(q)) and torch.equal(S[-300:], s)
+    a, sa = B.brsvd_quantize_e4m3(randn(4, 300, cols).float().to(dev))
+    for m in (4, 300):
+        got = B.brsvd_gemm_e4m3(a[:m], sa[:m], Q, S, block_rows=1)
+        check_product(got[:, -300:], B.brsvd_dequantize_e4m3(a[:m], sa[:m]).double().cpu(), B.brsvd_dequantize_e4m3(q, s).double().cpu(), torch.bfloat16)
+        assert not bool(got[:, :-300].any())
+
+
+def test_repeats_itself_in_graphs_and_on_other_streams():
+    dev = need_gpu()
+    X = randn(8, 300, 700).to(torch.bfloat16).to(dev)
+    W, SW = B.brsvd_quantize_e4m3(randn(9, 400, 700).float().to(dev), block_rows=128)
+    want, few = B.brsvd_linear_e4m3(X, W, SW), B.brsvd_linear_e4m3(X[:5], W, SW)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = B.brsvd_linear_e4m3(X, W, SW, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    x = X.clone()
+    with torch.cuda.graph(graph):
+        y, z = B.brsvd_linear_e4m3(x, W, SW), B.brsvd_linear_e4m3(x[:5], W, SW)
+    for i in range(4):
+        x.copy_(X * (1 if i % 2 == 0 else -1))
+        graph.replay()
+        torch.cuda.synchronize()
+        sign = 1 if i % 2 == 0 else -1
+        assert torch.equal(y, sign * want) and torch.equal(z, sign * few)
+        torch.randn(1000, 1000, device=dev).sum().item()
+
+
+def test_refusals():
+    dev = need_gpu()
+    X = torch.ones(4, 256, device=dev)
+    Q, S = B.brsvd_quantize_e4m3(X)
+    for call in (lambda: B.brsvd_quantize_e4m3(X.double()), lambda: B.brsvd_quantize_e4m3(X.cpu()), lambda: B.brsvd_quantize_e4m3(X.t()),
+                 lambda: B.brsvd_quantize_e4m3(X[0]), lambda: B.brsvd_gemm_e4m3(Q, S, Q[:, :128], S[:, :1]), lambda: B.brsvd_gemm_e4m3(Q, S[:2], Q, S),
+                 lambda: B.brsvd_gemm_e4m3(Q, S, Q, S), lambda: B.brsvd_linear_e4m3(X, X, S), lambda: B.brsvd_dequantize_e4m3(X, S),
+                 lambda: B.brsvd_gemm_e4m3(Q, S, Q, S, block_rows=1, out=torch.empty(4, 5, device=dev)),
+                 lambda: B.brsvd_dequantize_e4m3(Q, S.double()), lambda: B.brsvd_gemm_e4m3(Q, S, Q, S, block_rows=1, dtype=torch.float64)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: B.brsvd_quantize_e4m3(X, block_rows=64), lambda: B.brsvd_gemm_e4m3(Q, S, Q, S, block_rows=2)):
+        with pytest.raises(ValueError):
+            call()
