@@ -7,75 +7,93 @@
 
 namespace brsvd {
 
-// Eight numbers of a row from `src` on, of which `valid` are there.
+// How a workgroup of 256 threads lies over a 128 x 128 part: a thread has 16 bytes (kWide numbers) of each of kRows rows that follow each other, so
+// that 16 (fp32: 32) lanes read a row's 128 numbers as one piece of memory, and the kRows numbers of a column in a thread are neighbours in the
+// transpose.
+template <int DT> struct Part {
+  static constexpr int kBytes = DT == BRSVD_DTYPE_F32 ? 4 : 2, kWide = 16 / kBytes, kLanes = kBlock / kWide, kRows = kBlock / (256 / kLanes);
+};
+
+// The numbers of 16 bytes from `src` on, of which `valid` are there.
 template <int DT>
-__device__ __forceinline__ void eight(const char* src, int valid, float (&x)[8]) {
-  constexpr int EB = DT == BRSVD_DTYPE_F32 ? 4 : 2;
-  if (valid >= 8) {
-    uint32_t w[2 * EB];
+__device__ __forceinline__ void numbers(const char* src, int valid, float (&x)[Part<DT>::kWide]) {
+  constexpr int EB = Part<DT>::kBytes;
+  const uint4 v = piece_of<EB>(src, valid * EB);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < EB / 2; ++i) {
-      const Piece v = *(const Piece*)(src + 16 * i);
+  for (int i = 0; i < Part<DT>::kWide; ++i)
+    x[i] = EB == 4 ? __uint_as_float(w[EB == 4 ? i : 0])
+                   : DT == BRSVD_DTYPE_BF16 ? from16<Bf16>((uint16_t)(w[i / 2] >> (16 * (i & 1)))) : from16<Fp16>((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+}
+
+// N bytes to memory at any address, of which `valid` are wanted
+template <int N>
+__device__ __forceinline__ void put_bytes(void* dst, int valid, const uint32_t (&v)[N / 4]) {
+  struct __attribute__((packed, aligned(1))) Bytes { uint32_t x[N / 4]; };
+  if (valid >= N) {
+    Bytes b;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[4 * i + j] = v.x[j];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = DT == BRSVD_DTYPE_F32 ? __uint_as_float(w[EB == 4 ? i : 0])
-             : DT == BRSVD_DTYPE_BF16 ? from16<Bf16>((uint16_t)(w[i / 2] >> (16 * (i & 1)))) : from16<Fp16>((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+    for (int i = 0; i < N / 4; ++i) b.x[i] = v[i];
+    *(Bytes*)dst = b;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = i >= valid ? 0.f : DT == BRSVD_DTYPE_F32 ? ((const float*)src)[i]
-             : DT == BRSVD_DTYPE_BF16 ? from16<Bf16>(((const uint16_t*)src)[i]) : from16<Fp16>(((const uint16_t*)src)[i]);
+    for (int i = 0; i < N; ++i)
+      if (i < valid) ((uint8_t*)dst)[i] = (uint8_t)(v[i / 4] >> (8 * (i & 3)));
   }
 }
 
-// Up to eight bytes to a row of numbers of 8 bits
-__device__ __forceinline__ void put_eight(uint8_t* dst, int valid, uint2 v) {
-  if (valid >= 8 && ((uintptr_t)dst & 7) == 0) *(uint2*)dst = v;
-  else
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < valid) dst[i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
+// Largest of 16 neighbouring lanes, in all of them (rotations inside a row of 16: no LDS)
+__device__ __forceinline__ float max16(float x) {
+#define BRSVD_ROTATED_MAX(N) x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true)))
+  BRSVD_ROTATED_MAX(8);
+  BRSVD_ROTATED_MAX(4);
+  BRSVD_ROTATED_MAX(2);
+  BRSVD_ROTATED_MAX(1);
+#undef BRSVD_ROTATED_MAX
+  return x;
 }
 
-// One workgroup per 128 x 128 part: lane group of 16 per row, eight numbers a lane, 16 rows of the workgroup at a time.  Bound by memory: what it reads and
-// writes once.
+// One workgroup per 128 x 128 part.  Bound by memory: what it reads and writes once.  The transpose goes through LDS in words of a thread's kRows
+// numbers of a column, word g of column c at g ^ (c / kWide): the lanes that write, and those that read, then lie in different banks.
 template <int DT, bool SQUARE, bool STRAIGHT, bool TRANSPOSED>
 __global__ void __launch_bounds__(256)
 k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S,
            uint8_t* __restrict__ Qt, int64_t ldqt, float* __restrict__ St) {
-  constexpr int EB = DT == BRSVD_DTYPE_F32 ? 4 : 2;
+  using P = Part<DT>;
+  constexpr int W = P::kWide, R = P::kRows, L = P::kLanes, GROUPS = kBlock / R;
   __shared__ float top[4][kBlock];
-  __shared__ __attribute__((aligned(16))) uint8_t turned[TRANSPOSED ? kBlock : 1][kBlock + 16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = (tid & 15) * 8, r = tid >> 4;
+  __shared__ __attribute__((aligned(16))) uint8_t turned[TRANSPOSED ? kBlock * kBlock : 16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid % L, c = cg * W, g = tid / L;
   const int64_t ncb = (cols + kBlock - 1) / kBlock, nrb = (rows + kBlock - 1) / kBlock;
   const int64_t rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, row0 = rb * kBlock, col0 = cb * kBlock;
-  const int width = (int)(cols - col0 - c < 8 ? (cols - col0 - c > 0 ? cols - col0 - c : 0) : 8);
-  float x[8][8], rowtop[8];
+  const int width = (int)(cols - col0 - c < W ? (cols - col0 - c > 0 ? cols - col0 - c : 0) : W);
+  float x[R][W];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t row = row0 + r + 16 * i;
-    eight<DT>(X + row * ldx + (col0 + c) * EB, row < rows ? width : 0, x[i]);
+  for (int i = 0; i < R; ++i) {
+    const int64_t row = row0 + g * R + i;
+    numbers<DT>(X + row * ldx + (col0 + c) * P::kBytes, row < rows ? width : 0, x[i]);
   }
+  float rowtop[R], all = 0.f;
+  if (STRAIGHT || SQUARE) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float t = 0.f;
+    for (int i = 0; i < R; ++i) {
+      float t = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t = fmaxf(t, finite_abs(x[i][j]));
-#pragma unroll
-    for (int s = 1; s < 16; s <<= 1) t = fmaxf(t, __shfl_xor(t, s));
-    rowtop[i] = t;
+      for (int j = 0; j < W; ++j) t = fmaxf(t, finite_abs(x[i][j]));
+      if (SQUARE) all = fmaxf(all, t);
+      else {
+        t = max16(t);
+        if (L == 32) t = fmaxf(t, __shfl_xor(t, 16));
+      }
+      rowtop[i] = t;
+    }
   }
   int e_square = 0;
   if (SQUARE) {
-    float t = rowtop[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) t = fmaxf(t, rowtop[i]);
-    t = fmaxf(t, __shfl_xor(t, 16));
-    t = fmaxf(t, __shfl_xor(t, 32));
-    if (lane == 0) top[wave][0] = t;
+    all = max16(all);
+    all = fmaxf(all, __shfl_xor(all, 16));
+    all = fmaxf(all, __shfl_xor(all, 32));
+    if (lane == 0) top[wave][0] = all;
     __syncthreads();
     e_square = block_exponent(fmaxf(fmaxf(top[0][0], top[1][0]), fmaxf(top[2][0], top[3][0])));
     if (tid == 0 && STRAIGHT) S[rb * ncb + cb] = power_of_two(e_square);
@@ -83,113 +101,125 @@ k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, 
   }
   if (STRAIGHT) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = row0 + r + 16 * i;
+    for (int i = 0; i < R; ++i) {
+      const int64_t row = row0 + g * R + i;
       const int e = SQUARE ? e_square : block_exponent(rowtop[i]);
       const float f = power_of_two(-e);
-      const uint2 v = make_uint2(pack_e4m3(x[i][0] * f, x[i][1] * f, x[i][2] * f, x[i][3] * f), pack_e4m3(x[i][4] * f, x[i][5] * f, x[i][6] * f, x[i][7] * f));
+      uint32_t v[W / 4];
+#pragma unroll
+      for (int j = 0; j < W; j += 4) v[j / 4] = pack_e4m3(x[i][j] * f, x[i][j + 1] * f, x[i][j + 2] * f, x[i][j + 3] * f);
       if (row < rows) {
-        put_eight(Q + row * ldq + col0 + c, width, v);
-        if (!SQUARE && (tid & 15) == 0) S[row * ncb + cb] = power_of_two(e);
+        put_bytes<W>(Q + row * ldq + col0 + c, width, v);
+        if (!SQUARE && cg == 0) S[row * ncb + cb] = power_of_two(e);
       }
     }
   }
   if (TRANSPOSED) {
-    float f[8];
+    float f[W];
     if (!SQUARE) {
-      float t[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        t[j] = 0.f;
+      for (int j = 0; j < W; ++j) {
+        float t = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[j] = fmaxf(t[j], finite_abs(x[i][j]));
-        t[j] = fmaxf(t[j], __shfl_xor(t[j], 16));
-        t[j] = fmaxf(t[j], __shfl_xor(t[j], 32));
-        if (lane < 16) top[wave][c + j] = t[j];
+        for (int i = 0; i < R; ++i) t = fmaxf(t, finite_abs(x[i][j]));
+        if (L == 16) t = fmaxf(t, __shfl_xor(t, 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        if (lane < L) top[wave][c + j] = t;
       }
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < W; ++j) {
         const int e = block_exponent(fmaxf(fmaxf(top[0][c + j], top[1][c + j]), fmaxf(top[2][c + j], top[3][c + j])));
         f[j] = power_of_two(-e);
-        if (r == 0 && j < width) St[(col0 + c + j) * nrb + rb] = power_of_two(e);
+        if (g == 0 && j < width) St[(col0 + c + j) * nrb + rb] = power_of_two(e);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = power_of_two(-e_square);
+      for (int j = 0; j < W; ++j) f[j] = power_of_two(-e_square);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int j = 0; j < W; ++j) {
+      uint32_t v[R / 4];
 #pragma unroll
-      for (int j = 0; j < 8; j += 4) {
-        const uint32_t v = pack_e4m3(x[i][j] * f[j], x[i][j + 1] * f[j + 1], x[i][j + 2] * f[j + 2], x[i][j + 3] * f[j + 3]);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) turned[c + j + b][r + 16 * i] = (uint8_t)(v >> (8 * b));
-      }
+      for (int i = 0; i < R; i += 4) v[i / 4] = pack_e4m3(x[i][j] * f[j], x[i + 1][j] * f[j], x[i + 2][j] * f[j], x[i + 3][j] * f[j]);
+      uint8_t* at = turned + (c + j) * kBlock + R * (g ^ (cg & (GROUPS - 1)));
+      if (R == 16) *(uint4*)at = make_uint4(v[0], v[1], v[R / 4 - 2], v[R / 4 - 1]);
+      else *(uint2*)at = make_uint2(v[0], v[1]);
     }
     __syncthreads();
-    const int height = (int)(rows - row0 - c < 8 ? (rows - row0 - c > 0 ? rows - row0 - c : 0) : 8);
+    // eight threads a column, 16 bytes each
+    const int part = tid & 7;
+    const int height = (int)(rows - row0 - 16 * part < 16 ? rows - row0 - 16 * part : 16);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t col = col0 + r + 16 * i;
-      if (col < cols) put_eight(Qt + col * ldqt + row0 + c, height, *(const uint2*)&turned[r + 16 * i][c]);
+    for (int i = 0; i < 4; ++i) {
+      const int cc = (tid >> 3) + 32 * i, mix = cc / W & (GROUPS - 1);
+      if (col0 + cc >= cols || height <= 0) continue;
+      const uint8_t* at = turned + cc * kBlock;
+      uint32_t v[4];
+      if (R == 16) {
+        const uint4 w = *(const uint4*)(at + 16 * (part ^ mix));
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+      } else {
+        const uint2 lo = *(const uint2*)(at + 8 * ((2 * part) ^ mix)), hi = *(const uint2*)(at + 8 * ((2 * part + 1) ^ mix));
+        v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
+      }
+      put_bytes<16>(Qt + (col0 + cc) * ldqt + row0 + 16 * part, height, v);
     }
   }
 }
 
-// X = Q * S, a lane takes eight numbers of a row.
+// X = Q * S: a thread writes 16 bytes of X at a time, neighbouring lanes neighbouring pieces.
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_dequantize(const uint8_t* __restrict__ Q, int64_t ldq, const float* __restrict__ S, int64_t rows, int64_t cols, int block_rows, char* __restrict__ X, int64_t ldx) {
-  const int c = (threadIdx.x & 15) * 8, r = threadIdx.x >> 4;
-  const int64_t ncb = (cols + kBlock - 1) / kBlock, rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, col = cb * kBlock + c;
-  const int width = (int)(cols - col < 8 ? cols - col : 8);
+  using P = Part<DT>;
+  constexpr int W = P::kWide, R = P::kRows, STEP = 256 / P::kLanes;
+  const int c = (int)(threadIdx.x % P::kLanes) * W, r = threadIdx.x / P::kLanes;
+  const int64_t ncb = (cols + kBlock - 1) / kBlock, rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, col = cb * kBlock + c, row0 = rb * kBlock + r;
+  const int width = (int)(cols - col < W ? cols - col : W);
   if (width <= 0) return;
+  uint32_t w[R][W / 4];
+  float f[R];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t row = rb * kBlock + r + 16 * i;
-    if (row >= rows) return;
+  for (int i = 0; i < R; ++i) {
+    const int64_t row = row0 + STEP * i;
+    if (row >= rows) continue;
     const uint8_t* src = Q + row * ldq + col;
-    const float f = S[(block_rows == 1 ? row : row / kBlock) * ncb + cb];
-    uint32_t w[2] = {0u, 0u};
-    if (width == 8) {
-      struct __attribute__((packed, aligned(1))) Two { uint32_t x[2]; };
-      const Two v = *(const Two*)src;
-      w[0] = v.x[0];
-      w[1] = v.x[1];
+    f[i] = S[(block_rows == 1 ? row : rb) * ncb + cb];
+    struct __attribute__((packed, aligned(1))) Bytes { uint32_t x[W / 4]; };
+    if (width == W) {
+      const Bytes v = *(const Bytes*)src;
+#pragma unroll
+      for (int j = 0; j < W / 4; ++j) w[i][j] = v.x[j];
     } else {
-      for (int j = 0; j < width; ++j) w[j / 4] |= (uint32_t)src[j] << (8 * (j & 3));
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        if (j % 4 == 0) w[i][j / 4] = 0;
+        if (j < width) w[i][j / 4] |= (uint32_t)src[j] << (8 * (j & 3));
+      }
     }
-    float x[8];
+  }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
-      x[4 * j] = lo[0] * f;
-      x[4 * j + 1] = lo[1] * f;
-      x[4 * j + 2] = hi[0] * f;
-      x[4 * j + 3] = hi[1] * f;
+  for (int i = 0; i < R; ++i) {
+    const int64_t row = row0 + STEP * i;
+    if (row >= rows) continue;
+    float x[W];
+#pragma unroll
+    for (int j = 0; j < W / 4; ++j) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i][j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i][j], true);
+      x[4 * j] = lo[0] * f[i];
+      x[4 * j + 1] = lo[1] * f[i];
+      x[4 * j + 2] = hi[0] * f[i];
+      x[4 * j + 3] = hi[1] * f[i];
     }
-    if (DT == BRSVD_DTYPE_F32) {
-      float* out = (float*)(X + row * ldx) + col;
-      if (width == 8 && ((uintptr_t)out & 15) == 0) {
-        ((floatx4*)out)[0] = floatx4{x[0], x[1], x[2], x[3]};
-        ((floatx4*)out)[1] = floatx4{x[4], x[5], x[6], x[7]};
-      } else
+    uint32_t v[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < width) out[j] = x[j];
-    } else {
-      uint16_t* out = (uint16_t*)(X + row * ldx) + col;
-      uint16_t h[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = DT == BRSVD_DTYPE_BF16 ? to16<Bf16>(x[j]) : to16<Fp16>(x[j]);
-      if (width == 8 && ((uintptr_t)out & 15) == 0)
-        *(uint4*)out = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < width) out[j] = h[j];
+    for (int j = 0; j < 4; ++j) {
+      if (DT == BRSVD_DTYPE_F32) v[j] = __float_as_uint(x[W == 4 ? j : 0]);
+      else if (DT == BRSVD_DTYPE_BF16) v[j] = to16<Bf16>(x[W == 8 ? 2 * j : 0]) | (uint32_t)to16<Bf16>(x[W == 8 ? 2 * j + 1 : 0]) << 16;
+      else v[j] = to16<Fp16>(x[W == 8 ? 2 * j : 0]) | (uint32_t)to16<Fp16>(x[W == 8 ? 2 * j + 1 : 0]) << 16;
     }
+    put_bytes<16>(X + row * ldx + col * P::kBytes, width * P::kBytes, v);
   }
 }
 
