@@ -187,11 +187,11 @@ k_join_splits(const float* __restrict__ part, int splits, int64_t m, int64_t n, 
   put_four(C, row * ldc + col, n - col, dtype, sum);
 }
 
-// Up to 16 MT rows of A.  A wave has 16 NT rows of B and every 16th... block of the contraction; the waves of a workgroup share the rows of B and split the
+// Up to 16 MT rows of A.  A wave has 16 NT rows of B and every eighth block of the contraction: the waves of a workgroup share the rows of B and split the
 // contraction, their sums are added through LDS in wave order.  B goes from memory to the instruction's registers (a lane: 16 bytes at two places of a
-// row's block); so does A, which all workgroups read and the caches hold.  CAST: A comes in numbers of more bits, and a block of it is cast where it is
-// used, in registers: four lanes hold a row's block, its largest number takes two exchanges.
-template <int MT, int NT, int DT>     // DT: type of A's numbers, -1: 8 bits with scales
+// row's block), the U blocks that a wave takes next at once; so does A, which all workgroups read and the caches hold.  DT >= 0: A comes in numbers of more
+// bits, and a block of it is cast where it is used, in registers: four lanes hold a row's block, its largest number takes two exchanges.
+template <int MT, int NT, int U, int DT>     // DT: type of A's numbers, -1: 8 bits with scales
 __global__ void __launch_bounds__(512)
 k_rows_e4m3(const E4m3Args g) {
   constexpr int WAVES = 8;
@@ -207,12 +207,11 @@ k_rows_e4m3(const E4m3Args g) {
 #pragma unroll
     for (int u = 0; u < NT; ++u) acc[t][u] = floatx4{0.f, 0.f, 0.f, 0.f};
   const char* rb[NT];
-  const float* sb[NT];
+  const float* sb = g.SB + n0 / kBlock * g.blocks;        // 16 NT rows from a multiple of 16 NT on: one row of scales
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     const int64_t n = n0 + 16 * u + row, in = n < g.B.n ? n : g.B.n - 1;
     rb[u] = g.B.base + in * g.B.ld + piece;
-    sb[u] = g.SB + (n0 + 16 * u < g.B.n ? (n0 + 16 * u) / kBlock : 0) * g.blocks;
   }
   const char* ra[MT];
   const float* sa[MT];
@@ -222,84 +221,106 @@ k_rows_e4m3(const E4m3Args g) {
     ra[t] = g.A.base + m * g.A.ld + piece * EB;
     sa[t] = CAST ? nullptr : g.SA + m * g.blocks;
   }
-  const int b0 = blockIdx.y * g.per_split, b1 = b0 + g.per_split < g.blocks ? b0 + g.per_split : g.blocks;
-  for (int b = b0 + wave; b < b1; b += WAVES) {
-    const int64_t at = (int64_t)b * kBlock, left = g.k - at - piece;
-    Wide8 ew[NT];
+  // what a lane has of a block: [piece at 0, piece at 64]
+  struct Block {
+    uint4 b[NT][2], a[MT][2 * EB];
+    float sb, sa[MT];
+  };
+  auto fetch = [&](Block& x, int blk, bool whole, int64_t left) {       // left: numbers of the row from this lane's first piece on
+    const int64_t at = (int64_t)blk * kBlock;
 #pragma unroll
-    for (int u = 0; u < NT; ++u) {
-      int4v e[2];
+    for (int u = 0; u < NT; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint4 v = piece_of<1>(rb[u] + at + 64 * h, left - 64 * h);
-        e[h] = int4v{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
-      }
-      ew[u] = widen(e[0], e[1]);
-    }
+      for (int h = 0; h < 2; ++h) x.b[u][h] = piece_of<1>(rb[u] + at + 64 * h, whole ? 16 : left - 64 * h);
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      int4v f[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < EB; ++j) x.a[t][h * EB + j] = piece_of<EB>(ra[t] + (at + 64 * h) * EB + 16 * j, whole ? 16 : (left - 64 * h) * EB - 16 * j);
+      if (!CAST) x.sa[t] = sa[t][blk];
+    }
+    x.sb = sb[blk];
+  };
+  auto multiply = [&](const Block& x) {
+    Wide8 ew[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) ew[u] = widen(__builtin_bit_cast(int4v, x.b[u][0]), __builtin_bit_cast(int4v, x.b[u][1]));
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      Wide8 fw;
       float s;
       if constexpr (CAST) {
-        float x[2][16], top = 0.f;
+        float v[2][16], top = 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int j = 0; j < 16 * EB; j += 16) {
-            const uint4 v = piece_of<EB>(ra[t] + (at + 64 * h) * EB + j, (left - 64 * h) * EB - j);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          for (int j = 0; j < EB; ++j) {
+            const uint4 p = x.a[t][h * EB + j];
+            const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
             for (int i = 0; i < 16 / EB; ++i)
-              x[h][j / EB + i] = DT == BRSVD_DTYPE_F32 ? __uint_as_float(w[EB == 4 ? i : 0])
-                                 : DT == BRSVD_DTYPE_BF16 ? from16<Bf16>((uint16_t)(w[i / 2] >> (16 * (i & 1)))) : from16<Fp16>((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+              v[h][16 / EB * j + i] = DT == BRSVD_DTYPE_F32 ? __uint_as_float(w[EB == 4 ? i : 0])
+                                      : DT == BRSVD_DTYPE_BF16 ? from16<Bf16>((uint16_t)(w[i / 2] >> (16 * (i & 1)))) : from16<Fp16>((uint16_t)(w[i / 2] >> (16 * (i & 1))));
           }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, finite_abs(x[h][i]));
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, finite_abs(v[h][i]));
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const int ex = block_exponent(top);
         const float inv = power_of_two(-ex);
         s = power_of_two(ex);
+        int4v f[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) f[h][i] = (int)pack_e4m3(x[h][4 * i] * inv, x[h][4 * i + 1] * inv, x[h][4 * i + 2] * inv, x[h][4 * i + 3] * inv);
+          for (int i = 0; i < 4; ++i) f[h][i] = (int)pack_e4m3(v[h][4 * i] * inv, v[h][4 * i + 1] * inv, v[h][4 * i + 2] * inv, v[h][4 * i + 3] * inv);
+        fw = widen(f[0], f[1]);
       } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint4 v = piece_of<1>(ra[t] + at + 64 * h, left - 64 * h);
-          f[h] = int4v{(int)v.x, (int)v.y, (int)v.z, (int)v.w};
-        }
-        s = sa[t][b];
+        fw = widen(__builtin_bit_cast(int4v, x.a[t][0]), __builtin_bit_cast(int4v, x.a[t][1]));
+        s = x.sa[t];
       }
-      const Wide8 fw = widen(f[0], f[1]);
+      s *= x.sb;
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
         const floatx4 d = mfma_wide(ew[u], fw);
-        const float c = s * sb[u][b];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[t][u][r] += d[r] * c;
+        for (int r = 0; r < 4; ++r) acc[t][u][r] += d[r] * s;
       }
     }
+  };
+  const int whole = (int)(g.k / kBlock);
+  for (int b = wave; b < whole; b += WAVES * U) {
+    Block x[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) fetch(x[i], b + WAVES * i < whole ? b + WAVES * i : b, true, 0);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (b + WAVES * i < whole) multiply(x[i]);
+  }
+  if (whole < g.blocks && whole % WAVES == wave) {          // the contraction's end, after the wave's other blocks
+    Block x;
+    fetch(x, whole, false, g.k - (int64_t)whole * kBlock - piece);
+    multiply(x);
   }
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int u = 0; u < NT; ++u) parts[wave][t * NT + u][lane] = acc[t][u];
   __syncthreads();
-  char* C = (char*)g.C + (g.splits > 1 ? (int64_t)blockIdx.y * g.A.n * g.B.n * 4 : 0);
   for (int i = wave; i < MT * NT; i += WAVES) {
     floatx4 sum = parts[0][i][lane];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) sum += parts[w][i][lane];
     const int64_t m = 16 * (i / NT) + row, n = n0 + 16 * (i % NT) + 4 * (lane >> 4);
-    if (m < g.A.n && n < g.B.n) put_four(C, m * g.ldc + n, g.B.n - n, g.dtype, sum);
+    if (m < g.A.n && n < g.B.n) put_four(g.C, m * g.ldc + n, g.B.n - n, g.dtype, sum);
   }
 }
 
 constexpr int64_t kFewRows = 64;      // rows up to which the read of B bounds the product
+constexpr int64_t kCastRows = 16;     // rows up to which they are cast inside it
 
 // How often the contraction is cut so that there are workgroups for every CU: only while a part keeps `least` blocks.
 static int splits_for(int64_t workgroups, int blocks, int least) {
@@ -325,12 +346,22 @@ static E4m3Plan e4m3_plan(int64_t m, int64_t n, int64_t k, bool per_row, int dty
 }
 static uint64_t split_bytes(const E4m3Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? (uint64_t)p.splits * m * n * 4 : 0; }
 
-template <int DT>
+// NT: rows of A are read (and cast) once for 16 NT rows of B, as many as leave workgroups for every CU
+template <int MT, int NT, int U, int DT>
 static void launch_rows(const E4m3Args& g, hipStream_t stream) {
-  const dim3 grid((unsigned)ceil_div(g.B.n, 16), (unsigned)g.splits);
-  if (g.A.n <= 16) hipLaunchKernelGGL((k_rows_e4m3<1, 1, DT>), grid, dim3(512), 0, stream, g);
-  else if (g.A.n <= 32) hipLaunchKernelGGL((k_rows_e4m3<2, 1, DT>), grid, dim3(512), 0, stream, g);
-  else hipLaunchKernelGGL((k_rows_e4m3<4, 1, DT>), grid, dim3(512), 0, stream, g);
+  hipLaunchKernelGGL((k_rows_e4m3<MT, NT, U, DT>), dim3((unsigned)ceil_div(g.B.n, 16 * NT)), dim3(512), 0, stream, g);
+}
+template <int DT>
+static void launch_few(const E4m3Args& g, hipStream_t stream) {
+  if (g.B.n >= 32 * 512) launch_rows<1, 4, 1, DT>(g, stream);
+  else if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, DT>(g, stream);
+  else launch_rows<1, 1, 4, DT>(g, stream);
+}
+static void launch_more(const E4m3Args& g, hipStream_t stream) {
+  if (g.A.n <= 32 && g.B.n >= 32 * 512) launch_rows<2, 2, 2, -1>(g, stream);
+  else if (g.A.n <= 32) launch_rows<2, 1, 4, -1>(g, stream);
+  else if (g.B.n >= 32 * 512) launch_rows<4, 2, 1, -1>(g, stream);
+  else launch_rows<4, 1, 2, -1>(g, stream);
 }
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
 static void launch_tiles(const E4m3Args& g, hipStream_t stream) {
@@ -364,10 +395,11 @@ static int gemm_e4m3(const void* A, int64_t lda_bytes, int a_type, const float* 
   g.tiles_n = ceil_div(n, 256);
   g.tiles_m = ceil_div(m, plan.bq);
   if (plan.rows) {
-    if (a_type == BRSVD_DTYPE_F32) launch_rows<BRSVD_DTYPE_F32>(g, stream);
-    else if (a_type == BRSVD_DTYPE_BF16) launch_rows<BRSVD_DTYPE_BF16>(g, stream);
-    else if (a_type == BRSVD_DTYPE_F16) launch_rows<BRSVD_DTYPE_F16>(g, stream);
-    else launch_rows<-1>(g, stream);
+    if (m > kCastRows) launch_more(g, stream);
+    else if (a_type == BRSVD_DTYPE_F32) launch_few<BRSVD_DTYPE_F32>(g, stream);
+    else if (a_type == BRSVD_DTYPE_BF16) launch_few<BRSVD_DTYPE_BF16>(g, stream);
+    else if (a_type == BRSVD_DTYPE_F16) launch_few<BRSVD_DTYPE_F16>(g, stream);
+    else launch_few<-1>(g, stream);
   } else {
     const bool direct = aligned_pieces(A, lda_bytes) && aligned_pieces(B, ldb);
     const bool wide = dtype == BRSVD_DTYPE_F32;
@@ -405,7 +437,7 @@ extern "C" uint64_t brsvd_gemm_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t 
 extern "C" uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t dtype) {
   if (!product_sizes(m, n, k) || !product_type(dtype) || m == 0 || n == 0 || k == 0) return 0;
   const E4m3Plan p = e4m3_plan(m, n, k, false, dtype);
-  return split_bytes(p, m, n) + (p.rows ? 0 : cast_bytes(m, k));
+  return split_bytes(p, m, n) + (m <= kCastRows ? 0 : cast_bytes(m, k));
 }
 
 extern "C" int brsvd_gemm_e4m3(const uint8_t* A, int64_t lda, const float* SA, const uint8_t* B, int64_t ldb, const float* SB, int32_t block_rows, int64_t m,
@@ -435,11 +467,11 @@ extern "C" int brsvd_linear_e4m3(const void* X, int64_t ldx, int32_t dtype, cons
   const int eb = dtype == BRSVD_DTYPE_F32 ? 4 : 2;
   if (!X || !W || !SW || !Y || ldx < k || ldw < k || ldy < n || ldx * eb >= kMaxPitch * 4 || ldw >= kMaxPitch) return BRSVD_ERR_ARG;
   const E4m3Plan p = e4m3_plan(m, n, k, false, dtype);
-  const uint64_t parts = split_bytes(p, m, n), need = parts + (p.rows ? 0 : cast_bytes(m, k));
+  const uint64_t parts = split_bytes(p, m, n), need = parts + (m <= kCastRows ? 0 : cast_bytes(m, k));
   if (need && (!scratch || (uintptr_t)scratch % 256)) return BRSVD_ERR_ARG;
   if (scratch_bytes < need) return BRSVD_ERR_BUDGET;
   hipStream_t s = (hipStream_t)stream;
-  if (p.rows) return gemm_e4m3(X, ldx * eb, dtype, nullptr, W, ldw, SW, false, m, n, k, dtype, Y, ldy, p, (float*)scratch, s);
+  if (m <= kCastRows) return gemm_e4m3(X, ldx * eb, dtype, nullptr, W, ldw, SW, false, m, n, k, dtype, Y, ldy, p, (float*)scratch, s);
   uint8_t* q = (uint8_t*)scratch;
   float* sq = (float*)(q + ((uint64_t)m * cast_pitch(k) + 255) / 256 * 256);
   BRSVD_TRY(quantize(X, ldx, m, k, dtype, 1, q, (int64_t)cast_pitch(k), sq, nullptr, 0, nullptr, s));
