@@ -435,34 +435,37 @@ def brsvd_small_svd_static(R, stream=None, out=None):
 
 def _model_dtype(dtype, name, half=False):
     import torch
-    types = {torch.bfloat16: BRSVD_DTYPE_BF16, torch.float16: BRSVD_DTYPE_F16}
-    if not half:
-        types[torch.float32] = BRSVD_DTYPE_F32
-    if dtype not in types:
-        raise TypeError(f"{name} must be of dtype {' or '.join(str(t) for t in types)}, not {dtype}")
-    return types[dtype]
+    if dtype is torch.bfloat16:
+        return BRSVD_DTYPE_BF16
+    if dtype is torch.float16:
+        return BRSVD_DTYPE_F16
+    if dtype is torch.float32 and not half:
+        return BRSVD_DTYPE_F32
+    raise TypeError(f"{name} must be of dtype torch.bfloat16, torch.float16{'' if half else ' or torch.float32'}, not {dtype}")
 
 
-def _rows(t, dtype, shape, name):
-    """(address, leading dimension) of a CUDA matrix with neighbouring elements in a row; shape: None where any size will do."""
+def _rows(t, dtype, cols, name, rows=None):
+    """(address, leading dimension) of a CUDA matrix with neighbouring elements in a row; cols, rows: None where any number will do."""
     import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 2):
         raise TypeError(f"{name} must be a 2-d CUDA tensor of dtype {dtype}")
-    if any(want is not None and have != want for have, want in zip(t.shape, shape)):
-        raise TypeError(f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if s is None else s for s in shape)}")
-    rows, cols = t.shape
-    if rows and cols and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols)):
-        raise TypeError(f"{name} must have unit column stride and rows that do not overlap")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(cols, 1))
+    r, c = t.shape
+    if (cols is not None and c != cols) or (rows is not None and r != rows):
+        raise TypeError(f"{name} has shape {(r, c)}, expected {tuple('any' if s is None else s for s in (rows, cols))}")
+    ld, step = t.stride()
+    if r <= 1 or not c:
+        ld = -(-c // 16) * 16 or 1        # of one row any pitch is right, and whole 16 bytes are read fastest
+    elif ld < c:
+        raise TypeError(f"{name} must have rows that do not overlap")
+    if step != 1 and c > 1 and r:
+        raise TypeError(f"{name} must have unit column stride")
+    return t.data_ptr(), ld
 
 
 def _scope(stream):
     """Memory taken inside belongs to the stream that the call runs on: what a call frees at its end, or the caller later, is not handed out
     to work of another stream before the call is through with it."""
-    import contextlib
     import torch
-    if stream is None:
-        return contextlib.nullcontext()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     return torch.cuda.stream(stream)
@@ -474,19 +477,23 @@ def _scoped(call):
 
     @functools.wraps(call)
     def wrapped(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
         with _scope(stream):
             return call(*args, **kw)
     return wrapped
 
 
-def _blocks(n):
-    return -(-n // 128)
+def _current(device):
+    """torch's current stream on a device, as an address (torch.cuda.current_stream() makes an object of it, at several times the cost)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index) or None
 
 
 def _scales(S, rows, cols, block_rows, name):
     import torch
-    shape = (rows if block_rows == 1 else _blocks(rows), _blocks(cols))
-    if tuple(S.shape) != shape:
+    shape = (rows if block_rows == 1 else -(-rows // 128), -(-cols // 128))
+    if S.shape != shape:
         raise TypeError(f"{name} has shape {tuple(S.shape)}, expected {shape}")
     return _dev(S, torch.float32, name)
 
@@ -494,7 +501,7 @@ def _scales(S, rows, cols, block_rows, name):
 def _eight_bit(rows, cols, device):
     """rows x cols numbers of 8 bits in rows of whole 16 bytes, which the products read fastest."""
     import torch
-    return torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    return torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=torch.float8_e4m3fn, device=device)
 
 
 @_scoped
@@ -506,17 +513,17 @@ def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
     if block_rows not in (1, 128):
         raise ValueError("block_rows must be 1 or 128")
     dt = _model_dtype(X.dtype, "X")
-    x, ldx = _rows(X, X.dtype, (None, None), "X")
+    x, ldx = _rows(X, X.dtype, None, "X")
     rows, cols = X.shape
     dev = X.device
 
     def result(r, c):
-        return _eight_bit(r, c, dev), torch.empty(r if block_rows == 1 else _blocks(r), _blocks(c), device=dev)
+        return _eight_bit(r, c, dev), torch.empty(r if block_rows == 1 else -(-r // 128), -(-c // 128), device=dev)
     Q, S = result(rows, cols)
     Qt, St = result(cols, rows) if transpose else (None, None)
     _check(lib().brsvd_quantize_e4m3(x, ldx, rows, cols, dt, block_rows, Q.data_ptr(), -(-cols // 16) * 16, S.data_ptr(),
                                      Qt.data_ptr() if transpose else None, -(-rows // 16) * 16 if transpose else 0,
-                                     St.data_ptr() if transpose else None, _stream_ptr(None)), "brsvd_quantize_e4m3")
+                                     St.data_ptr() if transpose else None, _current(X.device)), "brsvd_quantize_e4m3")
     return (Q, S, Qt, St) if transpose else (Q, S)
 
 
@@ -528,11 +535,11 @@ def brsvd_dequantize_e4m3(Q, S, block_rows=1, dtype=None):
         raise ValueError("block_rows must be 1 or 128")
     dtype = dtype or torch.float32
     dt = _model_dtype(dtype, "the result")
-    q, ldq = _rows(Q, torch.float8_e4m3fn, (None, None), "Q")
+    q, ldq = _rows(Q, torch.float8_e4m3fn, None, "Q")
     rows, cols = Q.shape
     X = torch.empty(rows, cols, dtype=dtype, device=Q.device)
     _check(lib().brsvd_dequantize_e4m3(q, ldq, _scales(S, rows, cols, block_rows, "S"), rows, cols, block_rows, dt,
-                                       X.data_ptr(), max(cols, 1), _stream_ptr(None)), "brsvd_dequantize_e4m3")
+                                       X.data_ptr(), max(cols, 1), _current(Q.device)), "brsvd_dequantize_e4m3")
     return X
 
 
@@ -543,19 +550,19 @@ def brsvd_gemm_e4m3(A, SA, Bm, SB, block_rows=128, dtype=None, out=None):
     import torch
     if block_rows not in (1, 128):
         raise ValueError("block_rows must be 1 or 128")
-    a, lda = _rows(A, torch.float8_e4m3fn, (None, None), "A")
+    a, lda = _rows(A, torch.float8_e4m3fn, None, "A")
     m, k = A.shape
-    b, ldb = _rows(Bm, torch.float8_e4m3fn, (None, k), "Bm")
+    b, ldb = _rows(Bm, torch.float8_e4m3fn, k, "Bm")
     n = Bm.shape[0]
     sa, sb = _scales(SA, m, k, 1, "SA"), _scales(SB, n, k, block_rows, "SB")
     dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
     dt = _model_dtype(dtype, "the result")
     Cm = torch.empty(m, n, dtype=dtype, device=A.device) if out is None else out
-    c, ldc = _rows(Cm, dtype, (m, n), "out")
+    c, ldc = _rows(Cm, dtype, n, "out", m)
     nbytes = lib().brsvd_gemm_e4m3_scratch_bytes(m, n, k, block_rows, dt)
     scr = _byte_scratch(nbytes, A.device) if nbytes else None
     _check(lib().brsvd_gemm_e4m3(a, lda, sa, b, ldb, sb, block_rows, m, n, k, dt, c, ldc,
-                                 scr.data_ptr() if nbytes else None, nbytes, _stream_ptr(None)), "brsvd_gemm_e4m3")
+                                 scr.data_ptr() if nbytes else None, nbytes, _current(A.device)), "brsvd_gemm_e4m3")
     return Cm
 
 
@@ -565,29 +572,29 @@ def brsvd_linear_e4m3(X, W, SW, out=None):
     for each 128 x 128 block.  The result has X's type."""
     import torch
     dt = _model_dtype(X.dtype, "X")
-    x, ldx = _rows(X, X.dtype, (None, None), "X")
+    x, ldx = _rows(X, X.dtype, None, "X")
     m, k = X.shape
-    w, ldw = _rows(W, torch.float8_e4m3fn, (None, k), "W")
+    w, ldw = _rows(W, torch.float8_e4m3fn, k, "W")
     n = W.shape[0]
     sw = _scales(SW, n, k, 128, "SW")
     Y = torch.empty(m, n, dtype=X.dtype, device=X.device) if out is None else out
-    y, ldy = _rows(Y, X.dtype, (m, n), "out")
+    y, ldy = _rows(Y, X.dtype, n, "out", m)
     nbytes = lib().brsvd_linear_e4m3_scratch_bytes(m, n, k, dt)
     scr = _byte_scratch(nbytes, X.device) if nbytes else None
     _check(lib().brsvd_linear_e4m3(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes,
-                                   _stream_ptr(None)), "brsvd_linear_e4m3")
+                                   _current(X.device)), "brsvd_linear_e4m3")
     return Y
 
 
 def _head(H, W):
     dt = _model_dtype(H.dtype, "H", half=True)
-    h, ldh = _rows(H, H.dtype, (None, None), "H")
-    w, ldw = _rows(W, H.dtype, (None, H.shape[1]), "W")
+    h, ldh = _rows(H, H.dtype, None, "H")
+    w, ldw = _rows(W, H.dtype, H.shape[1], "W")
     return (h, ldh, w, ldw), (H.shape[0], W.shape[0], H.shape[1]), dt
 
 
 def _vector(t, dtype, n, name):
-    if tuple(t.shape) != (n,):
+    if t.shape != (n,):
         raise TypeError(f"{name} has shape {tuple(t.shape)}, expected {(n,)}")
     return _dev(t, dtype, name)
 
@@ -623,7 +630,7 @@ def brsvd_xent_forward(H, W, labels):
     loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
     ws, nbytes = _head_workspace(sizes, 0, 0, 0, H.device)
     _check(lib().brsvd_xent_forward(*ops, y, *sizes, dt, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes,
-                                    _stream_ptr(None)), "brsvd_xent_forward")
+                                    _current(H.device)), "brsvd_xent_forward")
     return loss, lse
 
 
@@ -648,7 +655,7 @@ def brsvd_xent_backward(H, W, labels, lse, grad, need_dH=True, need_dW=True, pie
     dH, dW, outs = _gradients(H, W, need_dH, need_dW)
     ws, nbytes = _head_workspace(sizes, piece, 0, 1, H.device)
     _check(lib().brsvd_xent_backward(*ops, y, l, g, stride, *sizes, piece, dt, *outs, ws.data_ptr(), nbytes,
-                                     _stream_ptr(None)), "brsvd_xent_backward")
+                                     _current(H.device)), "brsvd_xent_backward")
     return dH, dW
 
 
@@ -671,7 +678,7 @@ def brsvd_distill_forward(H, W, ids, logits, temperature=1.0):
     z = torch.empty(ids.shape, device=H.device)
     ws, nbytes = _head_workspace(sizes, 0, te[2], 0, H.device)
     _check(lib().brsvd_distill_forward(*ops, *te, temperature, *sizes, dt, loss.data_ptr(), lse.data_ptr(), z.data_ptr(),
-                                       ws.data_ptr(), nbytes, _stream_ptr(None)), "brsvd_distill_forward")
+                                       ws.data_ptr(), nbytes, _current(H.device)), "brsvd_distill_forward")
     return loss, lse, z
 
 
@@ -688,7 +695,7 @@ def brsvd_distill_backward(H, W, ids, logits, temperature, lse, z, grad, need_dH
     dH, dW, outs = _gradients(H, W, need_dH, need_dW)
     ws, nbytes = _head_workspace(sizes, piece, te[2], 1, H.device)
     _check(lib().brsvd_distill_backward(*ops, *te, temperature, l, _dev(z, torch.float32, "z"), g, stride, *sizes, piece, dt,
-                                        *outs, ws.data_ptr(), nbytes, _stream_ptr(None)), "brsvd_distill_backward")
+                                        *outs, ws.data_ptr(), nbytes, _current(H.device)), "brsvd_distill_backward")
     return dH, dW
 
 
