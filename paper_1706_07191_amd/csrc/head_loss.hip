@@ -13,7 +13,8 @@
 
 namespace brsvd {
 
-// 256 x 256 tiles of eight waves; 256 x 128 and 256 x 64 where there are few tokens, so that a tile's columns are not mostly empty.
+// Tiles of eight waves, 256 of the vocabulary (or of dim) x 256 tokens; x 128 or 64 where there are few tokens, so that a tile's columns are not mostly
+// empty.
 template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT, int BQ> struct Tiles;
 template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT>
 struct Tiles<El, OP, OQ, DIRECT, EXACT, 256> : TileProduct<El, 8, 4, 2, 4, OP, OQ, DIRECT, EXACT> {};
@@ -22,8 +23,15 @@ struct Tiles<El, OP, OQ, DIRECT, EXACT, 128> : TileProduct<El, 8, 2, 2, 4, OP, O
 template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT>
 struct Tiles<El, OP, OQ, DIRECT, EXACT, 64> : TileProduct<El, 2, 4, 8, 1, OP, OQ, DIRECT, EXACT> {};
 constexpr int kTileP = 256, kTileThreads = 512;
+// The logits, both operands with dim in their rows: up to 64 tokens without LDS, four waves.
+template <class El, bool DIRECT, int BQ> struct Logits : Tiles<El, kRows, kRows, DIRECT, true, BQ> {};
+template <class El, bool DIRECT> struct Logits<El, DIRECT, 64> : RowsProduct<El, 2, 4, 4, 2> {};
+template <class El, bool DIRECT> struct Logits<El, DIRECT, 32> : RowsProduct<El, 2, 2, 4, 4> {};
+template <class El, bool DIRECT> struct Logits<El, DIRECT, 16> : RowsProduct<El, 2, 1, 4, 4> {};
 // Tokens of a tile: 256 x 256 has no registers left for pieces on their way through them.
 static int tokens_tile(int64_t tokens, bool direct) { return tokens <= 64 ? 64 : tokens <= 128 || !direct ? 128 : 256; }
+static int logits_tile(int64_t tokens, bool direct) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens_tile(tokens, direct); }
+static int logits_rows(int bq) { return bq <= 64 ? 128 : kTileP; }     // of the vocabulary
 
 // What the backward pass knows on the device: how many tokens count, and the power of two that G is multiplied by so that its numbers of 16 bits hold what
 // matters: 2^e max |g_t| is at most 2^14, and a probability of 2^-28 is still a normal number of fp16.
@@ -49,69 +57,82 @@ struct HeadArgs {
   int64_t pitch;
 };
 
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
+// Exponentials are powers of two of x log2(e); what is kept of a row is in units of log 2, too.
 template <class El, bool DIRECT, int BQ>
-__global__ void __launch_bounds__(kTileThreads, 2)
+__global__ void __launch_bounds__((Logits<El, DIRECT, BQ>::kThreads), 2)
 k_head_lse(const HeadArgs g) {
-  using T = Tiles<El, kRows, kRows, DIRECT, true, BQ>;
+  using T = Logits<El, DIRECT, BQ>;
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tv, tt;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 4, &tv, &tt)) return;
   floatx4 acc[NP][NQ];
-  const int64_t v0 = tv * kTileP, t0 = tt * BQ;
+  const int64_t v0 = tv * T::BP, t0 = tt * BQ;
   T::run(acc, g.W, v0, g.H, t0, 0, g.dim, lds);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % WP, wq = wave / WP;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave % WP, wq = wave / WP;
   float2* red = (float2*)lds;           // [WP][BQ]
-  const int64_t vlane = v0 + 16 * wp * NP + 4 * (lane >> 4);
+  const int64_t vwave = v0 + 16 * wp * NP, vlane = vwave + 4 * (lane >> 4);
+  const float scale = g.scale * kLog2e;
+  if (vwave + 16 * NP > g.W.n) {        // words beyond the last one
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const int col = 16 * (wq * NQ + q) + (lane & 15);
-    const int64_t t = t0 + col;
-    if (g.label) {
-      const int64_t at = (t < g.H.n ? g.label[t] : -1) - vlane;
-      const bool mine = at >= 0 && at < 16 * NP && (at & 15) < 4 && at + vlane < g.W.n;
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (vlane + 16 * p + r >= g.W.n)
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) acc[p][q][r] = -INFINITY;
+  }
+  if (g.label) {
+    int64_t at[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int64_t t = t0 + 16 * (wq * NQ + q) + (lane & 15);
+      at[q] = g.label[t < g.H.n ? t : g.H.n - 1] - vlane;
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int64_t t = t0 + 16 * (wq * NQ + q) + (lane & 15);
+      const bool mine = at[q] >= 0 && at[q] < 16 * NP && (at[q] & 15) < 4 && at[q] + vlane < g.W.n && t < g.H.n;
       if (__any(mine)) {
         float z = 0.f;
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (at == 16 * p + r) z = acc[p][q][r];
+            if (at[q] == 16 * p + r) z = acc[p][q][r];
         if (mine) g.zlabel[t] = z;
       }
     }
+  }
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float z = acc[p][q][r] * g.scale;
-        if (vlane + 16 * p + r >= g.W.n) z = -INFINITY;
-        acc[p][q][r] = z;
-        top = fmaxf(top, z);
-      }
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[p][q][r]);
     top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f((acc[p][q][r] - ref) * kLog2e);
+      for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[p][q][r], scale, -ref));
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (lane < 16) red[wp * BQ + col] = make_float2(top, sum);
+    if (lane < 16) red[wp * BQ + 16 * (wq * NQ + q) + lane] = make_float2(top, sum);
   }
   __syncthreads();
-  for (int col = threadIdx.x; col < BQ; col += kTileThreads) {
+  for (int col = threadIdx.x; col < BQ; col += T::kThreads) {
     if (t0 + col >= g.H.n) continue;
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < WP; ++w) top = fmaxf(top, red[w * BQ + col].x);
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int w = 0; w < WP; ++w) sum += red[w * BQ + col].y * __builtin_amdgcn_exp2f((red[w * BQ + col].x - ref) * kLog2e);
+    for (int w = 0; w < WP; ++w) sum += red[w * BQ + col].y * __builtin_amdgcn_exp2f(red[w * BQ + col].x - ref);
     g.part[tv * g.H.n + t0 + col] = make_float2(top, sum);
   }
 }
@@ -124,13 +145,22 @@ k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t tokens, cons
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
   const int64_t t = (int64_t)blockIdx.x * 16 + c;
   float top = -INFINITY, sum = 0.f;
-  if (t < tokens)
-    for (int64_t i = r; i < tiles; i += 16) {
-      const float2 v = part[i * tokens + t];
-      const float to = fmaxf(top, v.x), ref = to == -INFINITY ? 0.f : to;
-      sum = sum * __builtin_amdgcn_exp2f((top - ref) * kLog2e) + v.y * __builtin_amdgcn_exp2f((v.x - ref) * kLog2e);
-      top = to;
+  auto add = [&](float2 v) {
+    const float to = fmaxf(top, v.x), ref = to == -INFINITY ? 0.f : to;
+    sum = sum * __builtin_amdgcn_exp2f(top - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
+    top = to;
+  };
+  if (t < tokens) {
+    int64_t i = r;
+    for (; i + 48 < tiles; i += 64) {
+      float2 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = part[(i + 16 * j) * tokens + t];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add(v[j]);
     }
+    for (; i < tiles; i += 16) add(part[i * tokens + t]);
+  }
   red[r][c] = make_float2(top, sum);
   __syncthreads();
   if (r != 0 || t >= tokens) return;
@@ -138,8 +168,8 @@ k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t tokens, cons
   for (int i = 0; i < 16; ++i) all = fmaxf(all, red[i][c].x);
   const float ref = all == -INFINITY ? 0.f : all;
   sum = 0.f;
-  for (int i = 0; i < 16; ++i) sum += red[i][c].y * __builtin_amdgcn_exp2f((red[i][c].x - ref) * kLog2e);
-  const float l = all + logf(sum);
+  for (int i = 0; i < 16; ++i) sum += red[i][c].y * __builtin_amdgcn_exp2f(red[i][c].x - ref);
+  const float l = (all + log2f(sum)) * kLn2;
   lse[t] = l;
   if (label) loss[t] = label[t] >= 0 && label[t] < vocab ? l - zlabel[t] : 0.f;
 }
@@ -328,38 +358,54 @@ k_head_gather(const Operand H, int64_t dim, const HeadMeta* __restrict__ meta, c
 
 // A piece of G: the logits again, then the gradient with respect to them.
 template <class El, bool DIRECT, int BQ>
-__global__ void __launch_bounds__(kTileThreads, 2)
+__global__ void __launch_bounds__((Logits<El, DIRECT, BQ>::kThreads), 2)
 k_head_grad(const HeadArgs g) {
-  using T = Tiles<El, kRows, kRows, DIRECT, true, BQ>;
+  using T = Logits<El, DIRECT, BQ>;
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tv, tt;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 4, &tv, &tt)) return;
-  const int64_t count = g.meta->count, p0 = tv * kTileP, t0 = tt * BQ;
+  const int64_t count = g.meta->count, p0 = tv * T::BP, t0 = tt * BQ;
   if (t0 >= count) return;
   Operand H = g.H;
   H.n = count;
   floatx4 acc[NP][NQ];
   T::run(acc, g.W, p0, H, t0, 0, g.dim, lds);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % WP, wq = wave / WP;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave % WP, wq = wave / WP;
+  const int vlane = (int)p0 + 16 * wp * NP + 4 * (lane >> 4), rows = (int)g.W.n;
+  const float scale = g.scale * kLog2e;
+  float l[NQ], s[NQ];
+  int at[NQ];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    const int64_t c = t0 + 16 * (wq * NQ + q) + (lane & 15), in = c < count ? c : count - 1;
+    l[q] = g.lse[in] * kLog2e;
+    s[q] = g.coef[in];
+    at[q] = g.label_c[in] - (int)g.v0 - vlane;
+  }
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     const int64_t c = t0 + 16 * (wq * NQ + q) + (lane & 15);
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[p][q][r] = __builtin_amdgcn_exp2f(fmaf(acc[p][q][r], scale, -l[q]));
+    if (__any(at[q] >= 0 && at[q] < 16 * NP)) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (at[q] == 16 * p + r) acc[p][q][r] -= 1.f;
+    }
     if (c >= count) continue;
-    const float l = g.lse[c], s = g.coef[c];
-    const int64_t at = (int64_t)g.label_c[c] - g.v0;
+    uint16_t* row = g.G + c * g.pitch;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const int64_t v = p0 + 16 * (wp * NP + p) + 4 * (lane >> 4);
       uint16_t h[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float e = __builtin_amdgcn_exp2f((acc[p][q][r] * g.scale - l) * kLog2e);
-        if (v + r == at) e -= 1.f;
-        h[r] = to16<El>(s * e);
-      }
+      for (int r = 0; r < 4; ++r) h[r] = to16<El>(s[q] * acc[p][q][r]);
       // the pitch is a multiple of eight: what is written beyond the piece's last row stays inside the token's row of G
-      if (v < g.W.n) *(uint2*)(g.G + c * g.pitch + v) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+      if (vlane + 16 * p < rows) *(uint2*)(row + vlane + 16 * p) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
     }
   }
 }
@@ -499,7 +545,7 @@ static HeadPlan head_plan(int64_t tokens, int64_t vocab, int64_t dim, int64_t pi
   p.per_split = ceil_div(ceil_div(p.piece, s), 64) * 64;
   p.splits = (int)ceil_div(p.piece, p.per_split);
   p.part = 0;
-  p.zlabel = whole256((uint64_t)ceil_div(vocab, kTileP) * tokens * 8);
+  p.zlabel = whole256((uint64_t)ceil_div(vocab, logits_rows(logits_tile(tokens, true))) * tokens * 8);
   p.forward_bytes = p.zlabel + whole256((uint64_t)tokens * 4);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t here = at; at += whole256(bytes); return here; };
@@ -523,6 +569,15 @@ static bool head_sizes(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece
 }
 static bool half_type(int dtype) { return dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16; }
 
+#define BRSVD_LOGITS(KERNEL, El, DIRECT, grid, stream, args)                                                      \
+  do {                                                                                                           \
+    const dim3 few(Logits<El, true, 16>::kThreads);                                                              \
+    if (bl == 256 && DIRECT) hipLaunchKernelGGL((KERNEL<El, true, 256>), grid, dim3(kTileThreads), 0, stream, args); \
+    else if (bl >= 128) hipLaunchKernelGGL((KERNEL<El, DIRECT, 128>), grid, dim3(kTileThreads), 0, stream, args); \
+    else if (bl == 64) hipLaunchKernelGGL((KERNEL<El, true, 64>), grid, few, 0, stream, args);                    \
+    else if (bl == 32) hipLaunchKernelGGL((KERNEL<El, true, 32>), grid, few, 0, stream, args);                    \
+    else hipLaunchKernelGGL((KERNEL<El, true, 16>), grid, few, 0, stream, args);                                  \
+  } while (0)
 #define BRSVD_BY_TILE(KERNEL, El, DIRECT, grid, stream, args)                                                    \
   do {                                                                                                           \
     if (bq == 256 && DIRECT) hipLaunchKernelGGL((KERNEL<El, true, 256>), grid, dim3(kTileThreads), 0, stream, args); \
@@ -548,16 +603,16 @@ static int head_forward(const HeadCall& c, const HeadPlan& plan, char* ws, float
   g.H = rows_of(c.H, c.ldh, c.tokens);
   g.dim = c.dim;
   g.scale = c.scale;
-  g.tiles_v = ceil_div(c.vocab, kTileP);
   const bool direct = aligned_pieces(c.W, 2 * c.ldw) && aligned_pieces(c.H, 2 * c.ldh);
-  const int bq = tokens_tile(c.tokens, direct);
-  g.tiles_t = ceil_div(c.tokens, bq);
+  const int bl = logits_tile(c.tokens, direct);
+  g.tiles_v = ceil_div(c.vocab, logits_rows(bl));
+  g.tiles_t = ceil_div(c.tokens, bl);
   g.label = c.label;
   g.part = (float2*)(ws + plan.part);
   g.zlabel = (float*)(ws + plan.zlabel);
   const dim3 grid(tile_workgroups(g.tiles_v, g.tiles_t));
-  if (direct) BRSVD_BY_TILE(k_head_lse, El, true, grid, stream, g);
-  else BRSVD_BY_TILE(k_head_lse, El, false, grid, stream, g);
+  if (direct) BRSVD_LOGITS(k_head_lse, El, true, grid, stream, g);
+  else BRSVD_LOGITS(k_head_lse, El, false, grid, stream, g);
   hipLaunchKernelGGL(k_head_join, dim3((unsigned)ceil_div(c.tokens, 16)), dim3(256), 0, stream, g.part, g.tiles_v, c.tokens, c.label, c.vocab, g.zlabel, lse, loss);
   if (!c.label) hipLaunchKernelGGL(k_distill_loss<El>, dim3((unsigned)c.tokens), dim3(256), 0, stream, g.W, g.H, c.dim, c.teacher, lse, z, loss);
   BRSVD_HIP_TRY(hipGetLastError());
@@ -578,7 +633,7 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   hipLaunchKernelGGL(k_head_gather, dim3((unsigned)c.tokens), dim3(256), 0, stream, H, c.dim, meta, index, lse, c.label, hc, plan.pitch_h, lse_c, coef, label_c);
   if (dH) hipLaunchKernelGGL(k_head_zero, dim3((unsigned)c.tokens), dim3(256), 0, stream, (uint16_t*)dH, lddh, c.tokens, c.dim);
   const bool direct = aligned_pieces(c.W, 2 * c.ldw);
-  const int bq = tokens_tile(c.tokens, direct);
+  const int bq = tokens_tile(c.tokens, direct), bl = logits_tile(c.tokens, direct);
   const int64_t tiles_t = ceil_div(c.tokens, bq);
   for (int64_t v0 = 0; v0 < c.vocab; v0 += plan.piece) {
     const int64_t rows = c.vocab - v0 < plan.piece ? c.vocab - v0 : plan.piece;
@@ -587,8 +642,8 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
     g.H = Operand{hc, plan.pitch_h, c.tokens};
     g.dim = c.dim;
     g.scale = c.scale;
-    g.tiles_v = ceil_div(rows, kTileP);
-    g.tiles_t = tiles_t;
+    g.tiles_v = ceil_div(rows, logits_rows(bl));
+    g.tiles_t = ceil_div(c.tokens, bl);
     g.meta = meta;
     g.lse = lse_c;
     g.coef = coef;
@@ -597,8 +652,8 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
     g.G = G;
     g.pitch = plan.piece;
     const dim3 grid(tile_workgroups(g.tiles_v, g.tiles_t));
-    if (direct) BRSVD_BY_TILE(k_head_grad, El, true, grid, stream, g);
-    else BRSVD_BY_TILE(k_head_grad, El, false, grid, stream, g);
+    if (direct) BRSVD_LOGITS(k_head_grad, El, true, grid, stream, g);
+    else BRSVD_LOGITS(k_head_grad, El, false, grid, stream, g);
     if (!c.label)
       hipLaunchKernelGGL(k_distill_scatter<El>, dim3((unsigned)ceil_div(c.tokens * c.teacher.top, 256)), dim3(256), 0, stream, c.teacher, q, z, meta, index, lse_c, coef,
                          v0, rows, c.vocab, G, plan.piece);

@@ -280,6 +280,73 @@ struct TileProduct {
   }
 };
 
+// The same for up to 64 rows of Q, where the read of P is what it takes: no LDS, a wave has 16 NP rows of P and all rows of Q, and both go from memory (Q
+// from the caches) to the instruction's registers, U steps ahead.  Rows at any alignment.  Sums start from zero every step.
+template <class El, int NP_, int NQ_, int WP_, int U>
+struct RowsProduct {
+  static constexpr int NP = NP_, NQ = NQ_, WP = WP_, WQ = 1;
+  static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ, kThreads = 64 * WP;
+  static constexpr int kLds = WP * BQ * 8;                       // for what follows the product
+  struct Step { uint4 p[NP][2], q[NQ][2]; };
+
+  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char*) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, piece = 16 * (lane >> 4);
+    const char *rp[NP], *rq[NQ];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int64_t r = p0 + 16 * (wave * NP + p) + row;
+      rp[p] = P.base + (r < P.n ? r : P.n - 1) * P.ld + 2 * k0 + piece;
+    }
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int64_t r = q0 + 16 * q + row;
+      rq[q] = Q.base + (r < Q.n ? r : Q.n - 1) * Q.ld + 2 * k0 + piece;
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int64_t bytes = 2 * (k1 - k0);
+    const int whole = (int)(bytes / kStepBytes);
+    auto fetch = [&](Step& x, int t, bool all, int64_t left) {            // left: bytes of the row from this lane's first piece on
+      const int64_t at = (int64_t)t * kStepBytes;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) x.p[p][h] = piece_of<2>(rp[p] + at + 64 * h, all ? 16 : left - 64 * h);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) x.q[q][h] = piece_of<2>(rq[q] + at + 64 * h, all ? 16 : left - 64 * h);
+      }
+    };
+    auto multiply = [&](const Step& x) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          floatx4 d = mfma16<El>(__builtin_bit_cast(int4v, x.p[p][0]), __builtin_bit_cast(int4v, x.q[q][0]), floatx4{0.f, 0.f, 0.f, 0.f});
+          d = mfma16<El>(__builtin_bit_cast(int4v, x.p[p][1]), __builtin_bit_cast(int4v, x.q[q][1]), d);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[p][q][r] += d[r];
+        }
+    };
+    Step x[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (i < whole) fetch(x[i], i, true, 0);
+    for (int t = 0; t < whole; t += U) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (t + i < whole) multiply(x[i]);
+        if (t + i + U < whole) fetch(x[i], t + i + U, true, 0);
+      }
+    }
+    if (bytes > (int64_t)whole * kStepBytes) {
+      fetch(x[0], whole, false, bytes - (int64_t)whole * kStepBytes - piece);
+      multiply(x[0]);
+    }
+  }
+};
+
 // 16-bit numbers from fp32, to the nearest
 template <class El> __device__ __forceinline__ uint16_t to16(float x) {
   if constexpr (__is_same(El, Bf16)) { const __bf16 h = (__bf16)x; return __builtin_bit_cast(uint16_t, h); }
