@@ -88,6 +88,7 @@ k_tiles_e4m3(const E4m3Args g) {
     for (int i = 0; i < 2; ++i)
       if (tid + i * THREADS < BQ + kPScales) scales[buffer][tid + i * THREADS] = v[i];
   };
+  const uint32_t bb = fragment_base<kRows, BP>(16 * wp * NP, lane), ba = fragment_base<kRows, BQ>(16 * wq * NQ, lane);
   float v[2];
   fetch(b0, v);
   sp.load(lds, tid, wave, g.k - (int64_t)b0 * kBlock);
@@ -111,15 +112,15 @@ k_tiles_e4m3(const E4m3Args g) {
     float sa[NQ];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      f0[q] = fragment<kRows, BQ>(ta, 16 * (wq * NQ + q), 0, lane);
-      f1[q] = fragment<kRows, BQ>(ta, 16 * (wq * NQ + q), 1, lane);
+      f0[q] = fragment<kRows, BQ>(ta, ba, q, 0);
+      f1[q] = fragment<kRows, BQ>(ta, ba, q, 1);
       if (WIDE) fw[q] = widen(f0[q], f1[q]);
       sa[q] = scales[buffer][16 * (wq * NQ + q) + (lane & 15)];
       if (!PER_ROW && 16 * NP <= kBlock) sa[q] *= scales[buffer][BQ + wp * 16 * NP / kBlock];
     }
     // The fragments of the next tile row are on their way while this one is multiplied, and a sum is added once the products of the next tile row are
     // issued; the fences keep the compiler from fetching all rows at once, which it has no registers for.
-    int4v e0 = fragment<kRows, BP>(tb, 16 * wp * NP, 0, lane), e1 = fragment<kRows, BP>(tb, 16 * wp * NP, 1, lane);
+    int4v e0 = fragment<kRows, BP>(tb, bb, 0, 0), e1 = fragment<kRows, BP>(tb, bb, 0, 1);
     floatx4 d[2][NQ], sb[2];
     sb[0] = sb[1] = floatx4{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
@@ -127,8 +128,8 @@ k_tiles_e4m3(const E4m3Args g) {
       if (p < NP) {
         const int4v c0 = e0, c1 = e1;
         if (p + 1 < NP) {
-          e0 = fragment<kRows, BP>(tb, 16 * (wp * NP + p + 1), 0, lane);
-          e1 = fragment<kRows, BP>(tb, 16 * (wp * NP + p + 1), 1, lane);
+          e0 = fragment<kRows, BP>(tb, bb, p + 1, 0);
+          e1 = fragment<kRows, BP>(tb, bb, p + 1, 1);
         }
         if (PER_ROW) sb[p & 1] = *(const floatx4*)&scales[buffer][BQ + 16 * (wp * NP + p) + 4 * (lane >> 4)];
         if (WIDE) {

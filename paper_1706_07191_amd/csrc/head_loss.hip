@@ -15,16 +15,10 @@ namespace brsvd {
 
 // Tiles of eight waves, 256 of the vocabulary (or of dim) x 256 tokens; x 128 or 64 where there are few tokens, so that a tile's columns are not mostly
 // empty.
-template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT, int BQ> struct Tiles;
-template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT>
-struct Tiles<El, OP, OQ, DIRECT, EXACT, 256> : TileProduct<El, 8, 4, 2, 4, OP, OQ, DIRECT, EXACT> {};
-template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT>
-struct Tiles<El, OP, OQ, DIRECT, EXACT, 128> : TileProduct<El, 8, 2, 2, 4, OP, OQ, DIRECT, EXACT> {};
-template <class El, Order OP, Order OQ, bool DIRECT, bool EXACT>
-struct Tiles<El, OP, OQ, DIRECT, EXACT, 64> : TileProduct<El, 2, 4, 8, 1, OP, OQ, DIRECT, EXACT> {};
+template <class El, Order OP, Order OQ, bool DIRECT, int BQ> using Tiles = TileProduct<El, BQ / 64, OP, OQ, DIRECT>;
 constexpr int kTileP = 256, kTileThreads = 512;
 // The logits, both operands with dim in their rows: up to 64 tokens without LDS, four waves.
-template <class El, bool DIRECT, int BQ> struct Logits : Tiles<El, kRows, kRows, DIRECT, true, BQ> {};
+template <class El, bool DIRECT, int BQ> struct Logits : Tiles<El, kRows, kRows, DIRECT, BQ> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 64> : RowsProduct<El, 2, 4, 4, 2> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 32> : RowsProduct<El, 2, 2, 4, 4> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 16> : RowsProduct<El, 2, 1, 4, 4> {};
@@ -426,7 +420,7 @@ struct HeadProduct {
 template <class El, bool DIRECT, int BQ>
 __global__ void __launch_bounds__(kTileThreads, 2)
 k_head_dh(const HeadProduct g) {
-  using T = Tiles<El, kCols, kRows, DIRECT, false, BQ>;
+  using T = Tiles<El, kCols, kRows, DIRECT, BQ>;
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
@@ -464,7 +458,7 @@ k_head_dh(const HeadProduct g) {
 template <class El>
 __global__ void __launch_bounds__(kTileThreads, 2)
 k_head_dw(const HeadProduct g) {
-  using T = Tiles<El, kCols, kCols, true, false, 256>;
+  using T = Tiles<El, kCols, kCols, true, 256>;
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;

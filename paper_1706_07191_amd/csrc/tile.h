@@ -120,11 +120,15 @@ struct Stager {
   static __device__ __forceinline__ int mix(int row) { return (row & 3) | ((row >> 3) & 3) << 2; }
 
   // left: numbers of the contraction from this step on
+  __device__ __forceinline__ bool plain(int64_t left) const { return DIRECT && left >= kStepK && !ragged; }
+  // one of the kLoads parts of a plain step; the step is over with next()
+  __device__ __forceinline__ void load_part(char* tile, int wave, int i) const { load_to_lds(lds_address(tile) + 16 * (i * THREADS + 64 * wave), at + off[i]); }
+  __device__ __forceinline__ void next() { at += step; }
   __device__ __forceinline__ void load(char* tile, int tid, int wave, int64_t left) {
     const uint32_t dst = lds_address(tile);
-    if (DIRECT && left >= kStepK && !ragged) {
+    if (plain(left)) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) load_to_lds(dst + 16 * (i * THREADS + 64 * wave), at + off[i]);
+      for (int i = 0; i < kLoads; ++i) load_part(tile, wave, i);
     } else {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
@@ -144,22 +148,24 @@ struct Stager {
   }
 };
 
-// Fragments of 16 rows (columns) from `row` on: 16 bytes a lane of the half-step kk (kStepBytes / 2 of the contraction).
+// Where a lane reads fragments of 16 rows (columns) of a tile, 16 bytes of the half step kk (kStepBytes / 2 of the contraction): `first` (a multiple of
+// 128 rows, or of 16 N of them) is the wave's first row.  Tile row f of the wave is at this plus 16 f rows (kRows), or with f exchanged into it (kCols).
 template <Order O, int N>
-__device__ __forceinline__ int4v fragment(const char* tile, int row, int kk, int lane) {
-  if (O == kRows) {
-    const int r = row + (lane & 15), pc = (kk * 4 + (lane >> 4)) ^ (lane & 7);      // row is a multiple of 16
-    return *(const int4v*)(tile + r * kStepBytes + pc * 16);
-  } else {
-    const int g = lane >> 4, i = lane & 15, k = kk * 32 + 8 * g + (i >> 2);
-    const int pair = (row >> 4) ^ (((i >> 2) | g << 2) & (N / 16 - 1));
-    const char* at = tile + k * (N * 2) + pair * 32 + (i & 3) * 8;
-    typedef __attribute__((address_space(3))) short4v lds_short4;
-    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)at);
-    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at + 4 * N * 2));
-    const short8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    return __builtin_bit_cast(int4v, both);
-  }
+__device__ __forceinline__ uint32_t fragment_base(int first, int lane) {
+  const int g = lane >> 4, i = lane & 15;
+  if (O == kRows) return (first + i) * kStepBytes + ((g ^ (i & 7)) * 16);
+  const int mix = ((i >> 2) | g << 2) & (N / 16 - 1);
+  return (8 * g + (i >> 2)) * (N * 2) + (i & 3) * 8 + ((first >> 4) ^ mix) * 32;
+}
+template <Order O, int N>
+__device__ __forceinline__ int4v fragment(const char* tile, uint32_t base, int f, int kk) {
+  if (O == kRows) return *(const int4v*)(tile + (base ^ (kk * 64)) + f * 16 * kStepBytes);
+  const char* at = tile + (base ^ (f * 32)) + kk * 32 * (N * 2);
+  typedef __attribute__((address_space(3))) short4v lds_short4;
+  const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)at);
+  const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(at + 4 * N * 2));
+  const short8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return __builtin_bit_cast(int4v, both);
 }
 
 // Has a sum worked out here: left alone, the compiler puts the additions of a whole step behind its products and keeps all of them in registers.
@@ -198,17 +204,20 @@ __device__ __forceinline__ floatx4 mfma_wide(const Wide8& p, const Wide8& q) {
   return c;
 }
 
-// What a tile product of 16-bit numbers is made of.  EXACT: every step's sum starts from zero and is added in rounded fp32 (the instruction truncates;
-// over a long contraction that is a bias); otherwise the sum runs through the instructions.
-template <class El, int NP_, int NQ_, int WP_, int WQ_, Order OP, Order OQ, bool DIRECT, bool EXACT>
+// A tile product of 16-bit numbers.  A step is 2 NP slots, one for each tile row of a wave and half of the step; a slot is NQ instructions.
+// What a slot multiplies was read from LDS at least four slots before.  All of a step is read by slot 9 of 16: at slot 12 the
+// workgroup meets once, the next step's numbers, under way for a whole step, are there, the step after it is sent for into the buffer that has just been read,
+// and the first fragments of the next step are read while the last four slots multiply.  So no wave comes from the barrier with nothing to multiply.
+// 8192 x 57344 over 2048: 1.30 us a step against 1.9 where a step's fragments were read behind its barrier.
+template <class El, int NQ_, Order OP, Order OQ, bool DIRECT>
 struct TileProduct {
-  static constexpr int NP = NP_, NQ = NQ_, WP = WP_, WQ = WQ_;
+  static constexpr int NP = 8, NQ = NQ_, WP = 2, WQ = 4;
   static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
   static constexpr int kLds = 2 * (BP + BQ) * kStepBytes, kStepK = kStepBytes / El::kBytes;
 
   static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
-    constexpr int kHalf = (BP + BQ) * kStepBytes;
+    constexpr int kHalf = (BP + BQ) * kStepBytes, SLOTS = 2 * NP, MEET = SLOTS - 4;
     Stager<El, OP, BP, kThreads, DIRECT> sp;
     Stager<El, OQ, BQ, kThreads, DIRECT> sq;
     sp.init(P, p0, k0, tid);
@@ -218,70 +227,91 @@ struct TileProduct {
 #pragma unroll
       for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
     const int steps = (int)((k1 - k0 + kStepK - 1) / kStepK);
-    sp.load(lds, tid, wave, k1 - k0);
-    sq.load(lds + BP * kStepBytes, tid, wave, k1 - k0);
-    sp.store(lds, tid);
-    sq.store(lds + BP * kStepBytes, tid);
-    loads_done();
-    __syncthreads();
+    auto send = [&](int t) {
+      char* to = lds + (t & 1) * kHalf;
+      const int64_t left = k1 - k0 - (int64_t)t * kStepK;
+      sp.load(to, tid, wave, left);
+      sq.load(to + BP * kStepBytes, tid, wave, left);
+    };
+    auto keep = [&](int t) {
+      sp.store(lds + (t & 1) * kHalf, tid);
+      sq.store(lds + (t & 1) * kHalf + BP * kStepBytes, tid);
+    };
+    auto meet = [] {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int4v fp[8], fq[2][NQ];
+    uint32_t bp = fragment_base<OP, BP>(16 * wp * NP, lane), bq = fragment_base<OQ, BQ>(16 * wq * NQ, lane);
+    auto read_p = [&](const char* tile, int slot) { fp[slot & 7] = fragment<OP, BP>(tile, bp, slot & 7, slot >> 3); };
+    auto read_q = [&](const char* tile, int kk, int q) { fq[kk][q] = fragment<OQ, BQ>(tile + BP * kStepBytes, bq, q, kk); };
+    // the parts of a plain step, one a slot: sent all at once they would queue up before the memory unit, and the waves behind them
+    constexpr int PARTS = decltype(sp)::kLoads + decltype(sq)::kLoads;
+    auto send_part = [&](int t, int j) {
+      char* to = lds + (t & 1) * kHalf;
+      if (j < decltype(sp)::kLoads) sp.load_part(to, wave, j);
+      else if (j < PARTS) sq.load_part(to + BP * kStepBytes, wave, j - decltype(sp)::kLoads);
+    };
+    bool parts = false;          // the step after this one is being sent for in parts
+    if (steps == 0) return;
+    send(0);
+    keep(0);
+    if (steps > 1) {
+      send(1);
+      if (DIRECT) keep(1);
+    }
+    meet();
+    if (!DIRECT && steps > 1) keep(1);        // the pieces of step 1 have left their registers before those of step 2 come
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read_p(lds, i);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) read_q(lds, 0, q);
     for (int t = 0; t < steps; ++t) {
-      const int cur = (t & 1) * kHalf, nxt = kHalf - cur;
-      if (t + 1 < steps) {
-        const int64_t left = k1 - k0 - (int64_t)(t + 1) * kStepK;
-        sp.load(lds + nxt, tid, wave, left);
-        sq.load(lds + nxt + BP * kStepBytes, tid, wave, left);
-      }
-      const char *tp = lds + cur, *tq = tp + BP * kStepBytes;
-      int4v fq[2][NQ];
+      const char *cur = lds + (t & 1) * kHalf, *nxt = lds + kHalf - (t & 1) * kHalf;
+      const bool more = t + 1 < steps, sends = t + 2 < steps;
+      asm volatile("" : "+v"(bp), "+v"(bq));      // addresses are worked out from these where they are used, not kept
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) fq[kk][q] = fragment<OQ, BQ>(tq, 16 * (wq * NQ + q), kk, lane);
-      int4v f0 = fragment<OP, BP>(tp, 16 * wp * NP, 0, lane), f1 = fragment<OP, BP>(tp, 16 * wp * NP, 1, lane);
-      floatx4 d[2][NQ];
-      // The fragments of the next tile row are on their way while this one is multiplied (and with EXACT a sum is added once the products of the next
-      // tile row are issued); the fences keep the compiler from fetching all rows at once, which it has no registers for.
-#pragma unroll
-      for (int p = 0; p < NP + (EXACT ? 1 : 0); ++p) {
-        if (p < NP) {
-          const int4v c0 = f0, c1 = f1;
-          if (p + 1 < NP) {
-            f0 = fragment<OP, BP>(tp, 16 * (wp * NP + p + 1), 0, lane);
-            f1 = fragment<OP, BP>(tp, 16 * (wp * NP + p + 1), 1, lane);
-          }
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            if (EXACT) d[p & 1][q] = mfma16<El>(c0, fq[0][q], floatx4{0.f, 0.f, 0.f, 0.f});
-            else acc[p][q] = mfma16<El>(c0, fq[0][q], acc[p][q]);
-          }
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            if (EXACT) d[p & 1][q] = mfma16<El>(c1, fq[1][q], d[p & 1][q]);
-            else acc[p][q] = mfma16<El>(c1, fq[1][q], acc[p][q]);
+      for (int s = 0; s < SLOTS; ++s) {
+        if (s < 4) {
+          read_p(cur, s + 4);
+          if (s < NQ) read_q(cur, 1, s);
+        } else if (s < 6) {
+          read_p(cur, 2 * s);
+          read_p(cur, 2 * s + 1);
+        } else if (s < 10) {
+          read_p(cur, s + 6);
+        } else if (s == MEET) {
+          meet();
+          const int64_t left = k1 - k0 - (int64_t)(t + 2) * kStepK;
+          parts = sends && sp.plain(left) && sq.plain(left);
+          if (sends && !parts) send(t + 2);
+        }
+        if (parts) {
+          if (s >= MEET) send_part(t + 2, s - MEET);
+          else if (s < PARTS - 4) send_part(t + 1, s + 4);
+          if (s == PARTS - 5) {
+            sp.next();
+            sq.next();
+            parts = false;
           }
         }
-        if (EXACT && p > 0) {
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[p - 1][q][r] += d[(p - 1) & 1][q][r];
-            settle(acc[p - 1][q]);
-          }
+        if (s >= MEET && more) {
+          read_p(nxt, s - MEET);
+          if (s - MEET < NQ) read_q(nxt, 0, s - MEET);
         }
+        if (!DIRECT && s == SLOTS - 1 && sends) keep(t + 2);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) acc[s & 7][q] = mfma16<El>(fp[s & 7], fq[s >> 3][q], acc[s & 7][q]);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (!DIRECT && t + 1 < steps) {
-        sp.store(lds + nxt, tid);
-        sq.store(lds + nxt + BP * kStepBytes, tid);
-      }
-      loads_done();
-      __syncthreads();
     }
+    meet();          // LDS is free for what follows
   }
 };
 
 // The same for up to 64 rows of Q, where the read of P is what it takes: no LDS, a wave has 16 NP rows of P and all rows of Q, and both go from memory (Q
-// from the caches) to the instruction's registers, U steps ahead.  Rows at any alignment.  Sums start from zero every step.
+// from the caches) to the instruction's registers, U steps ahead.  Rows at any alignment.
 template <class El, int NP_, int NQ_, int WP_, int U>
 struct RowsProduct {
   static constexpr int NP = NP_, NQ = NQ_, WP = WP_, WQ = 1;
@@ -323,10 +353,8 @@ struct RowsProduct {
       for (int p = 0; p < NP; ++p)
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          floatx4 d = mfma16<El>(__builtin_bit_cast(int4v, x.p[p][0]), __builtin_bit_cast(int4v, x.q[q][0]), floatx4{0.f, 0.f, 0.f, 0.f});
-          d = mfma16<El>(__builtin_bit_cast(int4v, x.p[p][1]), __builtin_bit_cast(int4v, x.q[q][1]), d);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[p][q][r] += d[r];
+          const floatx4 d = mfma16<El>(__builtin_bit_cast(int4v, x.p[p][0]), __builtin_bit_cast(int4v, x.q[q][0]), acc[p][q]);
+          acc[p][q] = mfma16<El>(__builtin_bit_cast(int4v, x.p[p][1]), __builtin_bit_cast(int4v, x.q[q][1]), d);
         }
     };
     Step x[U];
