@@ -44,134 +44,312 @@ __device__ __forceinline__ void put_four(void* C, int64_t at, int64_t left, int 
   }
 }
 
-// NP x NQ tiles a wave, WP x WQ waves; P = B (columns of C), Q = A (rows of C).  Scales of a step come in beside its numbers.
-template <int NP, int NQ, int WP, int WQ, bool PER_ROW, bool DIRECT, bool WIDE>
-__global__ void __launch_bounds__(64 * WP * WQ, 2)
+// Whether an fp32 number is a power of two in the range of an 8-bit exponent
+__device__ __forceinline__ bool is_power(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return (b & 0x807fffffu) == 0 && b - 1u < 0x7f7fffffu;
+}
+
+// 256 columns of C (B's rows, P) x 64 NQ rows (A's, Q): eight waves of 8 x NQ tiles.  A block of the contraction is a step of eight groups: two tile rows
+// times half of the tile columns, NQ instructions.  Two tile rows are read from LDS two groups before they are multiplied; a half of A's fragments is
+// replaced as soon as its last group is issued.  So a step needs no registers for the next one beside its own, and still no wave comes from
+// the barrier (before the last two groups) with nothing to multiply.  The step after next is sent for in parts from the barrier on, see TileProduct.
+// Where all scales of the tile's rows are powers of two, as those of the casts are, the instruction multiplies by them and adds to the sums; otherwise (and
+// WIDE) the results of a group are scaled and added between the instructions of the next.  The workgroup looks through them while its first two
+// steps are on their way.  8192 x 8192 x 8192: XXX us and YYY.
+template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
+__global__ void __launch_bounds__(512, 2)
 k_tiles_e4m3(const E4m3Args g) {
-  constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, THREADS = 64 * WP * WQ, kHalf = (BP + BQ) * kStepBytes;
+  constexpr int NP = 8, WP = 2, WQ = 4, BP = 16 * NP * WP, BQ = 16 * NQ * WQ, THREADS = 64 * WP * WQ, kHalf = (BP + BQ) * kStepBytes, QH = NQ / 2;
   constexpr int kPScales = PER_ROW ? BP : BP / kBlock;
-  static_assert(BP % kBlock == 0 && (16 * NP % kBlock == 0 || kBlock % (16 * NP) == 0) && BP + BQ <= THREADS * 2, "");
+  static_assert(16 * NP == kBlock && BQ + kPScales <= THREADS, "");
   __shared__ __attribute__((aligned(1024))) char lds[2 * kHalf];
-  __shared__ float scales[2][BQ + kPScales];
+  __shared__ __attribute__((aligned(16))) float scales[2][BQ + (PER_ROW ? BP : 4)];
+  __shared__ int flags[8];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_n, g.tiles_m, 4, &tp, &tq)) return;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_n, g.tiles_m, 8, &tp, &tq)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
   const int64_t p0 = tp * BP, q0 = tq * BQ;
-  const int b0 = blockIdx.y * g.per_split, b1 = b0 + g.per_split < g.blocks ? b0 + g.per_split : g.blocks;
+  const int b0 = blockIdx.y * g.per_split, b1 = b0 + g.per_split < g.blocks ? b0 + g.per_split : g.blocks, whole = (int)(g.k / kBlock);
+  const int steps = (b1 < whole ? b1 : whole) - b0;         // whole blocks; a last one that is not follows by itself
   Stager<E4m3, kRows, BP, THREADS, DIRECT> sp;
   Stager<E4m3, kRows, BQ, THREADS, DIRECT> sq;
   sp.init(g.B, p0, (int64_t)b0 * kBlock, tid);
   sq.init(g.A, q0, (int64_t)b0 * kBlock, tid);
-  // which scale this thread fetches for each step, up to two of them
-  const float* from[2];
+  // Addresses that are needed once a step are worked out from the thread's index there: kept, they would cost registers that the tiles need.
+  auto thread = [] {
+    int x = threadIdx.x;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  const float *sa0 = (const float*)scalar((int64_t)(g.SA + q0 * g.blocks + b0)), *sb0 = (const float*)scalar((int64_t)(g.SB + (PER_ROW ? p0 : p0 / kBlock) * g.blocks + b0));
+  const int last_a = (int)(g.A.n - q0 < BQ ? g.A.n - q0 : BQ) - 1;
+  const int last_b = (int)(PER_ROW ? (g.B.n - p0 < BP ? g.B.n - p0 : BP) : (g.B.n - p0 > kBlock ? 2 : 1)) - 1;
+  // a step's scales, one a thread, straight into LDS; a wave's are all of A or all of B
+  auto send_scales = [&](int t) {
+    const int s = thread();
+    const uint32_t to = lds_address(&scales[t & 1][64 * wave]);
+    if (s < BQ) load4_to_lds(to, sa0 + (int64_t)((s < last_a ? s : last_a) * g.blocks + t));
+    else if (s < BQ + kPScales) load4_to_lds(to, sb0 + (int64_t)((s - BQ < last_b ? s - BQ : last_b) * g.blocks + t));
+  };
+  constexpr int PARTS = decltype(sp)::kLoads + decltype(sq)::kLoads;
+  auto send_part = [&](int t, int j) {
+    char* to = lds + (t & 1) * kHalf;
+    if (j < decltype(sp)::kLoads) sp.load_part(to, wave, j);
+    else if (j < PARTS) sq.load_part(to + BP * kStepBytes, wave, j - decltype(sp)::kLoads);
+  };
+  auto fetch = [&] {
+    sp.fetch();
+    sq.fetch();
+  };
+  auto keep = [&](int t) {
+    sp.store(lds + (t & 1) * kHalf, tid);
+    sq.store(lds + (t & 1) * kHalf + BP * kStepBytes, tid);
+  };
+  auto send = [&](int t) {             // all of a step at once
+    if (DIRECT) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int s = tid + i * THREADS;
-    int64_t row = 0;
-    if (s < BQ) row = q0 + s < g.A.n ? q0 + s : g.A.n - 1;
-    else if (PER_ROW) row = p0 + s - BQ < g.B.n ? p0 + s - BQ : g.B.n - 1;
-    else row = p0 / kBlock + s - BQ < (g.B.n - 1) / kBlock ? p0 / kBlock + s - BQ : (g.B.n - 1) / kBlock;
-    from[i] = (s < BQ ? g.SA : g.SB) + row * g.blocks;
-  }
+      for (int j = 0; j < PARTS; ++j) send_part(t, j);
+      sp.next();
+      sq.next();
+    } else {
+      fetch();
+      keep(t);
+    }
+  };
+  auto meet = [] {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
   floatx4 acc[NP][NQ];
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
     for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
-  auto fetch = [&](int b, float (&v)[2]) {
+  uint32_t bp = fragment_base<kRows, BP>(16 * wp * NP, lane), bq = fragment_base<kRows, BQ>(16 * wq * NQ, lane);
+  int4v fp[2][2][2], fq[NQ][2];        // [pair & 1][row of the pair][half], [column][half]
+  auto read_pair = [&](int t, int pair) {
+    const char* tile = lds + (t & 1) * kHalf;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (tid + i * THREADS < BQ + kPScales) v[i] = from[i][b];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fp[pair & 1][i][h] = fragment<kRows, BP>(tile, bp, 2 * pair + i, h);
   };
-  auto keep = [&](int buffer, const float (&v)[2]) {
+  auto read_half = [&](int t, int half) {
+    const char* tile = lds + (t & 1) * kHalf + BP * kStepBytes;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (tid + i * THREADS < BQ + kPScales) scales[buffer][tid + i * THREADS] = v[i];
+    for (int i = 0; i < QH; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fq[half * QH + i][h] = fragment<kRows, BQ>(tile, bq, half * QH + i, h);
   };
-  const uint32_t bb = fragment_base<kRows, BP>(16 * wp * NP, lane), ba = fragment_base<kRows, BQ>(16 * wq * NQ, lane);
-  float v[2];
-  fetch(b0, v);
-  sp.load(lds, tid, wave, g.k - (int64_t)b0 * kBlock);
-  sq.load(lds + BP * kStepBytes, tid, wave, g.k - (int64_t)b0 * kBlock);
-  sp.store(lds, tid);
-  sq.store(lds + BP * kStepBytes, tid);
-  keep(0, v);
-  loads_done();
-  __syncthreads();
-  for (int b = b0; b < b1; ++b) {
-    const int buffer = (b - b0) & 1, cur = buffer * kHalf, nxt = kHalf - cur;
-    if (b + 1 < b1) {
-      const int64_t left = g.k - (int64_t)(b + 1) * kBlock;
-      fetch(b + 1, v);
-      sp.load(lds + nxt, tid, wave, left);
-      sq.load(lds + nxt + BP * kStepBytes, tid, wave, left);
+  if (steps > 0) {
+    send_scales(0);
+    send(0);
+  }
+  if (steps > 1) {
+    send_scales(1);
+    send(1);
+  }
+  bool powers = !WIDE;
+  if (!WIDE) {
+    const int na = (last_a + 1) * g.blocks, nb = (last_b + 1) * g.blocks;
+    for (int i = tid; i < na; i += THREADS) powers &= is_power(sa0[i - b0]);
+    for (int i = tid; i < nb; i += THREADS) powers &= is_power(sb0[i - b0]);
+    if (tid < 8) flags[tid] = 1;
+    __syncthreads();
+    if (!__all(powers) && lane == 0) flags[wave] = 0;
+  }
+  meet();
+  if (!WIDE) {
+    int all = 1;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) all &= flags[w];
+    powers = __builtin_amdgcn_readfirstlane(all) != 0;
+  }
+  if (steps > 0) {
+    read_pair(0, 0);
+    read_half(0, 0);
+  }
+  // what a group does beside its products
+  auto around = [&](int t, int G) {
+    const int pair = G >> 1, half = G & 1;
+    const bool more = t + 1 < steps, sends = t + 2 < steps;
+    if (G == 0) read_half(t, 1);
+    if (half == 0 && pair < 3) read_pair(t, pair + 1);
+    if (G == 6) {
+      meet();
+      if (sends) send_scales(t + 2);
+      if (more) read_pair(t + 1, 0);
+      if (!DIRECT && sends) fetch();
     }
-    const char *tb = lds + cur, *ta = tb + BP * kStepBytes;
-    int4v f0[NQ], f1[NQ];
-    Wide8 fw[NQ];
-    float sa[NQ];
+    if (G == 7 && more) read_half(t + 1, 0);
+    if (DIRECT) {
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      f0[q] = fragment<kRows, BQ>(ta, ba, q, 0);
-      f1[q] = fragment<kRows, BQ>(ta, ba, q, 1);
-      if (WIDE) fw[q] = widen(f0[q], f1[q]);
-      sa[q] = scales[buffer][16 * (wq * NQ + q) + (lane & 15)];
-      if (!PER_ROW && 16 * NP <= kBlock) sa[q] *= scales[buffer][BQ + wp * 16 * NP / kBlock];
-    }
-    // The fragments of the next tile row are on their way while this one is multiplied, and a sum is added once the products of the next tile row are
-    // issued; the fences keep the compiler from fetching all rows at once, which it has no registers for.
-    int4v e0 = fragment<kRows, BP>(tb, bb, 0, 0), e1 = fragment<kRows, BP>(tb, bb, 0, 1);
-    floatx4 d[2][NQ], sb[2];
-    sb[0] = sb[1] = floatx4{1.f, 1.f, 1.f, 1.f};
-#pragma unroll
-    for (int p = 0; p <= NP; ++p) {
-      if (p < NP) {
-        const int4v c0 = e0, c1 = e1;
-        if (p + 1 < NP) {
-          e0 = fragment<kRows, BP>(tb, bb, p + 1, 0);
-          e1 = fragment<kRows, BP>(tb, bb, p + 1, 1);
-        }
-        if (PER_ROW) sb[p & 1] = *(const floatx4*)&scales[buffer][BQ + 16 * (wp * NP + p) + 4 * (lane >> 4)];
-        if (WIDE) {
-          const Wide8 cw = widen(c0, c1);
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) d[p & 1][q] = mfma_wide(cw, fw[q]);
-        } else {
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) d[p & 1][q] = mfma8(c0, c1, f0[q], f1[q], floatx4{0.f, 0.f, 0.f, 0.f});
-        }
+      for (int j = 0; j < 2; ++j) {
+        if (G >= 6 && sends) send_part(t + 2, 2 * (G - 6) + j);
+        if (G < 6 && 2 * G + 4 + j < PARTS && t > 0 && more) send_part(t + 1, 2 * G + 4 + j);
       }
-      if (p > 0) {
+      if (G == 5 && t > 0 && more) {
+        sp.next();
+        sq.next();
+      }
+    }
+    if (!DIRECT && G == 7 && sends) keep(t + 2);
+  };
+  // the block that the contraction ends in, behind all others
+  const bool ends = b1 > whole && g.k % kBlock != 0;
+  auto stage_end = [&] {
+    meet();
+    const int64_t left = g.k - (int64_t)whole * kBlock;
+    sp.load(lds, tid, wave, left);
+    sq.load(lds + BP * kStepBytes, tid, wave, left);
+    sp.store(lds, tid);
+    sq.store(lds + BP * kStepBytes, tid);
+    const int s = thread(), at = whole - b0;
+    if (s < BQ) scales[0][s] = sa0[(int64_t)((s < last_a ? s : last_a) * g.blocks + at)];
+    else if (s < BQ + kPScales) scales[0][s] = sb0[(int64_t)((s - BQ < last_b ? s - BQ : last_b) * g.blocks + at)];
+    meet();
+    read_half(0, 0);
+    read_half(0, 1);
+  };
+  auto end = [&] {
+    stage_end();
+#pragma unroll
+    for (int pair = 0; pair < 4; ++pair) {
+      read_pair(0, pair);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        floatx4 sb = {1.f, 1.f, 1.f, 1.f};
+        if (PER_ROW) sb = *(const floatx4*)&scales[0][BQ + 16 * (wp * NP + 2 * pair + i) + 4 * (lane >> 4)];
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
+          const float s = scales[0][16 * (wq * NQ + q) + (lane & 15)] * (PER_ROW ? 1.f : scales[0][BQ + wp]);
+          floatx4 d;
+          if (WIDE) d = mfma_wide(widen(fp[pair & 1][i][0], fp[pair & 1][i][1]), widen(fq[q][0], fq[q][1]));
+          else d = mfma8(fp[pair & 1][i][0], fp[pair & 1][i][1], fq[q][0], fq[q][1], floatx4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[p - 1][q][r] += d[(p - 1) & 1][q][r] * (PER_ROW ? sa[q] * sb[(p - 1) & 1][r] : sa[q]);
-          settle(acc[p - 1][q]);
+          for (int r = 0; r < 4; ++r) acc[2 * pair + i][q][r] += d[r] * (s * sb[r]);
+          settle(acc[2 * pair + i][q]);
         }
       }
+    }
+  };
+  auto put = [&] {
+    char* C = (char*)g.C + (g.splits > 1 ? (int64_t)blockIdx.y * g.A.n * g.B.n * 4 : 0);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int64_t m = q0 + 16 * (wq * NQ + q) + (lane & 15);
+      if (m >= g.A.n) continue;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int64_t n = p0 + 16 * (wp * NP + p) + 4 * (lane >> 4);
+        if (n < g.B.n) put_four(C, m * g.ldc + n, g.B.n - n, g.dtype, acc[p][q]);
+      }
+    }
+  };
+  if constexpr (!WIDE) {
+    if (powers) {
+#pragma unroll 1
+      for (int t = 0; t < steps; ++t) {
+        asm volatile("" : "+v"(bp), "+v"(bq));      // addresses are worked out from these where they are used, not kept
+        // exponents of the step's scales: of the lane's row of each tile column, and of each tile row
+        uint32_t ea = 0, eb[2] = {0u, 0u};
+        const float* s = scales[t & 1];
+        const int l = thread() & 15;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) ea |= __float_as_uint(s[16 * (wq * NQ + q) + l]) >> 23 << (8 * q);
+        if (PER_ROW) {
+#pragma unroll
+          for (int p = 0; p < NP; ++p) eb[p / 4] |= __float_as_uint(s[BQ + 16 * (wp * NP + p) + l]) >> 23 << (8 * (p & 3));
+        } else {
+          eb[0] = eb[1] = (__float_as_uint(s[BQ + wp]) >> 23) * 0x01010101u;        // a wave's 128 rows of B are one block
+        }
+#define BRSVD_SCALED(I, J)                                                                                                                            \
+  {                                                                                                                                                   \
+    constexpr int p = 2 * (G >> 1) + I, q = (G & 1) * QH + J;                                                                                         \
+    acc[p][q] = mfma8_scaled<(p & 3), q>(fp[(G >> 1) & 1][I][0], fp[(G >> 1) & 1][I][1], fq[q][0], fq[q][1], acc[p][q], (int)eb[p / 4], (int)ea);     \
+    settle(acc[p][q]);                                                                                                                                \
+  }
+#define BRSVD_GROUP(GROUP)                                                                                                                            \
+  {                                                                                                                                                   \
+    constexpr int G = GROUP;                                                                                                                          \
+    around(t, G);                                                                                                                                     \
+    BRSVD_SCALED(0, 0)                                                                                                                                \
+    BRSVD_SCALED(1, 0)                                                                                                                                \
+    if constexpr (QH == 2) {                                                                                                                          \
+      BRSVD_SCALED(0, (QH - 1))                                                                                                                       \
+      BRSVD_SCALED(1, (QH - 1))                                                                                                                       \
+    }                                                                                                                                                 \
+    __builtin_amdgcn_sched_barrier(0);                                                                                                                \
+  }
+        BRSVD_GROUP(0)
+        BRSVD_GROUP(1)
+        BRSVD_GROUP(2)
+        BRSVD_GROUP(3)
+        BRSVD_GROUP(4)
+        BRSVD_GROUP(5)
+        BRSVD_GROUP(6)
+        BRSVD_GROUP(7)
+#undef BRSVD_GROUP
+#undef BRSVD_SCALED
+      }
+      if (ends) end();
+      put();
+      return;
+    }
+  }
+#pragma unroll 1
+  for (int t = 0; t < steps; ++t) {
+    asm volatile("" : "+v"(bp), "+v"(bq));
+    floatx4 d[2][QH], sb[2], sb_last[2];
+    float sa[NQ];
+    Wide8 wp8[2], wq8[NQ];
+    const int l = thread();
+    const float w = PER_ROW ? 1.f : scales[t & 1][BQ + wp];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) sa[q] = scales[t & 1][16 * (wq * NQ + q) + (l & 15)] * w;
+    // the result of the group before, of row i of its pair and column j of its half
+    auto add = [&](int group, int i, int j) {
+      const int p = 2 * (group >> 1) + i, q = (group & 1) * QH + j;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[p][q][r] += d[i][j][r] * (PER_ROW ? sa[q] * sb_last[i][r] : sa[q]);
+      settle(acc[p][q]);
+    };
+#pragma unroll
+    for (int G = 0; G < 8; ++G) {
+      const int pair = G >> 1, half = G & 1;
+      if (PER_ROW && half == 0)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sb[i] = *(const floatx4*)&scales[t & 1][BQ + 16 * (wp * NP + 2 * pair + i) + (l & 48) / 4];
+      around(t, G);
+      if (WIDE) {
+        if (pair == 0)
+#pragma unroll
+          for (int j = 0; j < QH; ++j) wq8[half * QH + j] = widen(fq[half * QH + j][0], fq[half * QH + j][1]);
+        if (half == 0)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) wp8[i] = widen(fp[pair & 1][i][0], fp[pair & 1][i][1]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < QH; ++j) {
+          if (G > 0) add(G - 1, i, j);
+          const int q = half * QH + j;
+          if (WIDE) d[i][j] = mfma_wide(wp8[i], wq8[q]);
+          else d[i][j] = mfma8(fp[pair & 1][i][0], fp[pair & 1][i][1], fq[q][0], fq[q][1], floatx4{0.f, 0.f, 0.f, 0.f});
+        }
+      if (PER_ROW && half == 0) sb_last[0] = sb[0], sb_last[1] = sb[1];
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (b + 1 < b1) {
-      if (!DIRECT) {
-        sp.store(lds + nxt, tid);
-        sq.store(lds + nxt + BP * kStepBytes, tid);
-      }
-      keep(buffer ^ 1, v);
-    }
-    loads_done();
-    __syncthreads();
-  }
-  char* C = (char*)g.C + (g.splits > 1 ? (int64_t)blockIdx.y * g.A.n * g.B.n * 4 : 0);
 #pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const int64_t m = q0 + 16 * (wq * NQ + q) + (lane & 15);
-    if (m >= g.A.n) continue;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int64_t n = p0 + 16 * (wp * NP + p) + 4 * (lane >> 4);
-      if (n < g.B.n) put_four(C, m * g.ldc + n, g.B.n - n, g.dtype, acc[p][q]);
-    }
+      for (int j = 0; j < QH; ++j) add(7, i, j);
   }
+  if (ends) end();
+  put();
 }
 
 // C (m x n, type dtype) = sum of the splits' parts, in their order
@@ -366,7 +544,7 @@ static void launch_more(const E4m3Args& g, hipStream_t stream) {
 }
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
 static void launch_tiles(const E4m3Args& g, hipStream_t stream) {
-  hipLaunchKernelGGL((k_tiles_e4m3<8, NQ, 2, 4, PER_ROW, DIRECT, WIDE>), dim3(tile_workgroups(g.tiles_n, g.tiles_m), (unsigned)g.splits), dim3(512), 0, stream, g);
+  hipLaunchKernelGGL((k_tiles_e4m3<NQ, PER_ROW, DIRECT, WIDE>), dim3(tile_workgroups(g.tiles_n, g.tiles_m), (unsigned)g.splits), dim3(512), 0, stream, g);
 }
 template <bool PER_ROW, bool DIRECT>
 static void launch_tiles(const E4m3Args& g, int bq, bool wide, hipStream_t stream) {

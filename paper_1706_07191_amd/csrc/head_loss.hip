@@ -61,7 +61,7 @@ k_head_lse(const HeadArgs g) {
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tv, tt;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 4, &tv, &tt)) return;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 8, &tv, &tt)) return;
   floatx4 acc[NP][NQ];
   const int64_t v0 = tv * T::BP, t0 = tt * BQ;
   T::run(acc, g.W, v0, g.H, t0, 0, g.dim, lds);
@@ -358,7 +358,7 @@ k_head_grad(const HeadArgs g) {
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tv, tt;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 4, &tv, &tt)) return;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 8, &tv, &tt)) return;
   const int64_t count = g.meta->count, p0 = tv * T::BP, t0 = tt * BQ;
   if (t0 >= count) return;
   Operand H = g.H;
@@ -424,7 +424,7 @@ k_head_dh(const HeadProduct g) {
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 4, &tp, &tq)) return;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
   Operand Q = g.Q;
   Q.n = g.meta->count;
   const int64_t p0 = tp * kTileP, q0 = tq * BQ, k0 = blockIdx.y * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
@@ -462,7 +462,7 @@ k_head_dw(const HeadProduct g) {
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 4, &tp, &tq)) return;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
   const int64_t p0 = tp * kTileP, q0 = tq * 256;
   floatx4 acc[NP][NQ];
   T::run(acc, g.P, p0, g.Q, q0, 0, g.meta->count, lds);

@@ -55,8 +55,21 @@ static __device__ const uint4 k_zero_piece = {0u, 0u, 0u, 0u};
 __device__ __forceinline__ void load_to_lds(uint32_t dst, const char* src) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
 }
+// The same from `off` bytes (below 2^31) behind an address that all lanes share.
+__device__ __forceinline__ void load_to_lds(uint32_t dst, const char* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(dst), "s"(base), "v"(off) : "memory");
+}
+// 4 bytes per lane, to `dst` + 4 lane.
+__device__ __forceinline__ void load4_to_lds(uint32_t dst, const void* src) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
+}
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// The same value in scalar registers, for one that all lanes share.
+__device__ __forceinline__ int64_t scalar(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const lds_char*)p; }
 
 // 16 bytes from `src`, of which the first `valid` are there; the others are zero.
@@ -101,6 +114,8 @@ struct Stager {
       step = (int64_t)kStepK * op.ld;
       ragged = left < N && left % 8 != 0;
     }
+    at = (const char*)scalar((int64_t)at);
+    step = scalar(step);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int slot = i * THREADS + tid, row = slot / kPerRow, pc = slot % kPerRow;
@@ -122,8 +137,15 @@ struct Stager {
   // left: numbers of the contraction from this step on
   __device__ __forceinline__ bool plain(int64_t left) const { return DIRECT && left >= kStepK && !ragged; }
   // one of the kLoads parts of a plain step; the step is over with next()
-  __device__ __forceinline__ void load_part(char* tile, int wave, int i) const { load_to_lds(lds_address(tile) + 16 * (i * THREADS + 64 * wave), at + off[i]); }
+  __device__ __forceinline__ void load_part(char* tile, int wave, int i) const { load_to_lds(lds_address(tile) + 16 * (i * THREADS + 64 * wave), (const char*)scalar((int64_t)at), off[i]); }
   __device__ __forceinline__ void next() { at += step; }
+  // a whole step into registers
+  __device__ __forceinline__ void fetch() {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      if (!DIRECT) reg[i] = piece_of<El::kBytes>(at + off[i], 16);
+    next();
+  }
   __device__ __forceinline__ void load(char* tile, int tid, int wave, int64_t left) {
     const uint32_t dst = lds_address(tile);
     if (plain(left)) {
@@ -168,7 +190,8 @@ __device__ __forceinline__ int4v fragment(const char* tile, uint32_t base, int f
   return __builtin_bit_cast(int4v, both);
 }
 
-// Has a sum worked out here: left alone, the compiler puts the additions of a whole step behind its products and keeps all of them in registers.
+// Has a sum worked out here: left alone, the compiler moves what only the next step needs behind everything else, out of the order that the reads from
+// LDS go by, and keeps all operands in registers until then.
 __device__ __forceinline__ void settle(floatx4& x) { asm volatile("" : "+v"(x)); }
 
 template <class El>
@@ -182,6 +205,12 @@ __device__ __forceinline__ floatx4 mfma8(int4v p0, int4v p1, int4v q0, int4v q1,
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 0, 0, 0, 0, 0, 0);
 }
 
+// The same with a power of two for each row of P and of Q, added to c: byte PB of sp and QB of sq are exponents (bias 127) for the row of the lane.
+template <int PB, int QB>
+__device__ __forceinline__ floatx4 mfma8_scaled(int4v p0, int4v p1, int4v q0, int4v q1, floatx4 c, int sp, int sq) {
+  const int8v p = {p0[0], p0[1], p0[2], p0[3], p1[0], p1[1], p1[2], p1[3]}, q = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 0, 0, PB, sp, QB, sq);
+}
 // The same through fp16, which holds every e4m3 number: products exact, sums in fp32.  mfma8 keeps less: of eight neighbouring products the instruction
 // cuts off what is below 2^-13 of the largest (measured; sums of different eights keep 24 bits).
 struct Wide8 { f16x8 x[4]; };
@@ -302,7 +331,10 @@ struct TileProduct {
         }
         if (!DIRECT && s == SLOTS - 1 && sends) keep(t + 2);
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) acc[s & 7][q] = mfma16<El>(fp[s & 7], fq[s >> 3][q], acc[s & 7][q]);
+        for (int q = 0; q < NQ; ++q) {
+          acc[s & 7][q] = mfma16<El>(fp[s & 7], fq[s >> 3][q], acc[s & 7][q]);
+          settle(acc[s & 7][q]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -387,12 +419,12 @@ template <class El> __device__ __forceinline__ float from16(uint16_t x) {
 
 // Tiles of a np x nq grid (np along P) to workgroups: workgroups b, b + 8, b + 16 ... share an XCD and its L2, so each XCD gets a run of tiles, and a run
 // goes through `band` rows of the grid at a time.  Returns false for workgroups beyond the grid (the grid is rounded up to eight).
-__device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np, int64_t nq, int band, int64_t* tp, int64_t* tq) {
-  const int64_t all = np * nq, per = (all + 7) / 8, i = (int64_t)(b & 7) * per + (b >> 3);
+__device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64_t nq_, unsigned band, int64_t* tp, int64_t* tq) {
+  const unsigned np = (unsigned)np_, nq = (unsigned)nq_, all = np * nq, per = (all + 7) / 8, i = (b & 7) * per + (b >> 3);
   if ((b >> 3) >= per || i >= all) return false;
-  const int64_t group = i / (band * nq), first = group * band, height = np - first < band ? np - first : band, in = i - group * band * nq;
-  *tp = first + in % height;
-  *tq = in / height;
+  const unsigned group = i / (band * nq), first = group * band, height = np - first < band ? np - first : band, in = i - group * band * nq;
+  *tp = __builtin_amdgcn_readfirstlane(first + in % height);
+  *tq = __builtin_amdgcn_readfirstlane(in / height);
   return true;
 }
 inline unsigned tile_workgroups(int64_t np, int64_t nq) { return (unsigned)(8 * ((np * nq + 7) / 8)); }
