@@ -54,9 +54,8 @@ __device__ __forceinline__ bool is_power(float x) {
 // times half of the tile columns, NQ instructions.  Two tile rows are read from LDS two groups before they are multiplied; a half of A's fragments is
 // replaced as soon as its last group is issued.  So a step needs no registers for the next one beside its own, and still no wave comes from
 // the barrier (before the last two groups) with nothing to multiply.  The step after next is sent for in parts from the barrier on, see TileProduct.
-// Where all scales of the tile's rows are powers of two, as those of the casts are, the instruction multiplies by them and adds to the sums; otherwise (and
-// WIDE) the results of a group are scaled and added between the instructions of the next.  The workgroup looks through them while its first two
-// steps are on their way.  8192 x 8192 x 8192: XXX us and YYY.
+// As long as a wave's scales of a step are powers of two, as those of the casts are, the instruction multiplies by them and adds to the sums; from the
+// first step where they are not (and WIDE) the results of a group are scaled and added between the instructions of the next.
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
 __global__ void __launch_bounds__(512, 2)
 k_tiles_e4m3(const E4m3Args g) {
@@ -65,7 +64,6 @@ k_tiles_e4m3(const E4m3Args g) {
   static_assert(16 * NP == kBlock && BQ + kPScales <= THREADS, "");
   __shared__ __attribute__((aligned(1024))) char lds[2 * kHalf];
   __shared__ __attribute__((aligned(16))) float scales[2][BQ + (PER_ROW ? BP : 4)];
-  __shared__ int flags[8];
   int64_t tp, tq;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_n, g.tiles_m, 8, &tp, &tq)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
@@ -151,22 +149,7 @@ k_tiles_e4m3(const E4m3Args g) {
     send_scales(1);
     send(1);
   }
-  bool powers = !WIDE;
-  if (!WIDE) {
-    const int na = (last_a + 1) * g.blocks, nb = (last_b + 1) * g.blocks;
-    for (int i = tid; i < na; i += THREADS) powers &= is_power(sa0[i - b0]);
-    for (int i = tid; i < nb; i += THREADS) powers &= is_power(sb0[i - b0]);
-    if (tid < 8) flags[tid] = 1;
-    __syncthreads();
-    if (!__all(powers) && lane == 0) flags[wave] = 0;
-  }
   meet();
-  if (!WIDE) {
-    int all = 1;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) all &= flags[w];
-    powers = __builtin_amdgcn_readfirstlane(all) != 0;
-  }
   if (steps > 0) {
     read_pair(0, 0);
     read_half(0, 0);
@@ -235,36 +218,35 @@ k_tiles_e4m3(const E4m3Args g) {
       }
     }
   };
-  auto put = [&] {
-    char* C = (char*)g.C + (g.splits > 1 ? (int64_t)blockIdx.y * g.A.n * g.B.n * 4 : 0);
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      const int64_t m = q0 + 16 * (wq * NQ + q) + (lane & 15);
-      if (m >= g.A.n) continue;
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int64_t n = p0 + 16 * (wp * NP + p) + 4 * (lane >> 4);
-        if (n < g.B.n) put_four(C, m * g.ldc + n, g.B.n - n, g.dtype, acc[p][q]);
-      }
-    }
-  };
+  int t = 0;
   if constexpr (!WIDE) {
-    if (powers) {
 #pragma unroll 1
-      for (int t = 0; t < steps; ++t) {
-        asm volatile("" : "+v"(bp), "+v"(bq));      // addresses are worked out from these where they are used, not kept
-        // exponents of the step's scales: of the lane's row of each tile column, and of each tile row
-        uint32_t ea = 0, eb[2] = {0u, 0u};
-        const float* s = scales[t & 1];
-        const int l = thread() & 15;
+    for (; t < steps; ++t) {
+      asm volatile("" : "+v"(bp), "+v"(bq));      // addresses are worked out from these where they are used, not kept
+      // exponents of the step's scales: of the lane's row of each tile column, and of each tile row
+      uint32_t ea = 0, eb[2] = {0u, 0u};
+      bool powers = true;
+      const float* s = scales[t & 1];
+      const int l = thread() & 15;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) ea |= __float_as_uint(s[16 * (wq * NQ + q) + l]) >> 23 << (8 * q);
-        if (PER_ROW) {
+      for (int q = 0; q < NQ; ++q) {
+        const float x = s[16 * (wq * NQ + q) + l];
+        powers &= is_power(x);
+        ea |= __float_as_uint(x) >> 23 << (8 * q);
+      }
+      if (PER_ROW) {
 #pragma unroll
-          for (int p = 0; p < NP; ++p) eb[p / 4] |= __float_as_uint(s[BQ + 16 * (wp * NP + p) + l]) >> 23 << (8 * (p & 3));
-        } else {
-          eb[0] = eb[1] = (__float_as_uint(s[BQ + wp]) >> 23) * 0x01010101u;        // a wave's 128 rows of B are one block
+        for (int p = 0; p < NP; ++p) {
+          const float x = s[BQ + 16 * (wp * NP + p) + l];
+          powers &= is_power(x);
+          eb[p / 4] |= __float_as_uint(x) >> 23 << (8 * (p & 3));
         }
+      } else {
+        const float x = s[BQ + wp];                // a wave's 128 rows of B are one block
+        powers &= is_power(x);
+        eb[0] = eb[1] = (__float_as_uint(x) >> 23) * 0x01010101u;
+      }
+      if (!__all(powers)) break;
 #define BRSVD_SCALED(I, J)                                                                                                                            \
   {                                                                                                                                                   \
     constexpr int p = 2 * (G >> 1) + I, q = (G & 1) * QH + J;                                                                                         \
@@ -283,24 +265,20 @@ k_tiles_e4m3(const E4m3Args g) {
     }                                                                                                                                                 \
     __builtin_amdgcn_sched_barrier(0);                                                                                                                \
   }
-        BRSVD_GROUP(0)
-        BRSVD_GROUP(1)
-        BRSVD_GROUP(2)
-        BRSVD_GROUP(3)
-        BRSVD_GROUP(4)
-        BRSVD_GROUP(5)
-        BRSVD_GROUP(6)
-        BRSVD_GROUP(7)
+      BRSVD_GROUP(0)
+      BRSVD_GROUP(1)
+      BRSVD_GROUP(2)
+      BRSVD_GROUP(3)
+      BRSVD_GROUP(4)
+      BRSVD_GROUP(5)
+      BRSVD_GROUP(6)
+      BRSVD_GROUP(7)
 #undef BRSVD_GROUP
 #undef BRSVD_SCALED
-      }
-      if (ends) end();
-      put();
-      return;
     }
   }
 #pragma unroll 1
-  for (int t = 0; t < steps; ++t) {
+  for (; t < steps; ++t) {
     asm volatile("" : "+v"(bp), "+v"(bq));
     floatx4 d[2][QH], sb[2], sb_last[2];
     float sa[NQ];
@@ -349,7 +327,24 @@ k_tiles_e4m3(const E4m3Args g) {
       for (int j = 0; j < QH; ++j) add(7, i, j);
   }
   if (ends) end();
-  put();
+  if (g.dtype == BRSVD_DTYPE_F32) {
+    char* C = (char*)g.C + (g.splits > 1 ? (int64_t)blockIdx.y * g.A.n * g.B.n * 4 : 0);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int64_t m = q0 + 16 * (wq * NQ + q) + (lane & 15);
+      if (m >= g.A.n) continue;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int64_t n = p0 + 16 * (wp * NP + p) + 4 * (lane >> 4);
+        if (n < g.B.n) put_four(C, m * g.ldc + n, g.B.n - n, BRSVD_DTYPE_F32, acc[p][q]);
+      }
+    }
+  } else {
+    uint16_t* C = (uint16_t*)g.C + q0 * g.ldc + p0;
+    meet();
+    if (g.dtype == BRSVD_DTYPE_BF16) put_tile16<NQ>(acc, lds, C, g.ldc, g.A.n - q0, g.B.n - p0, [](float x, int) { return to16<Bf16>(x); });
+    else put_tile16<NQ>(acc, lds, C, g.ldc, g.A.n - q0, g.B.n - p0, [](float x, int) { return to16<Fp16>(x); });
+  }
 }
 
 // C (m x n, type dtype) = sum of the splits' parts, in their order

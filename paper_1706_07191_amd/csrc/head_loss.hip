@@ -391,17 +391,21 @@ k_head_grad(const HeadArgs g) {
         for (int r = 0; r < 4; ++r)
           if (at[q] == 16 * p + r) acc[p][q][r] -= 1.f;
     }
-    if (c >= count) continue;
-    uint16_t* row = g.G + c * g.pitch;
+    if constexpr (T::kThreads != kTileThreads) {
+      if (c >= count) continue;
+      uint16_t* row = g.G + c * g.pitch;
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      uint16_t h[4];
+      for (int p = 0; p < NP; ++p) {
+        uint16_t h[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) h[r] = to16<El>(s[q] * acc[p][q][r]);
-      // the pitch is a multiple of eight: what is written beyond the piece's last row stays inside the token's row of G
-      if (vlane + 16 * p < rows) *(uint2*)(row + vlane + 16 * p) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+        for (int r = 0; r < 4; ++r) h[r] = to16<El>(s[q] * acc[p][q][r]);
+        // the pitch is a multiple of eight: what is written beyond the piece's last row stays inside the token's row of G
+        if (vlane + 16 * p < rows) *(uint2*)(row + vlane + 16 * p) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+      }
     }
   }
+  if constexpr (T::kThreads == kTileThreads)
+    put_tile16<NQ>(acc, lds, g.G + t0 * g.pitch + p0, g.pitch, count - t0, g.pitch - p0, [&](float x, int q) { return to16<El>(s[q] * x); });
 }
 
 struct HeadProduct {
@@ -459,32 +463,14 @@ template <class El>
 __global__ void __launch_bounds__(kTileThreads, 2)
 k_head_dw(const HeadProduct g) {
   using T = Tiles<El, kCols, kCols, true, 256>;
-  constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
   const int64_t p0 = tp * kTileP, q0 = tq * 256;
-  floatx4 acc[NP][NQ];
+  floatx4 acc[T::NP][T::NQ];
   T::run(acc, g.P, p0, g.Q, q0, 0, g.meta->count, lds);
   const float down = g.meta->down;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % WP, wq = wave / WP;
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    const int64_t v = q0 + 16 * (wq * NQ + q) + (lane & 15);
-    if (v >= g.Q.n) continue;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int64_t d = p0 + 16 * (wp * NP + p) + 4 * (lane >> 4);
-      uint16_t h[4], *at = g.out + v * g.ldo + d;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) h[r] = to16<El>(acc[p][q][r] * down);
-      if (d + 4 <= g.P.n && ((uintptr_t)at & 7) == 0) *(uint2*)at = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-      else
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (d + r < g.P.n) at[r] = h[r];
-    }
-  }
+  put_tile16<T::NQ>(acc, lds, g.out + q0 * g.ldo + p0, g.ldo, g.Q.n - q0, g.P.n - p0, [&](float x, int) { return to16<El>(x * down); });
 }
 
 // Rows of dH that do not count are zero, the others the sum of the splits' parts in their order.  Two launches: all rows zero, then those that count.

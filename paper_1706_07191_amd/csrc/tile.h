@@ -417,6 +417,42 @@ template <class El> __device__ __forceinline__ float from16(uint16_t x) {
   else return (float)__builtin_bit_cast(_Float16, x);
 }
 
+// A workgroup's tile D (of sums, a wave has 8 x NQ tiles of it) to memory as 16-bit numbers: row j of `out` (pitch ldo numbers) gets column j of D, of which
+// `rows` and `cols` are there.  A lane's four numbers of a row go through LDS, so that a row's 256 leave as one piece of memory, 16 bytes a lane at any
+// alignment: stored from where they are, 32 bytes of a row at a time, an 8192 x 8192 result took 33 us.  Eight bytes u of row j lie at
+// u ^ 4 (j & 15): 16 rows in different banks.  LDS has to be free.  `number(x, q)` makes the 16 bits of a sum of the wave's tile column q.
+template <int NQ, class Number>
+__device__ __forceinline__ void put_tile16(const floatx4 (&acc)[8][NQ], char* lds, uint16_t* out, int64_t ldo, int64_t rows, int64_t cols, Number number) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wp = wave % 2, wq = wave / 2;
+#pragma unroll
+  for (int q = 0; q < NQ; ++q)
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      uint32_t h[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) h[r] = number(acc[p][q][r], q);
+      const int j = 16 * (wq * NQ + q) + (lane & 15), u = 4 * (8 * wp + p) + (lane >> 4);
+      *(uint2*)(lds + j * 512 + 8 * (u ^ (4 * (lane & 15)))) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+    }
+  __syncthreads();
+  const int piece = tid & 31;
+  const int64_t left = cols - 8 * piece;
+#pragma unroll
+  for (int i = 0; i < 4 * NQ; ++i) {
+    const int j = 16 * i + (tid >> 5);
+    const uint4 v = *(const uint4*)(lds + j * 512 + 8 * ((2 * piece) ^ (4 * (j & 15))));
+    if (j >= rows) continue;
+    uint16_t* at = out + j * ldo + 8 * piece;
+    if (left >= 8) *(Piece*)at = Piece{{v.x, v.y, v.z, v.w}};
+    else {
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < left) at[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+    }
+  }
+}
+
 // Tiles of a np x nq grid (np along P) to workgroups: workgroups b, b + 8, b + 16 ... share an XCD and its L2, so each XCD gets a run of tiles, and a run
 // goes through `band` rows of the grid at a time.  Returns false for workgroups beyond the grid (the grid is rounded up to eight).
 __device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64_t nq_, unsigned band, int64_t* tp, int64_t* tq) {
