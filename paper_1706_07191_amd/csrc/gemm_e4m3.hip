@@ -362,14 +362,13 @@ k_join_splits(const float* __restrict__ part, int splits, int64_t m, int64_t n, 
   put_four(C, row * ldc + col, n - col, dtype, sum);
 }
 
-// Up to 16 MT rows of A.  A wave has 16 NT rows of B and every eighth block of the contraction: the waves of a workgroup share the rows of B and split the
-// contraction, their sums are added through LDS in wave order.  B goes from memory to the instruction's registers (a lane: 16 bytes at two places of a
-// row's block), the U blocks that a wave takes next at once; so does A, which all workgroups read and the caches hold.  DT >= 0: A comes in numbers of more
+// Up to 16 MT rows of A.  The WAVES waves of a workgroup share 16 NT rows of B and take the blocks of the contraction in turn; their sums are added through
+// LDS in wave order.  B goes from memory to the instruction's registers (a lane: 16 bytes at two places of a
+// row's block), the U blocks that a wave takes next on their way; so does A, which all workgroups read and the caches hold.  DT >= 0: A comes in numbers of more
 // bits, and a block of it is cast where it is used, in registers: four lanes hold a row's block, its largest number takes two exchanges.
-template <int MT, int NT, int U, int DT>     // DT: type of A's numbers, -1: 8 bits with scales
-__global__ void __launch_bounds__(512)
+template <int MT, int NT, int U, int WAVES, int DT>     // DT: type of A's numbers, -1: 8 bits with scales
+__global__ void __launch_bounds__(64 * WAVES)
 k_rows_e4m3(const E4m3Args g) {
-  constexpr int WAVES = 8;
   constexpr bool CAST = DT >= 0;
   constexpr int EB = DT == BRSVD_DTYPE_F32 ? 4 : DT >= 0 ? 2 : 1;
   __shared__ floatx4 parts[WAVES][MT * NT][64];
@@ -467,18 +466,20 @@ k_rows_e4m3(const E4m3Args g) {
     }
   };
   const int whole = (int)(g.k / kBlock);
+  Block x[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if (wave + WAVES * i < whole) fetch(x[i], wave + WAVES * i, true, 0);
   for (int b = wave; b < whole; b += WAVES * U) {
-    Block x[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) fetch(x[i], b + WAVES * i < whole ? b + WAVES * i : b, true, 0);
-#pragma unroll
-    for (int i = 0; i < U; ++i)
+    for (int i = 0; i < U; ++i) {
       if (b + WAVES * i < whole) multiply(x[i]);
+      if (b + WAVES * (i + U) < whole) fetch(x[i], b + WAVES * (i + U), true, 0);
+    }
   }
   if (whole < g.blocks && whole % WAVES == wave) {          // the contraction's end, after the wave's other blocks
-    Block x;
-    fetch(x, whole, false, g.k - (int64_t)whole * kBlock - piece);
-    multiply(x);
+    fetch(x[0], whole, false, g.k - (int64_t)whole * kBlock - piece);
+    multiply(x[0]);
   }
 #pragma unroll
   for (int t = 0; t < MT; ++t)
@@ -522,21 +523,21 @@ static E4m3Plan e4m3_plan(int64_t m, int64_t n, int64_t k, bool per_row, int dty
 static uint64_t split_bytes(const E4m3Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? (uint64_t)p.splits * m * n * 4 : 0; }
 
 // NT: rows of A are read (and cast) once for 16 NT rows of B, as many as leave workgroups for every CU
-template <int MT, int NT, int U, int DT>
+template <int MT, int NT, int U, int WAVES, int DT>
 static void launch_rows(const E4m3Args& g, hipStream_t stream) {
-  hipLaunchKernelGGL((k_rows_e4m3<MT, NT, U, DT>), dim3((unsigned)ceil_div(g.B.n, 16 * NT)), dim3(512), 0, stream, g);
+  hipLaunchKernelGGL((k_rows_e4m3<MT, NT, U, WAVES, DT>), dim3((unsigned)ceil_div(g.B.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);
 }
 template <int DT>
 static void launch_few(const E4m3Args& g, hipStream_t stream) {
-  if (g.B.n >= 32 * 512) launch_rows<1, 4, 1, DT>(g, stream);
-  else if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, DT>(g, stream);
-  else launch_rows<1, 1, 4, DT>(g, stream);
+  if (g.B.n >= 32 * 512) launch_rows<1, 4, 2, 4, DT>(g, stream);
+  else if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, 4, DT>(g, stream);
+  else launch_rows<1, 1, 4, 8, DT>(g, stream);
 }
 static void launch_more(const E4m3Args& g, hipStream_t stream) {
-  if (g.A.n <= 32 && g.B.n >= 32 * 512) launch_rows<2, 2, 2, -1>(g, stream);
-  else if (g.A.n <= 32) launch_rows<2, 1, 4, -1>(g, stream);
-  else if (g.B.n >= 32 * 512) launch_rows<4, 2, 1, -1>(g, stream);
-  else launch_rows<4, 1, 2, -1>(g, stream);
+  if (g.A.n <= 32 && g.B.n >= 32 * 512) launch_rows<2, 2, 3, 4, -1>(g, stream);
+  else if (g.A.n <= 32) launch_rows<2, 1, 4, 8, -1>(g, stream);
+  else if (g.B.n >= 32 * 512) launch_rows<4, 2, 2, 4, -1>(g, stream);
+  else launch_rows<4, 1, 2, 8, -1>(g, stream);
 }
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
 static void launch_tiles(const E4m3Args& g, hipStream_t stream) {

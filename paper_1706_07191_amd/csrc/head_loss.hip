@@ -22,9 +22,15 @@ template <class El, bool DIRECT, int BQ> struct Logits : Tiles<El, kRows, kRows,
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 64> : RowsProduct<El, 2, 4, 4, 2> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 32> : RowsProduct<El, 2, 2, 4, 4> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 16> : RowsProduct<El, 2, 1, 4, 4> {};
-// Tokens of a tile: 256 x 256 has no registers left for pieces on their way through them.
-static int tokens_tile(int64_t tokens, bool direct) { return tokens <= 64 ? 64 : tokens <= 128 || !direct ? 128 : 256; }
-static int logits_tile(int64_t tokens, bool direct) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens_tile(tokens, direct); }
+// Tokens of a tile.  256 x 256 has no registers left for pieces on their way through them; and 256 x 128, six tenths of its time, is taken where that is
+// less in all on 256 CUs: 130 tokens over 32000 words 125 tiles of 256 x 256 or 250 of 256 x 128 in one round either way.  others: tiles along the
+// other side.
+static int tokens_tile(int64_t tokens, bool direct, int64_t others) {
+  if (tokens <= 64) return 64;
+  if (tokens <= 128 || !direct) return 128;
+  return 6 * ceil_div(others * ceil_div(tokens, 128), 256) < 10 * ceil_div(others * ceil_div(tokens, 256), 256) ? 128 : 256;
+}
+static int logits_tile(int64_t tokens, bool direct, int64_t words) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens_tile(tokens, direct, ceil_div(words, kTileP)); }
 static int logits_rows(int bq) { return bq <= 64 ? 128 : kTileP; }     // of the vocabulary
 
 // What the backward pass knows on the device: how many tokens count, and the power of two that G is multiplied by so that its numbers of 16 bits hold what
@@ -518,14 +524,14 @@ static HeadPlan head_plan(int64_t tokens, int64_t vocab, int64_t dim, int64_t pi
   p.piece = piece_rows(tokens, vocab, piece);
   p.pitch_h = ceil_div(dim, 8) * 16;
   // dH has few tiles where there are few tokens: then the piece's rows are cut, too
-  const int64_t tiles = ceil_div(dim, kTileP) * ceil_div(tokens, tokens_tile(tokens, true));
+  const int64_t tiles = ceil_div(dim, kTileP) * ceil_div(tokens, tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256);
   int64_t s = 256 / tiles;
   if (s > ceil_div(p.piece, 256)) s = ceil_div(p.piece, 256);
   if (s < 1) s = 1;
   p.per_split = ceil_div(ceil_div(p.piece, s), 64) * 64;
   p.splits = (int)ceil_div(p.piece, p.per_split);
   p.part = 0;
-  p.zlabel = whole256((uint64_t)ceil_div(vocab, logits_rows(logits_tile(tokens, true))) * tokens * 8);
+  p.zlabel = whole256((uint64_t)ceil_div(vocab, logits_rows(logits_tile(tokens, true, vocab))) * tokens * 8);
   p.forward_bytes = p.zlabel + whole256((uint64_t)tokens * 4);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t here = at; at += whole256(bytes); return here; };
@@ -584,7 +590,7 @@ static int head_forward(const HeadCall& c, const HeadPlan& plan, char* ws, float
   g.dim = c.dim;
   g.scale = c.scale;
   const bool direct = aligned_pieces(c.W, 2 * c.ldw) && aligned_pieces(c.H, 2 * c.ldh);
-  const int bl = logits_tile(c.tokens, direct);
+  const int bl = logits_tile(c.tokens, direct, c.vocab);
   g.tiles_v = ceil_div(c.vocab, logits_rows(bl));
   g.tiles_t = ceil_div(c.tokens, bl);
   g.label = c.label;
@@ -613,7 +619,7 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   hipLaunchKernelGGL(k_head_gather, dim3((unsigned)c.tokens), dim3(256), 0, stream, H, c.dim, meta, index, lse, c.label, hc, plan.pitch_h, lse_c, coef, label_c);
   if (dH) hipLaunchKernelGGL(k_head_zero, dim3((unsigned)c.tokens), dim3(256), 0, stream, (uint16_t*)dH, lddh, c.tokens, c.dim);
   const bool direct = aligned_pieces(c.W, 2 * c.ldw);
-  const int bq = tokens_tile(c.tokens, direct), bl = logits_tile(c.tokens, direct);
+  const int bq = tokens_tile(c.tokens, direct, ceil_div(c.dim, kTileP) * plan.splits), bl = logits_tile(c.tokens, direct, plan.piece < c.vocab ? plan.piece : c.vocab);
   const int64_t tiles_t = ceil_div(c.tokens, bq);
   for (int64_t v0 = 0; v0 < c.vocab; v0 += plan.piece) {
     const int64_t rows = c.vocab - v0 < plan.piece ? c.vocab - v0 : plan.piece;

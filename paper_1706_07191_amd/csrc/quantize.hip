@@ -168,14 +168,53 @@ k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, 
   }
 }
 
-// X = Q * S: a thread writes 16 bytes of X at a time, neighbouring lanes neighbouring pieces.
+// Blocks of a row by themselves: 16 (fp32: 32) lanes a block, the blocks of a row one after the other, SETS of them a thread at once.
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_quantize_rows(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S) {
+  using P = Part<DT>;
+  constexpr int W = P::kWide, L = P::kLanes, SETS = 4;
+  const int cg = threadIdx.x % L;
+  const unsigned ncb = (unsigned)((cols + kBlock - 1) / kBlock);
+  const int64_t first = (int64_t)blockIdx.x * (256 / L * SETS) + threadIdx.x / L, blocks = rows * ncb;
+  float x[SETS][W];
+  int64_t row[SETS];
+  int col[SETS], width[SETS];
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    const int64_t b = first + i * (256 / L);
+    row[i] = b / ncb;
+    col[i] = (int)(b - row[i] * ncb) * kBlock + cg * W;
+    const int64_t left = b < blocks ? cols - col[i] : 0;
+    width[i] = (int)(left < W ? (left > 0 ? left : 0) : W);
+    numbers<DT>(X + row[i] * ldx + (int64_t)col[i] * P::kBytes, width[i], x[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) t = fmaxf(t, finite_abs(x[i][j]));
+    t = max16(t);
+    if (L == 32) t = fmaxf(t, __shfl_xor(t, 16));
+    const int e = block_exponent(t);
+    const float f = power_of_two(-e);
+    uint32_t v[W / 4];
+#pragma unroll
+    for (int j = 0; j < W; j += 4) v[j / 4] = pack_e4m3(x[i][j] * f, x[i][j + 1] * f, x[i][j + 2] * f, x[i][j + 3] * f);
+    put_bytes<W>(Q + row[i] * ldq + col[i], width[i], v);
+    const int64_t b = first + i * (256 / L);
+    if (cg == 0 && b < blocks) S[b] = power_of_two(e);
+  }
+}
+
+// X = Q * S: a thread writes 16 bytes of X at a time, neighbouring lanes neighbouring pieces, four rows.
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_dequantize(const uint8_t* __restrict__ Q, int64_t ldq, const float* __restrict__ S, int64_t rows, int64_t cols, int block_rows, char* __restrict__ X, int64_t ldx) {
   using P = Part<DT>;
-  constexpr int W = P::kWide, R = P::kRows, STEP = 256 / P::kLanes;
+  constexpr int W = P::kWide, R = 4, STEP = 256 / P::kLanes;
   const int c = (int)(threadIdx.x % P::kLanes) * W, r = threadIdx.x / P::kLanes;
-  const int64_t ncb = (cols + kBlock - 1) / kBlock, rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, col = cb * kBlock + c, row0 = rb * kBlock + r;
+  const int64_t ncb = (cols + kBlock - 1) / kBlock, rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, col = cb * kBlock + c, row0 = rb * (STEP * R) + r;
   const int width = (int)(cols - col < W ? cols - col : W);
   if (width <= 0) return;
   uint32_t w[R][W / 4];
@@ -185,7 +224,7 @@ k_dequantize(const uint8_t* __restrict__ Q, int64_t ldq, const float* __restrict
     const int64_t row = row0 + STEP * i;
     if (row >= rows) continue;
     const uint8_t* src = Q + row * ldq + col;
-    f[i] = S[(block_rows == 1 ? row : rb) * ncb + cb];
+    f[i] = S[(block_rows == 1 ? row : row / kBlock) * ncb + cb];
     struct __attribute__((packed, aligned(1))) Bytes { uint32_t x[W / 4]; };
     if (width == W) {
       const Bytes v = *(const Bytes*)src;
@@ -228,8 +267,10 @@ static void launch_quantize(const char* X, int64_t ldx, int64_t rows, int64_t co
                             hipStream_t stream) {
   const dim3 grid((unsigned)(ceil_div(cols, kBlock) * ceil_div(rows, kBlock)));
   const int64_t pitch = ldx * (DT == BRSVD_DTYPE_F32 ? 4 : 2);
-  if (Q && Qt) hipLaunchKernelGGL((k_quantize<DT, SQUARE, true, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
-  else if (Q) hipLaunchKernelGGL((k_quantize<DT, SQUARE, true, false>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
+  if (!SQUARE && !Qt)
+    hipLaunchKernelGGL(k_quantize_rows<DT>, dim3((unsigned)ceil_div(rows * ceil_div(cols, kBlock), 256 / Part<DT>::kLanes * 4)), dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S);
+  else if (Q && Qt) hipLaunchKernelGGL((k_quantize<DT, SQUARE, true, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
+  else if (Q) hipLaunchKernelGGL((k_quantize<DT, true, true, false>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
   else hipLaunchKernelGGL((k_quantize<DT, SQUARE, false, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
 }
 
@@ -258,7 +299,7 @@ extern "C" int brsvd_quantize_e4m3(const void* X, int64_t ldx, int64_t rows, int
                                    float* S, uint8_t* Qt, int64_t ldqt, float* St, void* stream) {
   if (rows < 0 || cols < 0 || !model_type(dtype) || (block_rows != 1 && block_rows != kBlock)) return BRSVD_ERR_ARG;
   if (rows == 0 || cols == 0) return BRSVD_OK;
-  if (!X || (!Q && !Qt) || ldx < cols || (Q && (!S || ldq < cols)) || (Qt && (!St || ldqt < rows)) || ceil_div(rows, kBlock) * ceil_div(cols, kBlock) > kMaxGrid) return BRSVD_ERR_ARG;
+  if (!X || (!Q && !Qt) || ldx < cols || (Q && (!S || ldq < cols)) || (Qt && (!St || ldqt < rows)) || rows > (kMaxGrid << 2) / ceil_div(cols, kBlock)) return BRSVD_ERR_ARG;
   return quantize(X, ldx, rows, cols, dtype, block_rows, Q, ldq, S, Qt, ldqt, St, (hipStream_t)stream);
 }
 
@@ -266,8 +307,8 @@ extern "C" int brsvd_dequantize_e4m3(const uint8_t* Q, int64_t ldq, const float*
                                      int64_t ldx, void* stream) {
   if (rows < 0 || cols < 0 || !model_type(dtype) || (block_rows != 1 && block_rows != kBlock)) return BRSVD_ERR_ARG;
   if (rows == 0 || cols == 0) return BRSVD_OK;
-  if (!Q || !S || !X || ldq < cols || ldx < cols || ceil_div(rows, kBlock) * ceil_div(cols, kBlock) > kMaxGrid) return BRSVD_ERR_ARG;
-  const dim3 grid((unsigned)(ceil_div(cols, kBlock) * ceil_div(rows, kBlock)));
+  if (!Q || !S || !X || ldq < cols || ldx < cols || rows > (kMaxGrid << 2) / ceil_div(cols, kBlock)) return BRSVD_ERR_ARG;
+  const dim3 grid((unsigned)(ceil_div(cols, kBlock) * ceil_div(rows, dtype == BRSVD_DTYPE_F32 ? 32 : 64)));
   const int64_t pitch = ldx * (dtype == BRSVD_DTYPE_F32 ? 4 : 2);
   hipStream_t s = (hipStream_t)stream;
   if (dtype == BRSVD_DTYPE_F32) hipLaunchKernelGGL(k_dequantize<BRSVD_DTYPE_F32>, grid, dim3(256), 0, s, Q, ldq, S, rows, cols, block_rows, (char*)X, pitch);

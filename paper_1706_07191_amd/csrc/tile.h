@@ -48,14 +48,10 @@ inline bool aligned_pieces(const void* base, int64_t ld_bytes) { return (uintptr
 constexpr int64_t kMaxPitch = (int64_t)1 << 22;
 
 struct __attribute__((packed, aligned(1))) Piece { uint32_t x[4]; };
-static __device__ const uint4 k_zero_piece = {0u, 0u, 0u, 0u};
 
-// 16 bytes per lane from `src` into LDS at `dst` (the same in all lanes) + 16 lane.  Written out so that the compiler does not hold back reads of the
-// other buffer until it is done: loads_done() before the barrier that hands the buffer over is the wait for it.
-__device__ __forceinline__ void load_to_lds(uint32_t dst, const char* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory");
-}
-// The same from `off` bytes (below 2^31) behind an address that all lanes share.
+// 16 bytes per lane into LDS at `dst` (the same in all lanes) + 16 lane, from `off` bytes (below 2^31) behind an address that all lanes share.  Written
+// out so that the compiler does not hold back reads of the other buffer until it is done; the wait before the barrier that hands the
+// buffer over is written out, too.
 __device__ __forceinline__ void load_to_lds(uint32_t dst, const char* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(dst), "s"(base), "v"(off) : "memory");
 }
@@ -63,8 +59,6 @@ __device__ __forceinline__ void load_to_lds(uint32_t dst, const char* base, uint
 __device__ __forceinline__ void load4_to_lds(uint32_t dst, const void* src) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
 }
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
 // The same value in scalar registers, for one that all lanes share.
 __device__ __forceinline__ int64_t scalar(int64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
@@ -147,18 +141,31 @@ struct Stager {
     next();
   }
   __device__ __forceinline__ void load(char* tile, int tid, int wave, int64_t left) {
-    const uint32_t dst = lds_address(tile);
+    const int near = (int)(left < kStepK ? left : kStepK);
     if (plain(left)) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) load_part(tile, wave, i);
+    } else if (O == kRows) {
+      // the step that the contraction ends in: all of a thread's pieces are whole, or none
+      const int there = near * El::kBytes - 16 * ((tid ^ (tid >> 3)) & 7);
+      if (DIRECT && there >= 16) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_part(tile, wave, i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const uint4 v = there > 0 ? piece_of<El::kBytes>(at + off[i], there) : make_uint4(0u, 0u, 0u, 0u);
+          if (DIRECT) *(uint4*)(tile + 16 * (i * THREADS + tid)) = v;
+          else reg[i] = v;
+        }
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int slot = i * THREADS + tid, kpos = O == kRows ? ((slot % kPerRow) ^ (slot / kPerRow & 7)) * 16 : slot / kPerRow;
-        const int64_t there = O == kRows ? left * El::kBytes - kpos : (kpos < left ? valid[O == kRows ? 0 : i] : 0);
+        const int there = i * (THREADS / kPerRow) + tid / kPerRow < near ? valid[O == kRows ? 0 : i] : 0;
         if (!DIRECT) reg[i] = piece_of<El::kBytes>(at + off[i], there);
-        else if (there >= 16 || there <= 0) load_to_lds(dst + 16 * (i * THREADS + 64 * wave), there > 0 ? at + off[i] : (const char*)&k_zero_piece);
-        else *(uint4*)(tile + 16 * slot) = piece_of<El::kBytes>(at + off[i], there);
+        else if (there >= 16) load_part(tile, wave, i);
+        else *(uint4*)(tile + 16 * (i * THREADS + tid)) = there > 0 ? piece_of<El::kBytes>(at + off[i], there) : make_uint4(0u, 0u, 0u, 0u);
       }
     }
     at += step;
