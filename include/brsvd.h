@@ -267,10 +267,10 @@ int brsvd_dequantize_e4m3(const uint8_t* Q, int64_t ldq, const float* S, int64_t
 /* C (m x n, dtype F32, BF16 or F16) = A B^T with A m x k and B n x k in 8 bits; SA has a scale per row
  * and block of A, SB per row (block_rows = 1) or 128 rows (block_rows = 128) and block of B.  Scales are
  * any fp32 numbers, they need not come from brsvd_quantize_e4m3.  Products of a block are added, then
- * scaled and added to those of the other blocks in fp32; C is rounded once.  With an fp32 C, or up to 64
- * rows of A and block_rows 128, all sums are those of exact products in fp32.  Otherwise the 8-bit matrix
- * cores add the products of a block: of eight neighbouring products they drop what is below 2^-13 of the
- * largest one's power of two, parts of 1e-5 of the sum of |products|.
+ * scaled and added to those of the other blocks in fp32; C is rounded once.  With an fp32 C all sums are
+ * those of exact products in fp32.  Otherwise the 8-bit matrix cores add the products of a block: of eight
+ * neighbouring products they drop what is below 2^-13 of the largest one's power of two, parts of 1e-5 of
+ * the sum of |products|.
  * The three products of a linear layer Y = X W^T with weights W: Y from X and W (block_rows 128), dX from
  * dY and W^T (128), dW from dY^T and X^T (1), each operand cast along the contraction. */
 int brsvd_gemm_e4m3(const uint8_t* A, int64_t lda, const float* SA, const uint8_t* B, int64_t ldb,

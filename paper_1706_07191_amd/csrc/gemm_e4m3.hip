@@ -3,10 +3,10 @@
 // The inner sum of a block starts from zero, is multiplied by its two scales and added in fp32.  B (the weights) is the instruction's first operand: a
 // lane then holds four neighbouring columns of C for one row m, whose scale is one number of the lane.
 // For a C of 16 bits the inner sum is one v_mfma_f32_16x16x128_f8f6f4, at twice the rate of 16-bit numbers: it cuts products off below 2^-13 of the
-// largest of eight neighbours, a part of 1e-5 of the sum of |products| where C keeps 2^-8 or 2^-11 of itself.  An fp32 C, and products of few
-// rows, which wait for memory anyway, go through fp16, where nothing is lost (mfma_wide).
+// largest of eight neighbours, a part of 1e-5 of the sum of |products| where C keeps 2^-8 or 2^-11 of itself.  For an fp32 C numbers go through
+// fp16, where nothing is lost (mfma_wide).
 //
-// k_tiles_e4m3: for many rows, bound by the matrix cores.  k_rows_e4m3: for up to 64 rows, bound by the read of B.
+// k_tiles_e4m3: for many rows, bound by the matrix cores.  k_rows_e4m3: for few rows, bound by the read of B.
 #include "e4m3.h"
 #include "tile.h"
 
@@ -366,7 +366,7 @@ k_join_splits(const float* __restrict__ part, int splits, int64_t m, int64_t n, 
 // LDS in wave order.  B goes from memory to the instruction's registers (a lane: 16 bytes at two places of a
 // row's block), the U blocks that a wave takes next on their way; so does A, which all workgroups read and the caches hold.  DT >= 0: A comes in numbers of more
 // bits, and a block of it is cast where it is used, in registers: four lanes hold a row's block, its largest number takes two exchanges.
-template <int MT, int NT, int U, int WAVES, int DT>     // DT: type of A's numbers, -1: 8 bits with scales
+template <int MT, int NT, int U, int WAVES, int DT, bool WIDE>     // DT: type of A's numbers, -1: 8 bits with scales
 __global__ void __launch_bounds__(64 * WAVES)
 k_rows_e4m3(const E4m3Args g) {
   constexpr bool CAST = DT >= 0;
@@ -418,11 +418,12 @@ k_rows_e4m3(const E4m3Args g) {
   };
   auto multiply = [&](const Block& x) {
     Wide8 ew[NT];
+    if (WIDE)
 #pragma unroll
-    for (int u = 0; u < NT; ++u) ew[u] = widen(__builtin_bit_cast(int4v, x.b[u][0]), __builtin_bit_cast(int4v, x.b[u][1]));
+      for (int u = 0; u < NT; ++u) ew[u] = widen(__builtin_bit_cast(int4v, x.b[u][0]), __builtin_bit_cast(int4v, x.b[u][1]));
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      Wide8 fw;
+      int4v f[2];
       float s;
       if constexpr (CAST) {
         float v[2][16], top = 0.f;
@@ -446,20 +447,21 @@ k_rows_e4m3(const E4m3Args g) {
         const int ex = block_exponent(top);
         const float inv = power_of_two(-ex);
         s = power_of_two(ex);
-        int4v f[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[h][i] = (int)pack_e4m3(v[h][4 * i] * inv, v[h][4 * i + 1] * inv, v[h][4 * i + 2] * inv, v[h][4 * i + 3] * inv);
-        fw = widen(f[0], f[1]);
       } else {
-        fw = widen(__builtin_bit_cast(int4v, x.a[t][0]), __builtin_bit_cast(int4v, x.a[t][1]));
+        f[0] = __builtin_bit_cast(int4v, x.a[t][0]);
+        f[1] = __builtin_bit_cast(int4v, x.a[t][1]);
         s = x.sa[t];
       }
       s *= x.sb;
+      Wide8 fw;
+      if (WIDE) fw = widen(f[0], f[1]);
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        const floatx4 d = mfma_wide(ew[u], fw);
+        const floatx4 d = WIDE ? mfma_wide(ew[u], fw) : mfma8(__builtin_bit_cast(int4v, x.b[u][0]), __builtin_bit_cast(int4v, x.b[u][1]), f[0], f[1], floatx4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[t][u][r] += d[r] * s;
       }
@@ -495,7 +497,9 @@ k_rows_e4m3(const E4m3Args g) {
   }
 }
 
-constexpr int64_t kFewRows = 64;      // rows up to which the read of B bounds the product
+// Rows up to which the read of B bounds the product.  Above 32 the tiles are ahead where B has rows for them: 60 x 20000 x 5000 47 us and 82, the
+// other way round where it has not: 24 x 4096 x 4096 17.6 and 9.6, 24 x 20000 x 5000 43 and 41.
+static bool few_rows(int64_t m, int64_t n) { return m <= 32 || (m <= 64 && n < 16 * 512); }
 constexpr int64_t kCastRows = 16;     // rows up to which they are cast inside it
 
 // How often the contraction is cut so that there are workgroups for every CU: only while a part keeps `least` blocks.
@@ -511,9 +515,12 @@ struct E4m3Plan {
 static E4m3Plan e4m3_plan(int64_t m, int64_t n, int64_t k, bool per_row, int dtype) {
   E4m3Plan p;
   const int blocks = (int)ceil_div(k, kBlock);
-  p.rows = m <= kFewRows && !per_row;
+  p.rows = few_rows(m, n) && !per_row;
   p.nt = 1;
-  p.bq = m > 128 && dtype != BRSVD_DTYPE_F32 ? 256 : 128;      // a tile of 256 x 256 has no registers left for numbers of 16 bits
+  // A tile of 256 x 256 has no registers left for numbers of 16 bits; and one of 256 x 128, seven tenths of its time, is taken where that is less in all
+  // on 256 CUs: 1000 x 5000 from 3000 39 us and 57 (160 tiles and 80 in one round), 4096 x 6000 from 4001 161 and 142 (three rounds and two).
+  const int64_t cols = ceil_div(n, 256);
+  p.bq = dtype == BRSVD_DTYPE_F32 || m <= 128 || 7 * ceil_div(cols * ceil_div(m, 128), 256) < 10 * ceil_div(cols * ceil_div(m, 256), 256) ? 128 : 256;
   p.splits = 1;
   if (!p.rows) p.splits = splits_for(ceil_div(n, 256) * ceil_div(m, p.bq), blocks, 4);
   p.per_split = (int)ceil_div(blocks, p.splits);
@@ -523,21 +530,21 @@ static E4m3Plan e4m3_plan(int64_t m, int64_t n, int64_t k, bool per_row, int dty
 static uint64_t split_bytes(const E4m3Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? (uint64_t)p.splits * m * n * 4 : 0; }
 
 // NT: rows of A are read (and cast) once for 16 NT rows of B, as many as leave workgroups for every CU
-template <int MT, int NT, int U, int WAVES, int DT>
+template <int MT, int NT, int U, int WAVES, int DT, bool WIDE>
 static void launch_rows(const E4m3Args& g, hipStream_t stream) {
-  hipLaunchKernelGGL((k_rows_e4m3<MT, NT, U, WAVES, DT>), dim3((unsigned)ceil_div(g.B.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);
+  hipLaunchKernelGGL((k_rows_e4m3<MT, NT, U, WAVES, DT, WIDE>), dim3((unsigned)ceil_div(g.B.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);
 }
-template <int DT>
+template <int DT, bool WIDE>
 static void launch_few(const E4m3Args& g, hipStream_t stream) {
-  if (g.B.n >= 32 * 512) launch_rows<1, 4, 2, 4, DT>(g, stream);
-  else if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, 4, DT>(g, stream);
-  else launch_rows<1, 1, 4, 8, DT>(g, stream);
+  if (g.B.n >= 32 * 512) launch_rows<1, 2, 2, 4, DT, WIDE>(g, stream);
+  else if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, 4, DT, WIDE>(g, stream);
+  else launch_rows<1, 1, 4, 8, DT, WIDE>(g, stream);
 }
+template <bool WIDE>
 static void launch_more(const E4m3Args& g, hipStream_t stream) {
-  if (g.A.n <= 32 && g.B.n >= 32 * 512) launch_rows<2, 2, 3, 4, -1>(g, stream);
-  else if (g.A.n <= 32) launch_rows<2, 1, 4, 8, -1>(g, stream);
-  else if (g.B.n >= 32 * 512) launch_rows<4, 2, 2, 4, -1>(g, stream);
-  else launch_rows<4, 1, 2, 8, -1>(g, stream);
+  if (g.A.n <= 32 && g.B.n >= 32 * 512) launch_rows<2, 2, 2, 4, -1, WIDE>(g, stream);
+  else if (g.A.n <= 32) launch_rows<2, 1, 4, 8, -1, WIDE>(g, stream);
+  else launch_rows<4, 1, 2, 8, -1, WIDE>(g, stream);
 }
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
 static void launch_tiles(const E4m3Args& g, hipStream_t stream) {
@@ -571,11 +578,12 @@ static int gemm_e4m3(const void* A, int64_t lda_bytes, int a_type, const float* 
   g.tiles_n = ceil_div(n, 256);
   g.tiles_m = ceil_div(m, plan.bq);
   if (plan.rows) {
-    if (m > kCastRows) launch_more(g, stream);
-    else if (a_type == BRSVD_DTYPE_F32) launch_few<BRSVD_DTYPE_F32>(g, stream);
-    else if (a_type == BRSVD_DTYPE_BF16) launch_few<BRSVD_DTYPE_BF16>(g, stream);
-    else if (a_type == BRSVD_DTYPE_F16) launch_few<BRSVD_DTYPE_F16>(g, stream);
-    else launch_few<-1>(g, stream);
+    const bool wide = dtype == BRSVD_DTYPE_F32;
+    if (m > kCastRows) wide ? launch_more<true>(g, stream) : launch_more<false>(g, stream);
+    else if (a_type == BRSVD_DTYPE_F32) launch_few<BRSVD_DTYPE_F32, true>(g, stream);
+    else if (a_type == BRSVD_DTYPE_BF16) launch_few<BRSVD_DTYPE_BF16, false>(g, stream);
+    else if (a_type == BRSVD_DTYPE_F16) launch_few<BRSVD_DTYPE_F16, false>(g, stream);
+    else wide ? launch_few<-1, true>(g, stream) : launch_few<-1, false>(g, stream);
   } else {
     const bool direct = aligned_pieces(A, lda_bytes) && aligned_pieces(B, ldb);
     const bool wide = dtype == BRSVD_DTYPE_F32;

@@ -22,13 +22,13 @@ template <class El, bool DIRECT, int BQ> struct Logits : Tiles<El, kRows, kRows,
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 64> : RowsProduct<El, 2, 4, 4, 2> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 32> : RowsProduct<El, 2, 2, 4, 4> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 16> : RowsProduct<El, 2, 1, 4, 4> {};
-// Tokens of a tile.  256 x 256 has no registers left for pieces on their way through them; and 256 x 128, six tenths of its time, is taken where that is
-// less in all on 256 CUs: 130 tokens over 32000 words 125 tiles of 256 x 256 or 250 of 256 x 128 in one round either way.  others: tiles along the
+// Tokens of a tile.  256 x 256 has no registers left for pieces on their way through them; and 256 x 128, seven tenths of its time, is taken where that
+// is less in all on 256 CUs: 130 tokens over 32000 words of width 2000, 250 tiles or 125 in one round, 41 us and 53.  others: tiles along the
 // other side.
 static int tokens_tile(int64_t tokens, bool direct, int64_t others) {
   if (tokens <= 64) return 64;
   if (tokens <= 128 || !direct) return 128;
-  return 6 * ceil_div(others * ceil_div(tokens, 128), 256) < 10 * ceil_div(others * ceil_div(tokens, 256), 256) ? 128 : 256;
+  return 7 * ceil_div(others * ceil_div(tokens, 128), 256) < 10 * ceil_div(others * ceil_div(tokens, 256), 256) ? 128 : 256;
 }
 static int logits_tile(int64_t tokens, bool direct, int64_t words) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens_tile(tokens, direct, ceil_div(words, kTileP)); }
 static int logits_rows(int bq) { return bq <= 64 ? 128 : kTileP; }     // of the vocabulary
@@ -59,20 +59,13 @@ struct HeadArgs {
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// Exponentials are powers of two of x log2(e); what is kept of a row is in units of log 2, too.
-template <class El, bool DIRECT, int BQ>
-__global__ void __launch_bounds__((Logits<El, DIRECT, BQ>::kThreads), 2)
-k_head_lse(const HeadArgs g) {
-  using T = Logits<El, DIRECT, BQ>;
-  constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP;
-  __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
-  int64_t tv, tt;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 8, &tv, &tt)) return;
-  floatx4 acc[NP][NQ];
+// What a tile of logits leaves: the label's logit, and for every token the largest and the sum.  Exponentials are powers of two of x log2(e); what is
+// kept of a row is in units of log 2, too.
+template <class T>
+__device__ __forceinline__ void leave_tile(const HeadArgs& g, floatx4 (&acc)[T::NP][T::NQ], int64_t tv, int64_t tt, float2* red) {
+  constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP, BQ = T::BQ;
   const int64_t v0 = tv * T::BP, t0 = tt * BQ;
-  T::run(acc, g.W, v0, g.H, t0, 0, g.dim, lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave % WP, wq = wave / WP;
-  float2* red = (float2*)lds;           // [WP][BQ]
   const int64_t vwave = v0 + 16 * wp * NP, vlane = vwave + 4 * (lane >> 4);
   const float scale = g.scale * kLog2e;
   if (vwave + 16 * NP > g.W.n) {        // words beyond the last one
@@ -83,6 +76,24 @@ k_head_lse(const HeadArgs g) {
         if (vlane + 16 * p + r >= g.W.n)
 #pragma unroll
           for (int q = 0; q < NQ; ++q) acc[p][q][r] = -INFINITY;
+  }
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) {
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[p][q][r]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[p][q][r], scale, -ref));
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 16) red[wp * BQ + 16 * (wq * NQ + q) + lane] = make_float2(top, sum);
   }
   if (g.label) {
     int64_t at[NQ];
@@ -106,24 +117,6 @@ k_head_lse(const HeadArgs g) {
       }
     }
   }
-#pragma unroll
-  for (int q = 0; q < NQ; ++q) {
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[p][q][r]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-    const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[p][q][r], scale, -ref));
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (lane < 16) red[wp * BQ + 16 * (wq * NQ + q) + lane] = make_float2(top, sum);
-  }
   __syncthreads();
   for (int col = threadIdx.x; col < BQ; col += T::kThreads) {
     if (t0 + col >= g.H.n) continue;
@@ -134,6 +127,42 @@ k_head_lse(const HeadArgs g) {
 #pragma unroll
     for (int w = 0; w < WP; ++w) sum += red[w * BQ + col].y * __builtin_amdgcn_exp2f(red[w * BQ + col].x - ref);
     g.part[tv * g.H.n + t0 + col] = make_float2(top, sum);
+  }
+}
+
+// A workgroup takes every gridDim-th tile.  Without pieces in registers the next tile's first steps are on their way while this one's exponentials are
+// worked out.
+template <class El, bool DIRECT, int BQ>
+__global__ void __launch_bounds__((Logits<El, DIRECT, BQ>::kThreads), 2)
+k_head_lse(const HeadArgs g) {
+  using T = Logits<El, DIRECT, BQ>;
+  __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
+  __shared__ float2 red[T::WP * BQ];
+  floatx4 acc[T::NP][T::NQ];
+  int64_t tv, tt;
+  unsigned b = blockIdx.x;
+  if (!tile_of_workgroup(b, g.tiles_v, g.tiles_t, 8, &tv, &tt)) return;
+  if constexpr (T::kThreads == kTileThreads && DIRECT) {
+    T tile;
+    tile.begin(g.W, tv * T::BP, g.H, tt * BQ, 0, g.dim, lds);
+    while (true) {
+      tile.multiply(acc);
+      int64_t nv = 0, nt = 0;
+      b += gridDim.x;
+      const bool more = tile_of_workgroup(b, g.tiles_v, g.tiles_t, 8, &nv, &nt);
+      if (more) tile.begin(g.W, nv * T::BP, g.H, nt * BQ, 0, g.dim, lds);
+      leave_tile<T>(g, acc, tv, tt, red);
+      if (!more) break;
+      tv = nv;
+      tt = nt;
+    }
+  } else {
+    do {
+      T::run(acc, g.W, tv * T::BP, g.H, tt * BQ, 0, g.dim, lds);
+      leave_tile<T>(g, acc, tv, tt, red);
+      __syncthreads();
+      b += gridDim.x;
+    } while (tile_of_workgroup(b, g.tiles_v, g.tiles_t, 8, &tv, &tt));
   }
 }
 
@@ -596,7 +625,9 @@ static int head_forward(const HeadCall& c, const HeadPlan& plan, char* ws, float
   g.label = c.label;
   g.part = (float2*)(ws + plan.part);
   g.zlabel = (float*)(ws + plan.zlabel);
-  const dim3 grid(tile_workgroups(g.tiles_v, g.tiles_t));
+  unsigned workgroups = tile_workgroups(g.tiles_v, g.tiles_t);
+  if (bl >= 128 && workgroups > 256) workgroups = 256;        // as many as run at once
+  const dim3 grid(workgroups);
   if (direct) BRSVD_LOGITS(k_head_lse, El, true, grid, stream, g);
   else BRSVD_LOGITS(k_head_lse, El, false, grid, stream, g);
   hipLaunchKernelGGL(k_head_join, dim3((unsigned)ceil_div(c.tokens, 16)), dim3(256), 0, stream, g.part, g.tiles_v, c.tokens, c.label, c.vocab, g.zlabel, lse, loss);

@@ -251,33 +251,48 @@ struct TileProduct {
   static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
   static constexpr int kLds = 2 * (BP + BQ) * kStepBytes, kStepK = kStepBytes / El::kBytes;
 
-  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
-    constexpr int kHalf = (BP + BQ) * kStepBytes, SLOTS = 2 * NP, MEET = SLOTS - 4;
-    Stager<El, OP, BP, kThreads, DIRECT> sp;
-    Stager<El, OQ, BQ, kThreads, DIRECT> sq;
-    sp.init(P, p0, k0, tid);
-    sq.init(Q, q0, k0, tid);
+  static constexpr int kHalf = (BP + BQ) * kStepBytes;
+  Stager<El, OP, BP, kThreads, DIRECT> sp;
+  Stager<El, OQ, BQ, kThreads, DIRECT> sq;
+  char* lds;
+  int64_t k;         // of the contraction
+
+  static __device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ int steps() const { return (int)((k + kStepK - 1) / kStepK); }
+  __device__ __forceinline__ void send(int t, int wave) {
+    char* to = lds + (t & 1) * kHalf;
+    const int64_t left = k - (int64_t)t * kStepK;
+    sp.load(to, threadIdx.x, wave, left);
+    sq.load(to + BP * kStepBytes, threadIdx.x, wave, left);
+  }
+  __device__ __forceinline__ void keep(int t) {
+    sp.store(lds + (t & 1) * kHalf, threadIdx.x);
+    sq.store(lds + (t & 1) * kHalf + BP * kStepBytes, threadIdx.x);
+  }
+  // Sends for the first two steps of a tile.  LDS has to be free.
+  __device__ __forceinline__ void begin(const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds_) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lds = lds_;
+    k = scalar(k1 - k0);
+    sp.init(P, p0, k0, threadIdx.x);
+    sq.init(Q, q0, k0, threadIdx.x);
+    if (steps() == 0) return;
+    send(0, wave);
+    keep(0);
+    if (steps() > 1) send(1, wave);
+  }
+  // The tile that was begun; LDS is free afterwards.
+  __device__ __forceinline__ void multiply(floatx4 (&acc)[NP][NQ]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP, steps = this->steps();
+    constexpr int SLOTS = 2 * NP, MEET = SLOTS - 4;
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
       for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const int steps = (int)((k1 - k0 + kStepK - 1) / kStepK);
-    auto send = [&](int t) {
-      char* to = lds + (t & 1) * kHalf;
-      const int64_t left = k1 - k0 - (int64_t)t * kStepK;
-      sp.load(to, tid, wave, left);
-      sq.load(to + BP * kStepBytes, tid, wave, left);
-    };
-    auto keep = [&](int t) {
-      sp.store(lds + (t & 1) * kHalf, tid);
-      sq.store(lds + (t & 1) * kHalf + BP * kStepBytes, tid);
-    };
-    auto meet = [] {
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
     int4v fp[8], fq[2][NQ];
     uint32_t bp = fragment_base<OP, BP>(16 * wp * NP, lane), bq = fragment_base<OQ, BQ>(16 * wq * NQ, lane);
     auto read_p = [&](const char* tile, int slot) { fp[slot & 7] = fragment<OP, BP>(tile, bp, slot & 7, slot >> 3); };
@@ -291,12 +306,6 @@ struct TileProduct {
     };
     bool parts = false;          // the step after this one is being sent for in parts
     if (steps == 0) return;
-    send(0);
-    keep(0);
-    if (steps > 1) {
-      send(1);
-      if (DIRECT) keep(1);
-    }
     meet();
     if (!DIRECT && steps > 1) keep(1);        // the pieces of step 1 have left their registers before those of step 2 come
 #pragma unroll
@@ -319,9 +328,9 @@ struct TileProduct {
           read_p(cur, s + 6);
         } else if (s == MEET) {
           meet();
-          const int64_t left = k1 - k0 - (int64_t)(t + 2) * kStepK;
+          const int64_t left = k - (int64_t)(t + 2) * kStepK;
           parts = sends && sp.plain(left) && sq.plain(left);
-          if (sends && !parts) send(t + 2);
+          if (sends && !parts) send(t + 2, wave);
         }
         if (parts) {
           if (s >= MEET) send_part(t + 2, s - MEET);
@@ -345,7 +354,13 @@ struct TileProduct {
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    meet();          // LDS is free for what follows
+    meet();
+  }
+
+  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds) {
+    TileProduct x;
+    x.begin(P, p0, Q, q0, k0, k1, lds);
+    x.multiply(acc);
   }
 };
 
@@ -355,7 +370,7 @@ template <class El, int NP_, int NQ_, int WP_, int U>
 struct RowsProduct {
   static constexpr int NP = NP_, NQ = NQ_, WP = WP_, WQ = 1;
   static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ, kThreads = 64 * WP;
-  static constexpr int kLds = WP * BQ * 8;                       // for what follows the product
+  static constexpr int kLds = 16;                                // none
   struct Step { uint4 p[NP][2], q[NQ][2]; };
 
   static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char*) {
