@@ -431,10 +431,12 @@ def brsvd_small_svd_static(R, stream=None, out=None):
 
 
 # ---- a model's matrices: 8-bit products and losses over a large vocabulary -----------------------------------------
+# Looking torch up in every one of a call's helpers takes longer than what they do: the first call leaves it here.
+torch = None
+
 # Every call takes stream= (a torch stream or its address; default: torch's current stream), on which it runs and allocates.
 
 def _model_dtype(dtype, name, half=False):
-    import torch
     if dtype is torch.bfloat16:
         return BRSVD_DTYPE_BF16
     if dtype is torch.float16:
@@ -446,7 +448,6 @@ def _model_dtype(dtype, name, half=False):
 
 def _rows(t, dtype, cols, name, rows=None):
     """(address, leading dimension) of a CUDA matrix with neighbouring elements in a row; cols, rows: None where any number will do."""
-    import torch
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 2):
         raise TypeError(f"{name} must be a 2-d CUDA tensor of dtype {dtype}")
     r, c = t.shape
@@ -465,7 +466,6 @@ def _rows(t, dtype, cols, name, rows=None):
 def _scope(stream):
     """Memory taken inside belongs to the stream that the call runs on: what a call frees at its end, or the caller later, is not handed out
     to work of another stream before the call is through with it."""
-    import torch
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     return torch.cuda.stream(stream)
@@ -477,6 +477,9 @@ def _scoped(call):
 
     @functools.wraps(call)
     def wrapped(*args, stream=None, **kw):
+        global torch
+        if torch is None:
+            import torch
         if stream is None:
             return call(*args, **kw)
         with _scope(stream):
@@ -486,12 +489,10 @@ def _scoped(call):
 
 def _current(device):
     """torch's current stream on a device, as an address (torch.cuda.current_stream() makes an object of it, at several times the cost)."""
-    import torch
     return torch._C._cuda_getCurrentRawStream(device.index) or None
 
 
 def _scales(S, rows, cols, block_rows, name):
-    import torch
     shape = (rows if block_rows == 1 else -(-rows // 128), -(-cols // 128))
     if S.shape != shape:
         raise TypeError(f"{name} has shape {tuple(S.shape)}, expected {shape}")
@@ -500,7 +501,6 @@ def _scales(S, rows, cols, block_rows, name):
 
 def _eight_bit(rows, cols, device):
     """rows x cols numbers of 8 bits in rows of whole 16 bytes, which the products read fastest."""
-    import torch
     return torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=torch.float8_e4m3fn, device=device)
 
 
@@ -509,7 +509,6 @@ def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
     """X (rows, cols) CUDA, fp32, bf16 or fp16, as e4m3 numbers Q (float8_e4m3fn, rows 16-byte aligned) and power-of-two
     scales S, one for each 128 numbers of a row (block_rows=1) or each 128 x 128 block (block_rows=128).  Returns (Q, S), with
     transpose=True (Q, S, Qt, St), the last two those of X^T."""
-    import torch
     if block_rows not in (1, 128):
         raise ValueError("block_rows must be 1 or 128")
     dt = _model_dtype(X.dtype, "X")
@@ -530,7 +529,6 @@ def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
 @_scoped
 def brsvd_dequantize_e4m3(Q, S, block_rows=1, dtype=None):
     """What Q with its scales stands for, as fp32 (or bf16, fp16: dtype)."""
-    import torch
     if block_rows not in (1, 128):
         raise ValueError("block_rows must be 1 or 128")
     dtype = dtype or torch.float32
@@ -547,7 +545,6 @@ def brsvd_dequantize_e4m3(Q, S, block_rows=1, dtype=None):
 def brsvd_gemm_e4m3(A, SA, Bm, SB, block_rows=128, dtype=None, out=None):
     """A Bm^T of 8-bit matrices A (m, k) with a scale per row and 128 numbers and Bm (n, k) with one per 128 x 128 block, or
     with block_rows=1 like A's.  The result is bf16 unless dtype says fp32 or fp16; out: write it there."""
-    import torch
     if block_rows not in (1, 128):
         raise ValueError("block_rows must be 1 or 128")
     a, lda = _rows(A, torch.float8_e4m3fn, None, "A")
@@ -557,8 +554,12 @@ def brsvd_gemm_e4m3(A, SA, Bm, SB, block_rows=128, dtype=None, out=None):
     sa, sb = _scales(SA, m, k, 1, "SA"), _scales(SB, n, k, block_rows, "SB")
     dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
     dt = _model_dtype(dtype, "the result")
-    Cm = torch.empty(m, n, dtype=dtype, device=A.device) if out is None else out
-    c, ldc = _rows(Cm, dtype, n, "out", m)
+    if out is None:
+        Cm = torch.empty(m, n, dtype=dtype, device=A.device)
+        c, ldc = Cm.data_ptr(), n or 1
+    else:
+        Cm = out
+        c, ldc = _rows(Cm, dtype, n, "out", m)
     nbytes = lib().brsvd_gemm_e4m3_scratch_bytes(m, n, k, block_rows, dt)
     scr = _byte_scratch(nbytes, A.device) if nbytes else None
     _check(lib().brsvd_gemm_e4m3(a, lda, sa, b, ldb, sb, block_rows, m, n, k, dt, c, ldc,
@@ -570,15 +571,18 @@ def brsvd_gemm_e4m3(A, SA, Bm, SB, block_rows=128, dtype=None, out=None):
 def brsvd_linear_e4m3(X, W, SW, out=None):
     """X W^T: X (m, k) fp32, bf16 or fp16 is cast into 8 bits by rows of 128 on the way, W (n, k) is in 8 bits with a scale
     for each 128 x 128 block.  The result has X's type."""
-    import torch
     dt = _model_dtype(X.dtype, "X")
     x, ldx = _rows(X, X.dtype, None, "X")
     m, k = X.shape
     w, ldw = _rows(W, torch.float8_e4m3fn, k, "W")
     n = W.shape[0]
     sw = _scales(SW, n, k, 128, "SW")
-    Y = torch.empty(m, n, dtype=X.dtype, device=X.device) if out is None else out
-    y, ldy = _rows(Y, X.dtype, n, "out", m)
+    if out is None:
+        Y = torch.empty(m, n, dtype=X.dtype, device=X.device)
+        y, ldy = Y.data_ptr(), n or 1
+    else:
+        Y = out
+        y, ldy = _rows(Y, X.dtype, n, "out", m)
     nbytes = lib().brsvd_linear_e4m3_scratch_bytes(m, n, k, dt)
     scr = _byte_scratch(nbytes, X.device) if nbytes else None
     _check(lib().brsvd_linear_e4m3(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes,
@@ -601,7 +605,6 @@ def _vector(t, dtype, n, name):
 
 def _factors(grad, tokens):
     """(tensor, address, stride) of a factor for each token: a number, a tensor with one for all (also expanded) or one for each."""
-    import torch
     if not isinstance(grad, torch.Tensor):
         raise TypeError("grad must be a CUDA tensor of dtype torch.float32")
     if grad.dtype != torch.float32 or not grad.is_cuda:
@@ -624,7 +627,6 @@ def _head_workspace(sizes, piece, top, backward, device):
 def brsvd_xent_forward(H, W, labels):
     """Softmax cross entropy of the logits H W^T (H (tokens, dim), W (vocab, dim), bf16 or fp16) per token, without the
     logits: returns (loss, lse), fp32.  labels: int64, one outside [0, vocab) marks a token that does not count (loss 0)."""
-    import torch
     ops, sizes, dt = _head(H, W)
     y = _vector(labels, torch.int64, sizes[0], "labels")
     loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
@@ -635,7 +637,6 @@ def brsvd_xent_forward(H, W, labels):
 
 
 def _gradients(H, W, need_dH, need_dW):
-    import torch
     if not (need_dH or need_dW):
         raise ValueError("neither gradient is wanted")
     dH = torch.empty(H.shape, dtype=H.dtype, device=H.device) if need_dH else None
@@ -648,7 +649,6 @@ def _gradients(H, W, need_dH, need_dW):
 def brsvd_xent_backward(H, W, labels, lse, grad, need_dH=True, need_dW=True, piece=0):
     """Gradients (dH, dW) of sum_t grad_t loss_t, from the lse of the forward call; None for one that is not needed.  grad:
     fp32 tensor with a factor for each token or one for all.  piece: rows of W taken at a time (0: by the memory they need)."""
-    import torch
     ops, sizes, dt = _head(H, W)
     y, l = _vector(labels, torch.int64, sizes[0], "labels"), _vector(lse, torch.float32, sizes[0], "lse")
     keep, g, stride = _factors(grad, sizes[0])
@@ -660,7 +660,6 @@ def brsvd_xent_backward(H, W, labels, lse, grad, need_dH=True, need_dW=True, pie
 
 
 def _teacher(ids, logits, tokens):
-    import torch
     if ids.dim() != 2 or ids.shape[0] != tokens or ids.shape[1] < 1 or ids.shape != logits.shape:
         raise TypeError(f"ids and logits must have shape (tokens, top), not {tuple(ids.shape)} and {tuple(logits.shape)}")
     return (_dev(ids, torch.int64, "ids"), _dev(logits, torch.float32, "logits"), ids.shape[1])
@@ -671,7 +670,6 @@ def brsvd_distill_forward(H, W, ids, logits, temperature=1.0):
     """tau^2 KL(q || p) per token of the student's p = softmax(H W^T / tau) against the teacher's q, the softmax of its `top`
     kept logits / tau: ids int64, logits fp32, both (tokens, top); an entry with an id outside [0, vocab) or a logit of -inf
     does not count.  Returns (loss, lse, z), fp32: z (tokens, top) holds the student's logits of those words."""
-    import torch
     ops, sizes, dt = _head(H, W)
     te = _teacher(ids, logits, sizes[0])
     loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
@@ -685,7 +683,6 @@ def brsvd_distill_forward(H, W, ids, logits, temperature=1.0):
 @_scoped
 def brsvd_distill_backward(H, W, ids, logits, temperature, lse, z, grad, need_dH=True, need_dW=True, piece=0):
     """Gradients (dH, dW) of sum_t grad_t loss_t from the lse and z of the forward call; the rest as brsvd_xent_backward."""
-    import torch
     ops, sizes, dt = _head(H, W)
     te = _teacher(ids, logits, sizes[0])
     l = _vector(lse, torch.float32, sizes[0], "lse")

@@ -296,7 +296,7 @@ k_distill_loss(const Operand W, const Operand H, int64_t dim, const Teacher te, 
   if (threadIdx.x == 0) loss[t] = norm.y == 0.f ? 0.f : (part[0] + part[1] + part[2] + part[3]) / (te.scale * te.scale);
 }
 
-// q of every listed word (0 for the others), and whether the token has any.  A wave a token.
+// q of every listed word (0 for the others), added up over the token's entries with the same word, and whether the token has any.  A wave a token.
 __global__ void __launch_bounds__(256)
 k_distill_targets(const Teacher te, int64_t tokens, int64_t vocab, float* __restrict__ q, int* __restrict__ counts) {
   const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -304,27 +304,36 @@ k_distill_targets(const Teacher te, int64_t tokens, int64_t vocab, float* __rest
   if (t >= tokens) return;
   const float2 norm = teacher_norm(te, t, vocab, lane);
   const float inv = norm.y == 0.f ? 0.f : 1.f / norm.y;
-  for (int j = lane; j < te.top; j += 64) {
-    const int64_t at = t * te.top + j;
-    const float a = te.logits[at];
-    q[at] = is_listed(te.ids[at], a, vocab) ? __builtin_amdgcn_exp2f((a * te.scale - norm.x) * kLog2e) * inv : 0.f;
+  for (int j0 = 0; j0 < te.top; j0 += 64) {
+    const int64_t mine = j0 + lane < te.top ? te.ids[t * te.top + j0 + lane] : -1;
+    float sum = 0.f;
+    for (int i0 = 0; i0 < te.top; i0 += 64) {
+      const int64_t at = t * te.top + (i0 + lane < te.top ? i0 + lane : 0);
+      const float a = te.logits[at];
+      const int64_t id = i0 + lane < te.top && is_listed(te.ids[at], a, vocab) ? te.ids[at] : -1;
+      const float x = id >= 0 ? __builtin_amdgcn_exp2f((a * te.scale - norm.x) * kLog2e) * inv : 0.f;
+      const int last = te.top - i0 < 64 ? te.top - i0 : 64;
+      for (int i = 0; i < last; ++i) {
+        const int other = __builtin_amdgcn_readlane((int)id, i);           // words are below 2^30
+        const float y = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i));
+        if (other == (int)mine) sum += y;
+      }
+    }
+    if (j0 + lane < te.top) q[t * te.top + j0 + lane] = mine >= 0 && mine < vocab ? sum : 0.f;
   }
   if (lane == 0) counts[t] = norm.y != 0.f;
 }
 
-// The listed words of a piece in G: exp(z / tau - lse) - q, q added up over entries with the same word.  A thread an entry.
+// The listed words of a piece in G: exp(z / tau - lse) - q.  A thread an entry; entries with the same word write the same number.
 template <class El>
 __global__ void __launch_bounds__(256)
 k_distill_scatter(const Teacher te, const float* __restrict__ q, const float* __restrict__ z, const HeadMeta* __restrict__ meta, const int* __restrict__ index,
                   const float* __restrict__ lse, const float* __restrict__ coef, int64_t v0, int64_t rows, int64_t vocab, uint16_t* __restrict__ G, int64_t pitch) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, c = i / te.top;
   if (c >= meta->count) return;
-  const int64_t t = index[c], first = t * te.top, at = first + (i - c * te.top), id = te.ids[at];
+  const int64_t t = index[c], at = t * te.top + (i - c * te.top), id = te.ids[at];
   if (id < v0 || id >= v0 + rows || !is_listed(id, te.logits[at], vocab)) return;
-  float target = 0.f;
-  for (int j = 0; j < te.top; ++j)
-    if (te.ids[first + j] == id) target += q[first + j];
-  G[c * pitch + id - v0] = to16<El>(coef[c] * (__builtin_amdgcn_exp2f((z[at] * te.scale - lse[c]) * kLog2e) - target));
+  G[c * pitch + id - v0] = to16<El>(coef[c] * (__builtin_amdgcn_exp2f((z[at] * te.scale - lse[c]) * kLog2e) - q[at]));
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------
@@ -370,11 +379,15 @@ k_head_prepare(const int64_t* __restrict__ label, int64_t vocab, const int* __re
   }
 }
 
-// The rows of H that count next to each other (pitch in bytes, a multiple of 16, what lies beyond dim is never read), with their lse, factor and label.
+// The rows of H that count next to each other (pitch in bytes, a multiple of 16, what lies beyond dim is never read), with their lse, factor and label;
+// and zeros into the rows of dH (may be null) that do not.
 __global__ void __launch_bounds__(256)
-k_head_gather(const Operand H, int64_t dim, const HeadMeta* __restrict__ meta, const int* __restrict__ index, const float* __restrict__ lse,
-              const int64_t* __restrict__ label, char* __restrict__ Hc, int64_t pitch, float* __restrict__ lse_c, float* __restrict__ coef, int* __restrict__ label_c) {
+k_head_gather(const Operand H, int64_t dim, int64_t vocab, const HeadMeta* __restrict__ meta, const int* __restrict__ index, const float* __restrict__ lse,
+              const int64_t* __restrict__ label, const int* __restrict__ counts, char* __restrict__ Hc, int64_t pitch, float* __restrict__ lse_c,
+              float* __restrict__ coef, int* __restrict__ label_c, uint16_t* __restrict__ dH, int64_t lddh) {
   const int64_t c = blockIdx.x;
+  if (dH && !(label ? label[c] >= 0 && label[c] < vocab : counts[c] != 0))
+    for (int64_t d = threadIdx.x; d < dim; d += 256) dH[c * lddh + d] = 0;
   if (c >= meta->count) return;
   const int64_t t = index[c];
   for (int64_t k = 8 * (int64_t)threadIdx.x; k < dim; k += 2048) *(uint4*)(Hc + c * pitch + 2 * k) = piece_of<2>(H.base + t * H.ld + 2 * k, 2 * (dim - k));
@@ -508,23 +521,30 @@ k_head_dw(const HeadProduct g) {
   put_tile16<T::NQ>(acc, lds, g.out + q0 * g.ldo + p0, g.ldo, g.Q.n - q0, g.P.n - p0, [&](float x, int) { return to16<El>(x * down); });
 }
 
-// Rows of dH that do not count are zero, the others the sum of the splits' parts in their order.  Two launches: all rows zero, then those that count.
+// A matrix of zeros
 __global__ void __launch_bounds__(256)
-k_head_zero(uint16_t* __restrict__ dH, int64_t ld, int64_t rows, int64_t dim) {
-  for (int64_t d = threadIdx.x; d < dim; d += 256) dH[(int64_t)blockIdx.x * ld + d] = 0;
+k_head_zero(uint16_t* __restrict__ dW, int64_t ld, int64_t dim) {
+  for (int64_t d = threadIdx.x; d < dim; d += 256) dW[(int64_t)blockIdx.x * ld + d] = 0;
 }
+// The rows of dH that count: the sum of the splits' parts in their order.  A thread a number of a row, eight parts at a time on their way.
 template <class El>
 __global__ void __launch_bounds__(256)
 k_head_finish(const float* __restrict__ sum, int splits, int64_t tokens, int64_t dim, const HeadMeta* __restrict__ meta, const int* __restrict__ index,
               uint16_t* __restrict__ dH, int64_t ld) {
-  const int64_t c = blockIdx.x;
-  if (c >= meta->count) return;
-  uint16_t* out = dH + index[c] * ld;
-  for (int64_t d = threadIdx.x; d < dim; d += 256) {
-    float x = 0.f;
-    for (int s = 0; s < splits; ++s) x += sum[(s * tokens + c) * dim + d];
-    out[d] = to16<El>(x * meta->down);
+  const int64_t per = (dim + 255) / 256, c = blockIdx.x / per, d = (blockIdx.x - c * per) * 256 + threadIdx.x;
+  if (c >= meta->count || d >= dim) return;
+  const float* from = sum + c * dim + d;
+  float x = 0.f;
+  int s = 0;
+  for (; s + 8 <= splits; s += 8) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = from[(s + i) * tokens * dim];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x += v[i];
   }
+  for (; s < splits; ++s) x += from[s * tokens * dim];
+  dH[index[c] * ld + d] = to16<El>(x * meta->down);
 }
 
 // ---- plans ---------------------------------------------------------------------------------------------------------
@@ -580,7 +600,7 @@ static HeadPlan head_plan(int64_t tokens, int64_t vocab, int64_t dim, int64_t pi
 
 static bool head_sizes(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece, int64_t top) {
   return tokens >= 0 && vocab >= 1 && dim >= 1 && piece >= 0 && top >= 0 && dim < kMaxPitch / 2 && tokens < (int64_t)1 << 30 && vocab < (int64_t)1 << 30 &&
-         ceil_div(vocab, kTileP) * ceil_div(tokens, 64) <= kMaxGrid && (top == 0 || tokens <= kMaxGrid / top);
+         ceil_div(vocab, kTileP) * ceil_div(tokens, 16) <= kMaxGrid && tokens <= kMaxGrid / ceil_div(dim, 256) && (top == 0 || tokens <= kMaxGrid / top);
 }
 static bool half_type(int dtype) { return dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16; }
 
@@ -647,8 +667,8 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   const Operand H = rows_of(c.H, c.ldh, c.tokens);
   if (!c.label) hipLaunchKernelGGL(k_distill_targets, dim3((unsigned)ceil_div(c.tokens, 4)), dim3(256), 0, stream, c.teacher, c.tokens, c.vocab, q, counts);
   hipLaunchKernelGGL(k_head_prepare, dim3(1), dim3(1024), 0, stream, c.label, c.vocab, counts, c.tokens, grad, grad_stride, 1.f / c.scale, meta, index, coef);
-  hipLaunchKernelGGL(k_head_gather, dim3((unsigned)c.tokens), dim3(256), 0, stream, H, c.dim, meta, index, lse, c.label, hc, plan.pitch_h, lse_c, coef, label_c);
-  if (dH) hipLaunchKernelGGL(k_head_zero, dim3((unsigned)c.tokens), dim3(256), 0, stream, (uint16_t*)dH, lddh, c.tokens, c.dim);
+  hipLaunchKernelGGL(k_head_gather, dim3((unsigned)c.tokens), dim3(256), 0, stream, H, c.dim, c.vocab, meta, index, lse, c.label, counts, hc,
+                     plan.pitch_h, lse_c, coef, label_c, (uint16_t*)dH, lddh);
   const bool direct = aligned_pieces(c.W, 2 * c.ldw);
   const int bq = tokens_tile(c.tokens, direct, ceil_div(c.dim, kTileP) * plan.splits), bl = logits_tile(c.tokens, direct, plan.piece < c.vocab ? plan.piece : c.vocab);
   const int64_t tiles_t = ceil_div(c.tokens, bq);
@@ -705,7 +725,7 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   const int64_t first = c.vocab < plan.piece ? c.vocab : plan.piece;
   const int splits = (int)ceil_div(first, plan.per_split);
   if (dH)
-    hipLaunchKernelGGL(k_head_finish<El>, dim3((unsigned)c.tokens), dim3(256), 0, stream, sum, splits, c.tokens, c.dim, meta, index, (uint16_t*)dH, lddh);
+    hipLaunchKernelGGL(k_head_finish<El>, dim3((unsigned)(c.tokens * ceil_div(c.dim, 256))), dim3(256), 0, stream, sum, splits, c.tokens, c.dim, meta, index, (uint16_t*)dH, lddh);
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
 }
@@ -768,7 +788,7 @@ static int head_backward_call(const HeadCall& c, int64_t piece, const float* lse
   if ((dH && lddh < c.dim) || (dW && lddw < c.dim)) return BRSVD_ERR_ARG;
   if (c.tokens == 0) {
     if (!dW) return BRSVD_OK;
-    hipLaunchKernelGGL(k_head_zero, dim3((unsigned)c.vocab), dim3(256), 0, s, (uint16_t*)dW, lddw, c.vocab, c.dim);
+    hipLaunchKernelGGL(k_head_zero, dim3((unsigned)c.vocab), dim3(256), 0, s, (uint16_t*)dW, lddw, c.dim);
     BRSVD_HIP_TRY(hipGetLastError());
     return BRSVD_OK;
   }

@@ -117,6 +117,11 @@ k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, 
   if (TRANSPOSED) {
     float f[W];
     if (!SQUARE) {
+      // the columns' magnitudes anew: those of the rows, kept until here, would double the registers and halve the workgroups of a CU
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j) asm volatile("" : "+v"(x[i][j]));
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         float t = 0.f;
@@ -207,6 +212,42 @@ k_quantize_rows(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t c
   }
 }
 
+// 128 x 128 blocks by themselves: a wave reads 1 KiB of a row at a time, 2 (16-bit: 4) blocks next to each other, the waves share the 128 rows.
+template <int DT>
+__global__ void __launch_bounds__(DT == BRSVD_DTYPE_F32 ? 512 : 1024)
+k_quantize_square(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S) {
+  using P = Part<DT>;
+  constexpr int W = P::kWide, L = P::kLanes, BLOCKS = 64 / L, WAVES = DT == BRSVD_DTYPE_F32 ? 8 : 16, R = kBlock / WAVES;
+  __shared__ float top[WAVES][BLOCKS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = lane / L;
+  const unsigned ncb = (unsigned)((cols + kBlock - 1) / kBlock), across = (ncb + BLOCKS - 1) / BLOCKS, rb = blockIdx.x / across, cb = (blockIdx.x % across) * BLOCKS;
+  const int64_t row0 = (int64_t)rb * kBlock + wave * R, col = (int64_t)cb * kBlock + lane * W;
+  const int width = (int)(cols - col < W ? (cols - col > 0 ? cols - col : 0) : W);
+  float x[R][W], t = 0.f;
+#pragma unroll
+  for (int i = 0; i < R; ++i) numbers<DT>(X + (row0 + i) * ldx + col * P::kBytes, row0 + i < rows ? width : 0, x[i]);
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int j = 0; j < W; ++j) t = fmaxf(t, finite_abs(x[i][j]));
+  t = max16(t);
+  if (L == 32) t = fmaxf(t, __shfl_xor(t, 16));
+  if (lane % L == 0) top[wave][mine] = t;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) t = fmaxf(t, top[w][mine]);
+  const int e = block_exponent(t);
+  const float f = power_of_two(-e);
+  if (wave == 0 && lane % L == 0 && cb + mine < ncb) S[(int64_t)rb * ncb + cb + mine] = power_of_two(e);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    uint32_t v[W / 4];
+#pragma unroll
+    for (int j = 0; j < W; j += 4) v[j / 4] = pack_e4m3(x[i][j] * f, x[i][j + 1] * f, x[i][j + 2] * f, x[i][j + 3] * f);
+    if (row0 + i < rows) put_bytes<W>(Q + (row0 + i) * ldq + col, width, v);
+  }
+}
+
 // X = Q * S: a thread writes 16 bytes of X at a time, neighbouring lanes neighbouring pieces, four rows.
 template <int DT>
 __global__ void __launch_bounds__(256)
@@ -270,7 +311,9 @@ static void launch_quantize(const char* X, int64_t ldx, int64_t rows, int64_t co
   if (!SQUARE && !Qt)
     hipLaunchKernelGGL(k_quantize_rows<DT>, dim3((unsigned)ceil_div(rows * ceil_div(cols, kBlock), 256 / Part<DT>::kLanes * 4)), dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S);
   else if (Q && Qt) hipLaunchKernelGGL((k_quantize<DT, SQUARE, true, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
-  else if (Q) hipLaunchKernelGGL((k_quantize<DT, true, true, false>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
+  else if (Q)
+    hipLaunchKernelGGL(k_quantize_square<DT>, dim3((unsigned)(ceil_div(ceil_div(cols, kBlock), 64 / Part<DT>::kLanes) * ceil_div(rows, kBlock))),
+                       dim3(DT == BRSVD_DTYPE_F32 ? 512 : 1024), 0, stream, X, pitch, rows, cols, Q, ldq, S);
   else hipLaunchKernelGGL((k_quantize<DT, SQUARE, false, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
 }
 
