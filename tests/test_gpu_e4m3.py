@@ -156,6 +156,38 @@ def test_product(m, n, k, pad_a, pad_b, block):
     assert bool((wide[:, 0] == 5).all() and (wide[:, n + 1:] == 5).all())
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 8200, 300), (5, 16390, 300), (20, 16400, 700), (33, 8193, 300), (40, 4096, 1100), (130, 8200, 260), (1000, 2100, 400)])
+def test_product_with_many_columns(m, n, k):
+    """The ways that few rows are multiplied by their number and that of the columns, and tiles of both sizes."""
+    dev = need_gpu()
+    qa, sa, a = eight_bits(m + 7 * k, m, k, 1, dev)
+    qb, sb, b = eight_bits(n + 3 * k, n, k, 128, dev)
+    for dtype in (torch.float32, torch.bfloat16):
+        check_product(B.brsvd_gemm_e4m3(qa, sa, qb, sb, dtype=dtype), a, b, dtype)
+
+
+@pytest.mark.parametrize("block", [128, 1])
+@pytest.mark.parametrize("m", [100, 300])
+def test_scales_that_are_not_powers_of_two_from_some_block_on(m, block):
+    """Powers of two go into the instruction, others are multiplied afterwards: a product that meets its first other scale in the middle, for a few
+    rows only, in the first block, in the last; negative scales, zeros and scales outside the range of an exponent among them."""
+    dev = need_gpu()
+    k, n = 1300, 400
+    qa, _, _ = eight_bits(1, m, k, 1, dev)
+    qb, _, _ = eight_bits(2, n, k, block, dev)
+    g = torch.Generator().manual_seed(4)
+    blocks = -(-k // 128)
+    rows = n if block == 1 else -(-n // 128)
+    for where, value in ((0, 3.0), (4, 0.7), (5, -2.0), (7, 0.0), (blocks - 1, 1.5), (3, 1e-40)):
+        sa, sb = (torch.exp2(torch.randint(-6, 6, (r, blocks), generator=g).float()) for r in (m, rows))
+        for side in (sa, sb):
+            side[side.shape[0] - 1, where] = value
+            got = B.brsvd_gemm_e4m3(qa, sa.to(dev), qb, sb.to(dev), block_rows=block)
+            a = qa.float().double().cpu() * sa.double().repeat_interleave(128, 1)[:, :k]
+            b = qb.float().double().cpu() * sb.double().repeat_interleave(block, 0)[:n].repeat_interleave(128, 1)[:, :k]
+            check_product(got, a, b, torch.bfloat16)
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 40, 200), (70, 260, 200), (300, 300, 520)])
 def test_product_of_whole_numbers_is_exact(m, n, k):
     """Sums below 2^24 of whole numbers with scales of one have one answer, whatever the order: any index that is off shows."""

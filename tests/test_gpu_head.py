@@ -103,6 +103,25 @@ def test_xent(tokens, vocab, dim, dtype, pad, shift):
     assert none is None and torch.equal(only, B.brsvd_xent_backward(H, W, y.to(dev), lse, each)[1])
 
 
+@pytest.mark.parametrize("tokens,vocab,dim,pad", [(300, 70001, 24, 0), (300, 70001, 17, 0), (70, 40000, 136, 0), (20, 5000, 40, 8), (33, 5000, 1000, 0)])
+def test_xent_of_many_tiles(tokens, vocab, dim, pad):
+    """More tiles than workgroups at once, aligned and not, and the tiles for few tokens."""
+    dev = need_gpu()
+    H, W, y, g = problem(tokens, vocab, dim, torch.bfloat16, dev, pad)
+    y[0], y[1] = vocab - 1, -1
+    ref = Reference(H, W)
+    loss, lse = B.brsvd_xent_forward(H, W, y.to(dev))
+    ref.check_lse(lse)
+    counted = y >= 0
+    target = torch.zeros_like(ref.z)
+    target[torch.nonzero(counted)[:, 0], y[counted]] = 1.0
+    ref.check("loss", loss, torch.where(counted, ref.lse - (target * ref.z).sum(dim=1), 0.0), torch.where(counted, ref.dlse + ref.dz.amax(dim=1) + 2.0 ** -22 * (ref.lse + 9), 0.0))
+    grad = (torch.rand(tokens, generator=g) + 0.5).to(dev)
+    for piece in (0, 20000):
+        dH, dW = B.brsvd_xent_backward(H, W, y.to(dev), lse, grad, piece=piece)
+        ref.check_gradients(dH, dW, target, grad.double().cpu() * counted)
+
+
 @pytest.mark.parametrize("dtype", HALF)
 def test_what_does_not_count_reaches_nothing(dtype):
     """NaN and infinities in the hidden states of padding, half of the tokens: gradients are those of the others alone."""
