@@ -290,6 +290,30 @@ int main() {
     }
   }
 
+  // ---- the calls on a model's matrices: sizes of scratch and workspace over their whole range, refusals before any GPU call ----
+  for (int i = 0; i < 20000; ++i) {
+    const int64_t big[] = {1, 7, 64, 300, 5000, 100000, 3000000, (int64_t)1 << 29, (int64_t)1 << 31, (int64_t)1 << 40, INT64_MAX / 2};
+    const int64_t m = uniform(-1, big[next_u64() % 11]), n = uniform(-1, big[next_u64() % 11]), k = uniform(-1, big[next_u64() % 11]), piece = uniform(-1, big[next_u64() % 11]);
+    const int32_t dt = (int32_t)uniform(-1, 5), top = (int32_t)uniform(-1, 200), br = next_u64() & 1 ? 1 : 128;
+    const uint64_t linear = brsvd_linear_e4m3_scratch_bytes(m, n, k, dt), gemm = brsvd_gemm_e4m3_scratch_bytes(m, n, k, br, dt);
+    CHECK(gemm % 4 == 0 && (br == 1 || linear >= gemm));
+    const uint64_t fwd = brsvd_head_workspace_bytes(m, n, k, piece, top, 0), bwd = brsvd_head_workspace_bytes(m, n, k, piece, top, 1);
+    CHECK(fwd % 256 == 0 && bwd % 256 == 0 && (fwd == 0) == (bwd == 0));
+    if (bwd && m < 100000 && n < 1000000 && k < 10000) CHECK(bwd >= (uint64_t)m * k * 2 + (uint64_t)m * 256 * 2);
+    void* at = (void*)0x10000;
+    if (fwd > 256) {
+      CHECK(brsvd_xent_forward(at, k, at, k, (const int64_t*)at, m, n, k, BRSVD_DTYPE_BF16, (float*)at, (float*)at, at, fwd - 256 - 256 * (top > 0 ? (uint64_t)m * top : 0), nullptr) != BRSVD_OK);
+      CHECK(brsvd_distill_backward(at, k, at, k, (const int64_t*)at, (const float*)at, top > 0 ? top : 1, 1.f, (const float*)at, (const float*)at, (const float*)at, 1, m, n, k,
+                                   piece, BRSVD_DTYPE_F16, at, k, at, k, at, bwd / 2, nullptr) != BRSVD_OK);
+    }
+    if (gemm > 4)
+      CHECK(brsvd_gemm_e4m3((const uint8_t*)at, k, (const float*)at, (const uint8_t*)at, k, (const float*)at, br, m, n, k, dt, at, n, at, gemm - 4, nullptr) == BRSVD_ERR_BUDGET);
+  }
+  CHECK(brsvd_quantize_e4m3(nullptr, 0, 3, 3, BRSVD_DTYPE_F32, 1, nullptr, 0, nullptr, nullptr, 0, nullptr, nullptr) == BRSVD_ERR_ARG);
+  CHECK(brsvd_dequantize_e4m3((const uint8_t*)0x10000, INT64_MAX, (const float*)0x10000, INT64_MAX, INT64_MAX, 1, BRSVD_DTYPE_F32, (void*)0x10000, INT64_MAX, nullptr) ==
+        BRSVD_ERR_ARG);
+  CHECK(brsvd_dequantize_e4m3(nullptr, 0, nullptr, INT64_MAX, INT64_MAX, 128, BRSVD_DTYPE_F32, nullptr, 0, nullptr) == BRSVD_ERR_ARG);
+
   std::printf("host checks: %d run, %d failed\n", g_checks, g_failed);
   std::fflush(stdout);
   return g_failed ? 1 : 0;
