@@ -510,19 +510,19 @@ static int splits_for(int64_t workgroups, int blocks, int least) {
 }
 struct E4m3Plan {
   bool rows;               // k_rows_e4m3
-  int nt, bq, splits, per_split;
+  int splits, per_split;
+  int64_t large;           // columns of C in tiles of 256 rows, in 256; the others in tiles of 128
 };
 static E4m3Plan e4m3_plan(int64_t m, int64_t n, int64_t k, bool per_row, int dtype) {
   E4m3Plan p;
   const int blocks = (int)ceil_div(k, kBlock);
   p.rows = few_rows(m, n) && !per_row;
-  p.nt = 1;
-  // A tile of 256 x 256 has no registers left for numbers of 16 bits; and one of 256 x 128, seven tenths of its time, is taken where that is less in all
-  // on 256 CUs: 1000 x 5000 from 3000 39 us and 57 (160 tiles and 80 in one round), 4096 x 6000 from 4001 161 and 142 (three rounds and two).
+  // A tile of 256 x 256 has no registers left for the fp16 numbers of an fp32 result.  Rounds of 256 workgroups: 1000 x 5000 from 3000 39 us in 256 x 128 and
+  // 57 in 256 x 256 (160 tiles and 80, one round).
   const int64_t cols = ceil_div(n, 256);
-  p.bq = dtype == BRSVD_DTYPE_F32 || m <= 128 || 7 * ceil_div(cols * ceil_div(m, 128), 256) < 10 * ceil_div(cols * ceil_div(m, 256), 256) ? 128 : 256;
+  p.large = dtype == BRSVD_DTYPE_F32 || m <= 128 ? 0 : large_tiles(cols, ceil_div(m, 256), ceil_div(m, 128), blocks);
   p.splits = 1;
-  if (!p.rows) p.splits = splits_for(ceil_div(n, 256) * ceil_div(m, p.bq), blocks, 4);
+  if (!p.rows) p.splits = splits_for(p.large * ceil_div(m, 256) + (cols - p.large) * ceil_div(m, 128), blocks, 4);
   p.per_split = (int)ceil_div(blocks, p.splits);
   p.splits = (int)ceil_div(blocks, p.per_split);
   return p;
@@ -536,8 +536,7 @@ static void launch_rows(const E4m3Args& g, hipStream_t stream) {
 }
 template <int DT, bool WIDE>
 static void launch_few(const E4m3Args& g, hipStream_t stream) {
-  if (g.B.n >= 32 * 512) launch_rows<1, 2, 2, 4, DT, WIDE>(g, stream);
-  else if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, 4, DT, WIDE>(g, stream);
+  if (g.B.n >= 16 * 512) launch_rows<1, 2, 2, 4, DT, WIDE>(g, stream);
   else launch_rows<1, 1, 4, 8, DT, WIDE>(g, stream);
 }
 template <bool WIDE>
@@ -547,16 +546,27 @@ static void launch_more(const E4m3Args& g, hipStream_t stream) {
   else launch_rows<4, 1, 2, 8, -1, WIDE>(g, stream);
 }
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>
-static void launch_tiles(const E4m3Args& g, hipStream_t stream) {
+static void launch_tiles(E4m3Args g, hipStream_t stream) {
+  g.tiles_n = ceil_div(g.B.n, 256);
+  g.tiles_m = ceil_div(g.A.n, 64 * NQ);
   hipLaunchKernelGGL((k_tiles_e4m3<NQ, PER_ROW, DIRECT, WIDE>), dim3(tile_workgroups(g.tiles_n, g.tiles_m), (unsigned)g.splits), dim3(512), 0, stream, g);
 }
 template <bool PER_ROW, bool DIRECT>
-static void launch_tiles(const E4m3Args& g, int bq, bool wide, hipStream_t stream) {
-  if (wide) launch_tiles<2, PER_ROW, DIRECT, true>(g, stream);
-  else if constexpr (DIRECT) {
-    if (bq == 256) launch_tiles<4, PER_ROW, DIRECT, false>(g, stream);
-    else launch_tiles<2, PER_ROW, DIRECT, false>(g, stream);
-  } else launch_tiles<2, PER_ROW, DIRECT, false>(g, stream);
+static void launch_tiles(E4m3Args g, int64_t large, bool wide, hipStream_t stream) {
+  if (wide) return launch_tiles<2, PER_ROW, DIRECT, true>(g, stream);
+  if constexpr (DIRECT) {                       // nor for pieces on their way through them
+    const int64_t n = g.B.n, first = 256 * large < n ? 256 * large : n;
+    if (first > 0) {
+      g.B.n = first;
+      launch_tiles<4, PER_ROW, DIRECT, false>(g, stream);
+      if (first == n) return;
+      g.B.n = n - first;
+      g.B.base += first * g.B.ld;
+      g.SB += (PER_ROW ? first : first / kBlock) * g.blocks;
+      g.C = (char*)g.C + first * (g.dtype == BRSVD_DTYPE_F32 ? 4 : 2);
+    }
+  }
+  launch_tiles<2, PER_ROW, DIRECT, false>(g, stream);
 }
 
 // a_type: type of A's numbers, -1 for 8 bits with the scales SA
@@ -575,8 +585,6 @@ static int gemm_e4m3(const void* A, int64_t lda_bytes, int a_type, const float* 
   g.C = split ? part : C;
   g.ldc = split ? n : ldc;
   g.dtype = split ? BRSVD_DTYPE_F32 : dtype;
-  g.tiles_n = ceil_div(n, 256);
-  g.tiles_m = ceil_div(m, plan.bq);
   if (plan.rows) {
     const bool wide = dtype == BRSVD_DTYPE_F32;
     if (m > kCastRows) wide ? launch_more<true>(g, stream) : launch_more<false>(g, stream);
@@ -587,11 +595,10 @@ static int gemm_e4m3(const void* A, int64_t lda_bytes, int a_type, const float* 
   } else {
     const bool direct = aligned_pieces(A, lda_bytes) && aligned_pieces(B, ldb);
     const bool wide = dtype == BRSVD_DTYPE_F32;
-    if (!direct) g.tiles_m = ceil_div(m, 128);        // nor for pieces on their way through them
-    if (per_row && direct) launch_tiles<true, true>(g, plan.bq, wide, stream);
-    else if (per_row) launch_tiles<true, false>(g, plan.bq, wide, stream);
-    else if (direct) launch_tiles<false, true>(g, plan.bq, wide, stream);
-    else launch_tiles<false, false>(g, plan.bq, wide, stream);
+    if (per_row && direct) launch_tiles<true, true>(g, plan.large, wide, stream);
+    else if (per_row) launch_tiles<true, false>(g, plan.large, wide, stream);
+    else if (direct) launch_tiles<false, true>(g, plan.large, wide, stream);
+    else launch_tiles<false, false>(g, plan.large, wide, stream);
   }
   if (split) hipLaunchKernelGGL(k_join_splits, dim3((unsigned)ceil_div(m * ceil_div(n, 4), 256)), dim3(256), 0, stream, part, plan.splits, m, n, C, ldc, dtype);
   BRSVD_HIP_TRY(hipGetLastError());

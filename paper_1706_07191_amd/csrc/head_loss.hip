@@ -22,16 +22,27 @@ template <class El, bool DIRECT, int BQ> struct Logits : Tiles<El, kRows, kRows,
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 64> : RowsProduct<El, 2, 4, 4, 2> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 32> : RowsProduct<El, 2, 2, 4, 4> {};
 template <class El, bool DIRECT> struct Logits<El, DIRECT, 16> : RowsProduct<El, 2, 1, 4, 4> {};
-// Tokens of a tile.  256 x 256 has no registers left for pieces on their way through them; and 256 x 128, seven tenths of its time, is taken where that
-// is less in all on 256 CUs: 130 tokens over 32000 words of width 2000, 250 tiles or 125 in one round, 41 us and 53.  others: tiles along the
-// other side.
-static int tokens_tile(int64_t tokens, bool direct, int64_t others) {
-  if (tokens <= 64) return 64;
-  if (tokens <= 128 || !direct) return 128;
-  return 7 * ceil_div(others * ceil_div(tokens, 128), 256) < 10 * ceil_div(others * ceil_div(tokens, 256), 256) ? 128 : 256;
+// How many tiles along the other side (others) have 256 tokens, the rest 128 or fewer.  256 x 256 has no registers left for pieces on their way through
+// them.  130 tokens over 32000 words of width 2000, one round of 250 tiles or of 125: 41 us and 53.
+static int64_t large_token_tiles(int64_t tokens, bool direct, int64_t others, int64_t contraction) {
+  return tokens <= 128 || !direct ? 0 : large_tiles(others, ceil_div(tokens, 256), ceil_div(tokens, 128), ceil_div(contraction, 64));
 }
-static int logits_tile(int64_t tokens, bool direct, int64_t words) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens_tile(tokens, direct, ceil_div(words, kTileP)); }
-static int logits_rows(int bq) { return bq <= 64 ? 128 : kTileP; }     // of the vocabulary
+static int small_tile(int64_t tokens) { return tokens <= 64 ? 64 : 128; }
+// The logits of `words` words: the first `large` in tiles of 256 words x 256 tokens, the others in tiles of `rows` words x `bl` tokens.
+struct LogitTiles {
+  int64_t large;
+  int bl, rows;
+  int64_t first, count;      // tiles along the vocabulary: large ones, all
+};
+static LogitTiles logit_tiles(int64_t tokens, bool direct, int64_t words, int64_t dim) {
+  LogitTiles t;
+  t.first = large_token_tiles(tokens, direct, ceil_div(words, kTileP), dim);
+  t.large = kTileP * t.first < words ? kTileP * t.first : words;
+  t.bl = tokens <= 16 ? 16 : tokens <= 32 ? 32 : small_tile(tokens);
+  t.rows = t.bl <= 64 ? 128 : kTileP;
+  t.count = t.first + ceil_div(words - t.large, t.rows);
+  return t;
+}
 
 // What the backward pass knows on the device: how many tokens count, and the power of two that G is multiplied by so that its numbers of 16 bits hold what
 // matters: 2^e max |g_t| is at most 2^14, and a probability of 2^-28 is still a normal number of fp16.
@@ -52,6 +63,7 @@ struct HeadArgs {
   const HeadMeta* meta;    // backward
   const float *lse, *coef; // backward, of the tokens that count
   const int* label_c;
+  int64_t first;           // row of W that the first tile begins with
   int64_t v0;              // backward: the piece's first row
   uint16_t* G;             // backward: [token][pitch]
   int64_t pitch;
@@ -64,7 +76,7 @@ constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 template <class T>
 __device__ __forceinline__ void leave_tile(const HeadArgs& g, floatx4 (&acc)[T::NP][T::NQ], int64_t tv, int64_t tt, float2* red) {
   constexpr int NP = T::NP, NQ = T::NQ, WP = T::WP, BQ = T::BQ;
-  const int64_t v0 = tv * T::BP, t0 = tt * BQ;
+  const int64_t v0 = g.first + tv * T::BP, t0 = tt * BQ;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = wave % WP, wq = wave / WP;
   const int64_t vwave = v0 + 16 * wp * NP, vlane = vwave + 4 * (lane >> 4);
   const float scale = g.scale * kLog2e;
@@ -144,13 +156,13 @@ k_head_lse(const HeadArgs g) {
   if (!tile_of_workgroup(b, g.tiles_v, g.tiles_t, 8, &tv, &tt)) return;
   if constexpr (T::kThreads == kTileThreads && DIRECT) {
     T tile;
-    tile.begin(g.W, tv * T::BP, g.H, tt * BQ, 0, g.dim, lds);
+    tile.begin(g.W, g.first + tv * T::BP, g.H, tt * BQ, 0, g.dim, lds);
     while (true) {
       tile.multiply(acc);
       int64_t nv = 0, nt = 0;
       b += gridDim.x;
       const bool more = tile_of_workgroup(b, g.tiles_v, g.tiles_t, 8, &nv, &nt);
-      if (more) tile.begin(g.W, nv * T::BP, g.H, nt * BQ, 0, g.dim, lds);
+      if (more) tile.begin(g.W, g.first + nv * T::BP, g.H, nt * BQ, 0, g.dim, lds);
       leave_tile<T>(g, acc, tv, tt, red);
       if (!more) break;
       tv = nv;
@@ -158,7 +170,7 @@ k_head_lse(const HeadArgs g) {
     }
   } else {
     do {
-      T::run(acc, g.W, tv * T::BP, g.H, tt * BQ, 0, g.dim, lds);
+      T::run(acc, g.W, g.first + tv * T::BP, g.H, tt * BQ, 0, g.dim, lds);
       leave_tile<T>(g, acc, tv, tt, red);
       __syncthreads();
       b += gridDim.x;
@@ -407,7 +419,7 @@ k_head_grad(const HeadArgs g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tv, tt;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_v, g.tiles_t, 8, &tv, &tt)) return;
-  const int64_t count = g.meta->count, p0 = tv * T::BP, t0 = tt * BQ;
+  const int64_t count = g.meta->count, p0 = g.first + tv * T::BP, t0 = tt * BQ;
   if (t0 >= count) return;
   Operand H = g.H;
   H.n = count;
@@ -465,6 +477,7 @@ struct HeadProduct {
   float* sum;              // dH: [split][token][dim], added to if `more`
   bool more;
   uint16_t* out;           // dW
+  int64_t first;           // dW: the word that the first tile begins with
   int64_t ldo;
 };
 
@@ -507,14 +520,14 @@ k_head_dh(const HeadProduct g) {
 }
 
 // dW = G^T H of a piece: both operands hold the tokens in their rows.
-template <class El>
+template <class El, int BQ>
 __global__ void __launch_bounds__(kTileThreads, 2)
 k_head_dw(const HeadProduct g) {
-  using T = Tiles<El, kCols, kCols, true, 256>;
+  using T = Tiles<El, kCols, kCols, true, BQ>;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
-  const int64_t p0 = tp * kTileP, q0 = tq * 256;
+  const int64_t p0 = tp * kTileP, q0 = g.first + tq * BQ;
   floatx4 acc[T::NP][T::NQ];
   T::run(acc, g.P, p0, g.Q, q0, 0, g.meta->count, lds);
   const float down = g.meta->down;
@@ -580,7 +593,7 @@ static HeadPlan head_plan(int64_t tokens, int64_t vocab, int64_t dim, int64_t pi
   p.per_split = ceil_div(ceil_div(p.piece, s), 64) * 64;
   p.splits = (int)ceil_div(p.piece, p.per_split);
   p.part = 0;
-  p.zlabel = whole256((uint64_t)ceil_div(vocab, logits_rows(logits_tile(tokens, true, vocab))) * tokens * 8);
+  p.zlabel = whole256((uint64_t)logit_tiles(tokens, true, vocab, dim).count * tokens * 8);
   p.forward_bytes = p.zlabel + whole256((uint64_t)tokens * 4);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t here = at; at += whole256(bytes); return here; };
@@ -604,7 +617,7 @@ static bool head_sizes(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece
 }
 static bool half_type(int dtype) { return dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16; }
 
-#define BRSVD_LOGITS(KERNEL, El, DIRECT, grid, stream, args)                                                      \
+#define BRSVD_LOGITS(KERNEL, El, DIRECT, bl, grid, stream, args)                                                  \
   do {                                                                                                           \
     const dim3 few(Logits<El, true, 16>::kThreads);                                                              \
     if (bl == 256 && DIRECT) hipLaunchKernelGGL((KERNEL<El, true, 256>), grid, dim3(kTileThreads), 0, stream, args); \
@@ -639,18 +652,26 @@ static int head_forward(const HeadCall& c, const HeadPlan& plan, char* ws, float
   g.dim = c.dim;
   g.scale = c.scale;
   const bool direct = aligned_pieces(c.W, 2 * c.ldw) && aligned_pieces(c.H, 2 * c.ldh);
-  const int bl = logits_tile(c.tokens, direct, c.vocab);
-  g.tiles_v = ceil_div(c.vocab, logits_rows(bl));
-  g.tiles_t = ceil_div(c.tokens, bl);
+  const LogitTiles tiles = logit_tiles(c.tokens, direct, c.vocab, c.dim);
   g.label = c.label;
   g.part = (float2*)(ws + plan.part);
   g.zlabel = (float*)(ws + plan.zlabel);
-  unsigned workgroups = tile_workgroups(g.tiles_v, g.tiles_t);
-  if (bl >= 128 && workgroups > 256) workgroups = 256;        // as many as run at once
-  const dim3 grid(workgroups);
-  if (direct) BRSVD_LOGITS(k_head_lse, El, true, grid, stream, g);
-  else BRSVD_LOGITS(k_head_lse, El, false, grid, stream, g);
-  hipLaunchKernelGGL(k_head_join, dim3((unsigned)ceil_div(c.tokens, 16)), dim3(256), 0, stream, g.part, g.tiles_v, c.tokens, c.label, c.vocab, g.zlabel, lse, loss);
+  auto launch = [&](int64_t tiles_v, int bl) {
+    g.tiles_v = tiles_v;
+    g.tiles_t = ceil_div(c.tokens, bl);
+    unsigned workgroups = tile_workgroups(g.tiles_v, g.tiles_t);
+    if (bl >= 128 && workgroups > 256) workgroups = 256;        // as many as run at once
+    const dim3 grid(workgroups);
+    if (direct) BRSVD_LOGITS(k_head_lse, El, true, bl, grid, stream, g);
+    else BRSVD_LOGITS(k_head_lse, El, false, bl, grid, stream, g);
+  };
+  if (tiles.first > 0) launch(tiles.first, 256);
+  if (tiles.first < tiles.count) {
+    g.first = tiles.large;
+    g.part += tiles.first * c.tokens;
+    launch(tiles.count - tiles.first, tiles.bl);
+  }
+  hipLaunchKernelGGL(k_head_join, dim3((unsigned)ceil_div(c.tokens, 16)), dim3(256), 0, stream, (const float2*)(ws + plan.part), tiles.count, c.tokens, c.label, c.vocab, g.zlabel, lse, loss);
   if (!c.label) hipLaunchKernelGGL(k_distill_loss<El>, dim3((unsigned)c.tokens), dim3(256), 0, stream, g.W, g.H, c.dim, c.teacher, lse, z, loss);
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
@@ -670,7 +691,7 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   hipLaunchKernelGGL(k_head_gather, dim3((unsigned)c.tokens), dim3(256), 0, stream, H, c.dim, c.vocab, meta, index, lse, c.label, counts, hc,
                      plan.pitch_h, lse_c, coef, label_c, (uint16_t*)dH, lddh);
   const bool direct = aligned_pieces(c.W, 2 * c.ldw);
-  const int bq = tokens_tile(c.tokens, direct, ceil_div(c.dim, kTileP) * plan.splits), bl = logits_tile(c.tokens, direct, plan.piece < c.vocab ? plan.piece : c.vocab);
+  const int bq = large_token_tiles(c.tokens, direct, ceil_div(c.dim, kTileP) * plan.splits, plan.per_split) > 0 ? 256 : small_tile(c.tokens);
   const int64_t tiles_t = ceil_div(c.tokens, bq);
   for (int64_t v0 = 0; v0 < c.vocab; v0 += plan.piece) {
     const int64_t rows = c.vocab - v0 < plan.piece ? c.vocab - v0 : plan.piece;
@@ -679,8 +700,6 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
     g.H = Operand{hc, plan.pitch_h, c.tokens};
     g.dim = c.dim;
     g.scale = c.scale;
-    g.tiles_v = ceil_div(rows, logits_rows(bl));
-    g.tiles_t = ceil_div(c.tokens, bl);
     g.meta = meta;
     g.lse = lse_c;
     g.coef = coef;
@@ -688,9 +707,19 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
     g.v0 = v0;
     g.G = G;
     g.pitch = plan.piece;
-    const dim3 grid(tile_workgroups(g.tiles_v, g.tiles_t));
-    if (direct) BRSVD_LOGITS(k_head_grad, El, true, grid, stream, g);
-    else BRSVD_LOGITS(k_head_grad, El, false, grid, stream, g);
+    const LogitTiles tiles = logit_tiles(c.tokens, direct, rows, c.dim);
+    auto launch = [&](int64_t tiles_v, int bl) {
+      g.tiles_v = tiles_v;
+      g.tiles_t = ceil_div(c.tokens, bl);
+      const dim3 grid(tile_workgroups(g.tiles_v, g.tiles_t));
+      if (direct) BRSVD_LOGITS(k_head_grad, El, true, bl, grid, stream, g);
+      else BRSVD_LOGITS(k_head_grad, El, false, bl, grid, stream, g);
+    };
+    if (tiles.first > 0) launch(tiles.first, 256);
+    if (tiles.first < tiles.count) {
+      g.first = tiles.large;
+      launch(tiles.count - tiles.first, tiles.bl);
+    }
     if (!c.label)
       hipLaunchKernelGGL(k_distill_scatter<El>, dim3((unsigned)ceil_div(c.tokens * c.teacher.top, 256)), dim3(256), 0, stream, c.teacher, q, z, meta, index, lse_c, coef,
                          v0, rows, c.vocab, G, plan.piece);
@@ -715,10 +744,16 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
       w.Q = Operand{(const char*)G, 2 * plan.piece, rows};
       w.meta = meta;
       w.tiles_p = ceil_div(c.dim, kTileP);
-      w.tiles_q = ceil_div(rows, 256);
       w.out = (uint16_t*)dW + v0 * lddw;
       w.ldo = lddw;
-      hipLaunchKernelGGL(k_head_dw<El>, dim3(tile_workgroups(w.tiles_p, w.tiles_q)), dim3(kTileThreads), 0, stream, w);
+      const int64_t all = ceil_div(rows, 256), large = large_tiles(all, w.tiles_p, 2 * w.tiles_p, ceil_div(c.tokens, 64));
+      w.tiles_q = large;
+      if (large > 0) hipLaunchKernelGGL((k_head_dw<El, 256>), dim3(tile_workgroups(w.tiles_p, w.tiles_q)), dim3(kTileThreads), 0, stream, w);
+      if (large < all) {
+        w.first = 256 * large;
+        w.tiles_q = ceil_div(rows - w.first, 128);
+        hipLaunchKernelGGL((k_head_dw<El, 128>), dim3(tile_workgroups(w.tiles_p, w.tiles_q)), dim3(kTileThreads), 0, stream, w);
+      }
     }
   }
   // a last piece that is shorter than the others may leave splits without rows: their parts hold what the pieces before gave

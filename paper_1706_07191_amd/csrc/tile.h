@@ -53,7 +53,7 @@ struct __attribute__((packed, aligned(1))) Piece { uint32_t x[4]; };
 // out so that the compiler does not hold back reads of the other buffer until it is done; the wait before the barrier that hands the
 // buffer over is written out, too.
 __device__ __forceinline__ void load_to_lds(uint32_t dst, const char* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(dst), "s"(base), "v"(off) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "s"(base), "v"(off) : "memory");
 }
 // 4 bytes per lane, to `dst` + 4 lane.
 __device__ __forceinline__ void load4_to_lds(uint32_t dst, const void* src) {
@@ -249,31 +249,39 @@ template <class El, int NQ_, Order OP, Order OQ, bool DIRECT>
 struct TileProduct {
   static constexpr int NP = 8, NQ = NQ_, WP = 2, WQ = 4;
   static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
-  static constexpr int kLds = 2 * (BP + BQ) * kStepBytes, kStepK = kStepBytes / El::kBytes;
+  static constexpr int kStepK = kStepBytes / El::kBytes;
+  // Steps in LDS: the one that is multiplied and those on their way, two where there is room: a step of a smaller tile is over before memory has answered.
+  // Loss of 500 tokens, 8000 words of width 4000: 59 us, with one 69; 100, 32000, 2000: 38 and 44.
+  static constexpr int NB = DIRECT && NQ <= 2 ? 3 : 2, kPart = (BP + BQ) * kStepBytes, kLds = NB * kPart;
 
-  static constexpr int kHalf = (BP + BQ) * kStepBytes;
+  static constexpr int PARTS = Stager<El, OP, BP, kThreads, DIRECT>::kLoads + Stager<El, OQ, BQ, kThreads, DIRECT>::kLoads;
   Stager<El, OP, BP, kThreads, DIRECT> sp;
   Stager<El, OQ, BQ, kThreads, DIRECT> sq;
   char* lds;
   int64_t k;         // of the contraction
 
-  static __device__ __forceinline__ void meet() {
+  // The workgroup's barrier; `late`: but for the last PARTS loads, all have come.
+  static __device__ __forceinline__ void meet(bool late = false) {
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (late) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PARTS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
   __device__ __forceinline__ int steps() const { return (int)((k + kStepK - 1) / kStepK); }
-  __device__ __forceinline__ void send(int t, int wave) {
-    char* to = lds + (t & 1) * kHalf;
+  __device__ __forceinline__ bool plain(int t) const {
+    const int64_t left = k - (int64_t)t * kStepK;
+    return sp.plain(left) && sq.plain(left);
+  }
+  __device__ __forceinline__ void send(int t, char* to, int wave) {
     const int64_t left = k - (int64_t)t * kStepK;
     sp.load(to, threadIdx.x, wave, left);
     sq.load(to + BP * kStepBytes, threadIdx.x, wave, left);
   }
-  __device__ __forceinline__ void keep(int t) {
-    sp.store(lds + (t & 1) * kHalf, threadIdx.x);
-    sq.store(lds + (t & 1) * kHalf + BP * kStepBytes, threadIdx.x);
+  __device__ __forceinline__ void keep(char* to) {
+    sp.store(to, threadIdx.x);
+    sq.store(to + BP * kStepBytes, threadIdx.x);
   }
-  // Sends for the first two steps of a tile.  LDS has to be free.
+  // Sends for the first NB steps of a tile.  LDS has to be free.
   __device__ __forceinline__ void begin(const Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds_) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     lds = lds_;
@@ -281,9 +289,11 @@ struct TileProduct {
     sp.init(P, p0, k0, threadIdx.x);
     sq.init(Q, q0, k0, threadIdx.x);
     if (steps() == 0) return;
-    send(0, wave);
-    keep(0);
-    if (steps() > 1) send(1, wave);
+    send(0, lds, wave);
+    keep(lds);
+#pragma unroll
+    for (int t = 1; t < NB; ++t)
+      if (steps() > t) send(t, lds + t * kPart, wave);
   }
   // The tile that was begun; LDS is free afterwards.
   __device__ __forceinline__ void multiply(floatx4 (&acc)[NP][NQ]) {
@@ -298,23 +308,25 @@ struct TileProduct {
     auto read_p = [&](const char* tile, int slot) { fp[slot & 7] = fragment<OP, BP>(tile, bp, slot & 7, slot >> 3); };
     auto read_q = [&](const char* tile, int kk, int q) { fq[kk][q] = fragment<OQ, BQ>(tile + BP * kStepBytes, bq, q, kk); };
     // the parts of a plain step, one a slot: sent all at once they would queue up before the memory unit, and the waves behind them
-    constexpr int PARTS = decltype(sp)::kLoads + decltype(sq)::kLoads;
-    auto send_part = [&](int t, int j) {
-      char* to = lds + (t & 1) * kHalf;
+    auto send_part = [&](char* to, int j) {
       if (j < decltype(sp)::kLoads) sp.load_part(to, wave, j);
       else if (j < PARTS) sq.load_part(to + BP * kStepBytes, wave, j - decltype(sp)::kLoads);
     };
     bool parts = false;          // the step after this one is being sent for in parts
     if (steps == 0) return;
     meet();
-    if (!DIRECT && steps > 1) keep(1);        // the pieces of step 1 have left their registers before those of step 2 come
+    if (!DIRECT && steps > 1) keep(lds + kPart);        // the pieces of step 1 have left their registers before those of step 2 come
 #pragma unroll
     for (int i = 0; i < 4; ++i) read_p(lds, i);
 #pragma unroll
     for (int q = 0; q < NQ; ++q) read_q(lds, 0, q);
+    int slot = 0;                // t % NB
     for (int t = 0; t < steps; ++t) {
-      const char *cur = lds + (t & 1) * kHalf, *nxt = lds + kHalf - (t & 1) * kHalf;
-      const bool more = t + 1 < steps, sends = t + 2 < steps;
+      // of the step before, this one and the next in LDS
+      slot = __builtin_amdgcn_readfirstlane(NB == 2 ? t & 1 : slot);
+      const int at = slot * kPart, nat = slot == NB - 1 ? 0 : at + kPart, pat = slot == 0 ? (NB - 1) * kPart : at - kPart;
+      const char *cur = lds + at, *nxt = lds + nat;
+      const bool more = t + 1 < steps, sends = t + NB < steps;
       asm volatile("" : "+v"(bp), "+v"(bq));      // addresses are worked out from these where they are used, not kept
 #pragma unroll
       for (int s = 0; s < SLOTS; ++s) {
@@ -327,14 +339,13 @@ struct TileProduct {
         } else if (s < 10) {
           read_p(cur, s + 6);
         } else if (s == MEET) {
-          meet();
-          const int64_t left = k - (int64_t)(t + 2) * kStepK;
-          parts = sends && sp.plain(left) && sq.plain(left);
-          if (sends && !parts) send(t + 2, wave);
+          meet(NB > 2 && plain(t + 2));
+          parts = sends && plain(t + NB);
+          if (sends && !parts) send(t + NB, lds + at, wave);
         }
         if (parts) {
-          if (s >= MEET) send_part(t + 2, s - MEET);
-          else if (s < PARTS - 4) send_part(t + 1, s + 4);
+          if (s >= MEET) send_part(lds + at, s - MEET);
+          else if (s < PARTS - 4) send_part(lds + pat, s + 4);
           if (s == PARTS - 5) {
             sp.next();
             sq.next();
@@ -345,7 +356,7 @@ struct TileProduct {
           read_p(nxt, s - MEET);
           if (s - MEET < NQ) read_q(nxt, 0, s - MEET);
         }
-        if (!DIRECT && s == SLOTS - 1 && sends) keep(t + 2);
+        if (!DIRECT && s == SLOTS - 1 && sends) keep(lds + at);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           acc[s & 7][q] = mfma16<El>(fp[s & 7], fq[s >> 3][q], acc[s & 7][q]);
@@ -353,6 +364,7 @@ struct TileProduct {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
+      slot = slot == NB - 1 ? 0 : slot + 1;
     }
     meet();
   }
@@ -486,5 +498,20 @@ __device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64
   return true;
 }
 inline unsigned tile_workgroups(int64_t np, int64_t nq) { return (unsigned)(8 * ((np * nq + 7) / 8)); }
+
+// A product's tiles on 256 CUs: np of them along one side, each a column of q256 tiles of 256 x 256 or of q128 of half the size (seven tenths of the time).  The
+// first so many of the np go in large ones (what it returns): all, none, or those of the full rounds, so that only the last round is of small ones.  A tile
+// takes as long as its steps and three more, the second launch is taken to cost four steps.  8 bits: 4096 x 6000 over 4001 130 us and 142 without,
+// 4001 x 6000 over 4096 93 and 104; loss and gradients of 999 tokens, 50001 words of width 1000 525 and 539.  With five steps (width 272) and 24 full rounds
+// the cut cost 1 %, so it is not made there.
+inline int64_t large_tiles(int64_t np, int64_t q256, int64_t q128, int64_t steps) {
+  auto rounds = [](int64_t tiles) { return (tiles + 255) / 256; };
+  const int64_t large = 10 * rounds(np * q256), small = 7 * rounds(np * q128), full = np * q256 / 256 * 256 / q256;
+  if (full > 0 && full < np) {
+    const int64_t best = large < small ? large : small;
+    if ((best - 10 * rounds(full * q256) - 7 * rounds((np - full) * q128)) * (steps + 3) > 40) return full;
+  }
+  return small < large ? 0 : np;
+}
 
 }  // namespace brsvd
