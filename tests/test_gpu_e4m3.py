@@ -167,6 +167,18 @@ def test_product_with_many_columns(m, n, k):
 
 
 @pytest.mark.parametrize("block", [128, 1])
+def test_product_whose_last_round_of_tiles_is_cut(block):
+    """270 tiles of 256 x 256: most of them as they are, the columns of the others in halves, by a launch of their own."""
+    dev = need_gpu()
+    m, n, k = 500, 34433, 1403
+    qa, sa, a = eight_bits(5, m, k, 1, dev, 5)
+    qb, sb, b = eight_bits(6, n, k, block, dev, 5)
+    out = torch.full((m, n + 3), 5.0, dtype=torch.bfloat16, device=dev)
+    check_product(B.brsvd_gemm_e4m3(qa, sa, qb, sb, block_rows=block, out=out[:, 1:n + 1]), a, b, torch.bfloat16)
+    assert bool((out[:, 0] == 5).all() and (out[:, n + 1:] == 5).all())
+
+
+@pytest.mark.parametrize("block", [128, 1])
 @pytest.mark.parametrize("m", [100, 300])
 def test_scales_that_are_not_powers_of_two_from_some_block_on(m, block):
     """Powers of two go into the instruction, others are multiplied afterwards: a product that meets its first other scale in the middle, for a few

@@ -122,6 +122,26 @@ def test_xent_of_many_tiles(tokens, vocab, dim, pad):
         ref.check_gradients(dH, dW, target, grad.double().cpu() * counted)
 
 
+def test_xent_whose_last_round_of_tiles_is_cut():
+    """1000 x 22433 logits are 352 tiles of 256 x 256, dW 264: most of them as they are, the others in halves, by a launch of their own.  Labels on both sides
+    of the cut and at its edge."""
+    dev = need_gpu()
+    tokens, vocab, dim = 1000, 22433, 750
+    H, W, y, g = problem(tokens, vocab, dim, torch.bfloat16, dev, 2)
+    y[0], y[1], y[2], y[3], y[4] = vocab - 1, -1, 64 * 256 - 1, 64 * 256, 85 * 256
+    ref = Reference(H, W)
+    loss, lse = B.brsvd_xent_forward(H, W, y.to(dev))
+    ref.check_lse(lse)
+    counted = y >= 0
+    target = torch.zeros_like(ref.z)
+    target[torch.nonzero(counted)[:, 0], y[counted]] = 1.0
+    zy = (target * ref.z).sum(dim=1)
+    ref.check("loss", loss, torch.where(counted, ref.lse - zy, 0.0), torch.where(counted, ref.dlse + ref.dz.amax(dim=1) + 2.0 ** -22 * (ref.lse - zy).abs(), 0.0))
+    grad = (torch.rand(tokens, generator=g) + 0.5).to(dev)
+    dH, dW = B.brsvd_xent_backward(H, W, y.to(dev), lse, grad)
+    ref.check_gradients(dH, dW, target, grad.double().cpu() * counted)
+
+
 @pytest.mark.parametrize("dtype", HALF)
 def test_what_does_not_count_reaches_nothing(dtype):
     """NaN and infinities in the hidden states of padding, half of the tokens: gradients are those of the others alone."""
