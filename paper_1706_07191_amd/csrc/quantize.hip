@@ -53,100 +53,145 @@ __device__ __forceinline__ float max16(float x) {
   return x;
 }
 
-// One workgroup per 128 x 128 part.  Bound by memory: what it reads and writes once, 4001 x 6000 bf16 with its transpose 30 us (96 MB, 3.2 TB/s).  The transpose goes through LDS in words of a thread's kRows
+// Magnitudes in a word of memory as it is, one number or two: keys that order as they do, and below all of them what is not finite.  A largest key costs three
+// instructions for two numbers of 16 bits, their floats twice that each.
+template <int DT> struct Keys {
+  typedef short Two __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kFrom = DT == BRSVD_DTYPE_F32 ? 0x00800000u : DT == BRSVD_DTYPE_BF16 ? 0x0080u : 0x0400u;    // of zero
+  static constexpr uint32_t kNone = DT == BRSVD_DTYPE_F32 ? kFrom : kFrom << 16 | kFrom;
+  static __device__ __forceinline__ uint32_t of(uint32_t w) {
+    if (DT == BRSVD_DTYPE_F32) return (w & 0x7fffffffu) + kFrom;
+    const Two from = {(short)kFrom, (short)kFrom};
+    return __builtin_bit_cast(uint32_t, (Two)(__builtin_bit_cast(Two, w & 0x7fff7fffu) + from));
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    if (DT == BRSVD_DTYPE_F32) return (uint32_t)max((int32_t)a, (int32_t)b);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Two, a), __builtin_bit_cast(Two, b)));
+  }
+  // the magnitude of a word's number i
+  static __device__ __forceinline__ float magnitude(uint32_t key, int i) {
+    if (DT == BRSVD_DTYPE_F32) return __uint_as_float(key - kFrom);
+    const uint16_t h = (uint16_t)((uint16_t)(key >> (16 * i)) - kFrom);
+    return DT == BRSVD_DTYPE_BF16 ? from16<Bf16>(h) : from16<Fp16>(h);
+  }
+  // of a word's numbers
+  static __device__ __forceinline__ float largest(uint32_t key) {
+    return DT == BRSVD_DTYPE_F32 ? magnitude(key, 0) : fmaxf(magnitude(key, 0), magnitude(key, 1));
+  }
+  // of 16 neighbouring lanes, in all of them
+  static __device__ __forceinline__ uint32_t largest16(uint32_t x) {
+#define BRSVD_ROTATED_KEYS(N) x = larger(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, true))
+    BRSVD_ROTATED_KEYS(8);
+    BRSVD_ROTATED_KEYS(4);
+    BRSVD_ROTATED_KEYS(2);
+    BRSVD_ROTATED_KEYS(1);
+#undef BRSVD_ROTATED_KEYS
+    return x;
+  }
+};
+template <int DT>
+__device__ __forceinline__ float number_of(const uint32_t (&w)[4], int j) {
+  if (DT == BRSVD_DTYPE_F32) return __uint_as_float(w[j & 3]);
+  const uint16_t h = (uint16_t)(w[j / 2 & 3] >> (16 * (j & 1)));
+  return DT == BRSVD_DTYPE_BF16 ? from16<Bf16>(h) : from16<Fp16>(h);
+}
+
+// One workgroup per 128 x 128 part.  Bound by memory: what it reads and writes once.  Numbers stay as they came in registers, so that all workgroups of a
+// matrix of some 4000 x 6000 run at once: 4001 x 6000 bf16 by rows with its transpose 24 us (96 MB, 3.9 TB/s), 27 with floats.  The transpose goes through LDS in words of a thread's kRows
 // numbers of a column, word g of column c at g ^ (c / kWide): the lanes that write, and those that read, then lie in different banks.
 template <int DT, bool SQUARE, bool STRAIGHT, bool TRANSPOSED>
 __global__ void __launch_bounds__(256)
 k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S,
            uint8_t* __restrict__ Qt, int64_t ldqt, float* __restrict__ St) {
   using P = Part<DT>;
+  using K = Keys<DT>;
   constexpr int W = P::kWide, R = P::kRows, L = P::kLanes, GROUPS = kBlock / R;
-  __shared__ float top[4][kBlock];
+  __shared__ uint32_t top[4][4 * L];
   __shared__ __attribute__((aligned(16))) uint8_t turned[TRANSPOSED ? kBlock * kBlock : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid % L, c = cg * W, g = tid / L;
   const int64_t ncb = (cols + kBlock - 1) / kBlock, nrb = (rows + kBlock - 1) / kBlock;
   const int64_t rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, row0 = rb * kBlock, col0 = cb * kBlock;
   const int width = (int)(cols - col0 - c < W ? (cols - col0 - c > 0 ? cols - col0 - c : 0) : W);
-  float x[R][W];
+  uint32_t x[R][4];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int64_t row = row0 + g * R + i;
-    numbers<DT>(X + row * ldx + (col0 + c) * P::kBytes, row < rows ? width : 0, x[i]);
+    const uint4 v = piece_of<P::kBytes>(X + row * ldx + (col0 + c) * P::kBytes, row < rows ? width * P::kBytes : 0);
+    x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
   }
-  float rowtop[R], all = 0.f;
-  if (STRAIGHT || SQUARE) {
+  // the numbers' floats are worked out again where they are used: kept, they would double the registers
+  auto again = [&] {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      float t = 0.f;
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int j = 0; j < W; ++j) t = fmaxf(t, finite_abs(x[i][j]));
-      if (SQUARE) all = fmaxf(all, t);
-      else {
-        t = max16(t);
-        if (L == 32) t = fmaxf(t, __shfl_xor(t, 16));
-      }
-      rowtop[i] = t;
-    }
-  }
-  int e_square = 0;
+      for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(x[i][j]));
+  };
+  auto row_key = [&](int i) { return K::larger(K::larger(K::of(x[i][0]), K::of(x[i][1])), K::larger(K::of(x[i][2]), K::of(x[i][3]))); };
+  float f_square = 1.f;
   if (SQUARE) {
-    all = max16(all);
-    all = fmaxf(all, __shfl_xor(all, 16));
-    all = fmaxf(all, __shfl_xor(all, 32));
+    uint32_t all = K::kNone;
+#pragma unroll
+    for (int i = 0; i < R; ++i) all = K::larger(all, row_key(i));
+    all = K::largest16(all);
+    all = K::larger(all, __shfl_xor(all, 16));
+    all = K::larger(all, __shfl_xor(all, 32));
     if (lane == 0) top[wave][0] = all;
     __syncthreads();
-    e_square = block_exponent(fmaxf(fmaxf(top[0][0], top[1][0]), fmaxf(top[2][0], top[3][0])));
-    if (tid == 0 && STRAIGHT) S[rb * ncb + cb] = power_of_two(e_square);
-    if (tid == 0 && TRANSPOSED) St[cb * nrb + rb] = power_of_two(e_square);
+    const int e = block_exponent(K::largest(K::larger(K::larger(top[0][0], top[1][0]), K::larger(top[2][0], top[3][0]))));
+    f_square = power_of_two(-e);
+    if (tid == 0 && STRAIGHT) S[rb * ncb + cb] = power_of_two(e);
+    if (tid == 0 && TRANSPOSED) St[cb * nrb + rb] = power_of_two(e);
   }
   if (STRAIGHT) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int64_t row = row0 + g * R + i;
-      const int e = SQUARE ? e_square : block_exponent(rowtop[i]);
-      const float f = power_of_two(-e);
+      float f = f_square;
+      if (!SQUARE) {
+        uint32_t t = K::larger(K::kNone, K::largest16(row_key(i)));
+        if (L == 32) t = K::larger(t, __shfl_xor(t, 16));
+        const int e = block_exponent(K::largest(t));
+        f = power_of_two(-e);
+        if (row < rows && cg == 0) S[row * ncb + cb] = power_of_two(e);
+      }
       uint32_t v[W / 4];
 #pragma unroll
-      for (int j = 0; j < W; j += 4) v[j / 4] = pack_e4m3(x[i][j] * f, x[i][j + 1] * f, x[i][j + 2] * f, x[i][j + 3] * f);
-      if (row < rows) {
-        put_bytes<W>(Q + row * ldq + col0 + c, width, v);
-        if (!SQUARE && cg == 0) S[row * ncb + cb] = power_of_two(e);
-      }
+      for (int j = 0; j < W; j += 4)
+        v[j / 4] = pack_e4m3(number_of<DT>(x[i], j) * f, number_of<DT>(x[i], j + 1) * f, number_of<DT>(x[i], j + 2) * f, number_of<DT>(x[i], j + 3) * f);
+      if (row < rows) put_bytes<W>(Q + row * ldq + col0 + c, width, v);
     }
   }
   if (TRANSPOSED) {
     float f[W];
+    again();
     if (!SQUARE) {
-      // the columns' magnitudes anew: those of the rows, kept until here, would double the registers and halve the workgroups of a CU
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+      for (int j = 0; j < 4; ++j) {
+        uint32_t t = K::kNone;
 #pragma unroll
-        for (int j = 0; j < W; ++j) asm volatile("" : "+v"(x[i][j]));
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        float t = 0.f;
-#pragma unroll
-        for (int i = 0; i < R; ++i) t = fmaxf(t, finite_abs(x[i][j]));
-        if (L == 16) t = fmaxf(t, __shfl_xor(t, 16));
-        t = fmaxf(t, __shfl_xor(t, 32));
-        if (lane < L) top[wave][c + j] = t;
+        for (int i = 0; i < R; ++i) t = K::larger(t, K::of(x[i][j]));
+        if (L == 16) t = K::larger(t, __shfl_xor(t, 16));
+        t = K::larger(t, __shfl_xor(t, 32));
+        if (lane < L) top[wave][4 * cg + j] = t;
       }
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < W; ++j) {
-        const int e = block_exponent(fmaxf(fmaxf(top[0][c + j], top[1][c + j]), fmaxf(top[2][c + j], top[3][c + j])));
+        const int w = 4 * cg + j * 4 / W;
+        const int e = block_exponent(K::magnitude(K::larger(K::larger(top[0][w], top[1][w]), K::larger(top[2][w], top[3][w])), j % (W / 4)));
         f[j] = power_of_two(-e);
         if (g == 0 && j < width) St[(col0 + c + j) * nrb + rb] = power_of_two(e);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < W; ++j) f[j] = power_of_two(-e_square);
+      for (int j = 0; j < W; ++j) f[j] = f_square;
     }
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       uint32_t v[R / 4];
 #pragma unroll
-      for (int i = 0; i < R; i += 4) v[i / 4] = pack_e4m3(x[i][j] * f[j], x[i + 1][j] * f[j], x[i + 2][j] * f[j], x[i + 3][j] * f[j]);
+      for (int i = 0; i < R; i += 4)
+        v[i / 4] = pack_e4m3(number_of<DT>(x[i], j) * f[j], number_of<DT>(x[i + 1], j) * f[j], number_of<DT>(x[i + 2], j) * f[j], number_of<DT>(x[i + 3], j) * f[j]);
       uint8_t* at = turned + (c + j) * kBlock + R * (g ^ (cg & (GROUPS - 1)));
       if (R == 16) *(uint4*)at = make_uint4(v[0], v[1], v[R / 4 - 2], v[R / 4 - 1]);
       else *(uint2*)at = make_uint2(v[0], v[1]);
