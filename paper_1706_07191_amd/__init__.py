@@ -500,13 +500,15 @@ def _scales(S, rows, cols, block_rows, name):
 
 
 def _eight_bit(rows, cols, device):
-    """rows x cols numbers of 8 bits in rows of whole 16 bytes, which the products read fastest."""
-    return torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=torch.float8_e4m3fn, device=device)
+    """rows x cols numbers of 8 bits in rows of whole 16 bytes, long ones of whole 128 (lines of the caches), which the products
+    read fastest."""
+    whole = 16 if cols < 1024 else 128
+    return torch.empty_strided((rows, cols), (-(-cols // whole) * whole, 1), dtype=torch.float8_e4m3fn, device=device)
 
 
 @_scoped
 def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
-    """X (rows, cols) CUDA, fp32, bf16 or fp16, as e4m3 numbers Q (float8_e4m3fn, rows 16-byte aligned) and power-of-two
+    """X (rows, cols) CUDA, fp32, bf16 or fp16, as e4m3 numbers Q (float8_e4m3fn, rows 16- or 128-byte aligned) and power-of-two
     scales S, one for each 128 numbers of a row (block_rows=1) or each 128 x 128 block (block_rows=128).  Returns (Q, S), with
     transpose=True (Q, S, Qt, St), the last two those of X^T."""
     if block_rows not in (1, 128):
@@ -520,8 +522,8 @@ def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
         return _eight_bit(r, c, dev), torch.empty(r if block_rows == 1 else -(-r // 128), -(-c // 128), device=dev)
     Q, S = result(rows, cols)
     Qt, St = result(cols, rows) if transpose else (None, None)
-    _check(lib().brsvd_quantize_e4m3(x, ldx, rows, cols, dt, block_rows, Q.data_ptr(), -(-cols // 16) * 16, S.data_ptr(),
-                                     Qt.data_ptr() if transpose else None, -(-rows // 16) * 16 if transpose else 0,
+    _check(lib().brsvd_quantize_e4m3(x, ldx, rows, cols, dt, block_rows, Q.data_ptr(), Q.stride(0), S.data_ptr(),
+                                     Qt.data_ptr() if transpose else None, Qt.stride(0) if transpose else 0,
                                      St.data_ptr() if transpose else None, _current(X.device)), "brsvd_quantize_e4m3")
     return (Q, S, Qt, St) if transpose else (Q, S)
 

@@ -610,8 +610,8 @@ static bool product_type(int dtype) { return dtype == BRSVD_DTYPE_F32 || dtype =
 static bool product_sizes(int64_t m, int64_t n, int64_t k) {
   return m >= 0 && n >= 0 && k >= 0 && k < kMaxPitch && m < (int64_t)1 << 31 && n < (int64_t)1 << 31 && ceil_div(m, 128) * ceil_div(n, 16) <= kMaxGrid;
 }
-// The cast of the activations for a product that takes them in 8 bits: rows of whole 16 bytes, then their scales.
-static uint64_t cast_pitch(int64_t k) { return (uint64_t)ceil_div(k, 16) * 16; }
+// The cast of the activations for a product that takes them in 8 bits: rows, then their scales.
+static uint64_t cast_pitch(int64_t k) { return (uint64_t)line_pitch(k); }
 static uint64_t cast_bytes(int64_t m, int64_t k) { return ((uint64_t)m * cast_pitch(k) + 255) / 256 * 256 + ((uint64_t)m * ceil_div(k, kBlock) * 4 + 255) / 256 * 256; }
 
 int quantize(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dtype, int block_rows, uint8_t* Q, int64_t ldq, float* S, uint8_t* Qt, int64_t ldqt,

@@ -589,7 +589,7 @@ struct HeadPlan {
 static HeadPlan head_plan(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece, int top) {
   HeadPlan p;
   p.piece = piece_rows(tokens, vocab, piece);
-  p.pitch_h = ceil_div(dim, 8) * 16;
+  p.pitch_h = line_pitch(2 * dim);
   // dH has few tiles where there are few tokens: then the piece's rows are cut, too
   const int64_t tiles = ceil_div(dim, kTileP) * ceil_div(tokens, tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256);
   int64_t s = 256 / tiles;

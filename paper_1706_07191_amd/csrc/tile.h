@@ -44,6 +44,9 @@ struct Operand {
 
 // Whether the pieces of 16 bytes that an operand's rows are read in lie at 16-byte addresses.
 inline bool aligned_pieces(const void* base, int64_t ld_bytes) { return (uintptr_t)base % 16 == 0 && ld_bytes % 16 == 0; }
+// Bytes between rows of an operand that a call lays out itself: a step takes 128 bytes of every row, one line of the caches and not parts of two.  8-bit products
+// of 4096 x 6000 over 4001 116 us, in rows of 4016 bytes 131; short rows are only made whole pieces, lines would be much of them.
+inline int64_t line_pitch(int64_t bytes) { return bytes < 1024 ? (bytes + 15) / 16 * 16 : (bytes + 127) / 128 * 128; }
 // Bytes between rows up to which a tile's pieces are addressed with 32 bits.
 constexpr int64_t kMaxPitch = (int64_t)1 << 22;
 
