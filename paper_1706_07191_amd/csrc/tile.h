@@ -5,7 +5,7 @@
 // contiguous in memory: it is stored four numbers at a time.
 //
 // A step of the contraction takes 128 bytes of every row of P and Q (64 numbers of 16 bits, 128 of 8) into LDS, straight from memory
-// (global_load_lds, 16 bytes a lane) into one of two buffers while the other is multiplied; one barrier a step.  An operand is
+// (global_load_lds, 16 bytes a lane) into one of two buffers (three, TileProduct) while another is multiplied; one barrier a step.  An operand is
 //   kRows: its rows hold the contraction, [rows][K].  A tile is [rows][128 bytes] in LDS, the 16-byte pieces of row r at piece ^ (r & 7): the 16
 //          rows that a fragment is read from then lie in different banks.
 //   kCols: the contraction runs down its rows, [K][cols] (16-bit numbers).  A tile is [64][cols]; fragments come out transposed
@@ -245,7 +245,7 @@ __device__ __forceinline__ floatx4 mfma_wide(const Wide8& p, const Wide8& q) {
 
 // A tile product of 16-bit numbers.  A step is 2 NP slots, one for each tile row of a wave and half of the step; a slot is NQ instructions.
 // What a slot multiplies was read from LDS at least four slots before.  All of a step is read by slot 9 of 16: at slot 12 the
-// workgroup meets once, the next step's numbers, under way for a whole step, are there, the step after it is sent for into the buffer that has just been read,
+// workgroup meets once, the next step's numbers, under way for a whole step, are there, the step two (three) ahead is sent for into the buffer that has just been read,
 // and the first fragments of the next step are read while the last four slots multiply.  So no wave comes from the barrier with nothing to multiply.
 // Bound by the matrix cores: a tile of 256 x 256 takes 1.46 us a step (1.47 Pflop/s on 256 CUs); 1.66 where fragments are read behind the barrier, 1.90 where
 // a step is sent for at once, too (4096 x 65536 logits, widths from 256 to 2048).
