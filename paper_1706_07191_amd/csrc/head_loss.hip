@@ -481,6 +481,7 @@ struct HeadProduct {
   bool more;
   uint16_t* out;           // dW
   int64_t first;           // dW: the word that the first tile begins with
+  int64_t words, width;    // dW: its rows and columns
   int64_t ldo;
 };
 
@@ -536,7 +537,7 @@ k_head_dw(const HeadProduct g) {
   floatx4 acc[T::NP][T::NQ];
   T::run(acc, g.P, p0, g.Q, q0, 0, g.meta->count, lds);
   const float down = g.meta->down;
-  put_tile16<T::NQ>(acc, lds, g.out + q0 * g.ldo + p0, g.ldo, g.Q.n - q0, g.P.n - p0, [&](float x, int) { return to16<El>(x * down); });
+  put_tile16<T::NQ>(acc, lds, g.out + q0 * g.ldo + p0, g.ldo, g.words - q0, g.width - p0, [&](float x, int) { return to16<El>(x * down); });
 }
 
 // A matrix of zeros
@@ -745,8 +746,11 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
     }
     if (dW) {
       HeadProduct w = {};
-      w.P = Operand{hc, plan.pitch_h, c.dim};
-      w.Q = Operand{(const char*)G, 2 * plan.piece, rows};
+      // rows of both end behind whole pieces: what a piece holds beyond the last column goes into sums that are not stored
+      w.P = Operand{hc, plan.pitch_h, ceil_div(c.dim, 8) * 8};
+      w.Q = Operand{(const char*)G, 2 * plan.piece, ceil_div(rows, 8) * 8};
+      w.words = rows;
+      w.width = c.dim;
       w.meta = meta;
       w.tiles_p = ceil_div(c.dim, kTileP);
       w.out = (uint16_t*)dW + v0 * lddw;
