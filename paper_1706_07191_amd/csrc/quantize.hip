@@ -229,16 +229,16 @@ k_quantize_rows(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t c
   const unsigned ncb = (unsigned)((cols + kBlock - 1) / kBlock);
   const int64_t first = (int64_t)blockIdx.x * (256 / L * SETS) + threadIdx.x / L, blocks = rows * ncb;
   float x[SETS][W];
-  int64_t row[SETS];
-  int col[SETS], width[SETS];
+  int64_t row[SETS], col[SETS];
+  int width[SETS];
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
     const int64_t b = first + i * (256 / L);
     row[i] = b / ncb;
-    col[i] = (int)(b - row[i] * ncb) * kBlock + cg * W;
+    col[i] = (b - row[i] * ncb) * kBlock + cg * W;
     const int64_t left = b < blocks ? cols - col[i] : 0;
     width[i] = (int)(left < W ? (left > 0 ? left : 0) : W);
-    numbers<DT>(X + row[i] * ldx + (int64_t)col[i] * P::kBytes, width[i], x[i]);
+    numbers<DT>(X + row[i] * ldx + col[i] * P::kBytes, width[i], x[i]);
   }
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
