@@ -245,7 +245,9 @@ int brsvd_destroy(brsvd_handle h);
  * passed it; one too small is BRSVD_ERR_BUDGET.  Sizes may be zero where nothing else is said: an
  * output without elements is not touched, one that is a sum of nothing is zero.  Every result repeats
  * itself bit for bit.  Rows of operands may begin at any element; 16-byte-aligned rows (address and
- * leading dimension) are faster, 128-byte-aligned ones fastest.  Leading dimensions are below 2^21. */
+ * leading dimension) are faster, 128-byte-aligned ones fastest.  Leading dimensions are below 2^21.
+ * A product, or what a loss multiplies, of 2^23 tiles of 128 x 256 numbers or more (2^29 columns where A has
+ * few rows) is BRSVD_ERR_ARG. */
 
 /* Numbers of 8 bits: e4m3 (OCP: four bits of exponent, three of fraction, largest 448, no infinities)
  * times a scale in fp32 for each block.  A block is 128 neighbouring numbers of a row (block_rows = 1:

@@ -18,6 +18,15 @@ constexpr int kTile = 16;        // MFMA tile edge (v_mfma_f32_16x16x4_f32)
 inline int padded_l(int l) { return (l + kTile - 1) / kTile * kTile; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Workgroups that one launch may have along a direction: it is to have fewer than 2^32 threads there.  Of more than that only a part runs, and no error says so.
+inline int64_t launch_workgroups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+// Work of any number of workgroups below 2^32: launch(first, grid) for as many at a time as a launch may have; a kernel adds `first` to its blockIdx.x.
+template <class Launch>
+inline void in_launches(int64_t workgroups, int threads, Launch launch) {
+  const int64_t most = launch_workgroups(threads);
+  for (int64_t first = 0; first < workgroups; first += most) launch((unsigned)first, dim3((unsigned)(workgroups - first < most ? workgroups - first : most)));
+}
+
 #define BRSVD_HIP_TRY(expr)                         \
   do {                                              \
     hipError_t e__ = (expr);                        \

@@ -350,8 +350,8 @@ k_tiles_e4m3(const E4m3Args g) {
 
 // C (m x n, type dtype) = sum of the splits' parts, in their order
 __global__ void __launch_bounds__(256)
-k_join_splits(const float* __restrict__ part, int splits, int64_t m, int64_t n, void* __restrict__ C, int64_t ldc, int dtype) {
-  const int64_t quads = (n + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+k_join_splits(const float* __restrict__ part, int splits, int64_t m, int64_t n, void* __restrict__ C, int64_t ldc, int dtype, unsigned first_wg) {
+  const int64_t quads = (n + 3) / 4, i = ((int64_t)first_wg + blockIdx.x) * 256 + threadIdx.x;
   if (i >= m * quads) return;
   const int64_t row = i / quads, col = (i - row * quads) * 4, at = row * n + col;
   floatx4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -498,6 +498,12 @@ k_rows_e4m3(const E4m3Args g) {
   }
 }
 
+static void join_splits(const float* part, int splits, int64_t m, int64_t n, void* C, int64_t ldc, int dtype, hipStream_t stream) {
+  in_launches(ceil_div(m * ceil_div(n, 4), 256), 256, [&](unsigned first, dim3 grid) {
+    hipLaunchKernelGGL(k_join_splits, grid, dim3(256), 0, stream, part, splits, m, n, C, ldc, dtype, first);
+  });
+}
+
 // Rows up to which the read of B bounds the product.  Above 32 the tiles are ahead where B has rows for them: 60 x 20000 x 5000 47 us and 82, the
 // other way round where it has not: 24 x 4096 x 4096 17.6 and 9.6, 24 x 20000 x 5000 43 and 41.
 static bool few_rows(int64_t m, int64_t n) { return m <= 32 || (m <= 64 && n < 16 * 512); }
@@ -527,6 +533,12 @@ static E4m3Plan e4m3_plan(int64_t m, int64_t n, int64_t k, bool per_row, int dty
   p.per_split = (int)ceil_div(blocks, p.splits);
   p.splits = (int)ceil_div(blocks, p.per_split);
   return p;
+}
+// Whether the launches of a plan may have their workgroups.  direct: rows of both operands at 16-byte addresses.
+static bool e4m3_plan_fits(const E4m3Plan& p, int64_t m, int64_t n, bool direct, int dtype) {
+  if (p.rows) return ceil_div(n, 32) <= launch_workgroups(256);          // as launch_rows where there are that many rows of B
+  const int64_t cols = ceil_div(n, 256), large = direct && dtype != BRSVD_DTYPE_F32 ? p.large : 0;
+  return tiles_fit(large, ceil_div(m, 256), 512) && tiles_fit(cols - large, ceil_div(m, 128), 512);
 }
 static uint64_t split_bytes(const E4m3Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? (uint64_t)p.splits * m * n * 4 : 0; }
 
@@ -601,7 +613,7 @@ static int gemm_e4m3(const void* A, int64_t lda_bytes, int a_type, const float* 
     else if (direct) launch_tiles<false, true>(g, plan.large, wide, stream);
     else launch_tiles<false, false>(g, plan.large, wide, stream);
   }
-  if (split) hipLaunchKernelGGL(k_join_splits, dim3((unsigned)ceil_div(m * ceil_div(n, 4), 256)), dim3(256), 0, stream, part, plan.splits, m, n, C, ldc, dtype);
+  if (split) join_splits(part, plan.splits, m, n, C, ldc, dtype, stream);
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
 }
@@ -640,12 +652,13 @@ extern "C" int brsvd_gemm_e4m3(const uint8_t* A, int64_t lda, const float* SA, c
   hipStream_t s = (hipStream_t)stream;
   if (k == 0) {
     // an empty sum: the join of no parts
-    hipLaunchKernelGGL(k_join_splits, dim3((unsigned)ceil_div(m * ceil_div(n, 4), 256)), dim3(256), 0, s, (const float*)nullptr, 0, m, n, C, ldc, dtype);
+    join_splits(nullptr, 0, m, n, C, ldc, dtype, s);
     BRSVD_HIP_TRY(hipGetLastError());
     return BRSVD_OK;
   }
   if (!A || !B || !SA || !SB || lda < k || ldb < k || lda >= kMaxPitch || ldb >= kMaxPitch) return BRSVD_ERR_ARG;
   const E4m3Plan p = e4m3_plan(m, n, k, block_rows == 1, dtype);
+  if (!e4m3_plan_fits(p, m, n, aligned_pieces(A, lda) && aligned_pieces(B, ldb), dtype)) return BRSVD_ERR_ARG;
   const uint64_t need = split_bytes(p, m, n);
   if (need && (!scratch || (uintptr_t)scratch % 256)) return BRSVD_ERR_ARG;
   if (scratch_bytes < need) return BRSVD_ERR_BUDGET;
@@ -659,6 +672,7 @@ extern "C" int brsvd_linear_e4m3(const void* X, int64_t ldx, int32_t dtype, cons
   const int eb = dtype == BRSVD_DTYPE_F32 ? 4 : 2;
   if (!X || !W || !SW || !Y || ldx < k || ldw < k || ldy < n || ldx * eb >= kMaxPitch * 4 || ldw >= kMaxPitch) return BRSVD_ERR_ARG;
   const E4m3Plan p = e4m3_plan(m, n, k, false, dtype);
+  if (!e4m3_plan_fits(p, m, n, aligned_pieces(W, ldw), dtype)) return BRSVD_ERR_ARG;      // the cast of X lies at such addresses
   const uint64_t parts = split_bytes(p, m, n), need = parts + (m <= kCastRows ? 0 : cast_bytes(m, k));
   if (need && (!scratch || (uintptr_t)scratch % 256)) return BRSVD_ERR_ARG;
   if (scratch_bytes < need) return BRSVD_ERR_BUDGET;

@@ -183,10 +183,10 @@ k_head_lse(const HeadArgs g) {
 // end at different times.
 __global__ void __launch_bounds__(256)
 k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t tokens, const int64_t* __restrict__ label, int64_t vocab, const float* __restrict__ zlabel,
-            float* __restrict__ lse, float* __restrict__ loss) {
+            float* __restrict__ lse, float* __restrict__ loss, unsigned first_wg) {
   __shared__ float2 red[16][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
-  const int64_t t = (int64_t)blockIdx.x * 16 + c;
+  const int64_t t = ((int64_t)first_wg + blockIdx.x) * 16 + c;
   float top = -INFINITY, sum = 0.f;
   auto add = [&](float2 v) {
     const float to = fmaxf(top, v.x), ref = to == -INFINITY ? 0.f : to;
@@ -265,9 +265,10 @@ __device__ __forceinline__ float2 teacher_norm(const Teacher& te, int64_t t, int
 // it reads, tokens x top of them: 4096 tokens x 64 words of width 2048 149 us (1.07 GB, 7.2 TB/s, much of it from the caches).
 template <class El>
 __global__ void __launch_bounds__(256)
-k_distill_loss(const Operand W, const Operand H, int64_t dim, const Teacher te, const float* __restrict__ lse, float* __restrict__ z, float* __restrict__ loss) {
+k_distill_loss(const Operand W, const Operand H, int64_t dim, const Teacher te, const float* __restrict__ lse, float* __restrict__ z, float* __restrict__ loss,
+               unsigned first_wg) {
   __shared__ float part[4];
-  const int64_t t = blockIdx.x;
+  const int64_t t = first_wg + blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float2 norm = teacher_norm(te, t, W.n, lane);
   const float l = lse[t], logsum = logf(norm.y);
@@ -312,8 +313,8 @@ k_distill_loss(const Operand W, const Operand H, int64_t dim, const Teacher te, 
 
 // q of every listed word (0 for the others), added up over the token's entries with the same word, and whether the token has any.  A wave a token.
 __global__ void __launch_bounds__(256)
-k_distill_targets(const Teacher te, int64_t tokens, int64_t vocab, float* __restrict__ q, int* __restrict__ counts) {
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+k_distill_targets(const Teacher te, int64_t tokens, int64_t vocab, float* __restrict__ q, int* __restrict__ counts, unsigned first_wg) {
+  const int64_t t = ((int64_t)first_wg + blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (t >= tokens) return;
   const float2 norm = teacher_norm(te, t, vocab, lane);
@@ -342,8 +343,9 @@ k_distill_targets(const Teacher te, int64_t tokens, int64_t vocab, float* __rest
 template <class El>
 __global__ void __launch_bounds__(256)
 k_distill_scatter(const Teacher te, const float* __restrict__ q, const float* __restrict__ z, const HeadMeta* __restrict__ meta, const int* __restrict__ index,
-                  const float* __restrict__ lse, const float* __restrict__ coef, int64_t v0, int64_t rows, int64_t vocab, uint16_t* __restrict__ G, int64_t pitch) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, c = i / te.top;
+                  const float* __restrict__ lse, const float* __restrict__ coef, int64_t v0, int64_t rows, int64_t vocab, uint16_t* __restrict__ G, int64_t pitch,
+                  unsigned first_wg) {
+  const int64_t i = ((int64_t)first_wg + blockIdx.x) * 256 + threadIdx.x, c = i / te.top;
   if (c >= meta->count) return;
   const int64_t t = index[c], at = t * te.top + (i - c * te.top), id = te.ids[at];
   if (id < v0 || id >= v0 + rows || !is_listed(id, te.logits[at], vocab)) return;
@@ -398,8 +400,8 @@ k_head_prepare(const int64_t* __restrict__ label, int64_t vocab, const int* __re
 __global__ void __launch_bounds__(256)
 k_head_gather(const Operand H, int64_t dim, int64_t vocab, const HeadMeta* __restrict__ meta, const int* __restrict__ index, const float* __restrict__ lse,
               const int64_t* __restrict__ label, const int* __restrict__ counts, char* __restrict__ Hc, int64_t pitch, float* __restrict__ lse_c,
-              float* __restrict__ coef, int* __restrict__ label_c, uint16_t* __restrict__ dH, int64_t lddh) {
-  const int64_t c = blockIdx.x;
+              float* __restrict__ coef, int* __restrict__ label_c, uint16_t* __restrict__ dH, int64_t lddh, unsigned first_wg) {
+  const int64_t c = first_wg + blockIdx.x;
   if (dH && !(label ? label[c] >= 0 && label[c] < vocab : counts[c] != 0))
     for (int64_t d = threadIdx.x; d < dim; d += 256) dH[c * lddh + d] = 0;
   if (c >= meta->count) return;
@@ -542,15 +544,15 @@ k_head_dw(const HeadProduct g) {
 
 // A matrix of zeros
 __global__ void __launch_bounds__(256)
-k_head_zero(uint16_t* __restrict__ dW, int64_t ld, int64_t dim) {
-  for (int64_t d = threadIdx.x; d < dim; d += 256) dW[(int64_t)blockIdx.x * ld + d] = 0;
+k_head_zero(uint16_t* __restrict__ dW, int64_t ld, int64_t dim, unsigned first_wg) {
+  for (int64_t d = threadIdx.x; d < dim; d += 256) dW[((int64_t)first_wg + blockIdx.x) * ld + d] = 0;
 }
 // The rows of dH that count: the sum of the splits' parts in their order.  A thread a number of a row, eight parts at a time on their way.
 template <class El>
 __global__ void __launch_bounds__(256)
 k_head_finish(const float* __restrict__ sum, int splits, int64_t tokens, int64_t dim, const HeadMeta* __restrict__ meta, const int* __restrict__ index,
-              uint16_t* __restrict__ dH, int64_t ld) {
-  const int64_t per = (dim + 255) / 256, c = blockIdx.x / per, d = (blockIdx.x - c * per) * 256 + threadIdx.x;
+              uint16_t* __restrict__ dH, int64_t ld, unsigned first_wg) {
+  const int64_t per = (dim + 255) / 256, wg = first_wg + blockIdx.x, c = wg / per, d = (wg - c * per) * 256 + threadIdx.x;
   if (c >= meta->count || d >= dim) return;
   const float* from = sum + c * dim + d;
   float x = 0.f;
@@ -617,9 +619,15 @@ static HeadPlan head_plan(int64_t tokens, int64_t vocab, int64_t dim, int64_t pi
   return p;
 }
 
+// Tiles that launches may not have, with 128 tokens each (64 where there are no more; 256 in some): the logits of a piece, dH, dW of a piece.
+static bool head_tiles_fit(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece) {
+  const int64_t rows = piece_rows(tokens, vocab, piece), tiles_t = ceil_div(tokens, 128), tiles_d = ceil_div(dim, kTileP);
+  return tiles_fit(ceil_div(rows, kTileP), tiles_t, kTileThreads) && tiles_fit(tiles_d, tiles_t, kTileThreads) && tiles_fit(tiles_d, ceil_div(rows, 128), kTileThreads);
+}
 static bool head_sizes(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece, int64_t top) {
   return tokens >= 0 && vocab >= 1 && dim >= 1 && piece >= 0 && top >= 0 && dim < kMaxPitch / 2 && tokens < (int64_t)1 << 30 && vocab < (int64_t)1 << 30 &&
-         ceil_div(vocab, kTileP) * ceil_div(tokens, 16) <= kMaxGrid && tokens <= kMaxGrid / ceil_div(dim, 256) && (top == 0 || tokens <= kMaxGrid / top);
+         ceil_div(vocab, kTileP) * ceil_div(tokens, 16) <= kMaxGrid && tokens <= kMaxGrid / ceil_div(dim, 256) && (top == 0 || tokens <= kMaxGrid / top) &&
+         head_tiles_fit(tokens, vocab, dim, piece);
 }
 static bool half_type(int dtype) { return dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16; }
 
@@ -677,8 +685,13 @@ static int head_forward(const HeadCall& c, const HeadPlan& plan, char* ws, float
     g.part += tiles.first * c.tokens;
     launch(tiles.count - tiles.first, tiles.bl);
   }
-  hipLaunchKernelGGL(k_head_join, dim3((unsigned)ceil_div(c.tokens, 16)), dim3(256), 0, stream, (const float2*)(ws + plan.part), tiles.count, c.tokens, c.label, c.vocab, g.zlabel, lse, loss);
-  if (!c.label) hipLaunchKernelGGL(k_distill_loss<El>, dim3((unsigned)c.tokens), dim3(256), 0, stream, g.W, g.H, c.dim, c.teacher, lse, z, loss);
+  in_launches(ceil_div(c.tokens, 16), 256, [&](unsigned first, dim3 grid) {
+    hipLaunchKernelGGL(k_head_join, grid, dim3(256), 0, stream, (const float2*)(ws + plan.part), tiles.count, c.tokens, c.label, c.vocab, g.zlabel, lse, loss, first);
+  });
+  if (!c.label)
+    in_launches(c.tokens, 256, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(k_distill_loss<El>, grid, dim3(256), 0, stream, g.W, g.H, c.dim, c.teacher, lse, z, loss, first);
+    });
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
 }
@@ -692,10 +705,15 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   char* hc = ws + plan.hc;
   uint16_t* G = (uint16_t*)(ws + plan.grad);
   const Operand H = rows_of(c.H, c.ldh, c.tokens);
-  if (!c.label) hipLaunchKernelGGL(k_distill_targets, dim3((unsigned)ceil_div(c.tokens, 4)), dim3(256), 0, stream, c.teacher, c.tokens, c.vocab, q, counts);
+  if (!c.label)
+    in_launches(ceil_div(c.tokens, 4), 256, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(k_distill_targets, grid, dim3(256), 0, stream, c.teacher, c.tokens, c.vocab, q, counts, first);
+    });
   hipLaunchKernelGGL(k_head_prepare, dim3(1), dim3(1024), 0, stream, c.label, c.vocab, counts, c.tokens, grad, grad_stride, 1.f / c.scale, meta, index, coef);
-  hipLaunchKernelGGL(k_head_gather, dim3((unsigned)c.tokens), dim3(256), 0, stream, H, c.dim, c.vocab, meta, index, lse, c.label, counts, hc,
-                     plan.pitch_h, lse_c, coef, label_c, (uint16_t*)dH, lddh);
+  in_launches(c.tokens, 256, [&](unsigned first, dim3 grid) {
+    hipLaunchKernelGGL(k_head_gather, grid, dim3(256), 0, stream, H, c.dim, c.vocab, meta, index, lse, c.label, counts, hc, plan.pitch_h, lse_c, coef, label_c,
+                       (uint16_t*)dH, lddh, first);
+  });
   const bool direct = aligned_pieces(c.W, 2 * c.ldw);
   const int bq = large_token_tiles(c.tokens, direct, ceil_div(c.dim, kTileP) * plan.splits, plan.per_split) > 0 ? 256 : small_tile(c.tokens);
   const int64_t tiles_t = ceil_div(c.tokens, bq);
@@ -727,8 +745,9 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
       launch(tiles.count - tiles.first, tiles.bl);
     }
     if (!c.label)
-      hipLaunchKernelGGL(k_distill_scatter<El>, dim3((unsigned)ceil_div(c.tokens * c.teacher.top, 256)), dim3(256), 0, stream, c.teacher, q, z, meta, index, lse_c, coef,
-                         v0, rows, c.vocab, G, plan.piece);
+      in_launches(ceil_div(c.tokens * c.teacher.top, 256), 256, [&](unsigned first, dim3 grid) {
+        hipLaunchKernelGGL(k_distill_scatter<El>, grid, dim3(256), 0, stream, c.teacher, q, z, meta, index, lse_c, coef, v0, rows, c.vocab, G, plan.piece, first);
+      });
     if (dH) {
       HeadProduct h = {};
       h.P = Operand{g.W.base, g.W.ld, c.dim};
@@ -769,7 +788,9 @@ static int head_backward(const HeadCall& c, const HeadPlan& plan, char* ws, cons
   const int64_t first = c.vocab < plan.piece ? c.vocab : plan.piece;
   const int splits = (int)ceil_div(first, plan.per_split);
   if (dH)
-    hipLaunchKernelGGL(k_head_finish<El>, dim3((unsigned)(c.tokens * ceil_div(c.dim, 256))), dim3(256), 0, stream, sum, splits, c.tokens, c.dim, meta, index, (uint16_t*)dH, lddh);
+    in_launches(c.tokens * ceil_div(c.dim, 256), 256, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(k_head_finish<El>, grid, dim3(256), 0, stream, sum, splits, c.tokens, c.dim, meta, index, (uint16_t*)dH, lddh, first);
+    });
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
 }
@@ -832,7 +853,7 @@ static int head_backward_call(const HeadCall& c, int64_t piece, const float* lse
   if ((dH && lddh < c.dim) || (dW && lddw < c.dim)) return BRSVD_ERR_ARG;
   if (c.tokens == 0) {
     if (!dW) return BRSVD_OK;
-    hipLaunchKernelGGL(k_head_zero, dim3((unsigned)c.vocab), dim3(256), 0, s, (uint16_t*)dW, lddw, c.dim);
+    in_launches(c.vocab, 256, [&](unsigned first, dim3 grid) { hipLaunchKernelGGL(k_head_zero, grid, dim3(256), 0, s, (uint16_t*)dW, lddw, c.dim, first); });
     BRSVD_HIP_TRY(hipGetLastError());
     return BRSVD_OK;
   }

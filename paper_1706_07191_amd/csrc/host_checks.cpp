@@ -290,6 +290,21 @@ int main() {
     }
   }
 
+  // ---- work of more workgroups than a launch may have: every one once, in order, and each launch below 2^32 threads ----
+  for (int i = 0; i < 3000; ++i) {
+    const int threads = 64 << (next_u64() % 5);
+    const int64_t edge = brsvd::launch_workgroups(threads);
+    const int64_t work = i % 3 == 0 ? uniform(0, UINT32_MAX) : i % 3 == 1 ? edge * uniform(1, 3) + uniform(-2, 2) : uniform(0, 1000);
+    if (work > (int64_t)UINT32_MAX) continue;
+    int64_t next = 0;
+    bool good = edge * threads < ((int64_t)1 << 32) && (edge + 1) * threads >= ((int64_t)1 << 32);
+    brsvd::in_launches(work, threads, [&](unsigned first, dim3 grid) {
+      good &= (int64_t)first == next && grid.x > 0 && grid.y == 1 && grid.z == 1 && (uint64_t)grid.x * threads < ((uint64_t)1 << 32);
+      next += grid.x;
+    });
+    CHECK(good && next == work);
+  }
+
   // ---- the calls on a model's matrices: sizes of scratch and workspace over their whole range, refusals before any GPU call ----
   for (int i = 0; i < 20000; ++i) {
     const int64_t big[] = {1, 7, 64, 300, 5000, 100000, 3000000, (int64_t)1 << 29, (int64_t)1 << 31, (int64_t)1 << 40, INT64_MAX / 2};

@@ -102,7 +102,7 @@ __device__ __forceinline__ float number_of(const uint32_t (&w)[4], int j) {
 template <int DT, bool SQUARE, bool STRAIGHT, bool TRANSPOSED>
 __global__ void __launch_bounds__(256)
 k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S,
-           uint8_t* __restrict__ Qt, int64_t ldqt, float* __restrict__ St) {
+           uint8_t* __restrict__ Qt, int64_t ldqt, float* __restrict__ St, unsigned first_wg) {
   using P = Part<DT>;
   using K = Keys<DT>;
   constexpr int W = P::kWide, R = P::kRows, L = P::kLanes, GROUPS = kBlock / R;
@@ -110,7 +110,8 @@ k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, 
   __shared__ __attribute__((aligned(16))) uint8_t turned[TRANSPOSED ? kBlock * kBlock : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid % L, c = cg * W, g = tid / L;
   const int64_t ncb = (cols + kBlock - 1) / kBlock, nrb = (rows + kBlock - 1) / kBlock;
-  const int64_t rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, row0 = rb * kBlock, col0 = cb * kBlock;
+  const unsigned wg = first_wg + blockIdx.x;
+  const int64_t rb = wg / (unsigned)ncb, cb = wg % (unsigned)ncb, row0 = rb * kBlock, col0 = cb * kBlock;
   const int width = (int)(cols - col0 - c < W ? (cols - col0 - c > 0 ? cols - col0 - c : 0) : W);
   uint32_t x[R][4];
 #pragma unroll
@@ -222,12 +223,12 @@ k_quantize(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, 
 // way for the memory, which is the bound.  8192 x 8192 bf16 37 us (201 MB, 5.4 TB/s); small parts, so that small matrices reach all CUs.
 template <int DT>
 __global__ void __launch_bounds__(256)
-k_quantize_rows(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S) {
+k_quantize_rows(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S, unsigned first_wg) {
   using P = Part<DT>;
   constexpr int W = P::kWide, L = P::kLanes, SETS = 4;
   const int cg = threadIdx.x % L;
   const unsigned ncb = (unsigned)((cols + kBlock - 1) / kBlock);
-  const int64_t first = (int64_t)blockIdx.x * (256 / L * SETS) + threadIdx.x / L, blocks = rows * ncb;
+  const int64_t first = ((int64_t)first_wg + blockIdx.x) * (256 / L * SETS) + threadIdx.x / L, blocks = rows * ncb;
   float x[SETS][W];
   int64_t row[SETS], col[SETS];
   int width[SETS];
@@ -262,12 +263,12 @@ k_quantize_rows(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t c
 // memory: 20000 x 20000 fp32 455 us (2.0 GB, 4.4 TB/s).
 template <int DT>
 __global__ void __launch_bounds__(DT == BRSVD_DTYPE_F32 ? 512 : 1024)
-k_quantize_square(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S) {
+k_quantize_square(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* __restrict__ Q, int64_t ldq, float* __restrict__ S, unsigned first_wg) {
   using P = Part<DT>;
   constexpr int W = P::kWide, L = P::kLanes, BLOCKS = 64 / L, WAVES = DT == BRSVD_DTYPE_F32 ? 8 : 16, R = kBlock / WAVES;
   __shared__ float top[WAVES][BLOCKS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = lane / L;
-  const unsigned ncb = (unsigned)((cols + kBlock - 1) / kBlock), across = (ncb + BLOCKS - 1) / BLOCKS, rb = blockIdx.x / across, cb = (blockIdx.x % across) * BLOCKS;
+  const unsigned wg = first_wg + blockIdx.x, ncb = (unsigned)((cols + kBlock - 1) / kBlock), across = (ncb + BLOCKS - 1) / BLOCKS, rb = wg / across, cb = (wg % across) * BLOCKS;
   const int64_t row0 = (int64_t)rb * kBlock + wave * R, col = (int64_t)cb * kBlock + lane * W;
   const int width = (int)(cols - col < W ? (cols - col > 0 ? cols - col : 0) : W);
   float x[R][W], t = 0.f;
@@ -299,11 +300,13 @@ k_quantize_square(const char* __restrict__ X, int64_t ldx, int64_t rows, int64_t
 // 5.6 TB/s).
 template <int DT>
 __global__ void __launch_bounds__(256)
-k_dequantize(const uint8_t* __restrict__ Q, int64_t ldq, const float* __restrict__ S, int64_t rows, int64_t cols, int block_rows, char* __restrict__ X, int64_t ldx) {
+k_dequantize(const uint8_t* __restrict__ Q, int64_t ldq, const float* __restrict__ S, int64_t rows, int64_t cols, int block_rows, char* __restrict__ X, int64_t ldx,
+             unsigned first_wg) {
   using P = Part<DT>;
   constexpr int W = P::kWide, R = 4, STEP = 256 / P::kLanes;
   const int c = (int)(threadIdx.x % P::kLanes) * W, r = threadIdx.x / P::kLanes;
-  const int64_t ncb = (cols + kBlock - 1) / kBlock, rb = blockIdx.x / (unsigned)ncb, cb = blockIdx.x % (unsigned)ncb, col = cb * kBlock + c, row0 = rb * (STEP * R) + r;
+  const unsigned wg = first_wg + blockIdx.x;
+  const int64_t ncb = (cols + kBlock - 1) / kBlock, rb = wg / (unsigned)ncb, cb = wg % (unsigned)ncb, col = cb * kBlock + c, row0 = rb * (STEP * R) + r;
   const int width = (int)(cols - col < W ? cols - col : W);
   if (width <= 0) return;
   uint32_t w[R][W / 4];
@@ -354,15 +357,26 @@ k_dequantize(const uint8_t* __restrict__ Q, int64_t ldq, const float* __restrict
 template <int DT, bool SQUARE>
 static void launch_quantize(const char* X, int64_t ldx, int64_t rows, int64_t cols, uint8_t* Q, int64_t ldq, float* S, uint8_t* Qt, int64_t ldqt, float* St,
                             hipStream_t stream) {
-  const dim3 grid((unsigned)(ceil_div(cols, kBlock) * ceil_div(rows, kBlock)));
+  const int64_t parts = ceil_div(cols, kBlock) * ceil_div(rows, kBlock);
   const int64_t pitch = ldx * (DT == BRSVD_DTYPE_F32 ? 4 : 2);
-  if (!SQUARE && !Qt)
-    hipLaunchKernelGGL(k_quantize_rows<DT>, dim3((unsigned)ceil_div(rows * ceil_div(cols, kBlock), 256 / Part<DT>::kLanes * 4)), dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S);
-  else if (Q && Qt) hipLaunchKernelGGL((k_quantize<DT, SQUARE, true, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
-  else if (Q)
-    hipLaunchKernelGGL(k_quantize_square<DT>, dim3((unsigned)(ceil_div(ceil_div(cols, kBlock), 64 / Part<DT>::kLanes) * ceil_div(rows, kBlock))),
-                       dim3(DT == BRSVD_DTYPE_F32 ? 512 : 1024), 0, stream, X, pitch, rows, cols, Q, ldq, S);
-  else hipLaunchKernelGGL((k_quantize<DT, SQUARE, false, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St);
+  if (!SQUARE && !Qt) {
+    in_launches(ceil_div(rows * ceil_div(cols, kBlock), 256 / Part<DT>::kLanes * 4), 256, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(k_quantize_rows<DT>, grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, first);
+    });
+  } else if (Q && Qt) {
+    in_launches(parts, 256, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL((k_quantize<DT, SQUARE, true, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St, first);
+    });
+  } else if (Q) {
+    const int threads = DT == BRSVD_DTYPE_F32 ? 512 : 1024;
+    in_launches(ceil_div(ceil_div(cols, kBlock), 64 / Part<DT>::kLanes) * ceil_div(rows, kBlock), threads, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL(k_quantize_square<DT>, grid, dim3(threads), 0, stream, X, pitch, rows, cols, Q, ldq, S, first);
+    });
+  } else {
+    in_launches(parts, 256, [&](unsigned first, dim3 grid) {
+      hipLaunchKernelGGL((k_quantize<DT, SQUARE, false, true>), grid, dim3(256), 0, stream, X, pitch, rows, cols, Q, ldq, S, Qt, ldqt, St, first);
+    });
+  }
 }
 
 int quantize(const void* X, int64_t ldx, int64_t rows, int64_t cols, int dtype, int block_rows, uint8_t* Q, int64_t ldq, float* S, uint8_t* Qt, int64_t ldqt,
@@ -399,12 +413,13 @@ extern "C" int brsvd_dequantize_e4m3(const uint8_t* Q, int64_t ldq, const float*
   if (rows < 0 || cols < 0 || !model_type(dtype) || (block_rows != 1 && block_rows != kBlock)) return BRSVD_ERR_ARG;
   if (rows == 0 || cols == 0) return BRSVD_OK;
   if (!Q || !S || !X || ldq < cols || ldx < cols || cols > kMaxGrid * kBlock || rows > (kMaxGrid << 2) / ceil_div(cols, kBlock)) return BRSVD_ERR_ARG;
-  const dim3 grid((unsigned)(ceil_div(cols, kBlock) * ceil_div(rows, dtype == BRSVD_DTYPE_F32 ? 32 : 64)));
   const int64_t pitch = ldx * (dtype == BRSVD_DTYPE_F32 ? 4 : 2);
-  hipStream_t s = (hipStream_t)stream;
-  if (dtype == BRSVD_DTYPE_F32) hipLaunchKernelGGL(k_dequantize<BRSVD_DTYPE_F32>, grid, dim3(256), 0, s, Q, ldq, S, rows, cols, block_rows, (char*)X, pitch);
-  else if (dtype == BRSVD_DTYPE_BF16) hipLaunchKernelGGL(k_dequantize<BRSVD_DTYPE_BF16>, grid, dim3(256), 0, s, Q, ldq, S, rows, cols, block_rows, (char*)X, pitch);
-  else hipLaunchKernelGGL(k_dequantize<BRSVD_DTYPE_F16>, grid, dim3(256), 0, s, Q, ldq, S, rows, cols, block_rows, (char*)X, pitch);
+  in_launches(ceil_div(cols, kBlock) * ceil_div(rows, dtype == BRSVD_DTYPE_F32 ? 32 : 64), 256, [&](unsigned first, dim3 grid) {
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, Q, ldq, S, rows, cols, block_rows, (char*)X, pitch, first); };
+    if (dtype == BRSVD_DTYPE_F32) launch(k_dequantize<BRSVD_DTYPE_F32>);
+    else if (dtype == BRSVD_DTYPE_BF16) launch(k_dequantize<BRSVD_DTYPE_BF16>);
+    else launch(k_dequantize<BRSVD_DTYPE_F16>);
+  });
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
 }

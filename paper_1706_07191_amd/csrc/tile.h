@@ -32,7 +32,7 @@ struct Fp16 { static constexpr int kBytes = 2; };
 struct E4m3 { static constexpr int kBytes = 1; };
 
 constexpr int kStepBytes = 128;          // of the contraction per step
-constexpr int64_t kMaxGrid = (int64_t)1 << 30;   // workgroups of a launch
+constexpr int64_t kMaxGrid = (int64_t)1 << 30;   // tiles or pieces of work of a call, which kernels count in 32 bits
 enum Order { kRows = 0, kCols = 1 };
 
 // One operand as a kernel gets it.
@@ -502,6 +502,8 @@ __device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64
   return true;
 }
 inline unsigned tile_workgroups(int64_t np, int64_t nq) { return (unsigned)(8 * ((np * nq + 7) / 8)); }
+// Whether a launch may have that many tiles
+inline bool tiles_fit(int64_t np, int64_t nq, int threads) { return nq == 0 || (np <= kMaxGrid / nq && tile_workgroups(np, nq) <= launch_workgroups(threads)); }
 
 // A product's tiles on 256 CUs: np of them along one side, each a column of q256 tiles of 256 x 256 or of q128 of half the size (seven tenths of the time).  The
 // first so many of the np go in large ones (what it returns): all, none, or those of the full rounds, so that only the last round is of small ones.  A tile

@@ -5,6 +5,7 @@ import torch
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
 from tests.test_gpu_e4m3 import codes, randn
+from tests.test_gpu_head import problem
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +25,92 @@ def test_cast_of_more_than_2_to_the_31_columns(dtype):
     assert bool((S[:, :-5] == 1).all())
     for i in range(0, cols - 556, 2 ** 28):
         assert not bool(Q[:, i:min(i + 2 ** 28, cols - 556)].view(torch.uint8).any()), i
+
+
+MANY = 2 ** 24 + 77            # workgroups of 256 threads that are more than the 2^32 threads of a launch
+
+
+def test_gradients_of_more_tokens_than_a_launch_has_workgroups():
+    """2^24 + 77 tokens, whose rows repeat after 2^16: each part has the bits of the first."""
+    dev = need_gpu()
+    vocab, dim, period = 40, 8, 2 ** 16
+    H, W, y, g = problem(period, vocab, dim, torch.bfloat16, dev)
+    y[1::5] = -1
+    each = torch.rand(period, generator=g) + 0.5
+    where = torch.arange(MANY, device=dev) % period
+    big, labels, grad = H[where], y.to(dev)[where], each.to(dev)[where]
+    loss, lse = B.brsvd_xent_forward(big, W, labels)
+    dH, dW = B.brsvd_xent_backward(big, W, labels, lse, grad)
+    loss1, lse1 = B.brsvd_xent_forward(H, W, y.to(dev))
+    dH1, dW1 = B.brsvd_xent_backward(H, W, y.to(dev), lse1, each.to(dev))
+    for i in range(0, MANY, period):
+        n = min(period, MANY - i)
+        assert torch.equal(loss[i:i + n], loss1[:n]) and torch.equal(lse[i:i + n], lse1[:n]) and torch.equal(dH[i:i + n], dH1[:n]), i
+    # dW: 256 of the first part's and 77 tokens; 2^19 additions a sum (32 tokens an instruction) that lose at most a step each, of the sum of |terms|, and 2^-9 of bf16
+    h = H.double().cpu()
+    p = torch.softmax(h @ W.double().cpu().t(), dim=1)
+    size = ((p + 1.0 * (torch.arange(vocab) == y[:, None])) * each.double()[:, None] * (y >= 0)[:, None]).t() @ h.abs()
+    bound = 257 * size * (2.0 ** -4 + 2.0 ** -8) + 77 * 2 * 1.5 * float(h.abs().max())
+    assert bool(((dW.double() - 256 * dW1.double()).abs().cpu() <= bound).all())
+
+
+def test_distillation_of_more_tokens_than_a_launch_has_workgroups():
+    dev = need_gpu()
+    vocab, dim, period, top = 40, 8, 2 ** 16, 2
+    H, W, _, g = problem(period, vocab, dim, torch.bfloat16, dev)
+    ids = torch.randint(-1, vocab, (period, top), generator=g).to(dev)
+    a = torch.randn(period, top, generator=g).to(dev)
+    where = torch.arange(MANY, device=dev) % period
+    one = torch.ones(1, device=dev)
+    big, bids, ba = H[where], ids[where], a[where]
+    loss, lse, z = B.brsvd_distill_forward(big, W, bids, ba, 2.0)
+    dH, _ = B.brsvd_distill_backward(big, W, bids, ba, 2.0, lse, z, one, need_dW=False)
+    loss1, lse1, z1 = B.brsvd_distill_forward(H, W, ids, a, 2.0)
+    dH1, _ = B.brsvd_distill_backward(H, W, ids, a, 2.0, lse1, z1, one, need_dW=False)
+    for i in range(0, MANY, period):
+        n = min(period, MANY - i)
+        assert torch.equal(loss[i:i + n], loss1[:n]) and torch.equal(z[i:i + n], z1[:n]) and torch.equal(dH[i:i + n], dH1[:n]), i
+
+
+def test_no_tokens_of_more_words_than_a_launch_has_workgroups():
+    dev = need_gpu()
+    W = torch.ones(MANY, 1, dtype=torch.bfloat16, device=dev)
+    none = torch.empty(0, device=dev)
+    dW = B.brsvd_xent_backward(W[:0], W, none.long(), none, none)[1]
+    assert dW.shape == W.shape and not bool(dW.any())
+
+
+def test_casts_of_more_rows_than_a_launch_has_workgroups():
+    """2^29 + 77 rows of one number, whose values repeat after 2^20."""
+    dev = need_gpu()
+    rows, period = 2 ** 29 + 77, 2 ** 20
+    x = randn(11, period).float().to(dev)
+    X = x.repeat(-(-rows // period))[:rows, None]
+    Q, S = B.brsvd_quantize_e4m3(X)
+    q, s = B.brsvd_quantize_e4m3(x[:, None])
+    back = B.brsvd_dequantize_e4m3(Q, S)
+    del X
+    one = B.brsvd_dequantize_e4m3(q, s)
+    for i in (0, period, 2 ** 28, rows // period * period - period, rows // period * period):
+        n = min(period, rows - i)
+        assert torch.equal(codes(Q[i:i + n]), codes(q[:n])) and torch.equal(S[i:i + n], s[:n]) and torch.equal(back[i:i + n], one[:n]), i
+
+
+def test_casts_of_more_columns_than_a_launch_has_workgroups():
+    """2^31 + 300 columns in all ways of a cast: the blocks at the end are those of the end alone."""
+    dev = need_gpu()
+    cols = 2 ** 31 + 300
+    X = torch.zeros(1, cols, dtype=torch.bfloat16, device=dev)
+    tail = randn(5, 1, 556).to(torch.bfloat16).to(dev)
+    X[:, -556:] = tail                     # from a multiple of 128 on
+    Q, S, Qt, St = B.brsvd_quantize_e4m3(X, transpose=True)
+    q, s, qt, st = B.brsvd_quantize_e4m3(tail, transpose=True)
+    assert torch.equal(codes(Q[:, -556:]), codes(q)) and torch.equal(S[:, -5:], s)
+    assert torch.equal(codes(Qt[-556:]), codes(qt)) and torch.equal(St[-556:], st)
+    assert not bool(Qt[:2 ** 20].view(torch.uint8).any()) and bool((St[:-556] == 1).all())
+    del Qt, St
+    back = B.brsvd_dequantize_e4m3(Q, S)
+    assert torch.equal(back[:, -556:], B.brsvd_dequantize_e4m3(q, s)) and not bool(back[:, :2 ** 20].any())
+    del back
+    Q, S = B.brsvd_quantize_e4m3(X, block_rows=128)
+    assert torch.equal(codes(Q[:, -556:]), codes(q)) and torch.equal(S[:, -5:], s) and not bool(Q[:, :2 ** 20].view(torch.uint8).any())

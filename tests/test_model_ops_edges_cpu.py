@@ -1,0 +1,45 @@
+"""Refusals of the calls on a model's matrices at the ends of what they take, before any GPU call, with addresses that are never followed."""
+import pytest
+
+import paper_1706_07191_amd as B
+from tests.test_model_ops_cpu import ARG, BF16, BUDGET, F32, gemm, linear, xent
+
+LAUNCH = 2 ** 32               # threads that a launch has fewer of along a direction
+
+
+def ceil_div(a, b):
+    return -(-a // b)
+
+
+@pytest.mark.parametrize("tokens,vocab,dim,piece", [(2 ** 30 - 1024, 300, 1, 0), (2 ** 24 + 5, 300, 8, 0), (2 ** 20, 1000, 4096, 0), (600000, 1000, 8192, 0),
+                                                    (2 ** 28, 1000, 8, 256), (2 ** 17, 2 ** 20, 64, 2 ** 20), (1, 2 ** 17, 2 ** 20, 0)])
+def test_losses_take_what_launches_may_have(tokens, vocab, dim, piece):
+    """Sizes whose tiles are fewer than 2^32 threads in all are accepted; the other kernels go in several launches."""
+    assert B.lib().brsvd_head_workspace_bytes(tokens, vocab, dim, piece, 1, 1) > 0
+
+
+@pytest.mark.parametrize("tokens,vocab,dim,piece", [(2 ** 30 - 127, 300, 1, 0), (2 ** 30 - 1, 300, 1, 0), (2 ** 20, 2 ** 20, 64, 2 ** 20), (2 ** 22, 1000, 2 ** 16, 0),
+                                                    (1, 2 ** 18, 2 ** 20, 0)])
+def test_losses_refuse_tiles_that_a_launch_may_not_have(tokens, vocab, dim, piece):
+    """Logits of a piece, dH or dW in 2^23 tiles of 512 threads: of such a launch only a part would run."""
+    rows = min(piece or max(256, 2 ** 27 // tokens // 256 * 256), 2 ** 20, ceil_div(vocab, 256) * 256)
+    tiles = max(ceil_div(rows, 256) * ceil_div(tokens, 128), ceil_div(dim, 256) * ceil_div(tokens, 128), ceil_div(dim, 256) * ceil_div(rows, 128))
+    assert tiles * 512 >= LAUNCH
+    for backward in (0, 1):
+        if piece == 0 or backward:
+            assert B.lib().brsvd_head_workspace_bytes(tokens, vocab, dim, piece, 1, backward) == 0
+    assert xent(True, tokens=tokens, vocab=vocab, dim=dim, ldh=dim, ldw=dim, lddh=dim, lddw=dim, piece=piece) == ARG
+
+
+def test_products_refuse_what_a_launch_may_not_have():
+    # up to 32 rows: 256 threads for 32 columns
+    n = 2 ** 29
+    assert gemm(m=1, n=n, k=128, lda=128, ldb=128, ldc=n) == ARG
+    assert linear(m=20, n=n, k=128, ldx=128, ldw=128, ldy=n) == ARG
+    assert linear(m=20, n=n - 32, k=128, ldx=128, ldw=128, ldy=n, bytes=0) == BUDGET          # accepted: the cast's scratch is missing
+    # tiles of 128 rows and 256 columns, 512 threads each; of 256 rows for a 16-bit result of aligned rows
+    m = 2 ** 30
+    assert linear(m=m, n=100, k=128, ldx=128, ldw=128, ldy=100, dtype=F32, bytes=0) == ARG
+    assert linear(m=m - 1024, n=100, k=128, ldx=128, ldw=128, ldy=100, dtype=F32, bytes=0) == BUDGET
+    assert linear(m=m, n=100, k=128, ldx=128, ldw=130, ldy=100, dtype=BF16, bytes=0) == ARG
+    assert linear(m=m, n=100, k=128, ldx=128, ldw=128, ldy=100, dtype=BF16, bytes=0) == BUDGET
