@@ -295,7 +295,8 @@ uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_
  * Backward, for the gradient of sum_t grad_t loss_t, from the lse of the forward call:
  *   G_tv = grad_t (exp(z_tv - lse_t) - [v = labels_t]),   dH = G W,   dW = G^T H      (of dtype)
  * Rows of dH of tokens that do not count are 0, and what stands in those rows of H reaches nothing, NaN
- * and infinities included.  grad_stride: 1, or 0 for one factor for all tokens.  dH or dW may be NULL.
+ * and infinities included.  grad_stride: 1, or 0 for one factor for all tokens.  dH or dW may be NULL,
+ * both where there are no tokens.
  * G is formed in 16 bits for `piece` rows of W at a time (0: so many that it takes up to 256 MiB of the
  * workspace; otherwise rounded down to a multiple of 256, at least 256), dH is added up in fp32.
  * With no tokens dW is 0.

@@ -848,7 +848,7 @@ extern "C" int brsvd_distill_forward(const void* H, int64_t ldh, const void* W, 
 // Backward of either loss; with no tokens dW is zero
 static int head_backward_call(const HeadCall& c, int64_t piece, const float* lse, const float* z, const float* grad, int64_t grad_stride, void* dH, int64_t lddh,
                               void* dW, int64_t lddw, void* workspace, uint64_t workspace_bytes, hipStream_t s) {
-  if ((!dH && !dW) || grad_stride < 0) return BRSVD_ERR_ARG;
+  if ((c.tokens > 0 && !dH && !dW) || grad_stride < 0) return BRSVD_ERR_ARG;      // of no tokens dH has no elements and may be NULL
   BRSVD_TRY(check_head(c, piece));
   if ((dH && lddh < c.dim) || (dW && lddw < c.dim)) return BRSVD_ERR_ARG;
   if (c.tokens == 0) {

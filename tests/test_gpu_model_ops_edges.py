@@ -114,3 +114,14 @@ def test_casts_of_more_columns_than_a_launch_has_workgroups():
     del back
     Q, S = B.brsvd_quantize_e4m3(X, block_rows=128)
     assert torch.equal(codes(Q[:, -556:]), codes(q)) and torch.equal(S[:, -5:], s) and not bool(Q[:, :2 ** 20].view(torch.uint8).any())
+
+
+@pytest.mark.parametrize("need_dH,need_dW", [(True, False), (False, True), (True, True)])
+def test_one_gradient_of_no_tokens(need_dH, need_dW):
+    dev = need_gpu()
+    H, W, y, _ = problem(3, 300, 40, torch.float16, dev)
+    none, ids = torch.empty(0, device=dev), torch.empty(0, 4, dtype=torch.int64, device=dev)
+    for dH, dW in (B.brsvd_xent_backward(H[:0], W, y[:0].to(dev), none, none, need_dH=need_dH, need_dW=need_dW),
+                   B.brsvd_distill_backward(H[:0], W, ids, ids.float(), 2.0, none, ids.float(), none, need_dH=need_dH, need_dW=need_dW)):
+        assert dH.shape == (0, 40) if need_dH else dH is None
+        assert (dW.shape == W.shape and not bool(dW.any())) if need_dW else dW is None

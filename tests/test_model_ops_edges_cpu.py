@@ -2,13 +2,20 @@
 import pytest
 
 import paper_1706_07191_amd as B
-from tests.test_model_ops_cpu import ARG, BF16, BUDGET, F32, gemm, linear, xent
+from tests.test_model_ops_cpu import ARG, AT, BF16, BUDGET, F32, OK, gemm, linear, xent
 
 LAUNCH = 2 ** 32               # threads that a launch has fewer of along a direction
 
 
 def ceil_div(a, b):
     return -(-a // b)
+
+
+def distill_backward(_, **kw):
+    a = dict(H=AT, ldh=64, W=AT, ldw=64, ids=AT, logits=AT, top=5, tau=2.0, lse=AT, z=AT, grad=AT, stride=1, tokens=10, vocab=1000, dim=64, piece=0, dtype=BF16,
+             dH=AT, lddh=64, dW=AT, lddw=64, ws=AT, bytes=1 << 50)
+    a.update(kw)
+    return B.lib().brsvd_distill_backward(*a.values(), None)
 
 
 @pytest.mark.parametrize("tokens,vocab,dim,piece", [(2 ** 30 - 1024, 300, 1, 0), (2 ** 24 + 5, 300, 8, 0), (2 ** 20, 1000, 4096, 0), (600000, 1000, 8192, 0),
@@ -43,3 +50,13 @@ def test_products_refuse_what_a_launch_may_not_have():
     assert linear(m=m - 1024, n=100, k=128, ldx=128, ldw=128, ldy=100, dtype=F32, bytes=0) == BUDGET
     assert linear(m=m, n=100, k=128, ldx=128, ldw=130, ldy=100, dtype=BF16, bytes=0) == ARG
     assert linear(m=m, n=100, k=128, ldx=128, ldw=128, ldy=100, dtype=BF16, bytes=0) == BUDGET
+
+
+@pytest.mark.parametrize("loss", [xent, distill_backward])
+def test_no_tokens_have_any_of_the_gradients(loss):
+    """An empty dH may be NULL, as an empty tensor's address is; with tokens one gradient has to be wanted."""
+    none = dict(tokens=0, H=None, lse=None, grad=None, ws=None, bytes=0)
+    for out in (dict(dH=None, dW=None), dict(dW=None)):
+        assert loss(True, **none, **out) == OK
+        assert loss(True, **dict(none, tokens=-1), **out) == ARG
+    assert loss(True, dH=None, dW=None) == ARG
