@@ -70,6 +70,8 @@ struct HeadArgs {
 };
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+// What is taken off before exponentials: the largest, but nothing where that is infinite, so that a row of -inf sums to 0 and one with a +inf to infinity.
+__device__ __forceinline__ float reference(float top) { return fabsf(top) == INFINITY ? 0.f : top; }
 
 // What a tile of logits leaves: the label's logit, and for every token the largest and the sum.  Exponentials are powers of two of x log2(e); what is
 // kept of a row is in units of log 2, too.
@@ -98,7 +100,7 @@ __device__ __forceinline__ void leave_tile(const HeadArgs& g, floatx4 (&acc)[T::
       for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[p][q][r]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-    const float ref = top == -INFINITY ? 0.f : top;
+    const float ref = reference(top);
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -135,7 +137,7 @@ __device__ __forceinline__ void leave_tile(const HeadArgs& g, floatx4 (&acc)[T::
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < WP; ++w) top = fmaxf(top, red[w * BQ + col].x);
-    const float ref = top == -INFINITY ? 0.f : top;
+    const float ref = reference(top);
 #pragma unroll
     for (int w = 0; w < WP; ++w) sum += red[w * BQ + col].y * __builtin_amdgcn_exp2f(red[w * BQ + col].x - ref);
     g.part[tv * g.H.n + t0 + col] = make_float2(top, sum);
@@ -189,7 +191,7 @@ k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t tokens, cons
   const int64_t t = ((int64_t)first_wg + blockIdx.x) * 16 + c;
   float top = -INFINITY, sum = 0.f;
   auto add = [&](float2 v) {
-    const float to = fmaxf(top, v.x), ref = to == -INFINITY ? 0.f : to;
+    const float to = fmaxf(top, v.x), ref = reference(to);
     sum = sum * __builtin_amdgcn_exp2f(top - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
     top = to;
   };
@@ -209,7 +211,7 @@ k_head_join(const float2* __restrict__ part, int64_t tiles, int64_t tokens, cons
   if (r != 0 || t >= tokens) return;
   float all = -INFINITY;
   for (int i = 0; i < 16; ++i) all = fmaxf(all, red[i][c].x);
-  const float ref = all == -INFINITY ? 0.f : all;
+  const float ref = reference(all);
   sum = 0.f;
   for (int i = 0; i < 16; ++i) sum += red[i][c].y * __builtin_amdgcn_exp2f(red[i][c].x - ref);
   const float l = (all + log2f(sum)) * kLn2;

@@ -1,11 +1,13 @@
 """The calls on a model's matrices where numbers or sizes leave the usual range."""
+import math
+
 import pytest
 import torch
 
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
 from tests.test_gpu_e4m3 import codes, randn
-from tests.test_gpu_head import problem
+from tests.test_gpu_head import HALF, problem
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +127,35 @@ def test_one_gradient_of_no_tokens(need_dH, need_dW):
                    B.brsvd_distill_backward(H[:0], W, ids, ids.float(), 2.0, none, ids.float(), none, need_dH=need_dH, need_dW=need_dW)):
         assert dH.shape == (0, 40) if need_dH else dH is None
         assert (dW.shape == W.shape and not bool(dW.any())) if need_dW else dW is None
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("tokens,vocab", [(10, 600), (66, 600), (300, 512), (300, 700)])
+def test_rows_of_infinite_logits(tokens, vocab, dtype):
+    """A logit of +inf makes lse +inf, a row of -inf makes it -inf; the loss is the difference, and no other row changes a bit."""
+    dev = need_gpu()
+    H, W, y, _ = problem(tokens, vocab, 64, dtype, dev)
+    W[:, 0] = -1.0
+    W[:, 5] = torch.where(torch.arange(vocab, device=dev) % 3 == 0, -0.5, 0.25)
+    want = B.brsvd_xent_forward(H, W, y.to(dev))
+    grad = torch.ones(tokens, device=dev)
+    dH_want = B.brsvd_xent_backward(H, W, y.to(dev), want[1], grad, need_dW=False)[0]
+    H[3, 5] = math.inf             # +inf and -inf
+    H[4, 0] = math.inf             # -inf everywhere
+    H[6, 0] = -math.inf            # +inf everywhere
+    H[7, 9] = math.nan
+    y[3] = 3                       # a logit of -inf: the loss is +inf
+    z = H.double().cpu() @ W.double().cpu().t()
+    ref = torch.logsumexp(z, dim=1)
+    loss, lse = B.brsvd_xent_forward(H, W, y.to(dev))
+    odd = torch.tensor([3, 4, 6, 7])
+    assert ref[odd][:3].tolist() == [math.inf, -math.inf, math.inf]
+    torch.testing.assert_close(lse.double().cpu()[odd], ref[odd], rtol=0, atol=0, equal_nan=True)
+    torch.testing.assert_close(loss.double().cpu()[odd], (ref - z.gather(1, y[:, None])[:, 0])[odd], rtol=0, atol=0, equal_nan=True)
+    keep = torch.ones(tokens, dtype=torch.bool, device=dev)
+    keep[odd] = False
+    dH = B.brsvd_xent_backward(H, W, y.to(dev), lse, grad, need_dW=False)[0]
+    for a, b in ((loss, want[0]), (lse, want[1]), (dH, dH_want)):
+        assert torch.equal(a[keep], b[keep])
+    ids, a = y[:, None].to(dev).contiguous(), torch.zeros(tokens, 1, device=dev)
+    assert torch.equal(B.brsvd_distill_forward(H, W, ids, a)[1].nan_to_num(7.0, 8.0, 9.0), lse.nan_to_num(7.0, 8.0, 9.0))
