@@ -248,17 +248,18 @@ struct Teacher {
   float scale;          // 1 / tau
 };
 __device__ __forceinline__ bool is_listed(int64_t id, float a, int64_t vocab) { return id >= 0 && id < vocab && a > -INFINITY; }
-// Largest listed logit / tau of token t, and the sum of exponentials relative to it, in every lane of the wave
+// Largest listed logit of token t, and the sum of exponentials of (logit - largest) / tau, in every lane of the wave.  Taken off before the division: a mask of the
+// lowest fp32 number over a tau below one would be -inf.
 __device__ __forceinline__ float2 teacher_norm(const Teacher& te, int64_t t, int64_t vocab, int lane) {
   float top = -INFINITY, sum = 0.f;
   for (int j = lane; j < te.top; j += 64) {
     const float a = te.logits[t * te.top + j];
-    if (is_listed(te.ids[t * te.top + j], a, vocab)) top = fmaxf(top, a * te.scale);
+    if (is_listed(te.ids[t * te.top + j], a, vocab)) top = fmaxf(top, a);
   }
   top = wave_max(top);
   for (int j = lane; j < te.top; j += 64) {
     const float a = te.logits[t * te.top + j];
-    if (is_listed(te.ids[t * te.top + j], a, vocab)) sum += __builtin_amdgcn_exp2f((a * te.scale - top) * kLog2e);
+    if (is_listed(te.ids[t * te.top + j], a, vocab)) sum += __builtin_amdgcn_exp2f((a - top) * te.scale * kLog2e);
   }
   return make_float2(top, wave_sum(sum));
 }
@@ -302,8 +303,8 @@ k_distill_loss(const Operand W, const Operand H, int64_t dim, const Teacher te, 
       if (j0 + i >= te.top) continue;
       const int64_t at = t * te.top + j0 + i;
       if (in[i]) {
-        const float logq = te.logits[at] * te.scale - norm.x - logsum;
-        sum += __builtin_amdgcn_exp2f(logq * kLog2e) * (logq - acc[i] * te.scale + l);
+        const float logq = (te.logits[at] - norm.x) * te.scale - logsum, q = __builtin_amdgcn_exp2f(logq * kLog2e);
+        if (q != 0.f) sum += q * (logq - acc[i] * te.scale + l);          // q log q is 0 for q = 0, where log q may be -inf
       }
       if (lane == 0) z[at] = in[i] ? acc[i] : 0.f;
     }
@@ -328,7 +329,7 @@ k_distill_targets(const Teacher te, int64_t tokens, int64_t vocab, float* __rest
       const int64_t at = t * te.top + (i0 + lane < te.top ? i0 + lane : 0);
       const float a = te.logits[at];
       const int64_t id = i0 + lane < te.top && is_listed(te.ids[at], a, vocab) ? te.ids[at] : -1;
-      const float x = id >= 0 ? __builtin_amdgcn_exp2f((a * te.scale - norm.x) * kLog2e) * inv : 0.f;
+      const float x = id >= 0 ? __builtin_amdgcn_exp2f((a - norm.x) * te.scale * kLog2e) * inv : 0.f;
       const int last = te.top - i0 < 64 ? te.top - i0 : 64;
       for (int i = 0; i < last; ++i) {
         const int other = __builtin_amdgcn_readlane((int)id, i);           // words are below 2^30

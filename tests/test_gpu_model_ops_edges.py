@@ -7,7 +7,7 @@ import torch
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
 from tests.test_gpu_e4m3 import codes, randn
-from tests.test_gpu_head import HALF, problem
+from tests.test_gpu_head import HALF, Reference, problem, teacher_reference
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +159,25 @@ def test_rows_of_infinite_logits(tokens, vocab, dtype):
         assert torch.equal(a[keep], b[keep])
     ids, a = y[:, None].to(dev).contiguous(), torch.zeros(tokens, 1, device=dev)
     assert torch.equal(B.brsvd_distill_forward(H, W, ids, a)[1].nan_to_num(7.0, 8.0, 9.0), lse.nan_to_num(7.0, 8.0, 9.0))
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.5, 0.25])
+def test_teacher_logits_of_the_lowest_value(tau):
+    """Masked with the lowest fp32 number instead of -inf: such an entry is listed and has no part, unless a token has no others: then they are alike."""
+    dev = need_gpu()
+    H, W, _, g = problem(70, 500, 40, torch.bfloat16, dev)
+    ids = torch.randint(0, 500, (70, 6), generator=g)
+    a = torch.randn(70, 6, generator=g) * 3
+    low = torch.finfo(torch.float32).min
+    a[::3, 2:] = low
+    a[5], a[6, 1:] = low, -math.inf
+    a[6, 0] = low
+    a[7] = torch.tensor([3e38, low, 0.0, 3e38, -1.0, 1.0])
+    ref = Reference(H, W, tau)
+    want, target, counted, zs, off = teacher_reference(ref, ids, a, tau, 500)
+    assert bool(torch.isfinite(want).all() and counted.all())
+    loss, lse, z = B.brsvd_distill_forward(H, W, ids.to(dev), a.to(dev), tau)
+    ref.check("loss", loss, want, off)
+    grad = torch.ones(1, device=dev)
+    dH, dW = B.brsvd_distill_backward(H, W, ids.to(dev), a.to(dev), tau, lse, z, grad)
+    ref.check_gradients(dH, dW, target, tau * counted.double())
