@@ -100,11 +100,17 @@ __device__ __forceinline__ void leave_tile(const HeadArgs& g, floatx4 (&acc)[T::
       for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[p][q][r]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-    const float ref = reference(top);
+    // The largest entry's exponent, less its rounded value, is up to 2^-24 of it: an exponential stands that up to 2^30.  Beyond, all exponents are taken down so
+    // that the largest is 2^28 (three roundings: off by 48 at most).  What that adds to log2 of the sum is within the rounding of the largest.
+    float ref = reference(top), s = scale;
+    if (fabsf(ref) > 0x1p30f) {
+      s = scale * (0x1p28f / fabsf(ref));
+      ref = copysignf(0x1p28f, ref);
+    }
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[p][q][r], scale, -ref));
+      for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[p][q][r], s, -ref));
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (lane < 16) red[wp * BQ + 16 * (wq * NQ + q) + lane] = make_float2(top, sum);

@@ -181,3 +181,17 @@ def test_teacher_logits_of_the_lowest_value(tau):
     grad = torch.ones(1, device=dev)
     dH, dW = B.brsvd_distill_backward(H, W, ids.to(dev), a.to(dev), tau, lse, z, grad)
     ref.check_gradients(dH, dW, target, tau * counted.double())
+
+
+@pytest.mark.parametrize("tokens", [10, 66, 300])
+@pytest.mark.parametrize("power", [10, 14, 20, 30])
+def test_finite_logits_of_any_size(tokens, power):
+    """Logits of up to 2^62, finite in fp32: lse is theirs to within their rounding, not an infinity."""
+    dev = need_gpu()
+    H, W, y, _ = problem(tokens, 600, 64, torch.bfloat16, dev, scale=2.0 ** power)
+    W *= 2.0 ** power
+    ref = Reference(H, W)
+    loss, lse = B.brsvd_xent_forward(H, W, y.to(dev))
+    ref.check_lse(lse)
+    zy = ref.z.gather(1, y[:, None])[:, 0]
+    ref.check("loss", loss, ref.lse - zy, ref.dlse + ref.dz.amax(dim=1) + 2.0 ** -22 * (ref.lse - zy).abs())
