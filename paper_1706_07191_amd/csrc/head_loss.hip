@@ -317,7 +317,8 @@ k_distill_loss(const Operand W, const Operand H, int64_t dim, const Teacher te, 
   }
   if (lane == 0) part[wave] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) loss[t] = norm.y == 0.f ? 0.f : (part[0] + part[1] + part[2] + part[3]) / (te.scale * te.scale);
+  // tau times tau, one after the other: tau^2 may leave fp32 where the loss does not
+  if (threadIdx.x == 0) loss[t] = norm.y == 0.f ? 0.f : (part[0] + part[1] + part[2] + part[3]) / te.scale / te.scale;
 }
 
 // q of every listed word (0 for the others), added up over the token's entries with the same word, and whether the token has any.  A wave a token.

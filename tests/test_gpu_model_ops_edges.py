@@ -195,3 +195,19 @@ def test_finite_logits_of_any_size(tokens, power):
     ref.check_lse(lse)
     zy = ref.z.gather(1, y[:, None])[:, 0]
     ref.check("loss", loss, ref.lse - zy, ref.dlse + ref.dz.amax(dim=1) + 2.0 ** -22 * (ref.lse - zy).abs())
+
+
+@pytest.mark.parametrize("power", [-70, -40, 40])
+def test_temperatures_whose_square_leaves_fp32(power):
+    """tau^2 and 1 / tau^2 need not be numbers of fp32: the loss does where it is one."""
+    dev = need_gpu()
+    tau = 2.0 ** power
+    H, W, _, g = problem(66, 300, 32, torch.bfloat16, dev)
+    ids = torch.randint(0, 300, (66, 3), generator=g)
+    a = torch.randn(66, 3, generator=g) * 3
+    ref = Reference(H, W, tau)
+    want, _, _, _, off = teacher_reference(ref, ids, a, tau, 300)
+    loss, _, _ = B.brsvd_distill_forward(H, W, ids.to(dev), a.to(dev), tau)
+    ref.check("loss", loss, want, off)
+    if power < 0:
+        assert float((off / want.abs().clamp(min=1e-300)).median()) < 2.0 ** -8
