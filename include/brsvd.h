@@ -298,7 +298,9 @@ uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_
  * and infinities included.  grad_stride: 1, or 0 for one factor for all tokens.  dH or dW may be NULL,
  * both where there are no tokens.
  * G is formed in 16 bits for `piece` rows of W at a time (0: so many that it takes up to 256 MiB of the
- * workspace; otherwise rounded down to a multiple of 256, at least 256), dH is added up in fp32.
+ * workspace; otherwise rounded down to a multiple of 256, at least 256), dH is added up in fp32.  With
+ * F16 an entry of G is off by up to 2^-39 max_t |grad_t| beside its rounding to eleven bits: factors
+ * should not differ by more than about 2^20.
  * With no tokens dW is 0.
  * workspace: at least brsvd_head_workspace_bytes of the same sizes (forward: piece 0; top 0). */
 int brsvd_xent_forward(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* labels,

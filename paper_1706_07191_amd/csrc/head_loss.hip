@@ -45,7 +45,8 @@ static LogitTiles logit_tiles(int64_t tokens, bool direct, int64_t words, int64_
 }
 
 // What the backward pass knows on the device: how many tokens count, and the power of two that G is multiplied by so that its numbers of 16 bits hold what
-// matters: 2^e max |g_t| is at most 2^14, and a probability of 2^-28 is still a normal number of fp16.
+// matters: 2^e max |g_t| is 2^14 to 2^15, which |p - target| <= 1 keeps inside fp16, and for the token with that factor a probability of 2^-28 is still a normal
+// number.  One power serves all tokens, as dW adds them up: in fp16 an entry is off by 2^-39 max |g_t| where it is small, whatever its own token's factor.
 struct HeadMeta {
   int count;
   float up, down;      // 2^e, 2^-e
@@ -397,7 +398,7 @@ k_head_prepare(const int64_t* __restrict__ label, int64_t vocab, const int* __re
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 0; w < 16; ++w) top = fmaxf(top, wave_top[w]);
-    int e = top > 0.f ? 13 - ((int)(__float_as_uint(top) >> 23) - 127) : 0;
+    int e = top > 0.f ? 14 - ((int)(__float_as_uint(top) >> 23) - 127) : 0;
     e = e > 120 ? 120 : e < -120 ? -120 : e;
     meta->count = (int)before;
     meta->up = __uint_as_float((uint32_t)(e + 127) << 23);

@@ -7,7 +7,7 @@ import torch
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
 from tests.test_gpu_e4m3 import codes, randn
-from tests.test_gpu_head import HALF, Reference, problem, teacher_reference
+from tests.test_gpu_head import FINEST, HALF, ROUND, Reference, problem, teacher_reference
 
 pytestmark = pytest.mark.gpu
 
@@ -211,3 +211,45 @@ def test_temperatures_whose_square_leaves_fp32(power):
     ref.check("loss", loss, want, off)
     if power < 0:
         assert float((off / want.abs().clamp(min=1e-300)).median()) < 2.0 ** -8
+
+
+def test_fp16_gradients_keep_probabilities_down_to_2_to_the_minus_28():
+    """Two words, the second with a probability p of 2^-28 to 2^-27 and a row of W that lets its gradient show in fp16: G = g p is rounded by half a step of
+    eleven bits, dH is that times a power of two and rounds nothing; beside that exp and lse in fp32 (z up to 20: 2^-17 is 16 of their steps)."""
+    dev = need_gpu()
+    tokens = 600
+    H = torch.zeros(tokens, 3, dtype=torch.float16)
+    H[:, 0] = 18.75
+    H[:, 1] = torch.linspace(0.0, 0.656, tokens)
+    W = torch.tensor([[1.0, 1.0, 0.0], [0.0, 0.0, 256.0]], dtype=torch.float16)
+    z = H.double() @ W.double().t()
+    p = torch.softmax(z, dim=1)[:, 1]
+    assert 2.0 ** -28 <= float(p.min()) and float(p.max()) < 2.0 ** -26.9
+    y = torch.zeros(tokens, dtype=torch.int64, device=dev)
+    H, W = H.to(dev), W.to(dev)
+    loss, lse = B.brsvd_xent_forward(H, W, y)
+    dH, _ = B.brsvd_xent_backward(H, W, y, lse, torch.full((1,), 1024.0, device=dev), need_dW=False)
+    want = 1024.0 * p * 256.0
+    err = (dH[:, 2].double().cpu() - want).abs() / want
+    assert float(err.max()) <= (1 + 2.0 ** -11) * (1 + 2.0 ** -17) - 1
+
+
+def test_fp16_gradients_of_factors_that_differ_by_orders_of_magnitude():
+    """One power of two serves all tokens: an entry of G is off by half a step of its eleven bits, or where it is small by max|g| 2^-39 (half of fp16's finest
+    step, 2^-25, over 2^14 / max|g|), whatever the token's own factor.  Each row of dH is held to that."""
+    dev = need_gpu()
+    tokens, vocab, dim = 300, 700, 64
+    H, W, y, _ = problem(tokens, vocab, dim, torch.float16, dev)
+    ref = Reference(H, W)
+    loss, lse = B.brsvd_xent_forward(H, W, y.to(dev))
+    factor = 2.0 ** (10 - torch.arange(tokens, dtype=torch.float64) % 25)
+    dH, _ = B.brsvd_xent_backward(H, W, y.to(dev), lse, factor.float().to(dev), need_dW=False)
+    target = torch.zeros_like(ref.z).scatter_(1, y[:, None], 1.0)
+    p = torch.exp(ref.z - ref.lse[:, None])
+    G = factor[:, None] * (p - target)
+    off = factor[:, None] * (p * (ref.dz + ref.dlse[:, None]) * 1.01 + 2.0 ** -20 * (p + target))
+    u = ROUND[torch.float16]
+    off = off + u * (G.abs() + off) + 2.0 ** 10 * 2.0 ** -39
+    want = G @ ref.w
+    bound = off @ ref.w.abs() + (G.abs() + off) @ ref.w.abs() * 2.0 ** -23 * (vocab + 70)
+    ref.check("dH", dH, want, bound + u * (want.abs() + bound) + FINEST[torch.float16])
