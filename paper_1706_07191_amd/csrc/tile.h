@@ -54,14 +54,17 @@ struct __attribute__((packed, aligned(1))) Piece { uint32_t x[4]; };
 
 // 16 bytes per lane into LDS at `dst` (the same in all lanes) + 16 lane, from `off` bytes (below 2^31) behind an address that all lanes share.  Written
 // out so that the compiler does not hold back reads of the other buffer until it is done; the wait before the barrier that hands the
-// buffer over is written out, too.
+// buffer over is written out, too.  m0 is among the registers that the compiler keeps for itself, and it warns of one that is named: here it has to know.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(uint32_t dst, const char* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "s"(base), "v"(off) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %1" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "s"(base), "v"(off) : "memory", "m0");
 }
 // 4 bytes per lane, to `dst` + 4 lane.
 __device__ __forceinline__ void load4_to_lds(uint32_t dst, const void* src) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // The same value in scalar registers, for one that all lanes share.
 __device__ __forceinline__ int64_t scalar(int64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));

@@ -1,4 +1,7 @@
 """Refusals of the calls on a model's matrices at the ends of what they take, before any GPU call, with addresses that are never followed."""
+import os
+import re
+
 import pytest
 
 import paper_1706_07191_amd as B
@@ -60,3 +63,17 @@ def test_no_tokens_have_any_of_the_gradients(loss):
         assert loss(True, **none, **out) == OK
         assert loss(True, **dict(none, tokens=-1), **out) == ARG
     assert loss(True, dH=None, dW=None) == ARG
+
+
+def test_inline_assembly_names_the_registers_that_it_writes():
+    """m0 holds where a load into LDS goes: a statement that writes it says so, as the compiler may have a value of its own there."""
+    csrc = os.path.join(os.path.dirname(B.__file__), "csrc")
+    found = 0
+    for name in sorted(os.listdir(csrc)):
+        if name.endswith((".hip", ".h")):
+            with open(os.path.join(csrc, name)) as f:
+                for statement in re.findall(r"asm(?: volatile)?\((?:[^;]|;(?!\n))*;\n", f.read()):
+                    if re.search(r"s_\w+ m0,", statement):
+                        found += 1
+                        assert re.search(r':\s*"memory",\s*"m0"\s*\)', statement), (name, statement)
+    assert found >= 2
