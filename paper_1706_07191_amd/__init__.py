@@ -431,10 +431,13 @@ def brsvd_small_svd_static(R, stream=None, out=None):
 
 
 # ---- a model's matrices: 8-bit products and losses over a large vocabulary -----------------------------------------
-# Looking torch up in every one of a call's helpers takes longer than what they do: the first call leaves it here.
+# Looking torch up in every one of a call's helpers takes longer than what they do: the first call leaves it here, and the number of
+# devices that the process sees.
 torch = None
+_devices = 0
 
-# Every call takes stream= (a torch stream or its address; default: torch's current stream), on which it runs and allocates.
+# Every call takes stream= (a torch stream of the operands' device or its address; default: torch's current stream there), on which it
+# runs and allocates.
 
 def _model_dtype(dtype, name, half=False):
     if dtype is torch.bfloat16:
@@ -463,26 +466,48 @@ def _rows(t, dtype, cols, name, rows=None):
     return t.data_ptr(), ld
 
 
-def _scope(stream):
+def _device_of(operands):
+    """Index of the one CUDA device that the tensors among the operands lie on, -1 where none does."""
+    index = -1
+    for t in operands:
+        if isinstance(t, torch.Tensor):
+            at = t.get_device()
+            if at >= 0 and at != index:
+                if index >= 0:
+                    raise TypeError(f"the operands must be on one device, not on cuda:{index} and cuda:{at}")
+                index = at
+    return index
+
+
+def _scope(stream, index):
     """Memory taken inside belongs to the stream that the call runs on: what a call frees at its end, or the caller later, is not handed out
     to work of another stream before the call is through with it."""
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    elif index >= 0 and stream.device_index != index:
+        raise ValueError(f"stream belongs to cuda:{stream.device_index}, the operands are on cuda:{index}")
     return torch.cuda.stream(stream)
 
 
 def _scoped(call):
-    """Runs a binding with `stream` as torch's current stream."""
+    """Runs a binding with the device of its operands as the current one, to which launches go, and `stream` as torch's current stream."""
     import functools
 
     @functools.wraps(call)
     def wrapped(*args, stream=None, **kw):
-        global torch
+        global torch, _devices
         if torch is None:
             import torch
+            _devices = torch.cuda.device_count()
+        index = -1
+        if _devices > 1:                   # with one device there is nothing to tell apart
+            index = _device_of((*args, *kw.values()))
+            if index >= 0 and index != torch.cuda.current_device():
+                with torch.cuda.device(index):
+                    return wrapped(*args, stream=stream, **kw)
         if stream is None:
             return call(*args, **kw)
-        with _scope(stream):
+        with _scope(stream, index):
             return call(*args, **kw)
     return wrapped
 

@@ -3,6 +3,7 @@ import os
 import re
 
 import pytest
+import torch
 
 import paper_1706_07191_amd as B
 from tests.test_model_ops_cpu import ARG, AT, BF16, BUDGET, F32, OK, gemm, linear, xent
@@ -77,3 +78,66 @@ def test_inline_assembly_names_the_registers_that_it_writes():
                         found += 1
                         assert re.search(r':\s*"memory",\s*"m0"\s*\)', statement), (name, statement)
     assert found >= 2
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor that says that it lies on a CUDA device."""
+    at = 0
+
+    is_cuda = True
+    device = property(lambda self: torch.device("cuda", self.at))
+
+    def get_device(self):
+        return self.at
+
+
+def on(index, *shape, dtype=torch.bfloat16):
+    t = torch.zeros(*shape, dtype=dtype).as_subclass(Elsewhere)
+    t.at = index
+    return t
+
+
+@pytest.fixture
+def two_devices(monkeypatch):
+    """Two devices, of which the first is current: what makes another current and when."""
+    monkeypatch.setattr(B, "torch", torch)
+    monkeypatch.setattr(B, "_devices", 2, raising=False)
+    now = [0]
+
+    class device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.index
+
+        def __exit__(self, *_):
+            now[0] = self.before
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    return now
+
+
+def test_operands_on_several_devices_are_refused(two_devices):
+    H, W, y = on(0, 4, 8), on(1, 6, 8), on(0, 4, dtype=torch.int64)
+    q, s = on(1, 4, 16, dtype=torch.float8_e4m3fn), on(0, 4, 1, dtype=torch.float32)
+    for call in (lambda: B.brsvd_xent_forward(H, W, y), lambda: B.brsvd_xent_forward(H=H, labels=on(1, 4, dtype=torch.int64), W=on(0, 6, 8)),
+                 lambda: B.brsvd_dequantize_e4m3(q, s), lambda: B.brsvd_gemm_e4m3(q, s, q, s, block_rows=1),
+                 lambda: B.brsvd_linear_e4m3(H, W, s), lambda: B.brsvd_gemm_e4m3(q, on(1, 4, 1, dtype=torch.float32), q, on(1, 4, 1, dtype=torch.float32), out=on(0, 4, 4))):
+        with pytest.raises(TypeError, match="one device"):
+            call()
+
+
+def test_calls_run_with_the_operands_device_current(two_devices):
+    seen = []
+    call = B._scoped(lambda X, block_rows=1: seen.append(two_devices[0]))
+    call(on(1, 2, 2))
+    call(X=on(1, 2, 2), block_rows=128)
+    call(on(0, 2, 2))
+    assert seen == [1, 1, 0] and two_devices == [0]
+
+    class stream:
+        device_index = 0
+    with pytest.raises(ValueError, match="stream"):
+        call(on(1, 2, 2), stream=stream())
+    assert seen == [1, 1, 0] and two_devices == [0]
