@@ -670,7 +670,7 @@ extern "C" int brsvd_linear_e4m3(const void* X, int64_t ldx, int32_t dtype, cons
   if (!product_sizes(m, n, k) || !product_type(dtype)) return BRSVD_ERR_ARG;
   if (m == 0 || n == 0 || k == 0) return brsvd_gemm_e4m3(nullptr, 0, nullptr, nullptr, 0, nullptr, kBlock, m, n, 0, dtype, Y, ldy, nullptr, 0, stream);
   const int eb = dtype == BRSVD_DTYPE_F32 ? 4 : 2;
-  if (!X || !W || !SW || !Y || ldx < k || ldw < k || ldy < n || ldx * eb >= kMaxPitch * 4 || ldw >= kMaxPitch) return BRSVD_ERR_ARG;
+  if (!X || !W || !SW || !Y || ldx < k || ldw < k || ldy < n || ldx >= kMaxPitch * 4 / eb || ldw >= kMaxPitch) return BRSVD_ERR_ARG;
   const E4m3Plan p = e4m3_plan(m, n, k, false, dtype);
   if (!e4m3_plan_fits(p, m, n, aligned_pieces(W, ldw), dtype)) return BRSVD_ERR_ARG;      // the cast of X lies at such addresses
   const uint64_t parts = split_bytes(p, m, n), need = parts + (m <= kCastRows ? 0 : cast_bytes(m, k));

@@ -404,7 +404,9 @@ extern "C" int brsvd_quantize_e4m3(const void* X, int64_t ldx, int64_t rows, int
                                    float* S, uint8_t* Qt, int64_t ldqt, float* St, void* stream) {
   if (rows < 0 || cols < 0 || !model_type(dtype) || (block_rows != 1 && block_rows != kBlock)) return BRSVD_ERR_ARG;
   if (rows == 0 || cols == 0) return BRSVD_OK;
-  if (!X || (!Q && !Qt) || ldx < cols || (Q && (!S || ldq < cols)) || (Qt && (!St || ldqt < rows)) || cols > kMaxGrid * kBlock || rows > (kMaxGrid << 2) / ceil_div(cols, kBlock)) return BRSVD_ERR_ARG;
+  if (!X || (!Q && !Qt) || ldx < cols || (Q && (!S || ldq < cols)) || (Qt && (!St || ldqt < rows)) || ldx > INT64_MAX / 4 || cols > kMaxGrid * kBlock ||
+      rows > (kMaxGrid << 2) / ceil_div(cols, kBlock))
+    return BRSVD_ERR_ARG;
   return quantize(X, ldx, rows, cols, dtype, block_rows, Q, ldq, S, Qt, ldqt, St, (hipStream_t)stream);
 }
 
@@ -412,7 +414,9 @@ extern "C" int brsvd_dequantize_e4m3(const uint8_t* Q, int64_t ldq, const float*
                                      int64_t ldx, void* stream) {
   if (rows < 0 || cols < 0 || !model_type(dtype) || (block_rows != 1 && block_rows != kBlock)) return BRSVD_ERR_ARG;
   if (rows == 0 || cols == 0) return BRSVD_OK;
-  if (!Q || !S || !X || ldq < cols || ldx < cols || cols > kMaxGrid * kBlock || rows > (kMaxGrid << 2) / ceil_div(cols, kBlock)) return BRSVD_ERR_ARG;
+  if (!Q || !S || !X || ldq < cols || ldx < cols || ldx > INT64_MAX / 4 || cols > kMaxGrid * kBlock ||
+      rows > (kMaxGrid << 2) / ceil_div(cols, kBlock))
+    return BRSVD_ERR_ARG;
   const int64_t pitch = ldx * (dtype == BRSVD_DTYPE_F32 ? 4 : 2);
   in_launches(ceil_div(cols, kBlock) * ceil_div(rows, dtype == BRSVD_DTYPE_F32 ? 32 : 64), 256, [&](unsigned first, dim3 grid) {
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, Q, ldq, S, rows, cols, block_rows, (char*)X, pitch, first); };

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_1706_07191_amd as B
-from tests.test_model_ops_cpu import ARG, AT, BF16, BUDGET, F32, OK, gemm, linear, xent
+from tests.test_model_ops_cpu import ARG, AT, BF16, BUDGET, F32, OK, dequantize, gemm, linear, quantize, xent
 
 LAUNCH = 2 ** 32               # threads that a launch has fewer of along a direction
 
@@ -141,3 +141,12 @@ def test_calls_run_with_the_operands_device_current(two_devices):
     with pytest.raises(ValueError, match="stream"):
         call(on(1, 2, 2), stream=stream())
     assert seen == [1, 1, 0] and two_devices == [0]
+
+
+@pytest.mark.parametrize("ld", [2 ** 61, 2 ** 62, 2 ** 63 - 1])
+def test_leading_dimensions_whose_bytes_are_no_64_bit_number(ld):
+    for dtype in (F32, BF16):
+        if ld * (4 if dtype == F32 else 2) >= 2 ** 63:
+            for m in (8, 100):
+                assert linear(dtype=dtype, ldx=ld, m=m) == ARG
+            assert quantize(dtype=dtype, ldx=ld) == ARG and dequantize(dtype=dtype, ldx=ld) == ARG
