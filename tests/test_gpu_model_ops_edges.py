@@ -6,7 +6,7 @@ import torch
 
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
-from tests.test_gpu_e4m3 import codes, randn
+from tests.test_gpu_e4m3 import cast_by_definition, codes, placed, randn
 from tests.test_gpu_head import FINEST, HALF, ROUND, Reference, problem, teacher_reference
 
 pytestmark = pytest.mark.gpu
@@ -253,3 +253,21 @@ def test_fp16_gradients_of_factors_that_differ_by_orders_of_magnitude():
     want = G @ ref.w
     bound = off @ ref.w.abs() + (G.abs() + off) @ ref.w.abs() * 2.0 ** -23 * (vocab + 70)
     ref.check("dH", dH, want, bound + u * (want.abs() + bound) + FINEST[torch.float16])
+
+
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cols,pad,shift", [(1, 1, 0, 0), (3, 127, 1, 0), (128, 128, 0, 0), (129, 257, 0, 1), (260, 8, 8, 0)])
+def test_cast_of_the_transpose_alone(rows, cols, pad, shift, dtype, block):
+    """Q and S may be left out: Qt and St are the cast of X^T, and nothing beside them is written."""
+    dev = need_gpu()
+    X = placed(randn(rows * 1000 + cols, rows, cols), dtype, dev, pad, shift)
+    qt = torch.full((cols, rows + 3), 99, dtype=torch.uint8, device=dev)
+    st = torch.full((cols + 1 if block == 1 else -(-cols // 128) + 1, -(-rows // 128)), 9.0, device=dev)
+    kind = {torch.float32: B.BRSVD_DTYPE_F32, torch.bfloat16: B.BRSVD_DTYPE_BF16, torch.float16: B.BRSVD_DTYPE_F16}[dtype]
+    status = B.lib().brsvd_quantize_e4m3(X.data_ptr(), cols + pad, rows, cols, kind, block, None, 0, None, qt.data_ptr(), rows + 3, st.data_ptr(),
+                                         torch.cuda.current_stream().cuda_stream or None)
+    torch.cuda.synchronize()
+    q, s = cast_by_definition(X.double().cpu().t().contiguous(), block)
+    assert status == B.BRSVD_OK and torch.equal(codes(qt[:, :rows].view(torch.float8_e4m3fn)), q) and torch.equal(st[:-1].double().cpu(), s)
+    assert bool((qt[:, rows:] == 99).all() and (st[-1] == 9).all())
