@@ -544,7 +544,7 @@ def brsvd_quantize_e4m3(X, block_rows=1, transpose=False):
     dev = X.device
 
     def result(r, c):
-        return _eight_bit(r, c, dev), torch.empty(r if block_rows == 1 else -(-r // 128), -(-c // 128), device=dev)
+        return _eight_bit(r, c, dev), torch.empty(r if block_rows == 1 else -(-r // 128), -(-c // 128), dtype=torch.float32, device=dev)
     Q, S = result(rows, cols)
     Qt, St = result(cols, rows) if transpose else (None, None)
     _check(lib().brsvd_quantize_e4m3(x, ldx, rows, cols, dt, block_rows, Q.data_ptr(), Q.stride(0), S.data_ptr(),
@@ -656,7 +656,7 @@ def brsvd_xent_forward(H, W, labels):
     logits: returns (loss, lse), fp32.  labels: int64, one outside [0, vocab) marks a token that does not count (loss 0)."""
     ops, sizes, dt = _head(H, W)
     y = _vector(labels, torch.int64, sizes[0], "labels")
-    loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
+    loss, lse = torch.empty(2, sizes[0], dtype=torch.float32, device=H.device).unbind(0)
     ws, nbytes = _head_workspace(sizes, 0, 0, 0, H.device)
     _check(lib().brsvd_xent_forward(*ops, y, *sizes, dt, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes,
                                     _current(H.device)), "brsvd_xent_forward")
@@ -699,8 +699,8 @@ def brsvd_distill_forward(H, W, ids, logits, temperature=1.0):
     does not count.  Returns (loss, lse, z), fp32: z (tokens, top) holds the student's logits of those words."""
     ops, sizes, dt = _head(H, W)
     te = _teacher(ids, logits, sizes[0])
-    loss, lse = torch.empty(2, sizes[0], device=H.device).unbind(0)
-    z = torch.empty(ids.shape, device=H.device)
+    loss, lse = torch.empty(2, sizes[0], dtype=torch.float32, device=H.device).unbind(0)
+    z = torch.empty(ids.shape, dtype=torch.float32, device=H.device)
     ws, nbytes = _head_workspace(sizes, 0, te[2], 0, H.device)
     _check(lib().brsvd_distill_forward(*ops, *te, temperature, *sizes, dt, loss.data_ptr(), lse.data_ptr(), z.data_ptr(),
                                        ws.data_ptr(), nbytes, _current(H.device)), "brsvd_distill_forward")

@@ -271,3 +271,26 @@ def test_cast_of_the_transpose_alone(rows, cols, pad, shift, dtype, block):
     q, s = cast_by_definition(X.double().cpu().t().contiguous(), block)
     assert status == B.BRSVD_OK and torch.equal(codes(qt[:, :rows].view(torch.float8_e4m3fn)), q) and torch.equal(st[:-1].double().cpu(), s)
     assert bool((qt[:, rows:] == 99).all() and (st[-1] == 9).all())
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+def test_same_bits_whatever_torchs_default_type(default):
+    dev = need_gpu()
+    H, W, y, g = problem(70, 500, 40, torch.bfloat16, dev)
+    ids, a = torch.randint(0, 500, (70, 3), generator=g).to(dev), torch.randn(70, 3, generator=g).to(dev)
+    grad = torch.ones(70, device=dev)
+
+    def all_calls():
+        Q, S, Qt, St = B.brsvd_quantize_e4m3(H, transpose=True)
+        loss, lse = B.brsvd_xent_forward(H, W, y.to(dev))
+        distilled = B.brsvd_distill_forward(H, W, ids, a, 2.0)
+        q, s = B.brsvd_quantize_e4m3(W, block_rows=128)
+        return (codes(Q), S, codes(Qt), St, loss, lse, *B.brsvd_xent_backward(H, W, y.to(dev), lse, grad), *distilled,
+                *B.brsvd_distill_backward(H, W, ids, a, 2.0, distilled[1], distilled[2], grad), B.brsvd_dequantize_e4m3(Q, S), B.brsvd_linear_e4m3(H, q, s))
+    want = all_calls()
+    torch.set_default_dtype(default)
+    try:
+        got = all_calls()
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert all(x.dtype == w.dtype and torch.equal(x, w) for x, w in zip(got, want))

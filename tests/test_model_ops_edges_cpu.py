@@ -150,3 +150,29 @@ def test_leading_dimensions_whose_bytes_are_no_64_bit_number(ld):
             for m in (8, 100):
                 assert linear(dtype=dtype, ldx=ld, m=m) == ARG
             assert quantize(dtype=dtype, ldx=ld) == ARG and dequantize(dtype=dtype, ldx=ld) == ARG
+
+
+class NoLibrary:
+    """In the library's place: every call succeeds, every size is a few KiB."""
+
+    def __getattr__(self, name):
+        return lambda *a: 4096 if name.endswith("_bytes") else 0
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_results_are_fp32_whatever_torchs_default_type(default, monkeypatch):
+    """A model's code may set the default to 16 bits: memory that the library writes fp32 into must not become half as large."""
+    monkeypatch.setattr(B, "torch", torch)
+    monkeypatch.setattr(B, "lib", NoLibrary)
+    monkeypatch.setattr(B, "_current", lambda device: None)
+    for name in ("empty", "empty_strided"):
+        monkeypatch.setattr(torch, name, lambda *a, real=getattr(torch, name), device=None, **kw: real(*a, **kw))
+    H, W, y = on(0, 4, 8), on(0, 6, 8), on(0, 4, dtype=torch.int64)
+    ids, a = on(0, 4, 3, dtype=torch.int64), on(0, 4, 3, dtype=torch.float32)
+    torch.set_default_dtype(default)
+    try:
+        Q, S, Qt, St = B.brsvd_quantize_e4m3(H, transpose=True)
+        fp32 = [S, St, *B.brsvd_xent_forward(H, W, y), *B.brsvd_distill_forward(H, W, ids, a), B.brsvd_dequantize_e4m3(on(0, 4, 16, dtype=torch.float8_e4m3fn), a[:, :1].contiguous())]
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert [t.dtype for t in fp32] == [torch.float32] * 8
