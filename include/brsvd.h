@@ -268,11 +268,11 @@ int brsvd_dequantize_e4m3(const uint8_t* Q, int64_t ldq, const float* S, int64_t
 
 /* C (m x n, dtype F32, BF16 or F16) = A B^T with A m x k and B n x k in 8 bits; SA has a scale per row
  * and block of A, SB per row (block_rows = 1) or 128 rows (block_rows = 128) and block of B.  Scales are
- * any fp32 numbers, they need not come from brsvd_quantize_e4m3.  Products of a block are added, then
- * scaled and added to those of the other blocks in fp32; C is rounded once.  With an fp32 C all sums are
- * those of exact products in fp32.  Otherwise the 8-bit matrix cores add the products of a block: of eight
- * neighbouring products they drop what is below 2^-13 of the largest one's power of two, parts of 1e-5 of
- * the sum of |products|.
+ * any fp32 numbers, they need not come from brsvd_quantize_e4m3; the product of two is formed in fp32.
+ * Products of a block are added, then scaled and added to those of the other blocks in fp32; C is rounded
+ * once.  With an fp32 C all sums are those of exact products in fp32.  Otherwise the 8-bit matrix cores
+ * add the products of a block: of eight neighbouring products they drop what is below 2^-13 of the largest
+ * one's power of two, up to 2e-5 of the sum of |products| over a thousand.
  * The three products of a linear layer Y = X W^T with weights W: Y from X and W (block_rows 128), dX from
  * dY and W^T (128), dW from dY^T and X^T (1), each operand cast along the contraction. */
 int brsvd_gemm_e4m3(const uint8_t* A, int64_t lda, const float* SA, const uint8_t* B, int64_t ldb,
@@ -291,7 +291,8 @@ uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_
 /* Softmax cross entropy of z = H W^T (H tokens x dim hidden states, W vocab x dim output matrix, both of
  * dtype BF16 or F16), per token, without keeping z:
  *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_{t, labels_t}
- * A label outside [0, vocab) marks a token that does not count: its loss is 0.  loss, lse: fp32.
+ * vocab and dim are at least 1.  A label outside [0, vocab) marks a token that does not count: its loss
+ * is 0.  loss, lse: fp32.
  * Backward, for the gradient of sum_t grad_t loss_t, from the lse of the forward call:
  *   G_tv = grad_t (exp(z_tv - lse_t) - [v = labels_t]),   dH = G W,   dW = G^T H      (of dtype)
  * Rows of dH of tokens that do not count are 0, and what stands in those rows of H reaches nothing, NaN
@@ -315,10 +316,10 @@ int brsvd_xent_backward(const void* H, int64_t ldh, const void* W, int64_t ldw, 
  *   q_t = softmax(logits_t / tau) over the listed entries,  lse_t = log sum_v exp(z_tv / tau)
  *   loss_t = tau^2 sum_j q_tj (log q_tj - z_{t, ids_tj} / tau + lse_t)
  *   G_tv = grad_t tau (exp(z_tv / tau - lse_t) - sum over j with ids_tj = v of q_tj)
- * ids, logits (fp32): tokens x top, dense.  An entry with an id outside [0, vocab) or a logit of -inf or
- * NaN is not listed; a token with nothing listed does not count.  z (fp32, tokens x top, OUT of the
- * forward and input of the backward call): z_{t, ids_tj}, 0 where not listed.  The rest as above, with
- * `top` in brsvd_head_workspace_bytes. */
+ * ids, logits (fp32): tokens x top, dense, top at least 1.  An entry with an id outside [0, vocab) or a
+ * logit of -inf or NaN is not listed; a token with nothing listed does not count.  z (fp32, tokens x top,
+ * OUT of the forward and input of the backward call): z_{t, ids_tj}, 0 where not listed.  The rest as
+ * above, with `top` in brsvd_head_workspace_bytes. */
 int brsvd_distill_forward(const void* H, int64_t ldh, const void* W, int64_t ldw, const int64_t* ids,
                           const float* logits, int32_t top, float temperature, int64_t tokens,
                           int64_t vocab, int64_t dim, int32_t dtype, float* loss, float* lse, float* z,

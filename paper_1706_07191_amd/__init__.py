@@ -437,7 +437,8 @@ torch = None
 _devices = 0
 
 # Every call takes stream= (a torch stream of the operands' device or its address; default: torch's current stream there), on which it
-# runs and allocates.
+# runs and allocates; operands have to stay until that stream has passed the call, and out= must not overlap them.  Results carry no
+# autograd graph, whatever an operand's requires_grad says: gradients are what the *_backward calls return.
 
 def _model_dtype(dtype, name, half=False):
     if dtype is torch.bfloat16:
@@ -653,7 +654,8 @@ def _head_workspace(sizes, piece, top, backward, device):
 @_scoped
 def brsvd_xent_forward(H, W, labels):
     """Softmax cross entropy of the logits H W^T (H (tokens, dim), W (vocab, dim), bf16 or fp16) per token, without the
-    logits: returns (loss, lse), fp32.  labels: int64, one outside [0, vocab) marks a token that does not count (loss 0)."""
+    logits: returns (loss, lse), fp32.  labels: int64, one outside [0, vocab) marks a token that does not count (loss 0).
+    No autograd graph: brsvd_xent_backward gives the gradients."""
     ops, sizes, dt = _head(H, W)
     y = _vector(labels, torch.int64, sizes[0], "labels")
     loss, lse = torch.empty(2, sizes[0], dtype=torch.float32, device=H.device).unbind(0)
@@ -696,7 +698,8 @@ def _teacher(ids, logits, tokens):
 def brsvd_distill_forward(H, W, ids, logits, temperature=1.0):
     """tau^2 KL(q || p) per token of the student's p = softmax(H W^T / tau) against the teacher's q, the softmax of its `top`
     kept logits / tau: ids int64, logits fp32, both (tokens, top); an entry with an id outside [0, vocab) or a logit of -inf
-    does not count.  Returns (loss, lse, z), fp32: z (tokens, top) holds the student's logits of those words."""
+    does not count.  Returns (loss, lse, z), fp32: z (tokens, top) holds the student's logits of those words.  No autograd
+    graph: brsvd_distill_backward gives the gradients."""
     ops, sizes, dt = _head(H, W)
     te = _teacher(ids, logits, sizes[0])
     loss, lse = torch.empty(2, sizes[0], dtype=torch.float32, device=H.device).unbind(0)

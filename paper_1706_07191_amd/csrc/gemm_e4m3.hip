@@ -54,7 +54,8 @@ __device__ __forceinline__ bool is_power(float x) {
 // times half of the tile columns, NQ instructions.  Two tile rows are read from LDS two groups before they are multiplied; a half of A's fragments is
 // replaced as soon as its last group is issued.  So a step needs no registers for the next one beside its own, and still no wave comes from
 // the barrier (before the last two groups) with nothing to multiply.  The step after next is sent for in parts from the barrier on, see TileProduct,
-// three a group: 8192 x 8192 x 8192 452 / 442 / 427 / 438 us with one / two / three / four (427: 2.58 Pflop/s, bound by the matrix cores and what feeds them).
+// three a group: 8192 x 8192 x 8192 452 / 442 / 427 / 438 us with one / two / three / four on one card; 437 to 452 on others (2.43 to 2.58 Pflop/s, bound by the matrix cores and what
+// feeds them: busy in 61 % of the cycles; a library product with one scale for all runs at 3.19).
 // As long as a wave's scales of a step are powers of two, as those of the casts are, the instruction multiplies by them and adds to the sums; from the
 // first step where they are not (and WIDE) the results of a group are scaled and added between the instructions of the next.
 template <int NQ, bool PER_ROW, bool DIRECT, bool WIDE>

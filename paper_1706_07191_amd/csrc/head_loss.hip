@@ -538,7 +538,7 @@ k_head_dh(const HeadProduct g) {
 }
 
 // dW = G^T H of a piece: both operands hold the tokens in their rows.  100000 x 4096 over 8192 5.2 ms (1.30 Pflop/s); with few tokens bound by the writing of dW and
-// the reading of G, which a round of tiles does at the same time: 50001 x 1000 over 999 148 us.
+// the reading of G, which a round of tiles does at the same time: 50001 x 1000 over 999 128 us.
 template <class El, int BQ>
 __global__ void __launch_bounds__(kTileThreads, 2)
 k_head_dw(const HeadProduct g) {
