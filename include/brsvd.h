@@ -288,6 +288,33 @@ int brsvd_linear_e4m3(const void* X, int64_t ldx, int32_t dtype, const uint8_t* 
                       void* scratch, uint64_t scratch_bytes, void* stream);
 uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t dtype);
 
+/* Numbers of 4 bits: e2m1 (OCP: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives; no infinities, no NaN), two in a byte, the
+ * first in its lower half, with a scale for each 32 neighbouring numbers of a row, the group at a row's end smaller.  A scale is
+ * a byte b (e8m0) for 2^(b - 127), 255 for NaN.  Q: rows of ceil(cols/2) bytes, leading dimension in bytes; S: rows x
+ * ceil(cols/32), dense.  Behind a row's last number the upper half of a byte is no part of it: written as zero, never read as a number.
+ *
+ * brsvd_quantize_e2m1: Q = round(X / S), S the least power of two >= 2^-126 for which no number of the group exceeds 6 S (1 for a
+ * group of zeros), to nearest, ties to an even code.  A group with an infinity or a NaN gets the scale NaN.  X: rows x cols of
+ * dtype BRSVD_DTYPE_F32, _BF16 or _F16.
+ * brsvd_dequantize_e2m1: X = Q S, rounded to dtype (a group of scale NaN: NaN). */
+int brsvd_quantize_e2m1(const void* X, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype, uint8_t* Q,
+                        int64_t ldq, uint8_t* S, void* stream);
+int brsvd_dequantize_e2m1(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64_t rows, int64_t cols,
+                          int32_t dtype, void* X, int64_t ldx, void* stream);
+
+/* Y (m x n) = X W^T with X m x k of dtype BF16 or F16 (Y has the same type) and W n x k in 4 bits, as brsvd_quantize_e2m1
+ * lays it out; and the gradient of X, dX (m x k) = dY W.  X is taken as it is.  A number of W times its scale is taken in X's type, as
+ * brsvd_dequantize_e2m1 rounds it: nothing is lost with BF16 from 2^-133 on and with F16 from 2^-24 on.  Products are exact, sums are fp32, the
+ * result is rounded once.  Scales are any bytes.
+ * scratch: brsvd_linear_e2m1_scratch_bytes (0 where none is needed) of the same sizes. */
+int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW,
+                      int64_t m, int64_t n, int64_t k, void* Y, int64_t ldy, void* scratch,
+                      uint64_t scratch_bytes, void* stream);
+int brsvd_linear_e2m1_backward(const void* dY, int64_t lddy, int32_t dtype, const uint8_t* W, int64_t ldw,
+                               const uint8_t* SW, int64_t m, int64_t n, int64_t k, void* dX, int64_t lddx,
+                               void* scratch, uint64_t scratch_bytes, void* stream);
+uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t backward);
+
 /* Softmax cross entropy of z = H W^T (H tokens x dim hidden states, W vocab x dim output matrix, both of
  * dtype BF16 or F16), per token, without keeping z:
  *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_{t, labels_t}

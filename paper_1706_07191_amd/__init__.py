@@ -66,7 +66,8 @@ EXPORTS = ["brsvd_workspace_bytes", "brsvd_create", "brsvd_run", "brsvd_run_f64"
            "brsvd_rpca_ialm_tol", "brsvd_rpca_ialm_tol_f64", "brsvd_norm2_power", "brsvd_norm2_power_f64",
            "brsvd_run_alg2", "brsvd_run_alg2_f64", "brsvd_philox_normal", "brsvd_philox_normal_f64",
            "brsvd_quantize_e4m3", "brsvd_dequantize_e4m3", "brsvd_gemm_e4m3", "brsvd_gemm_e4m3_scratch_bytes",
-           "brsvd_linear_e4m3", "brsvd_linear_e4m3_scratch_bytes", "brsvd_xent_forward", "brsvd_xent_backward",
+           "brsvd_linear_e4m3", "brsvd_linear_e4m3_scratch_bytes", "brsvd_quantize_e2m1", "brsvd_dequantize_e2m1",
+           "brsvd_linear_e2m1", "brsvd_linear_e2m1_backward", "brsvd_linear_e2m1_scratch_bytes", "brsvd_xent_forward", "brsvd_xent_backward",
            "brsvd_distill_forward", "brsvd_distill_backward", "brsvd_head_workspace_bytes",
            "brsvd_destroy", "brsvd_status_string"]
 STEP_EXPORTS = ["brsvd_gemm_an", "brsvd_gemm_at", "brsvd_gemm_scratch_bytes", "brsvd_gemm_an_f64",
@@ -133,6 +134,11 @@ def lib() -> C.CDLL:
     L.brsvd_gemm_e4m3_scratch_bytes.argtypes = [i64, i64, i64, i32, i32]
     L.brsvd_linear_e4m3.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp, i64, vp, u64, vp]
     L.brsvd_linear_e4m3_scratch_bytes.argtypes = [i64, i64, i64, i32]
+    L.brsvd_quantize_e2m1.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+    L.brsvd_dequantize_e2m1.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, vp]
+    L.brsvd_linear_e2m1.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp, i64, vp, u64, vp]
+    L.brsvd_linear_e2m1_backward.argtypes = L.brsvd_linear_e2m1.argtypes
+    L.brsvd_linear_e2m1_scratch_bytes.argtypes = [i64, i64, i64, i32]
     L.brsvd_xent_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i32, vp, vp, vp, u64, vp]
     L.brsvd_xent_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, i32, vp, i64, vp, i64, vp, u64, vp]
     L.brsvd_distill_forward.argtypes = [vp, i64, vp, i64, vp, vp, i32, flt, i64, i64, i64, i32, vp, vp, vp, vp, u64, vp]
@@ -141,7 +147,7 @@ def lib() -> C.CDLL:
     L.brsvd_head_workspace_bytes.argtypes = [i64, i64, i64, i64, i32, i32]
     sizes = ("brsvd_gemm_scratch_bytes", "brsvd_gemm_scratch_bytes_f64", "brsvd_orth_scratch_bytes",
              "brsvd_small_svd_scratch_bytes", "brsvd_gemm_e4m3_scratch_bytes", "brsvd_linear_e4m3_scratch_bytes",
-             "brsvd_head_workspace_bytes")
+             "brsvd_linear_e2m1_scratch_bytes", "brsvd_head_workspace_bytes")
     for name in EXPORTS + STEP_EXPORTS:
         if name in sizes:
             getattr(L, name).restype = u64
@@ -616,6 +622,83 @@ def brsvd_linear_e4m3(X, W, SW, out=None):
     _check(lib().brsvd_linear_e4m3(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes,
                                    _current(X.device)), "brsvd_linear_e4m3")
     return Y
+
+
+def _four_bit(W, S, cols, name, scales):
+    """Address and leading dimension of a matrix in 4 bits with `cols` numbers a row, and the address of its scales."""
+    w, ldw = _rows(W, torch.float4_e2m1fn_x2, (cols + 1) // 2, name)
+    shape = (W.shape[0], -(-cols // 32))
+    if S.shape != shape:
+        raise TypeError(f"{scales} has shape {tuple(S.shape)}, expected {shape}")
+    return w, ldw, _dev(S, torch.float8_e8m0fnu, scales)
+
+
+def _columns(Q, cols):
+    """Numbers of a row: two for each byte, or one less where cols says so."""
+    if cols is None:
+        return 2 * Q.shape[1]
+    if not isinstance(cols, int) or (cols + 1) // 2 != Q.shape[1]:
+        raise ValueError(f"cols must be {max(2 * Q.shape[1] - 1, 0)} or {2 * Q.shape[1]} for rows of {Q.shape[1]} bytes, not {cols}")
+    return cols
+
+
+@_scoped
+def brsvd_quantize_e2m1(X):
+    """X (rows, cols) CUDA, fp32, bf16 or fp16, as e2m1 numbers Q (float4_e2m1fn_x2, (rows, ceil(cols/2)): two in a byte, the first in its
+    lower half; rows 16- or 128-byte aligned) and power-of-two scales S (float8_e8m0fnu), one for each 32 numbers of a row.  A group with an
+    infinity or a NaN becomes NaN.  Returns (Q, S)."""
+    dt = _model_dtype(X.dtype, "X")
+    x, ldx = _rows(X, X.dtype, None, "X")
+    rows, cols = X.shape
+    width = (cols + 1) // 2
+    whole = 16 if width < 1024 else 128
+    Q = torch.empty_strided((rows, width), (-(-width // whole) * whole, 1), dtype=torch.float4_e2m1fn_x2, device=X.device)
+    S = torch.empty(rows, -(-cols // 32), dtype=torch.float8_e8m0fnu, device=X.device)
+    _check(lib().brsvd_quantize_e2m1(x, ldx, rows, cols, dt, Q.data_ptr(), Q.stride(0), S.data_ptr(), _current(X.device)), "brsvd_quantize_e2m1")
+    return Q, S
+
+
+@_scoped
+def brsvd_dequantize_e2m1(Q, S, cols=None, dtype=None):
+    """What Q with its scales stands for, as fp32 (or bf16, fp16: dtype).  cols: numbers of a row where they are odd."""
+    dtype = dtype or torch.float32
+    dt = _model_dtype(dtype, "the result")
+    cols = _columns(Q, cols)
+    q, ldq, s = _four_bit(Q, S, cols, "Q", "S")
+    X = torch.empty(Q.shape[0], cols, dtype=dtype, device=Q.device)
+    _check(lib().brsvd_dequantize_e2m1(q, ldq, s, Q.shape[0], cols, dt, X.data_ptr(), max(cols, 1), _current(Q.device)), "brsvd_dequantize_e2m1")
+    return X
+
+
+def _linear_e2m1(name, X, x_name, W, SW, k, backward, out):
+    dt = _model_dtype(X.dtype, x_name, half=True)
+    w, ldw, sw = _four_bit(W, SW, k, "W", "SW")
+    n = W.shape[0]
+    x, ldx = _rows(X, X.dtype, n if backward else k, x_name)
+    m, width = X.shape[0], k if backward else n
+    if out is None:
+        Y = torch.empty(m, width, dtype=X.dtype, device=X.device)
+        y, ldy = Y.data_ptr(), width or 1
+    else:
+        Y = out
+        y, ldy = _rows(Y, X.dtype, width, "out", m)
+    L = lib()
+    nbytes = L.brsvd_linear_e2m1_scratch_bytes(m, n, k, backward)
+    scr = _byte_scratch(nbytes, X.device) if nbytes else None
+    _check(getattr(L, name)(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes, _current(X.device)), name)
+    return Y
+
+
+@_scoped
+def brsvd_linear_e2m1(X, W, SW, out=None):
+    """X W^T: X (m, k) bf16 or fp16, W (n, k) in 4 bits with a scale for each 32 numbers of a row (brsvd_quantize_e2m1).  The result has X's type."""
+    return _linear_e2m1("brsvd_linear_e2m1", X, "X", W, SW, X.shape[1] if X.dim() == 2 else 0, 0, out)
+
+
+@_scoped
+def brsvd_linear_e2m1_backward(dY, W, SW, cols=None, out=None):
+    """The gradient dY W of brsvd_linear_e2m1's X from dY (m, n), the gradient of its result.  cols: numbers of a row of W where they are odd."""
+    return _linear_e2m1("brsvd_linear_e2m1_backward", dY, "dY", W, SW, _columns(W, cols), 1, out)
 
 
 def _head(H, W):

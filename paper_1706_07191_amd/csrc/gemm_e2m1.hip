@@ -1,0 +1,281 @@
+// Products with a matrix W (n x k) in 4 bits with a scale for each 32 numbers of a row, and 16-bit activations:
+//   Y = X W^T (X m x k),    dX = dY W (dY m x n)
+// A number of W times its scale is a number of the activations' type (bf16 holds every one, fp16 those from 2^-24 to 65504), so the 16-bit matrix cores multiply
+// exactly and add in fp32; Y is rounded once.  The conversion takes the scale with it: two numbers an instruction.  W is the instruction's first operand, a
+// lane has four neighbouring columns of Y for one row of X.
+//
+// k_rows_e2m1: for few rows of X, bound by the read of W.  k_tiles_e2m1: for many, bound by the matrix cores; W's numbers are made on their way into LDS.
+#include "e2m1.h"
+
+namespace brsvd {
+
+struct E2m1Args {
+  E2m1Operand W;
+  Operand X;               // rows: m; pitch in bytes
+  int64_t k;               // of the contraction
+  int64_t per_split;
+  void* C;                 // rows of ldc numbers of the activations' type; with splits: [split][m][cols] fp32
+  int64_t ldc, cols;
+  int splits;
+  int64_t tiles_p, tiles_q, first;     // tiles along W and along X; column that the first tile begins with
+};
+
+// Up to 16 MT rows of X.  The WAVES waves of a workgroup share 16 NT rows of W and take chunks of 128 numbers of the contraction in turn; their sums are added
+// through LDS in wave order.  A lane has one group of a chunk, 16 bytes, and with it its scale; the same 32 numbers of a row of X, which all workgroups read and the
+// caches hold: any order of the contraction that both sides share will do.  The U chunks that a wave takes next are on their way.
+template <class El, int MT, int NT, int U, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
+k_rows_e2m1(const E2m1Args g) {
+  constexpr int kChunk = 4 * kGroup;
+  __shared__ floatx4 parts[WAVES][MT * NT][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, group = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16 * NT;
+  floatx4 acc[MT][NT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int u = 0; u < NT; ++u) acc[t][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const uint8_t *rw[NT], *rs[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    const int64_t n = n0 + 16 * u + row, in = n < g.W.n ? n : g.W.n - 1;
+    rw[u] = g.W.base + in * g.W.ld + 16 * group;
+    rs[u] = g.W.scales + in * g.W.groups + group;
+  }
+  const char* rx[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int64_t m = 16 * t + row < g.X.n ? 16 * t + row : g.X.n - 1;
+    rx[t] = g.X.base + m * g.X.ld + 64 * group;
+  }
+  struct Chunk {
+    uint4 w[NT], x[MT][4];
+    uint32_t s[NT];
+  };
+  auto fetch = [&](Chunk& c, int at, bool whole, int64_t left) {       // left: numbers of the row from this lane's group on
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left);
+      c.s[u] = whole || left > 0 ? rs[u][(int64_t)at * 4] : 127;
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c.x[t][j] = piece_of<2>(rx[t] + (int64_t)at * 256 + 16 * j, whole ? 16 : 2 * (left - 8 * j));
+  };
+  auto multiply = [&](const Chunk& c) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      const float scale = scale_e8m0(c.s[u]);
+      const uint32_t w[4] = {c.w[u].x, c.w[u].y, c.w[u].z, c.w[u].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int4v p = __builtin_bit_cast(int4v, eight_e2m1<El>(w[j], scale));
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t][u] = mfma16<El>(p, __builtin_bit_cast(int4v, c.x[t][j]), acc[t][u]);
+      }
+    }
+  };
+  const int whole = (int)(g.k / kChunk);
+  Chunk c[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if (wave + WAVES * i < whole) fetch(c[i], wave + WAVES * i, true, 0);
+  for (int b = wave; b < whole; b += WAVES * U) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (b + WAVES * i < whole) multiply(c[i]);
+      if (b + WAVES * (i + U) < whole) fetch(c[i], b + WAVES * (i + U), true, 0);
+    }
+  }
+  if (g.k % kChunk != 0 && whole % WAVES == wave) {          // the contraction's end, after the wave's other chunks
+    fetch(c[0], whole, false, g.k - (int64_t)whole * kChunk - kGroup * group);
+    multiply(c[0]);
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int u = 0; u < NT; ++u) parts[wave][t * NT + u][lane] = acc[t][u];
+  __syncthreads();
+  for (int i = wave; i < MT * NT; i += WAVES) {
+    floatx4 sum = parts[0][i][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += parts[w][i][lane];
+    const int64_t m = 16 * (i / NT) + row, n = n0 + 16 * (i % NT) + 4 * group;
+    if (m < g.X.n && n < g.W.n) put_four(g.C, m * g.ldc + n, g.W.n - n, __is_same(El, Bf16) ? BRSVD_DTYPE_BF16 : BRSVD_DTYPE_F16, sum);
+  }
+}
+
+// 256 columns of the result x 64 NQ rows.  O = kRows: Y, W's rows hold the contraction.  kCols: dX, the contraction runs down W's rows.
+template <class El, int NQ, Order O>
+__global__ void __launch_bounds__(512, 2)
+k_tiles_e2m1(const E2m1Args g) {
+  using T = TileProduct<El, NQ, O, kRows, true, E2m1Stager<El, O>>;
+  __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
+  int64_t tp, tq;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
+  const int64_t p0 = g.first + tp * T::BP, q0 = tq * T::BQ, k0 = blockIdx.y * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
+  floatx4 acc[T::NP][NQ];
+  T::run(acc, g.W, p0, g.X, q0, k0, k1, lds);
+  if (g.splits > 1) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % T::WP, wq = wave / T::WP;
+    float* C = (float*)g.C + (int64_t)blockIdx.y * g.X.n * g.cols;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      const int64_t m = q0 + 16 * (wq * NQ + q) + (lane & 15);
+      if (m >= g.X.n) continue;
+#pragma unroll
+      for (int p = 0; p < T::NP; ++p) {
+        const int64_t n = p0 + 16 * (wp * T::NP + p) + 4 * (lane >> 4);
+        if (n < g.cols) put_four(C, m * g.cols + n, g.cols - n, BRSVD_DTYPE_F32, acc[p][q]);
+      }
+    }
+  } else {
+    put_tile16<NQ>(acc, lds, (uint16_t*)g.C + q0 * g.ldc + p0, g.ldc, g.X.n - q0, g.cols - p0, [](float x, int) { return to16<El>(x); });
+  }
+}
+
+// Rows of 16-bit numbers next to each other in rows of `pitch` bytes, a multiple of 16, with zeros to the end of the last piece.
+__global__ void __launch_bounds__(256)
+k_align_rows(const char* __restrict__ from, int64_t ld, int64_t rows, int64_t bytes, char* __restrict__ to, int64_t pitch, unsigned first_wg) {
+  const int64_t pieces = (bytes + 15) / 16, per = (pieces + 255) / 256, wg = (int64_t)first_wg + blockIdx.x, r = wg / per, c = (wg - r * per) * 256 + threadIdx.x;
+  if (r < rows && c < pieces) *(uint4*)(to + r * pitch + 16 * c) = piece_of<2>(from + r * ld + 16 * c, bytes - 16 * c);
+}
+void align_rows(const void* from, int64_t ld_bytes, int64_t rows, int64_t cols, void* to, int64_t pitch, hipStream_t stream) {
+  in_launches(rows * ceil_div(ceil_div(2 * cols, 16), 256), 256, [&](unsigned first, dim3 grid) {
+    hipLaunchKernelGGL(k_align_rows, grid, dim3(256), 0, stream, (const char*)from, ld_bytes, rows, 2 * cols, (char*)to, pitch, first);
+  });
+}
+
+static uint64_t whole256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// A product of m rows and `cols` columns over a contraction of k.
+struct E2m1Plan {
+  bool rows;                    // k_rows_e2m1
+  int nq;                       // rows of X in a tile, in 64, beside the large ones
+  int64_t large;                // columns in tiles of 256 rows, in 256
+  int splits;
+  int64_t per_split;
+  uint64_t part, x;             // bytes of the parts, and of X in aligned rows where it has to be laid out
+};
+static E2m1Plan e2m1_plan(int64_t m, int64_t cols, int64_t k, bool backward) {
+  E2m1Plan p;
+  p.rows = !backward && m <= 64;
+  const int64_t tiles = ceil_div(cols, 256), steps = ceil_div(k, 64);
+  p.nq = m <= 64 ? 1 : 2;
+  p.large = m <= 128 ? 0 : large_tiles(tiles, ceil_div(m, 256), ceil_div(m, 128), steps);
+  const int64_t workgroups = p.large * ceil_div(m, 256) + (tiles - p.large) * ceil_div(m, 64 * p.nq);
+  int64_t s = p.rows ? 1 : 256 / workgroups;
+  if (s > steps / 8) s = steps / 8;
+  if (s > 16) s = 16;
+  if (s < 1) s = 1;
+  p.per_split = ceil_div(steps, s) * 64;
+  p.splits = (int)ceil_div(steps * 64, p.per_split);
+  p.part = p.splits > 1 ? whole256((uint64_t)p.splits * m * cols * 4) : 0;
+  p.x = p.rows ? 0 : whole256((uint64_t)m * line_pitch(2 * k));
+  return p;
+}
+
+template <class El, int MT, int NT, int U, int WAVES>
+static void launch_rows(const E2m1Args& g, hipStream_t stream) {
+  hipLaunchKernelGGL((k_rows_e2m1<El, MT, NT, U, WAVES>), dim3((unsigned)ceil_div(g.W.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);
+}
+template <class El, int NQ, Order O>
+static void launch_tiles(E2m1Args g, hipStream_t stream) {
+  g.tiles_q = ceil_div(g.X.n, 64 * NQ);
+  hipLaunchKernelGGL((k_tiles_e2m1<El, NQ, O>), dim3(tile_workgroups(g.tiles_p, g.tiles_q), (unsigned)g.splits), dim3(512), 0, stream, g);
+}
+template <class El, Order O>
+static void launch_tiles(E2m1Args g, const E2m1Plan& p, hipStream_t stream) {
+  const int64_t tiles = ceil_div(g.cols, 256);
+  g.first = 0;
+  g.tiles_p = p.large;
+  if (p.large > 0) launch_tiles<El, 4, O>(g, stream);
+  g.first = 256 * p.large;
+  g.tiles_p = tiles - p.large;
+  if (g.tiles_p > 0) p.nq == 1 ? launch_tiles<El, 1, O>(g, stream) : launch_tiles<El, 2, O>(g, stream);
+}
+
+template <class El>
+static int product_e2m1(E2m1Args g, const E2m1Plan& p, bool backward, char* scratch, int dtype, hipStream_t stream) {
+  void* C = g.C;
+  const int64_t ldc = g.ldc;
+  if (p.rows) {
+    if (g.X.n <= 16) g.W.n >= 16 * 512 ? launch_rows<El, 1, 2, 2, 4>(g, stream) : launch_rows<El, 1, 1, 4, 8>(g, stream);
+    else if (g.X.n <= 32) launch_rows<El, 2, 1, 2, 8>(g, stream);
+    else launch_rows<El, 4, 1, 1, 8>(g, stream);
+  } else {
+    if (!aligned_pieces(g.X.base, g.X.ld)) {
+      const int64_t pitch = line_pitch(2 * g.k);
+      align_rows(g.X.base, g.X.ld, g.X.n, g.k, scratch + p.part, pitch, stream);
+      g.X.base = scratch + p.part;
+      g.X.ld = pitch;
+    }
+    g.splits = p.splits;
+    g.per_split = p.per_split;
+    if (p.splits > 1) g.C = scratch;
+    backward ? launch_tiles<El, kCols>(g, p, stream) : launch_tiles<El, kRows>(g, p, stream);
+    if (p.splits > 1) join_splits((const float*)scratch, p.splits, g.X.n, g.cols, C, ldc, dtype, stream);
+  }
+  BRSVD_HIP_TRY(hipGetLastError());
+  return BRSVD_OK;
+}
+
+static bool half_type(int dtype) { return dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16; }
+// A tile's rows are addressed with 32 bits, and launches have their workgroups.
+static bool e2m1_sizes(int64_t m, int64_t n, int64_t k, bool backward) {
+  if (m < 0 || n < 0 || k < 0 || m >= (int64_t)1 << 31 || n >= (int64_t)1 << 31 || k >= kMaxPitch / 2 || (backward && n >= kMaxPitch / 2)) return false;
+  const int64_t cols = backward ? k : n;
+  return tiles_fit(ceil_div(cols, 256), ceil_div(m, 64), 512) && ceil_div(n, 16) <= launch_workgroups(512) && m <= (int64_t)UINT32_MAX / ceil_div((backward ? n : k) + 1, 2048);
+}
+static int check_e2m1(const void* X, int64_t ldx, int64_t in, int dtype, const uint8_t* W, int64_t ldw, const uint8_t* S, int64_t m, int64_t n, int64_t k, const void* Y,
+                      int64_t ldy, int64_t out, bool backward) {
+  if (!half_type(dtype) || !e2m1_sizes(m, n, k, backward)) return BRSVD_ERR_ARG;
+  if (m == 0 || out == 0) return BRSVD_OK;
+  if (!Y || ldy < out || ldy >= (int64_t)1 << 40) return BRSVD_ERR_ARG;
+  if (in > 0 && (!X || !W || !S || ldx < in || ldx >= kMaxPitch / 2 || ldw < (k + 1) / 2 || ldw >= kMaxPitch / 2)) return BRSVD_ERR_ARG;
+  return BRSVD_OK;
+}
+
+static int call_e2m1(const void* X, int64_t ldx, int64_t in, int dtype, const uint8_t* W, int64_t ldw, const uint8_t* S, int64_t m, int64_t n, int64_t k, void* Y,
+                     int64_t ldy, int64_t out, bool backward, void* scratch, uint64_t scratch_bytes, hipStream_t s) {
+  BRSVD_TRY(check_e2m1(X, ldx, in, dtype, W, ldw, S, m, n, k, Y, ldy, out, backward));
+  if (m == 0 || out == 0) return BRSVD_OK;
+  if (in == 0) {               // an empty sum
+    join_splits(nullptr, 0, m, out, Y, ldy, dtype, s);
+    BRSVD_HIP_TRY(hipGetLastError());
+    return BRSVD_OK;
+  }
+  const E2m1Plan p = e2m1_plan(m, out, in, backward);
+  const uint64_t need = p.part + (p.rows || aligned_pieces(X, 2 * ldx) ? 0 : p.x);
+  if (need && (!scratch || (uintptr_t)scratch % 256)) return BRSVD_ERR_ARG;
+  if (scratch_bytes < need) return BRSVD_ERR_BUDGET;
+  E2m1Args g = {};
+  g.W = E2m1Operand{W, ldw, out, S, ceil_div(k, kGroup)};
+  g.X = Operand{(const char*)X, 2 * ldx, m};
+  g.k = in;
+  g.C = Y;
+  g.ldc = ldy;
+  g.cols = out;
+  return dtype == BRSVD_DTYPE_BF16 ? product_e2m1<Bf16>(g, p, backward, (char*)scratch, dtype, s) : product_e2m1<Fp16>(g, p, backward, (char*)scratch, dtype, s);
+}
+
+}  // namespace brsvd
+
+using namespace brsvd;
+
+extern "C" uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t backward) {
+  if (!e2m1_sizes(m, n, k, backward != 0) || m == 0 || n == 0 || k == 0) return 0;
+  const E2m1Plan p = e2m1_plan(m, backward ? k : n, backward ? n : k, backward != 0);
+  return p.part + p.x;
+}
+
+extern "C" int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW, int64_t m, int64_t n, int64_t k, void* Y,
+                                 int64_t ldy, void* scratch, uint64_t scratch_bytes, void* stream) {
+  return call_e2m1(X, ldx, k, dtype, W, ldw, SW, m, n, k, Y, ldy, n, false, scratch, scratch_bytes, (hipStream_t)stream);
+}
+
+extern "C" int brsvd_linear_e2m1_backward(const void* dY, int64_t lddy, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW, int64_t m, int64_t n, int64_t k,
+                                          void* dX, int64_t lddx, void* scratch, uint64_t scratch_bytes, void* stream) {
+  return call_e2m1(dY, lddy, n, dtype, W, ldw, SW, m, n, k, dX, lddx, k, true, scratch, scratch_bytes, (hipStream_t)stream);
+}

@@ -23,27 +23,6 @@ struct E4m3Args {
   int64_t tiles_n, tiles_m;
 };
 
-// Four neighbouring numbers of a row of C (of `left` that the row still has)
-__device__ __forceinline__ void put_four(void* C, int64_t at, int64_t left, int dtype, floatx4 v) {
-  if (dtype == BRSVD_DTYPE_F32) {
-    float* o = (float*)C + at;
-    if (left >= 4 && ((uintptr_t)o & 15) == 0) *(floatx4*)o = v;
-    else
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (r < left) o[r] = v[r];
-  } else {
-    uint16_t h[4], *o = (uint16_t*)C + at;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) h[r] = dtype == BRSVD_DTYPE_BF16 ? to16<Bf16>(v[r]) : to16<Fp16>(v[r]);
-    if (left >= 4 && ((uintptr_t)o & 7) == 0) *(uint2*)o = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-    else
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (r < left) o[r] = h[r];
-  }
-}
-
 // Whether an fp32 number is a power of two in the range of an 8-bit exponent
 __device__ __forceinline__ bool is_power(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -499,7 +478,7 @@ k_rows_e4m3(const E4m3Args g) {
   }
 }
 
-static void join_splits(const float* part, int splits, int64_t m, int64_t n, void* C, int64_t ldc, int dtype, hipStream_t stream) {
+void join_splits(const float* part, int splits, int64_t m, int64_t n, void* C, int64_t ldc, int dtype, hipStream_t stream) {
   in_launches(ceil_div(m * ceil_div(n, 4), 256), 256, [&](unsigned first, dim3 grid) {
     hipLaunchKernelGGL(k_join_splits, grid, dim3(256), 0, stream, part, splits, m, n, C, ldc, dtype, first);
   });
