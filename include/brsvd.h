@@ -315,6 +315,31 @@ int brsvd_linear_e2m1_backward(const void* dY, int64_t lddy, int32_t dtype, cons
                                void* scratch, uint64_t scratch_bytes, void* stream);
 uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t backward);
 
+/* The first half of a gated feed-forward block, X tokens x dim, Wg and Wu width x dim, all of dtype BF16 or F16:
+ *   G = X Wg^T,  U = X Wu^T,  H = a(G) U        (tokens x width, of dtype)
+ * with a the activation: BRSVD_ACT_SILU g / (1 + e^-g), _GELU g Phi(g), _GELU_TANH g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.  G and U
+ * stay in fp32 until H is rounded.  G and U may be NULL, both or neither; the backward pass wants them.  Wg and Wu may be
+ * halves of one matrix.
+ * Backward, from dH, the gradient of H, and G and U as the forward call left them:
+ *   dG = dH U a'(G),  dU = dH a(G),  dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X
+ * dG and dU are formed in 16 bits, with F16 times one power of two that their largest decides: an entry is off by up to 2^-39 of the
+ * largest finite one beside its rounding to eleven bits.  dX may be NULL, and dWg with dWu.
+ * workspace: at least brsvd_glu_workspace_bytes of the same sizes; aligned = 1 where rows of X, Wg and Wu all begin at
+ * 16-byte addresses (address and leading dimension) and ldwg = ldwu, 0 is enough always.  0 bytes: NULL will do. */
+#define BRSVD_ACT_SILU 0
+#define BRSVD_ACT_GELU 1
+#define BRSVD_ACT_GELU_TANH 2
+int brsvd_glu_forward(const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu,
+                      int64_t tokens, int64_t dim, int64_t width, int32_t dtype, int32_t act, void* H, int64_t ldh,
+                      void* G, int64_t ldg, void* U, int64_t ldu, void* workspace, uint64_t workspace_bytes,
+                      void* stream);
+int brsvd_glu_backward(const void* X, int64_t ldx, const void* Wg, int64_t ldwg, const void* Wu, int64_t ldwu,
+                       const void* G, int64_t ldg, const void* U, int64_t ldu, const void* dH, int64_t lddh,
+                       int64_t tokens, int64_t dim, int64_t width, int32_t dtype, int32_t act, void* dX,
+                       int64_t lddx, void* dWg, int64_t lddwg, void* dWu, int64_t lddwu, void* workspace,
+                       uint64_t workspace_bytes, void* stream);
+uint64_t brsvd_glu_workspace_bytes(int64_t tokens, int64_t dim, int64_t width, int32_t aligned, int32_t backward);
+
 /* Softmax cross entropy of z = H W^T (H tokens x dim hidden states, W vocab x dim output matrix, both of
  * dtype BF16 or F16), per token, without keeping z:
  *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_{t, labels_t}
@@ -359,6 +384,25 @@ int brsvd_distill_backward(const void* H, int64_t ldh, const void* W, int64_t ld
                            uint64_t workspace_bytes, void* stream);
 uint64_t brsvd_head_workspace_bytes(int64_t tokens, int64_t vocab, int64_t dim, int64_t piece,
                                     int32_t top, int32_t backward);
+
+/* The norm over a list of tensors, and the tensors clipped by it.  A tensor is rows x cols numbers of dtype F32, BF16 or F16
+ * with neighbouring numbers in a row and rows ld numbers apart; where neither matters, rows = 1 and cols numbers.  The lists are HOST
+ * memory, read before the call returns.  Tensors may begin at any number of their type; without elements data may be NULL.
+ *   brsvd_grad_norm:  *norm (DEVICE) = |scale| sqrt(sum of all x^2), squares and sums in fp64, rounded to fp32
+ *   brsvd_grad_clip:  y = x scale min(1, max_norm / *norm), rounded to out's dtype; max_norm >= 0
+ * scale: what the gradients are to be multiplied by, such as one over the factor of a loss.  A *norm that is infinite or NaN clips
+ * nothing: y = x scale.  out[i] has the shape of tensors[i], any dtype, and either its memory, type and ld or none of any tensor's: a
+ * number that two of a list share counts twice in the norm, and clipping in place refuses lists that name a tensor twice.
+ * workspace: at least brsvd_grad_norm_workspace_bytes of the same list. */
+typedef struct brsvd_tensor {
+  void* data;
+  int64_t rows, cols, ld, dtype;
+} brsvd_tensor;
+uint64_t brsvd_grad_norm_workspace_bytes(const brsvd_tensor* tensors, int64_t count);
+int brsvd_grad_norm(const brsvd_tensor* tensors, int64_t count, float scale, float* norm, void* workspace,
+                    uint64_t workspace_bytes, void* stream);
+int brsvd_grad_clip(const brsvd_tensor* tensors, const brsvd_tensor* out, int64_t count, float scale,
+                    float max_norm, const float* norm, void* stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* brsvd_status_string(int status);

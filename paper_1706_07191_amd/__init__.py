@@ -32,6 +32,9 @@ BRSVD_DTYPE_F32 = 0
 BRSVD_DTYPE_F64 = 1
 BRSVD_DTYPE_BF16 = 2
 BRSVD_DTYPE_F16 = 3
+BRSVD_ACT_SILU = 0
+BRSVD_ACT_GELU = 1
+BRSVD_ACT_GELU_TANH = 2
 
 
 class brsvd_params(C.Structure):
@@ -42,6 +45,10 @@ class brsvd_params(C.Structure):
                 ("compute_stream", C.c_void_p), ("copy_stream", C.c_void_p),
                 ("dtype", C.c_int32), ("timing_level", C.c_int32),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class brsvd_tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("dtype", C.c_int64)]
 
 
 class brsvd_stats(C.Structure):
@@ -67,7 +74,9 @@ EXPORTS = ["brsvd_workspace_bytes", "brsvd_create", "brsvd_run", "brsvd_run_f64"
            "brsvd_run_alg2", "brsvd_run_alg2_f64", "brsvd_philox_normal", "brsvd_philox_normal_f64",
            "brsvd_quantize_e4m3", "brsvd_dequantize_e4m3", "brsvd_gemm_e4m3", "brsvd_gemm_e4m3_scratch_bytes",
            "brsvd_linear_e4m3", "brsvd_linear_e4m3_scratch_bytes", "brsvd_quantize_e2m1", "brsvd_dequantize_e2m1",
-           "brsvd_linear_e2m1", "brsvd_linear_e2m1_backward", "brsvd_linear_e2m1_scratch_bytes", "brsvd_xent_forward", "brsvd_xent_backward",
+           "brsvd_linear_e2m1", "brsvd_linear_e2m1_backward", "brsvd_linear_e2m1_scratch_bytes", "brsvd_glu_forward",
+           "brsvd_glu_backward", "brsvd_glu_workspace_bytes", "brsvd_grad_norm", "brsvd_grad_norm_workspace_bytes", "brsvd_grad_clip",
+           "brsvd_xent_forward", "brsvd_xent_backward",
            "brsvd_distill_forward", "brsvd_distill_backward", "brsvd_head_workspace_bytes",
            "brsvd_destroy", "brsvd_status_string"]
 STEP_EXPORTS = ["brsvd_gemm_an", "brsvd_gemm_at", "brsvd_gemm_scratch_bytes", "brsvd_gemm_an_f64",
@@ -139,6 +148,13 @@ def lib() -> C.CDLL:
     L.brsvd_linear_e2m1.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp, i64, vp, u64, vp]
     L.brsvd_linear_e2m1_backward.argtypes = L.brsvd_linear_e2m1.argtypes
     L.brsvd_linear_e2m1_scratch_bytes.argtypes = [i64, i64, i64, i32]
+    L.brsvd_glu_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, u64, vp]
+    L.brsvd_glu_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64,
+                                     vp, u64, vp]
+    L.brsvd_glu_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    L.brsvd_grad_norm.argtypes = [vp, i64, flt, vp, vp, u64, vp]
+    L.brsvd_grad_norm_workspace_bytes.argtypes = [vp, i64]
+    L.brsvd_grad_clip.argtypes = [vp, vp, i64, flt, flt, vp, vp]
     L.brsvd_xent_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i32, vp, vp, vp, u64, vp]
     L.brsvd_xent_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, i32, vp, i64, vp, i64, vp, u64, vp]
     L.brsvd_distill_forward.argtypes = [vp, i64, vp, i64, vp, vp, i32, flt, i64, i64, i64, i32, vp, vp, vp, vp, u64, vp]
@@ -147,7 +163,8 @@ def lib() -> C.CDLL:
     L.brsvd_head_workspace_bytes.argtypes = [i64, i64, i64, i64, i32, i32]
     sizes = ("brsvd_gemm_scratch_bytes", "brsvd_gemm_scratch_bytes_f64", "brsvd_orth_scratch_bytes",
              "brsvd_small_svd_scratch_bytes", "brsvd_gemm_e4m3_scratch_bytes", "brsvd_linear_e4m3_scratch_bytes",
-             "brsvd_linear_e2m1_scratch_bytes", "brsvd_head_workspace_bytes")
+             "brsvd_linear_e2m1_scratch_bytes", "brsvd_glu_workspace_bytes", "brsvd_grad_norm_workspace_bytes",
+             "brsvd_head_workspace_bytes")
     for name in EXPORTS + STEP_EXPORTS:
         if name in sizes:
             getattr(L, name).restype = u64
@@ -479,10 +496,14 @@ def _device_of(operands):
     for t in operands:
         if isinstance(t, torch.Tensor):
             at = t.get_device()
-            if at >= 0 and at != index:
-                if index >= 0:
-                    raise TypeError(f"the operands must be on one device, not on cuda:{index} and cuda:{at}")
-                index = at
+        elif isinstance(t, (list, tuple)):
+            at = _device_of(t)
+        else:
+            continue
+        if at >= 0 and at != index:
+            if index >= 0:
+                raise TypeError(f"the operands must be on one device, not on cuda:{index} and cuda:{at}")
+            index = at
     return index
 
 
@@ -699,6 +720,133 @@ def brsvd_linear_e2m1(X, W, SW, out=None):
 def brsvd_linear_e2m1_backward(dY, W, SW, cols=None, out=None):
     """The gradient dY W of brsvd_linear_e2m1's X from dY (m, n), the gradient of its result.  cols: numbers of a row of W where they are odd."""
     return _linear_e2m1("brsvd_linear_e2m1_backward", dY, "dY", W, SW, _columns(W, cols), 1, out)
+
+
+_ACTIVATIONS = {"silu": BRSVD_ACT_SILU, "gelu": BRSVD_ACT_GELU, "gelu_tanh": BRSVD_ACT_GELU_TANH}
+
+
+def _glu(X, Wg, Wu, act):
+    dt = _model_dtype(X.dtype, "X", half=True)
+    if act not in _ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(_ACTIVATIONS)}, not {act!r}")
+    x, ldx = _rows(X, X.dtype, None, "X")
+    wg, ldwg = _rows(Wg, X.dtype, X.shape[1], "Wg")
+    wu, ldwu = _rows(Wu, X.dtype, X.shape[1], "Wu", Wg.shape[0])
+    sizes = (X.shape[0], X.shape[1], Wg.shape[0])
+    aligned = ldwg == ldwu and not ((x | wg | wu) & 15 or (ldx | ldwg | ldwu) & 7)
+    return (x, ldx, wg, ldwg, wu, ldwu), sizes, dt, _ACTIVATIONS[act], aligned
+
+
+def _glu_workspace(sizes, aligned, backward, device):
+    nbytes = lib().brsvd_glu_workspace_bytes(*sizes, aligned, backward)
+    if not nbytes:
+        return None, None, 0
+    ws = _byte_scratch(nbytes, device)
+    return ws, ws.data_ptr(), nbytes
+
+
+@_scoped
+def brsvd_glu_forward(X, Wg, Wu, act="silu", keep=False):
+    """H = a(X Wg^T) * (X Wu^T), the first half of a gated feed-forward block: X (tokens, dim), Wg and Wu (width, dim; they may be halves of
+    one matrix), bf16 or fp16.  act: silu, gelu or gelu_tanh.  keep=True returns (H, G, U) with G = X Wg^T and U = X Wu^T, which
+    brsvd_glu_backward wants.  No autograd graph."""
+    ops, (tokens, dim, width), dt, a, aligned = _glu(X, Wg, Wu, act)
+    n = 3 if keep else 1
+    outs = [torch.empty(tokens, width, dtype=X.dtype, device=X.device) for _ in range(n)]
+    ld = width or 1
+    at = [t.data_ptr() for t in outs] + [None] * (3 - n)
+    ws, w, nbytes = _glu_workspace((tokens, dim, width), aligned, 0, X.device)
+    _check(lib().brsvd_glu_forward(*ops, tokens, dim, width, dt, a, at[0], ld, at[1], ld, at[2], ld, w, nbytes, _current(X.device)),
+           "brsvd_glu_forward")
+    return tuple(outs) if keep else outs[0]
+
+
+@_scoped
+def brsvd_glu_backward(X, Wg, Wu, G, U, dH, act="silu", need_dX=True, need_dW=True):
+    """Gradients (dX, dWg, dWu) from dH, the gradient of H, and the G and U that the forward call kept; None for those that are not needed.
+    dWg and dWu are halves of one (2 width, dim) matrix."""
+    ops, (tokens, dim, width), dt, a, aligned = _glu(X, Wg, Wu, act)
+    kept = sum((_rows(t, X.dtype, width, name, tokens) for t, name in ((G, "G"), (U, "U"), (dH, "dH"))), ())
+    if not (need_dX or need_dW):
+        raise ValueError("neither gradient is wanted")
+    dX = torch.empty(tokens, dim, dtype=X.dtype, device=X.device) if need_dX else None
+    dWg, dWu = torch.empty(2, width, dim, dtype=X.dtype, device=X.device).unbind(0) if need_dW else (None, None)
+    d = dim or 1
+    ws, w, nbytes = _glu_workspace((tokens, dim, width), aligned, 1, X.device)
+    at = [None if t is None else t.data_ptr() for t in (dX, dWg, dWu)]
+    _check(lib().brsvd_glu_backward(*ops, *kept, tokens, dim, width, dt, a, at[0], d, at[1], d, at[2], d, w, nbytes, _current(X.device)),
+           "brsvd_glu_backward")
+    return dX, dWg, dWu
+
+
+_CODES = {}
+
+
+def _dense_order(t):
+    """Strides of a tensor whose numbers fill their memory without gaps in some order of its dimensions, else None."""
+    expected = 1
+    for size, step in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda x: (x[1], x[0])):
+        if step != expected:
+            return None
+        expected *= size
+    return t.stride()
+
+
+def _tensors(tensors, name, like=None):
+    """(array of brsvd_tensor, count) of a list of tensors; like: those whose numbers have to be in the same order."""
+    import array
+    if isinstance(tensors, torch.Tensor) or not isinstance(tensors, (list, tuple)):
+        raise TypeError(f"{name} must be a list of CUDA tensors")
+    if not _CODES:
+        _CODES.update({torch.float32: BRSVD_DTYPE_F32, torch.bfloat16: BRSVD_DTYPE_BF16, torch.float16: BRSVD_DTYPE_F16})
+    if like is not None and len(like) != len(tensors):
+        raise ValueError(f"{name} has {len(tensors)} tensors, expected {len(like)}")
+    flat = []
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided or t.dtype not in _CODES:
+            raise TypeError(f"{name}[{i}] must be a CUDA tensor of dtype torch.float32, torch.bfloat16 or torch.float16")
+        other = t if like is None else like[i]
+        if other is not t and other.shape != t.shape:
+            raise TypeError(f"{name}[{i}] has shape {tuple(t.shape)}, expected {tuple(other.shape)}")
+        n = t.numel()
+        if (t.is_contiguous() and (other is t or other.is_contiguous())) or not n:
+            flat += (t.data_ptr(), 1, n, n, _CODES[t.dtype])
+        elif t.dim() == 2 and all(x.stride(1) == 1 and x.stride(0) >= x.shape[1] for x in (t, other)):
+            flat += (t.data_ptr(), t.shape[0], t.shape[1], t.stride(0), _CODES[t.dtype])
+        elif _dense_order(t) is not None and _dense_order(other) == t.stride():
+            flat += (t.data_ptr(), 1, n, n, _CODES[t.dtype])
+        else:
+            raise TypeError(f"{name}[{i}] must be dense, or a matrix with unit column stride" + ("" if like is None else ", laid out as its original"))
+    return array.array("q", flat), len(tensors)
+
+
+@_scoped
+def brsvd_grad_norm(tensors, scale=1.0):
+    """|scale| times the 2-norm over all numbers of a list of CUDA tensors (fp32, bf16 or fp16, mixed; dense or matrices with strided rows), as a
+    tensor of one fp32 number.  Sums are fp64.  scale: what the gradients are to be multiplied by, such as one over a loss's factor."""
+    table, count = _tensors(tensors, "tensors")
+    device = tensors[0].device if count else torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty(1, dtype=torch.float32, device=device)
+    at = table.buffer_info()[0] if count else None
+    nbytes = lib().brsvd_grad_norm_workspace_bytes(at, count)
+    ws = _byte_scratch(nbytes, device)
+    _check(lib().brsvd_grad_norm(at, count, scale, norm.data_ptr(), ws.data_ptr(), nbytes, _current(device)), "brsvd_grad_norm")
+    return norm
+
+
+@_scoped
+def brsvd_grad_clip(tensors, norm, max_norm, scale=1.0, out=None):
+    """Multiplies every tensor of a list by scale min(1, max_norm / norm), norm being that of brsvd_grad_norm with the same scale (one fp32 number on
+    the device).  out: tensors of the same shapes, of any of the three types, that the results are written to instead of the tensors
+    themselves.  A norm that is infinite or NaN clips nothing.  A list that names a tensor twice is refused.  Returns the tensors written."""
+    if not isinstance(norm, torch.Tensor) or norm.numel() != 1:
+        raise TypeError("norm must be a CUDA tensor of one fp32 number")
+    n = _dev(norm, torch.float32, "norm")
+    table, count = _tensors(tensors, "tensors", out)
+    results = tensors if out is None else out
+    to = table if out is None else _tensors(out, "out", tensors)[0]
+    _check(lib().brsvd_grad_clip(table.buffer_info()[0] if count else None, to.buffer_info()[0], count, scale, max_norm, n, _current(norm.device)), "brsvd_grad_clip")
+    return results
 
 
 def _head(H, W):

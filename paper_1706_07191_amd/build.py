@@ -21,7 +21,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libbrsvd.so")
 SOURCES = ["gemm_half.hip", "gemm_split.hip", "gemm_thin.hip", "orth.hip", "tsqr.hip", "small_svd.hip", "rpca.hip", "philox.hip", "probe.hip",
-           "quantize.hip", "gemm_e4m3.hip", "quantize_e2m1.hip", "gemm_e2m1.hip", "head_loss.hip", "brsvd.hip"]
+           "quantize.hip", "gemm_e4m3.hip", "quantize_e2m1.hip", "gemm_e2m1.hip", "glu.hip", "grads.hip", "head_loss.hip", "brsvd.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

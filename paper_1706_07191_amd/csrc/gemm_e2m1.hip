@@ -135,7 +135,6 @@ k_tiles_e2m1(const E2m1Args g) {
   }
 }
 
-// Rows of 16-bit numbers next to each other in rows of `pitch` bytes, a multiple of 16, with zeros to the end of the last piece.
 __global__ void __launch_bounds__(256)
 k_align_rows(const char* __restrict__ from, int64_t ld, int64_t rows, int64_t bytes, char* __restrict__ to, int64_t pitch, unsigned first_wg) {
   const int64_t pieces = (bytes + 15) / 16, per = (pieces + 255) / 256, wg = (int64_t)first_wg + blockIdx.x, r = wg / per, c = (wg - r * per) * 256 + threadIdx.x;

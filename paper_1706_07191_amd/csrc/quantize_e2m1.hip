@@ -5,18 +5,6 @@
 
 namespace brsvd {
 
-// Division by a number that all threads share: an estimate that is right or one too low, from m = floor(2^32 / d) (2^32 - 1 for d = 1).
-struct Divisor {
-  uint32_t d, m;
-};
-static Divisor divisor(uint32_t d) { return Divisor{d, d == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / d)}; }
-__device__ __forceinline__ uint32_t divide(uint32_t i, Divisor by, uint32_t* rest) {
-  uint32_t q = __umulhi(i, by.m), r = i - q * by.d;
-  if (r >= by.d) ++q, r -= by.d;
-  *rest = r;
-  return q;
-}
-
 // Numbers that a thread takes of a group, 16 bytes of them, and lanes of a group
 template <int DT> struct Share {
   static constexpr int kBytes = DT == BRSVD_DTYPE_F32 ? 4 : 2, kWide = 16 / kBytes, kLanes = kGroup / kWide;
@@ -156,15 +144,6 @@ k_dequantize_e2m1(const uint8_t* __restrict__ Q, int64_t ldq, const uint8_t* __r
 
 static int bytes_of(int dtype) { return dtype == BRSVD_DTYPE_F32 ? 4 : dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16 ? 2 : 0; }
 
-// `rows` rows of `per` units: launch(first row, rows of it, workgroups) for as many rows at a time as have fewer than 2^31 units (a row has), U * per_wg of them a workgroup
-template <class Launch>
-static void by_rows(int64_t rows, int64_t per, int64_t per_wg, Launch launch) {
-  const int64_t some = ((int64_t)1 << 30) / per, most = some < 1 ? 1 : some;
-  for (int64_t r = 0; r < rows; r += most) {
-    const int64_t n = rows - r < most ? rows - r : most;
-    launch(r, n, dim3((unsigned)ceil_div(n * per, per_wg)));
-  }
-}
 // Sizes of a matrix in 4 bits: a row has at most 2^31 units of work, and bytes are numbers of 64 bits
 static bool sizes_e2m1(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 0 && rows < (int64_t)1 << 40 && cols <= (int64_t)1 << 33; }
 static bool pitch_fits(int64_t ld) { return ld < (int64_t)1 << 40; }

@@ -543,6 +543,27 @@ __device__ __forceinline__ void put_tile16(const floatx4 (&acc)[8][NQ], char* ld
   }
 }
 
+// Division by a number that all threads share: an estimate that is right or one too low, from m = floor(2^32 / d) (2^32 - 1 for d = 1).
+struct Divisor {
+  uint32_t d, m;
+};
+inline Divisor divisor(uint32_t d) { return Divisor{d, d == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / d)}; }
+__device__ __forceinline__ uint32_t divide(uint32_t i, Divisor by, uint32_t* rest) {
+  uint32_t q = __umulhi(i, by.m), r = i - q * by.d;
+  if (r >= by.d) ++q, r -= by.d;
+  *rest = r;
+  return q;
+}
+
+// `rows` rows of `per` units: launch(first row, rows of it, workgroups) for as many rows at a time as have fewer than 2^31 units (a row has), U * per_wg of them a workgroup
+template <class Launch>
+inline void by_rows(int64_t rows, int64_t per, int64_t per_wg, Launch launch) {
+  const int64_t some = ((int64_t)1 << 30) / per, most = some < 1 ? 1 : some;
+  for (int64_t r = 0; r < rows; r += most) {
+    const int64_t n = rows - r < most ? rows - r : most;
+    launch(r, n, dim3((unsigned)ceil_div(n * per, per_wg)));
+  }
+}
 // Tiles of a np x nq grid (np along P) to workgroups: workgroups b, b + 8, b + 16 ... share an XCD and its L2, so each XCD gets a run of tiles, and a run
 // goes through `band` rows of the grid at a time.  Returns false for workgroups beyond the grid (the grid is rounded up to eight).
 __device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64_t nq_, unsigned band, int64_t* tp, int64_t* tq) {
@@ -554,6 +575,9 @@ __device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64
   return true;
 }
 inline unsigned tile_workgroups(int64_t np, int64_t nq) { return (unsigned)(8 * ((np * nq + 7) / 8)); }
+// Rows of 16-bit numbers next to each other in rows of `pitch` bytes, a multiple of 16, with zeros to the end of the last piece (gemm_e2m1.hip).  rows * ceil(cols / 2048) is
+// below 2^32.
+void align_rows(const void* from, int64_t ld_bytes, int64_t rows, int64_t cols, void* to, int64_t pitch, hipStream_t stream);
 // C (m x n, type dtype) = sum of the parts of a contraction that was cut, [split][m][n] in fp32, in their order (gemm_e4m3.hip)
 void join_splits(const float* part, int splits, int64_t m, int64_t n, void* C, int64_t ldc, int dtype, hipStream_t stream);
 // Whether a launch may have that many tiles
