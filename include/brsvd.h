@@ -306,14 +306,15 @@ int brsvd_dequantize_e2m1(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64
  * lays it out; and the gradient of X, dX (m x k) = dY W.  X is taken as it is.  A number of W times its scale is taken in X's type, as
  * brsvd_dequantize_e2m1 rounds it: nothing is lost with BF16 from 2^-133 on and with F16 from 2^-24 on.  Products are exact, sums are fp32, the
  * result is rounded once.  Scales are any bytes.
- * scratch: brsvd_linear_e2m1_scratch_bytes (0 where none is needed) of the same sizes. */
+ * scratch: brsvd_linear_e2m1_scratch_bytes of the same sizes; aligned = 1 where rows of X (dY) and W all begin at 16-byte
+ * addresses (address and leading dimension), 0 is enough always.  0 bytes: NULL will do. */
 int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW,
                       int64_t m, int64_t n, int64_t k, void* Y, int64_t ldy, void* scratch,
                       uint64_t scratch_bytes, void* stream);
 int brsvd_linear_e2m1_backward(const void* dY, int64_t lddy, int32_t dtype, const uint8_t* W, int64_t ldw,
                                const uint8_t* SW, int64_t m, int64_t n, int64_t k, void* dX, int64_t lddx,
                                void* scratch, uint64_t scratch_bytes, void* stream);
-uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t backward);
+uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t aligned, int32_t backward);
 
 /* The first half of a gated feed-forward block, X tokens x dim, Wg and Wu width x dim, all of dtype BF16 or F16:
  *   G = X Wg^T,  U = X Wu^T,  H = a(G) U        (tokens x width, of dtype)

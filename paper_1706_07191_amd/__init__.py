@@ -147,7 +147,7 @@ def lib() -> C.CDLL:
     L.brsvd_dequantize_e2m1.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, vp]
     L.brsvd_linear_e2m1.argtypes = [vp, i64, i32, vp, i64, vp, i64, i64, i64, vp, i64, vp, u64, vp]
     L.brsvd_linear_e2m1_backward.argtypes = L.brsvd_linear_e2m1.argtypes
-    L.brsvd_linear_e2m1_scratch_bytes.argtypes = [i64, i64, i64, i32]
+    L.brsvd_linear_e2m1_scratch_bytes.argtypes = [i64, i64, i64, i32, i32]
     L.brsvd_glu_forward.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, u64, vp]
     L.brsvd_glu_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64,
                                      vp, u64, vp]
@@ -704,7 +704,7 @@ def _linear_e2m1(name, X, x_name, W, SW, k, backward, out):
         Y = out
         y, ldy = _rows(Y, X.dtype, width, "out", m)
     L = lib()
-    nbytes = L.brsvd_linear_e2m1_scratch_bytes(m, n, k, backward)
+    nbytes = L.brsvd_linear_e2m1_scratch_bytes(m, n, k, not ((x | w | ldw) & 15 or ldx & 7), backward)
     scr = _byte_scratch(nbytes, X.device) if nbytes else None
     _check(getattr(L, name)(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes, _current(X.device)), name)
     return Y

@@ -21,12 +21,16 @@ struct E2m1Args {
 };
 
 // Up to 16 MT rows of X.  The WAVES waves of a workgroup share 16 NT rows of W and take chunks of 128 numbers of the contraction in turn; their sums are added
-// through LDS in wave order.  A lane has one group of a chunk, 16 bytes, and with it its scale; the same 32 numbers of a row of X, which all workgroups read and the
-// caches hold: any order of the contraction that both sides share will do.  The U chunks that a wave takes next are on their way.
+// through LDS in wave order.  A lane reads one group of a chunk, 16 bytes, and the four scales of its row; lanes then exchange words, so that an instruction takes one
+// group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  The U chunks that a wave takes next are on their way.
 template <class El, int MT, int NT, int U, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 k_rows_e2m1(const E2m1Args g) {
   constexpr int kChunk = 4 * kGroup;
+  struct __attribute__((packed, aligned(1))) Word {
+    uint32_t x;
+    __device__ operator uint32_t() const { return x; }
+  };
   __shared__ floatx4 parts[WAVES][MT * NT][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, group = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16 * NT;
@@ -40,37 +44,44 @@ k_rows_e2m1(const E2m1Args g) {
   for (int u = 0; u < NT; ++u) {
     const int64_t n = n0 + 16 * u + row, in = n < g.W.n ? n : g.W.n - 1;
     rw[u] = g.W.base + in * g.W.ld + 16 * group;
-    rs[u] = g.W.scales + in * g.W.groups + group;
+    rs[u] = g.W.scales + in * g.W.groups;
   }
   const char* rx[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     const int64_t m = 16 * t + row < g.X.n ? 16 * t + row : g.X.n - 1;
-    rx[t] = g.X.base + m * g.X.ld + 64 * group;
+    rx[t] = g.X.base + m * g.X.ld + 16 * group;
   }
   struct Chunk {
     uint4 w[NT], x[MT][4];
     uint32_t s[NT];
   };
-  auto fetch = [&](Chunk& c, int at, bool whole, int64_t left) {       // left: numbers of the row from this lane's group on
+  auto fetch = [&](Chunk& c, int at, bool whole, int64_t left) {       // left: numbers of the row from the chunk on
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left);
-      c.s[u] = whole || left > 0 ? rs[u][(int64_t)at * 4] : 127;
+      c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left - kGroup * group);
+      const uint8_t* s = rs[u] + (int64_t)at * 4;
+      if (whole) c.s[u] = *(const Word*)s;
+      else {
+        c.s[u] = 0x7f7f7f7fu;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (left > kGroup * j) c.s[u] += (uint32_t)(s[j] - 127) << (8 * j);
+      }
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c.x[t][j] = piece_of<2>(rx[t] + (int64_t)at * 256 + 16 * j, whole ? 16 : 2 * (left - 8 * j));
+      for (int j = 0; j < 4; ++j) c.x[t][j] = piece_of<2>(rx[t] + (int64_t)at * 256 + 64 * j, whole ? 16 : 2 * (left - kGroup * j - 8 * group));
   };
   auto multiply = [&](const Chunk& c) {
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      const float scale = scale_e8m0(c.s[u]);
-      const uint32_t w[4] = {c.w[u].x, c.w[u].y, c.w[u].z, c.w[u].w};
+      uint32_t w[4] = {c.w[u].x, c.w[u].y, c.w[u].z, c.w[u].w};
+      turn_groups(w);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int4v p = __builtin_bit_cast(int4v, eight_e2m1<El>(w[j], scale));
+        const int4v p = __builtin_bit_cast(int4v, eight_e2m1<El>(w[j], scale_e8m0(c.s[u] >> (8 * j) & 255)));
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[t][u] = mfma16<El>(p, __builtin_bit_cast(int4v, c.x[t][j]), acc[t][u]);
       }
@@ -89,7 +100,7 @@ k_rows_e2m1(const E2m1Args g) {
     }
   }
   if (g.k % kChunk != 0 && whole % WAVES == wave) {          // the contraction's end, after the wave's other chunks
-    fetch(c[0], whole, false, g.k - (int64_t)whole * kChunk - kGroup * group);
+    fetch(c[0], whole, false, g.k - (int64_t)whole * kChunk);
     multiply(c[0]);
   }
 #pragma unroll
@@ -110,7 +121,7 @@ k_rows_e2m1(const E2m1Args g) {
 template <class El, int NQ, Order O>
 __global__ void __launch_bounds__(512, 2)
 k_tiles_e2m1(const E2m1Args g) {
-  using T = TileProduct<El, NQ, O, kRows, true, E2m1Stager<El, O>>;
+  using T = E2m1Product<El, NQ, O>;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
@@ -138,11 +149,11 @@ k_tiles_e2m1(const E2m1Args g) {
 __global__ void __launch_bounds__(256)
 k_align_rows(const char* __restrict__ from, int64_t ld, int64_t rows, int64_t bytes, char* __restrict__ to, int64_t pitch, unsigned first_wg) {
   const int64_t pieces = (bytes + 15) / 16, per = (pieces + 255) / 256, wg = (int64_t)first_wg + blockIdx.x, r = wg / per, c = (wg - r * per) * 256 + threadIdx.x;
-  if (r < rows && c < pieces) *(uint4*)(to + r * pitch + 16 * c) = piece_of<2>(from + r * ld + 16 * c, bytes - 16 * c);
+  if (r < rows && c < pieces) *(uint4*)(to + r * pitch + 16 * c) = piece_of<1>(from + r * ld + 16 * c, bytes - 16 * c);
 }
-void align_rows(const void* from, int64_t ld_bytes, int64_t rows, int64_t cols, void* to, int64_t pitch, hipStream_t stream) {
-  in_launches(rows * ceil_div(ceil_div(2 * cols, 16), 256), 256, [&](unsigned first, dim3 grid) {
-    hipLaunchKernelGGL(k_align_rows, grid, dim3(256), 0, stream, (const char*)from, ld_bytes, rows, 2 * cols, (char*)to, pitch, first);
+void align_rows(const void* from, int64_t ld, int64_t rows, int64_t bytes, void* to, int64_t pitch, hipStream_t stream) {
+  in_launches(rows * ceil_div(ceil_div(bytes, 16), 256), 256, [&](unsigned first, dim3 grid) {
+    hipLaunchKernelGGL(k_align_rows, grid, dim3(256), 0, stream, (const char*)from, ld, rows, bytes, (char*)to, pitch, first);
   });
 }
 
@@ -155,9 +166,11 @@ struct E2m1Plan {
   int64_t large;                // columns in tiles of 256 rows, in 256
   int splits;
   int64_t per_split;
-  uint64_t part, x;             // bytes of the parts, and of X in aligned rows where it has to be laid out
+  uint64_t x, w, bytes;         // scratch: the parts at 0, X and W in aligned rows where they are laid out anew, all
 };
-static E2m1Plan e2m1_plan(int64_t m, int64_t cols, int64_t k, bool backward) {
+// m rows of X, W n x k; aligned: rows of both begin at 16-byte addresses.
+static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k_, bool aligned, bool backward) {
+  const int64_t cols = backward ? k_ : n, k = backward ? n : k_;
   E2m1Plan p;
   p.rows = !backward && m <= 64;
   const int64_t tiles = ceil_div(cols, 256), steps = ceil_div(k, 64);
@@ -170,14 +183,41 @@ static E2m1Plan e2m1_plan(int64_t m, int64_t cols, int64_t k, bool backward) {
   if (s < 1) s = 1;
   p.per_split = ceil_div(steps, s) * 64;
   p.splits = (int)ceil_div(steps * 64, p.per_split);
-  p.part = p.splits > 1 ? whole256((uint64_t)p.splits * m * cols * 4) : 0;
-  p.x = p.rows ? 0 : whole256((uint64_t)m * line_pitch(2 * k));
+  p.x = p.splits > 1 ? whole256((uint64_t)p.splits * m * cols * 4) : 0;
+  p.w = p.x + (p.rows || aligned ? 0 : whole256((uint64_t)m * line_pitch(2 * k)));
+  p.bytes = p.w + (p.rows || aligned ? 0 : whole256((uint64_t)n * line_pitch((k_ + 1) / 2)));
   return p;
 }
 
+// Few rows of X: by the 16 rows of W in a wave (NT of them).  A CU takes a KiB of W in some time t, wherever it comes from, and the 16 rows of X that go with a chunk in 0.6 t;
+// with NT for which the workgroups fill rounds of 256 it has least to do: 16 x 12000 x 4096 11.3 us with three (250 workgroups), 16.5 with two (375), 18 with one (750);
+// 64 x 20000 x 5000 34, 43, 48 and 74 with five, three, two and one.  Up to eight rows the caches give X for less, and more than three are slower: 1 x 20000 x 5000 15.9 with
+// one, 17.9 with five.
+static int rows_in_wave(int64_t m, int64_t n) {
+  const int64_t tiles = ceil_div(n, 16), x = m <= 8 ? 3 : 6 * ceil_div(m, 16);
+  int best = 1;
+  int64_t least = 0;
+  for (int nt : {1, 2, 3, 5}) {
+    if (nt == 5 && m <= 8) continue;
+    const int64_t cost = ceil_div(ceil_div(tiles, nt), 256) * (10 * nt + x);
+    if (nt == 1 || cost < least) least = cost, best = nt;
+  }
+  return best;
+}
 template <class El, int MT, int NT, int U, int WAVES>
 static void launch_rows(const E2m1Args& g, hipStream_t stream) {
   hipLaunchKernelGGL((k_rows_e2m1<El, MT, NT, U, WAVES>), dim3((unsigned)ceil_div(g.W.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);
+}
+// Chunks on their way as registers allow: two in each of four waves or one in each of eight, two in each of eight where a wave has one tile.
+template <class El, int MT>
+static void launch_rows(const E2m1Args& g, hipStream_t stream) {
+  constexpr int U = MT <= 2 ? 2 : 1, WAVES = MT <= 2 ? 4 : 8;
+  switch (rows_in_wave(g.X.n, g.W.n)) {
+    case 1: return launch_rows<El, MT, 1, U, 8>(g, stream);
+    case 2: return launch_rows<El, MT, 2, U, WAVES>(g, stream);
+    case 3: return launch_rows<El, MT, 3, U, WAVES>(g, stream);
+    default: return launch_rows<El, MT, 5, U, WAVES>(g, stream);
+  }
 }
 template <class El, int NQ, Order O>
 static void launch_tiles(E2m1Args g, hipStream_t stream) {
@@ -196,19 +236,23 @@ static void launch_tiles(E2m1Args g, const E2m1Plan& p, hipStream_t stream) {
 }
 
 template <class El>
-static int product_e2m1(E2m1Args g, const E2m1Plan& p, bool backward, char* scratch, int dtype, hipStream_t stream) {
+static int product_e2m1(E2m1Args g, const E2m1Plan& p, int64_t wrows, int64_t wbytes, bool aligned, bool backward, char* scratch, int dtype, hipStream_t stream) {
   void* C = g.C;
   const int64_t ldc = g.ldc;
   if (p.rows) {
-    if (g.X.n <= 16) g.W.n >= 16 * 512 ? launch_rows<El, 1, 2, 2, 4>(g, stream) : launch_rows<El, 1, 1, 4, 8>(g, stream);
-    else if (g.X.n <= 32) launch_rows<El, 2, 1, 2, 8>(g, stream);
-    else launch_rows<El, 4, 1, 1, 8>(g, stream);
+    if (g.X.n <= 16) launch_rows<El, 1>(g, stream);
+    else if (g.X.n <= 32) launch_rows<El, 2>(g, stream);
+    else if (g.X.n <= 48) launch_rows<El, 3>(g, stream);
+    else launch_rows<El, 4>(g, stream);
   } else {
-    if (!aligned_pieces(g.X.base, g.X.ld)) {
-      const int64_t pitch = line_pitch(2 * g.k);
-      align_rows(g.X.base, g.X.ld, g.X.n, g.k, scratch + p.part, pitch, stream);
-      g.X.base = scratch + p.part;
-      g.X.ld = pitch;
+    if (!aligned) {
+      const int64_t px = line_pitch(2 * g.k), pw = line_pitch(wbytes);
+      align_rows(g.X.base, g.X.ld, g.X.n, 2 * g.k, scratch + p.x, px, stream);
+      align_rows(g.W.base, g.W.ld, wrows, wbytes, scratch + p.w, pw, stream);
+      g.X.base = scratch + p.x;
+      g.X.ld = px;
+      g.W.base = (const uint8_t*)scratch + p.w;
+      g.W.ld = pw;
     }
     g.splits = p.splits;
     g.per_split = p.per_split;
@@ -225,7 +269,8 @@ static bool half_type(int dtype) { return dtype == BRSVD_DTYPE_BF16 || dtype == 
 static bool e2m1_sizes(int64_t m, int64_t n, int64_t k, bool backward) {
   if (m < 0 || n < 0 || k < 0 || m >= (int64_t)1 << 31 || n >= (int64_t)1 << 31 || k >= kMaxPitch / 2 || (backward && n >= kMaxPitch / 2)) return false;
   const int64_t cols = backward ? k : n;
-  return tiles_fit(ceil_div(cols, 256), ceil_div(m, 64), 512) && ceil_div(n, 16) <= launch_workgroups(512) && m <= (int64_t)UINT32_MAX / ceil_div((backward ? n : k) + 1, 2048);
+  return tiles_fit(ceil_div(cols, 256), ceil_div(m, 64), 512) && ceil_div(n, 16) <= launch_workgroups(512) && m <= (int64_t)UINT32_MAX / ceil_div((backward ? n : k) + 1, 2048) &&
+         n <= (int64_t)UINT32_MAX / ceil_div(k + 1, 8192);
 }
 static int check_e2m1(const void* X, int64_t ldx, int64_t in, int dtype, const uint8_t* W, int64_t ldw, const uint8_t* S, int64_t m, int64_t n, int64_t k, const void* Y,
                       int64_t ldy, int64_t out, bool backward) {
@@ -245,10 +290,10 @@ static int call_e2m1(const void* X, int64_t ldx, int64_t in, int dtype, const ui
     BRSVD_HIP_TRY(hipGetLastError());
     return BRSVD_OK;
   }
-  const E2m1Plan p = e2m1_plan(m, out, in, backward);
-  const uint64_t need = p.part + (p.rows || aligned_pieces(X, 2 * ldx) ? 0 : p.x);
-  if (need && (!scratch || (uintptr_t)scratch % 256)) return BRSVD_ERR_ARG;
-  if (scratch_bytes < need) return BRSVD_ERR_BUDGET;
+  const bool aligned = aligned_pieces(X, 2 * ldx) && aligned_pieces(W, ldw);
+  const E2m1Plan p = e2m1_plan(m, n, k, aligned, backward);
+  if (p.bytes && (!scratch || (uintptr_t)scratch % 256)) return BRSVD_ERR_ARG;
+  if (scratch_bytes < p.bytes) return BRSVD_ERR_BUDGET;
   E2m1Args g = {};
   g.W = E2m1Operand{W, ldw, out, S, ceil_div(k, kGroup)};
   g.X = Operand{(const char*)X, 2 * ldx, m};
@@ -256,17 +301,17 @@ static int call_e2m1(const void* X, int64_t ldx, int64_t in, int dtype, const ui
   g.C = Y;
   g.ldc = ldy;
   g.cols = out;
-  return dtype == BRSVD_DTYPE_BF16 ? product_e2m1<Bf16>(g, p, backward, (char*)scratch, dtype, s) : product_e2m1<Fp16>(g, p, backward, (char*)scratch, dtype, s);
+  return dtype == BRSVD_DTYPE_BF16 ? product_e2m1<Bf16>(g, p, n, (k + 1) / 2, aligned, backward, (char*)scratch, dtype, s)
+                                   : product_e2m1<Fp16>(g, p, n, (k + 1) / 2, aligned, backward, (char*)scratch, dtype, s);
 }
 
 }  // namespace brsvd
 
 using namespace brsvd;
 
-extern "C" uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t backward) {
+extern "C" uint64_t brsvd_linear_e2m1_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_t aligned, int32_t backward) {
   if (!e2m1_sizes(m, n, k, backward != 0) || m == 0 || n == 0 || k == 0) return 0;
-  const E2m1Plan p = e2m1_plan(m, backward ? k : n, backward ? n : k, backward != 0);
-  return p.part + p.x;
+  return e2m1_plan(m, n, k, aligned != 0, backward != 0).bytes;
 }
 
 extern "C" int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW, int64_t m, int64_t n, int64_t k, void* Y,

@@ -49,7 +49,6 @@ struct PairOperand {
 
 // Fills P's tile from rows of both matrices: 64 of Wg, 64 of Wu, the next 64 of Wg and of Wu.
 struct PairStager {
-  static constexpr bool kAhead = false;
   static constexpr int kLoads = 4;
   using Source = PairOperand;
   uint32_t off_g[2], off_u[2];
@@ -378,7 +377,6 @@ struct StackOperand {
 };
 template <class El>
 struct StackStager {
-  static constexpr bool kAhead = false;
   using Source = StackOperand;
   using One = Stager<El, kCols, 256, 512, true>;
   static constexpr int kLoads = One::kLoads;
@@ -585,7 +583,7 @@ static bool rows_aligned(const GluCall& c) {
 
 static Operand laid_out(const void* base, int64_t ld, int64_t n, int64_t cols, bool as_it_is, char* to, int64_t pitch, hipStream_t stream) {
   if (as_it_is) return Operand{(const char*)base, 2 * ld, n};
-  align_rows(base, 2 * ld, n, cols, to, pitch, stream);
+  align_rows(base, 2 * ld, n, 2 * cols, to, pitch, stream);
   return Operand{to, pitch, n};
 }
 

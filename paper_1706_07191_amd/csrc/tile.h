@@ -95,7 +95,6 @@ struct Stager {
   static constexpr int kPieces = N * (kStepBytes / 16), kLoads = kPieces / THREADS;
   static constexpr int kPerRow = O == kRows ? kStepBytes / 16 : N * 2 / 16;      // pieces per row of the tile in LDS
   static constexpr int kStepK = kStepBytes / El::kBytes;
-  static constexpr bool kAhead = false;      // of operands whose numbers are made on the way into LDS: their pieces are in registers a step longer
   using Source = Operand;
   static_assert(kPieces % THREADS == 0 && (O == kRows || El::kBytes == 2), "");
   uint32_t off[kLoads];      // from `at`
@@ -255,17 +254,15 @@ __device__ __forceinline__ floatx4 mfma_wide(const Wide8& p, const Wide8& q) {
 // Bound by the matrix cores: a tile of 256 x 256 takes 1.46 us a step (1.47 Pflop/s on 256 CUs); 1.66 where fragments are read behind the barrier, 1.90 where
 // a step is sent for at once, too (4096 x 65536 logits, widths from 256 to 2048).
 //
-// SP: what fills P's tiles.  One with kAhead has a step's pieces in registers when the workgroup meets, makes numbers of 16 bits of them and writes them into the buffer
-// that has just been read, in four parts, and sends for those of the step after.
+// SP: what fills P's tiles.
 template <class El, int NQ_, Order OP, Order OQ, bool DIRECT, class SP = Stager<El, OP, 256, 512, DIRECT>>
 struct TileProduct {
   static constexpr int NP = 8, NQ = NQ_, WP = 2, WQ = 4;
   static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
-  static constexpr bool AHEAD = SP::kAhead;
   static constexpr int kStepK = kStepBytes / El::kBytes;
   // Steps in LDS: the one that is multiplied and those on their way, two where there is room: a step of a smaller tile is over before memory has answered.
   // Loss of 500 tokens, 8000 words of width 4000: 59 us, with one 69; 100, 32000, 2000: 38 and 44.
-  static constexpr int NB = DIRECT && NQ <= 2 && !AHEAD ? 3 : 2, kPart = (BP + BQ) * kStepBytes, kLds = NB * kPart;
+  static constexpr int NB = DIRECT && NQ <= 2 ? 3 : 2, kPart = (BP + BQ) * kStepBytes, kLds = NB * kPart;
 
   static constexpr int PARTS = SP::kLoads + Stager<El, OQ, BQ, kThreads, DIRECT>::kLoads;
   SP sp;
@@ -287,11 +284,11 @@ struct TileProduct {
   }
   __device__ __forceinline__ void send(int t, char* to, int wave) {
     const int64_t left = k - (int64_t)t * kStepK;
-    if constexpr (!AHEAD) sp.load(to, threadIdx.x, wave, left);
+    sp.load(to, threadIdx.x, wave, left);
     sq.load(to + BP * kStepBytes, threadIdx.x, wave, left);
   }
   __device__ __forceinline__ void keep(char* to) {
-    if constexpr (!AHEAD) sp.store(to, threadIdx.x);
+    sp.store(to, threadIdx.x);
     sq.store(to + BP * kStepBytes, threadIdx.x);
   }
   // Sends for the first NB steps of a tile.  LDS has to be free.
@@ -307,40 +304,23 @@ struct TileProduct {
 #pragma unroll
     for (int t = 1; t < NB; ++t)
       if (steps() > t) send(t, lds + t * kPart, wave);
-    if constexpr (AHEAD) {
-      typename SP::Pieces x[NB];
-#pragma unroll
-      for (int t = 0; t <= NB; ++t)
-        if (steps() > t) sp.fetch(t < NB ? x[t < NB ? t : 0] : sp.ahead, k - (int64_t)t * kStepK);
-#pragma unroll
-      for (int t = 0; t < NB; ++t)
-        if (steps() > t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sp.store_part(lds + t * kPart, x[t], i);
-    }
   }
-  // The tile that was begun; LDS is free afterwards.  add: to the sums that are there.
-  __device__ __forceinline__ void multiply(floatx4 (&acc)[NP][NQ], bool add = false) {
+  // The tile that was begun; LDS is free afterwards.
+  __device__ __forceinline__ void multiply(floatx4 (&acc)[NP][NQ]) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP, steps = this->steps();
-    constexpr int SLOTS = 2 * NP, MEET = SLOTS - 4, LAST = PARTS > 4 ? PARTS - 5 : MEET + PARTS - 1;
-    if (!add) {
+    constexpr int SLOTS = 2 * NP, MEET = SLOTS - 4;
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p)
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
+      for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
     int4v fp[8], fq[2][NQ];
     uint32_t bp = fragment_base<OP, BP>(16 * wp * NP, lane), bq = fragment_base<OQ, BQ>(16 * wq * NQ, lane);
     auto read_p = [&](const char* tile, int slot) { fp[slot & 7] = fragment<OP, BP>(tile, bp, slot & 7, slot >> 3); };
     auto read_q = [&](const char* tile, int kk, int q) { fq[kk][q] = fragment<OQ, BQ>(tile + BP * kStepBytes, bq, q, kk); };
     // the parts of a plain step, one a slot: sent all at once they would queue up before the memory unit, and the waves behind them
     auto send_part = [&](char* to, int j) {
-      if constexpr (AHEAD) {
-        if (j < PARTS) sq.load_part(to + BP * kStepBytes, wave, j);
-      } else {
-        if (j < SP::kLoads) sp.load_part(to, wave, j);
-        else if (j < PARTS) sq.load_part(to + BP * kStepBytes, wave, j - SP::kLoads);
-      }
+      if (j < SP::kLoads) sp.load_part(to, wave, j);
+      else if (j < PARTS) sq.load_part(to + BP * kStepBytes, wave, j - SP::kLoads);
     };
     bool parts = false;          // the step after this one is being sent for in parts
     if (steps == 0) return;
@@ -370,22 +350,17 @@ struct TileProduct {
           read_p(cur, s + 6);
         } else if (s == MEET) {
           meet(NB > 2 && plain(t + 2));
-          if constexpr (AHEAD) sp.arrived();
           parts = sends && plain(t + NB);
           if (sends && !parts) send(t + NB, lds + at, wave);
         }
         if (parts) {
           if (s >= MEET) send_part(lds + at, s - MEET);
           else if (s < PARTS - 4) send_part(lds + pat, s + 4);
-          if (s == LAST) {
-            if constexpr (!AHEAD) sp.next();
+          if (s == PARTS - 5) {
+            sp.next();
             sq.next();
             parts = false;
           }
-        }
-        if constexpr (AHEAD) {
-          if (s >= MEET && sends) sp.store_part(lds + at, sp.ahead, s - MEET);
-          if (s == SLOTS - 1 && t + NB + 1 < steps) sp.fetch(sp.ahead, k - (int64_t)(t + NB + 1) * kStepK);
         }
         if (s >= MEET && more) {
           read_p(nxt, s - MEET);
@@ -555,7 +530,7 @@ __device__ __forceinline__ uint32_t divide(uint32_t i, Divisor by, uint32_t* res
   return q;
 }
 
-// `rows` rows of `per` units: launch(first row, rows of it, workgroups) for as many rows at a time as have fewer than 2^31 units (a row has), U * per_wg of them a workgroup
+// `rows` rows of `per` units: launch(first row, rows of it, workgroups) for as many rows at a time as have at most 2^30 units (or one row), per_wg of them a workgroup
 template <class Launch>
 inline void by_rows(int64_t rows, int64_t per, int64_t per_wg, Launch launch) {
   const int64_t some = ((int64_t)1 << 30) / per, most = some < 1 ? 1 : some;
@@ -575,9 +550,9 @@ __device__ __forceinline__ bool tile_of_workgroup(unsigned b, int64_t np_, int64
   return true;
 }
 inline unsigned tile_workgroups(int64_t np, int64_t nq) { return (unsigned)(8 * ((np * nq + 7) / 8)); }
-// Rows of 16-bit numbers next to each other in rows of `pitch` bytes, a multiple of 16, with zeros to the end of the last piece (gemm_e2m1.hip).  rows * ceil(cols / 2048) is
+// Rows of `bytes` bytes, next to each other in rows of `pitch` bytes, a multiple of 16, with zeros to the end of the last piece (gemm_e2m1.hip).  rows * ceil(bytes / 4096) is
 // below 2^32.
-void align_rows(const void* from, int64_t ld_bytes, int64_t rows, int64_t cols, void* to, int64_t pitch, hipStream_t stream);
+void align_rows(const void* from, int64_t ld, int64_t rows, int64_t bytes, void* to, int64_t pitch, hipStream_t stream);
 // C (m x n, type dtype) = sum of the parts of a contraction that was cut, [split][m][n] in fp32, in their order (gemm_e4m3.hip)
 void join_splits(const float* part, int splits, int64_t m, int64_t n, void* C, int64_t ldc, int dtype, hipStream_t stream);
 // Whether a launch may have that many tiles

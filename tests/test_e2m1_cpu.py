@@ -52,14 +52,15 @@ def test_linear_refuses(bad, backward):
 @pytest.mark.parametrize("backward", [False, True])
 def test_scratch(backward):
     size = B.lib().brsvd_linear_e2m1_scratch_bytes
-    need = size(100, 4096, 4096, backward)
+    need = size(100, 4096, 4096, 0, backward)
+    assert size(100, 4096, 4096, 1, backward) < need
     wide = dict(n=4096, k=4096, ldx=4096, ldw=2048, ldy=4096)
     assert need > 0                                            # few tiles: the contraction is cut; rows may have to be laid out
     assert linear(backward, **wide, bytes=100) == BUDGET and linear(backward, **wide, scratch=None) == ARG and linear(backward, **wide, scratch=C.c_void_p(4100)) == ARG
     assert linear(backward, **dict(wide, ldx=4097), bytes=need - 1) == BUDGET        # rows that begin at any address
-    assert size(-1, 3, 3, backward) == 0 and size(0, 3, 3, backward) == 0 and size(5, 1 << 31, 3, backward) == 0
+    assert size(-1, 3, 3, 0, backward) == 0 and size(0, 3, 3, 0, backward) == 0 and size(5, 1 << 31, 3, 0, backward) == 0
     if not backward:
-        assert size(64, 512, 4096, 0) == 0 and linear(m=64, scratch=None, bytes=1, X=None) == ARG
+        assert size(64, 512, 4096, 0, 0) == 0 and linear(m=64, scratch=None, bytes=1, X=None) == ARG
 
 
 def test_operands_on_several_devices_are_refused(two_devices):  # noqa: F811
