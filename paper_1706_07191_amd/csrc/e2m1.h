@@ -84,23 +84,11 @@ __device__ __forceinline__ void load1_to_lds(uint32_t dst, const void* base, uin
 }
 #pragma clang diagnostic pop
 
-// A tile product like TileProduct's (its order of slots, fragments and sums) whose P is a matrix in 4 bits.  A step takes 256 x 64 numbers of it, two groups of 256 rows
-// (kRows) or eight groups of 64 rows (kCols), a group a thread.  Pieces of 16 bytes and their scales go straight into a ring in LDS, NB + 1 steps ahead; behind the
-// workgroup's barrier in step t each thread makes 32 numbers of 16 bits of its own group of step t + 2 and writes them, where Stager would put them, into the buffer that has
-// just been read.  So all loads are counted in the order they were sent, and the barrier waits only for those of the step that comes next; Q's tiles are NB deep.
-// W's rows begin at 16-byte addresses.
-template <class El, int NQ_, Order O>
-struct E2m1Product {
-  static constexpr int NP = 8, NQ = NQ_, WP = 2, WQ = 4;
-  static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
-  static constexpr int NB = NQ == 4 ? 2 : NQ == 2 ? 3 : 4;
-  static constexpr int kP = BP * kStepBytes, kQ = BQ * kStepBytes, kRing = kThreads * 20;
-  static constexpr int kLds = 2 * kP + NB * kQ + NB * kRing;
-  using StageQ = Stager<El, kRows, BQ, kThreads, true>;
-  static constexpr int PARTS = StageQ::kLoads;
-
-  StageQ sq;
-  char* lds;
+// What brings a matrix in 4 bits into LDS for tile products.  A step takes 64 numbers of the contraction: of 256 rows two groups each (kRows), or of 64 rows eight groups each
+// (kCols); a group a thread.  Its 16 bytes and its scale, a word, go straight into a slot of a ring.  Rows begin at 16-byte addresses.
+template <Order O>
+struct E2m1Feed {
+  static constexpr int kThreads = 512, kSlot = kThreads * 20, kLoads = 2;      // bytes; loads of a wave for a step
   int64_t k;                         // of the contraction
   const uint8_t *at, *scale_at;      // of the next step, the same in all lanes
   uint32_t off, scale_off;
@@ -112,18 +100,10 @@ struct E2m1Product {
     uint4 w;
     uint32_t s;
   };
-  __device__ __forceinline__ int steps() const { return (int)((k + 63) / 64); }
-  __device__ __forceinline__ char* p_tile(int t) const { return lds + (t & 1) * kP; }
-  __device__ __forceinline__ char* q_tile(int slot) const { return lds + 2 * kP + slot * kQ; }
-  __device__ __forceinline__ char* ring(int slot) const { return lds + 2 * kP + NB * kQ + slot * kRing; }
-  // Whether all of a step's pieces are there in whole: a row's last piece may lie on memory behind the matrix in its last row only
-  __device__ __forceinline__ bool plain(int t) const {
-    const int64_t left = k - (int64_t)t * 64;
-    return left >= 64 && !(O == kCols && ragged && left <= 64);
-  }
-  __device__ __forceinline__ void init(const E2m1Operand& op, int64_t first, int64_t k0) {
+  __device__ __forceinline__ void init(const E2m1Operand& op, int64_t first, int64_t k0, int64_t k1) {
     const int tid = threadIdx.x;
     const int64_t left = op.n - first;
+    k = scalar(k1 - k0);
     if (O == kRows) {
       const int64_t row = tid >> 1, r = row < left ? row : left - 1;
       at = op.base + first * op.ld + k0 / 2;
@@ -140,7 +120,7 @@ struct E2m1Product {
       scale_at = op.scales + k0 * op.groups + first / kGroup;
       step = 64 * op.ld;
       scale_step = 64 * op.groups;
-      ragged = left < BP && left % kGroup != 0;
+      ragged = left < 256 && left % kGroup != 0;
       valid = (int32_t)(left - kGroup * c < kGroup ? left - kGroup * c : kGroup);
       off = (uint32_t)(row * op.ld + 16 * c);
       scale_off = (uint32_t)(row * op.groups + c);
@@ -149,6 +129,12 @@ struct E2m1Product {
     scale_at = (const uint8_t*)scalar((int64_t)scale_at);
     step = scalar(step);
     scale_step = scalar(scale_step);
+  }
+  __device__ __forceinline__ int steps() const { return (int)((k + 63) / 64); }
+  // Whether all of a step's pieces are there in whole: a row's last piece may lie on memory behind the matrix in its last row only
+  __device__ __forceinline__ bool plain(int t) const {
+    const int64_t left = k - (int64_t)t * 64;
+    return left >= 64 && !(O == kCols && ragged && left <= 64);
   }
   // This thread's group of step t, which is the next
   __device__ __forceinline__ Group fetch(int t) {
@@ -161,7 +147,7 @@ struct E2m1Product {
     scale_at += scale_step;
     return x;
   }
-  __device__ __forceinline__ void send_group(int t, char* to) {
+  __device__ __forceinline__ void send(int t, char* to) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (plain(t)) {
       load_to_lds(lds_address(to) + 1024 * wave, (const char*)scalar((int64_t)at), off);
@@ -174,76 +160,187 @@ struct E2m1Product {
       *(uint32_t*)(to + kThreads * 16 + 4 * tid) = x.s;
     }
   }
-  __device__ __forceinline__ Group group_in(const char* from) const {
+  static __device__ __forceinline__ Group mine(const char* slot) {
     const int tid = threadIdx.x;
-    return Group{*(const uint4*)(from + 16 * tid), *(const uint32_t*)(from + kThreads * 16 + 4 * tid)};
+    return Group{*(const uint4*)(slot + 16 * tid), *(const uint32_t*)(slot + kThreads * 16 + 4 * tid)};
   }
-  // Eight of a group's numbers to where fragments of them are read
-  __device__ __forceinline__ void make_part(char* tile, const Group& x, int i) const {
-    const int tid = threadIdx.x;
-    const uint32_t w = i == 0 ? x.w.x : i == 1 ? x.w.y : i == 2 ? x.w.z : x.w.w;
-    uint32_t to;
-    if (O == kRows) {
-      const int row = tid >> 1;
-      to = row * kStepBytes + 16 * ((4 * (tid & 1) + i) ^ (row & 7));
-    } else {
-      const int row = tid >> 3, src = 4 * (tid & 7) + i;
-      to = row * (2 * BP) + 16 * (((src >> 1) ^ (Stager<El, kCols, BP, kThreads, true>::mix(row) & 15)) * 2 + (src & 1));
-    }
-    *(uint4*)(tile + to) = eight_e2m1<El>(w, scale_e8m0(x.s));
-  }
-  // The workgroup's barrier.  ahead: steps whose loads may still be on their way, sent in full, and the groups of the one before them.
-  template <int AHEAD>
-  static __device__ __forceinline__ void meet() {
-    __builtin_amdgcn_sched_barrier(0);
-    if (AHEAD >= 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD < 0 ? 0 : AHEAD) * (PARTS + 2) + 2) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  __device__ __forceinline__ void send_q(int t, char* to) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    sq.load(to, threadIdx.x, wave, k - (int64_t)t * 64);
-  }
+};
 
-  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const E2m1Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds_) {
-    E2m1Product x;
-    x.lds = lds_;
-    x.k = scalar(k1 - k0);
-    x.init(P, p0, k0);
-    x.sq.init(Q, q0, k0, threadIdx.x);
-    x.multiply(acc);
-  }
-  __device__ __forceinline__ void multiply(floatx4 (&acc)[NP][NQ]) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP, steps = this->steps();
+// The workgroup's barrier; up to LOADS of a wave's loads may still be on their way.
+template <int LOADS>
+__device__ __forceinline__ void meet_but() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tile products like TileProduct's (its slots, its fragments of Q, its sums) whose P is a matrix in 4 bits.  E2m1Product<.., kRows>: fragments of P are made where they are
+// multiplied.  Of a row's 64 numbers in a step lane group g has the 16 from 32 (g & 1) + 16 (g >> 1) on, one read of eight bytes for both halves of the step, and one
+// scale; Q's fragments are read in the same order.  That reads 14 KiB from LDS a wave and step, where fragments of 16 bits are 24, and
+// leaves room for NB steps in LDS: the barrier waits for the step that comes next only.
+template <class El, int NQ_, Order O> struct E2m1Product;
+template <class El, int NQ_>
+struct E2m1Product<El, NQ_, kRows> {
+  static constexpr int NP = 8, NQ = NQ_, WP = 2, WQ = 4;
+  static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
+  using Feed = E2m1Feed<kRows>;
+  using StageQ = Stager<El, kRows, BQ, kThreads, true>;
+  static constexpr int NB = NQ == 4 ? 3 : NQ == 2 ? 4 : 6, kQ = BQ * kStepBytes, kPart = kQ + Feed::kSlot, LOADS = StageQ::kLoads + Feed::kLoads;
+  static constexpr int kLds = NB * kPart > BQ * 512 ? NB * kPart : BQ * 512;        // put_tile16 takes BQ rows of 512 bytes
+
+  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const E2m1Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
     constexpr int SLOTS = 2 * NP, MEET = SLOTS - 4;
+    Feed feed;
+    StageQ sq;
+    feed.init(P, p0, k0, k1);
+    sq.init(Q, q0, k0, tid);
+    const int steps = feed.steps();
+    auto left = [&](int t) { return feed.k - (int64_t)t * 64; };
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
       for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
-    if (steps == 0) return;
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+      if (steps > t) {
+        sq.load(lds + t * kPart, tid, wave, left(t));
+        feed.send(t, lds + t * kPart + kQ);
+      }
+    uint2 w[NP];
+    uint32_t s[NP];
+    int4v fq[2][NQ];
+    const int row = lane & 15, g = lane >> 4;
+    uint32_t bp = 32 * (16 * wp * NP + row) + 16 * (g & 1) + 8 * (g >> 1), bs = kThreads * 16 + 8 * (16 * wp * NP + row) + 4 * (g & 1);
+    uint32_t bq = (16 * wq * NQ + row) * kStepBytes + 16 * ((4 * (g & 1) + 2 * (g >> 1)) ^ (row & 7));
+    auto read_p = [&](const char* part, int p) {
+      w[p] = *(const uint2*)(part + kQ + bp + 512 * p);
+      s[p] = *(const uint32_t*)(part + kQ + bs + 128 * p);
+    };
+    auto read_q = [&](const char* part, int kk, int q) { fq[kk][q] = *(const int4v*)(part + (bq ^ (16 * kk)) + q * 16 * kStepBytes); };
+    if (steps >= NB && feed.plain(NB - 1)) meet_but<(NB - 1) * LOADS>();
+    else meet_but<0>();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read_p(lds, i);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) read_q(lds, 0, q);
+    int slot = 0;                // t % NB
+    for (int t = 0; t < steps; ++t) {
+      slot = __builtin_amdgcn_readfirstlane(slot);
+      const int next = slot == NB - 1 ? 0 : slot + 1;
+      char* cur = lds + slot * kPart;
+      const char* nxt = lds + next * kPart;
+      const bool more = t + 1 < steps, sends = t + NB < steps;
+      bool parts = false;
+      asm volatile("" : "+v"(bp), "+v"(bq), "+v"(bs));      // addresses are worked out from these where they are used, not kept
+#pragma unroll
+      for (int i = 0; i < SLOTS; ++i) {
+        if (i < 4) {
+          read_p(cur, i + 4);
+          if (i < NQ) read_q(cur, 1, i);
+        } else if (i == MEET) {
+          if (t + NB - 1 < steps && feed.plain(t + NB - 1)) meet_but<(NB - 2) * LOADS>();
+          else meet_but<0>();
+          parts = sends && feed.plain(t + NB);
+          if (sends && !parts) {
+            sq.load(cur, tid, wave, left(t + NB));
+            feed.send(t + NB, cur + kQ);
+          }
+        }
+        if (i >= MEET) {
+          if (parts && i - MEET < StageQ::kLoads) sq.load_part(cur, wave, i - MEET);
+          if (parts && i == SLOTS - 1) {
+            sq.next();
+            feed.send(t + NB, cur + kQ);
+          }
+          if (more) {
+            read_p(nxt, i - MEET);
+            if (i - MEET < NQ) read_q(nxt, 0, i - MEET);
+          }
+        }
+        const int p = i & 7, kk = i >> 3;
+        // raw numbers of tile rows 0 to 3 are replaced from MEET on, their last use is before
+        const int4v f = __builtin_bit_cast(int4v, eight_e2m1<El>(kk ? w[p].y : w[p].x, scale_e8m0(s[p])));
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          acc[p][q] = mfma16<El>(f, fq[kk][q], acc[p][q]);
+          settle(acc[p][q]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      slot = next;
+    }
+    meet_but<0>();
+  }
+};
+
+// E2m1Product<.., kCols>: the contraction runs down W's rows, a fragment has numbers of eight of them, with scales of their own.  So behind the workgroup's barrier in
+// step t each thread makes 32 numbers of 16 bits of its group of step t + 2 and writes them where Stager would put them, into the buffer that has just been read; the groups
+// come NB + 2 steps ahead, Q's tiles NB.
+template <class El, int NQ_>
+struct E2m1Product<El, NQ_, kCols> {
+  static constexpr int NP = 8, NQ = NQ_, WP = 2, WQ = 4;
+  static constexpr int BP = 16 * NP * WP, BQ = 16 * NQ * WQ, kThreads = 64 * WP * WQ;
+  using Feed = E2m1Feed<kCols>;
+  using Group = Feed::Group;
+  using StageQ = Stager<El, kRows, BQ, kThreads, true>;
+  static constexpr int NB = NQ == 4 ? 2 : NQ == 2 ? 3 : 4;
+  static constexpr int kP = BP * kStepBytes, kQ = BQ * kStepBytes, kLds = 2 * kP + NB * kQ + NB * Feed::kSlot, LOADS = StageQ::kLoads + Feed::kLoads;
+
+  // Eight of a group's numbers to where fragments of them are read.  Threads of a row write its eight groups, in turns so that they meet no bank twice: `x` comes turned by
+  // half the group's number.
+  static __device__ __forceinline__ Group turned(Group x) {
+    const int r = threadIdx.x >> 1;
+    const uint32_t a = r & 1 ? x.w.y : x.w.x, b = r & 1 ? x.w.z : x.w.y, c = r & 1 ? x.w.w : x.w.z, d = r & 1 ? x.w.x : x.w.w;
+    return Group{r & 2 ? make_uint4(c, d, a, b) : make_uint4(a, b, c, d), x.s};
+  }
+  static __device__ __forceinline__ void make_part(char* tile, const Group& x, int i) {
+    const int tid = threadIdx.x, row = tid >> 3, src = 4 * (tid & 7) + ((i + (tid >> 1)) & 3);
+    const uint32_t w = i == 0 ? x.w.x : i == 1 ? x.w.y : i == 2 ? x.w.z : x.w.w;
+    *(uint4*)(tile + row * (2 * BP) + 16 * (((src >> 1) ^ (Stager<El, kCols, BP, kThreads, true>::mix(row) & 15)) * 2 + (src & 1))) = eight_e2m1<El>(w, scale_e8m0(x.s));
+  }
+
+  static __device__ __forceinline__ void run(floatx4 (&acc)[NP][NQ], const E2m1Operand& P, int64_t p0, const Operand& Q, int64_t q0, int64_t k0, int64_t k1, char* lds) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wq = wave / WP;
+    constexpr int SLOTS = 2 * NP, MEET = SLOTS - 4;
+    Feed feed;
+    StageQ sq;
+    feed.init(P, p0, k0, k1);
+    sq.init(Q, q0, k0, tid);
+    const int steps = feed.steps();
+    auto left = [&](int t) { return feed.k - (int64_t)t * 64; };
+    auto p_tile = [&](int t) { return lds + (t & 1) * kP; };
+    auto q_tile = [&](int slot) { return lds + 2 * kP + slot * kQ; };
+    auto ring = [&](int slot) { return lds + 2 * kP + NB * kQ + slot * Feed::kSlot; };
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) acc[p][q] = floatx4{0.f, 0.f, 0.f, 0.f};
     {
       // the first two steps' groups through registers, all else behind them
       Group x[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (steps > t) x[t] = fetch(t);
+        if (steps > t) x[t] = feed.fetch(t);
 #pragma unroll
       for (int t = 0; t < NB; ++t)
-        if (steps > t) send_q(t, q_tile(t));
+        if (steps > t) sq.load(q_tile(t), tid, wave, left(t));
 #pragma unroll
       for (int t = 2; t < NB + 2; ++t)
-        if (steps > t) send_group(t, ring(t % NB));
+        if (steps > t) feed.send(t, ring(t % NB));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (steps > t)
+        if (steps > t) {
+          x[t] = turned(x[t]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) make_part(p_tile(t), x[t], i);
+        }
     }
     int4v fp[8], fq[2][NQ];
-    uint32_t bp = fragment_base<O, BP>(16 * wp * NP, lane), bq = fragment_base<kRows, BQ>(16 * wq * NQ, lane);
-    auto read_p = [&](const char* tile, int slot) { fp[slot & 7] = fragment<O, BP>(tile, bp, slot & 7, slot >> 3); };
+    uint32_t bp = fragment_base<kCols, BP>(16 * wp * NP, lane), bq = fragment_base<kRows, BQ>(16 * wq * NQ, lane);
+    auto read_p = [&](const char* tile, int slot) { fp[slot & 7] = fragment<kCols, BP>(tile, bp, slot & 7, slot >> 3); };
     auto read_q = [&](const char* tile, int kk, int q) { fq[kk][q] = fragment<kRows, BQ>(tile, bq, q, kk); };
-    meet<-1>();
+    meet_but<0>();
 #pragma unroll
     for (int i = 0; i < 4; ++i) read_p(p_tile(0), i);
 #pragma unroll
@@ -270,25 +367,26 @@ struct E2m1Product {
         } else if (s < 10) {
           read_p(pc, s + 6);
         } else if (s == MEET) {
-          if (t + 1 + NB < steps && plain(t + 1 + NB)) meet<NB - 2>();
-          else meet<-1>();
-          if (makes) x = group_in(ring(rslot));
-          parts = sends && plain(t + NB);
-          if (sends && !parts) send_q(t + NB, qc);
+          // all loads but those sent since the ones for Q's next tile: its groups, and the steps after it
+          if (t + 1 + NB < steps && feed.plain(t + 1 + NB)) meet_but<(NB - 2) * LOADS + Feed::kLoads>();
+          else meet_but<0>();
+          if (makes) x = Feed::mine(ring(rslot));
+          parts = sends && feed.plain(t + NB);
+          if (sends && !parts) sq.load(qc, tid, wave, left(t + NB));
         }
         if (s >= MEET) {
-          if (parts && s - MEET < PARTS) sq.load_part(qc, wave, s - MEET);
-          if (parts && s == MEET + PARTS - 1) sq.next();
+          if (parts && s - MEET < StageQ::kLoads) sq.load_part(qc, wave, s - MEET);
+          if (parts && s == MEET + StageQ::kLoads - 1) sq.next();
           if (more) {
             read_p(pn, s - MEET);
             if (s - MEET < NQ) read_q(qn, 0, s - MEET);
           }
           if (makes) {
-            if (s == MEET + 1) make_part(pc, x, 0);
+            if (s == MEET + 1) x = turned(x), make_part(pc, x, 0);
             if (s == MEET + 2) make_part(pc, x, 1), make_part(pc, x, 2);
             if (s == MEET + 3) make_part(pc, x, 3);
           }
-          if (s == SLOTS - 1 && groups) send_group(t + NB + 2, ring(rslot));
+          if (s == SLOTS - 1 && groups) feed.send(t + NB + 2, ring(rslot));
         }
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
@@ -300,7 +398,7 @@ struct E2m1Product {
       slot = next;
       rslot = rslot == NB - 1 ? 0 : rslot + 1;
     }
-    meet<-1>();
+    meet_but<0>();
   }
 };
 

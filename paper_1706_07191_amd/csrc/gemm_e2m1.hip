@@ -122,6 +122,7 @@ template <class El, int NQ, Order O>
 __global__ void __launch_bounds__(512, 2)
 k_tiles_e2m1(const E2m1Args g) {
   using T = E2m1Product<El, NQ, O>;
+  static_assert(T::kLds >= T::BQ * 512, "put_tile16");
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
   if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
