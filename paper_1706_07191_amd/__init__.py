@@ -795,29 +795,41 @@ def _dense_order(t):
 def _tensors(tensors, name, like=None):
     """(array of brsvd_tensor, count) of a list of tensors; like: those whose numbers have to be in the same order."""
     import array
-    if isinstance(tensors, torch.Tensor) or not isinstance(tensors, (list, tuple)):
+    from operator import attrgetter
+    if not isinstance(tensors, (list, tuple)):
         raise TypeError(f"{name} must be a list of CUDA tensors")
+    n = len(tensors)
     if not _CODES:
         _CODES.update({torch.float32: BRSVD_DTYPE_F32, torch.bfloat16: BRSVD_DTYPE_BF16, torch.float16: BRSVD_DTYPE_F16})
-    if like is not None and len(like) != len(tensors):
-        raise ValueError(f"{name} has {len(tensors)} tensors, expected {len(like)}")
-    flat = []
+    if like is not None and len(like) != n:
+        raise ValueError(f"{name} has {n} tensors, expected {len(like)}")
+    T, flat = torch.Tensor, [1] * (5 * n)
+    try:
+        # lists are long, and each of these goes through one without a step of Python for a tensor
+        plain = (all(map(attrgetter("is_cuda"), tensors)) and all(map(T.is_contiguous, tensors))
+                 and (like is None or (all(map(T.is_contiguous, like)) and list(map(attrgetter("shape"), tensors)) == list(map(attrgetter("shape"), like)))))
+        if plain:
+            flat[0::5] = map(T.data_ptr, tensors)
+            flat[2::5] = flat[3::5] = list(map(T.numel, tensors))
+            flat[4::5] = map(_CODES.__getitem__, map(attrgetter("dtype"), tensors))
+            return array.array("q", flat), n
+    except (TypeError, KeyError, AttributeError, RuntimeError):
+        pass
     for i, t in enumerate(tensors):
         if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided or t.dtype not in _CODES:
             raise TypeError(f"{name}[{i}] must be a CUDA tensor of dtype torch.float32, torch.bfloat16 or torch.float16")
         other = t if like is None else like[i]
-        if other is not t and other.shape != t.shape:
-            raise TypeError(f"{name}[{i}] has shape {tuple(t.shape)}, expected {tuple(other.shape)}")
-        n = t.numel()
-        if (t.is_contiguous() and (other is t or other.is_contiguous())) or not n:
-            flat += (t.data_ptr(), 1, n, n, _CODES[t.dtype])
-        elif t.dim() == 2 and all(x.stride(1) == 1 and x.stride(0) >= x.shape[1] for x in (t, other)):
-            flat += (t.data_ptr(), t.shape[0], t.shape[1], t.stride(0), _CODES[t.dtype])
-        elif _dense_order(t) is not None and _dense_order(other) == t.stride():
-            flat += (t.data_ptr(), 1, n, n, _CODES[t.dtype])
-        else:
-            raise TypeError(f"{name}[{i}] must be dense, or a matrix with unit column stride" + ("" if like is None else ", laid out as its original"))
-    return array.array("q", flat), len(tensors)
+        if not isinstance(other, torch.Tensor) or other.layout is not torch.strided or other.shape != t.shape:
+            raise TypeError(f"{name}[{i}] has shape {tuple(t.shape)}, expected {tuple(other.shape) if isinstance(other, torch.Tensor) else other}")
+        numbers = t.numel()
+        rows, cols, ld = 1, numbers, numbers
+        if not (t.is_contiguous() and other.is_contiguous()) and numbers:
+            if t.dim() == 2 and all(x.stride(1) == 1 and x.stride(0) >= x.shape[1] for x in (t, other)):
+                rows, cols, ld = t.shape[0], t.shape[1], t.stride(0)
+            elif _dense_order(t) is None or _dense_order(other) != t.stride():
+                raise TypeError(f"{name}[{i}] must be dense, or a matrix with unit column stride" + ("" if like is None else ", laid out as its original"))
+        flat[5 * i:5 * i + 5] = t.data_ptr(), rows, cols, ld, _CODES[t.dtype]
+    return array.array("q", flat), n
 
 
 @_scoped

@@ -1,7 +1,7 @@
 // The norm over many tensors, and the tensors clipped by it:
 //   norm = |scale| sqrt(sum of x^2 over all numbers of all tensors),    y = x scale min(1, max_norm / norm)
-// Squares and their sums are fp64: neither a number of 1e30 nor one of 1e-30 is lost, and no order of a long sum shows.  A workgroup takes a piece of at most kPiece
-// numbers of one tensor; the pieces' sums are added in their order.
+// Squares and their sums are fp64: neither a number of 1e30 nor one of 1e-30 is lost, and no order of a long sum shows.  A workgroup takes a piece of one
+// tensor; the pieces' sums are added in their order.
 //
 // The tensors' addresses and sizes are arguments of the launches, as many tensors at a time as those hold: nothing is copied to the device, and a captured launch keeps them.
 #include <algorithm>
@@ -12,7 +12,10 @@
 namespace brsvd {
 
 constexpr int kTensors = 64;                  // of a launch
-constexpr int64_t kPiece = 1 << 15;           // numbers of a workgroup
+// Numbers of a piece: so many that there are some 2000 pieces, within these bounds.  10 tensors of 155 000 numbers: squares 4.3 us in pieces of 2^12, 8.0 in pieces of 2^15.
+// 740 million bf16 numbers into fp32, 7 launches: pieces of 2^15 140 us a launch, 2^14 131, 2^13 125, as the last round of workgroups is a smaller part; the norm's sums
+// are added by one workgroup, which has 16 us to do for 2^13 and 10 for 2^14.
+constexpr int64_t kLeastPiece = 1 << 12, kNormPiece = 1 << 14, kClipPiece = 1 << 13;
 
 // Tensors of a launch, and which pieces are theirs: those of tensor i are first[i] to first[i + 1].
 struct TensorList {
@@ -24,28 +27,59 @@ struct TensorList {
   int32_t rows[kTensors];      // rows, where pieces have several
   uint32_t first[kTensors + 1];
   uint8_t tx[kTensors], ty[kTensors];
-  int count;
+  int count, piece;
 };
 
 static int bytes_of(int dtype) { return dtype == BRSVD_DTYPE_F32 ? 4 : dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16 ? 2 : 0; }
 
-// Eight numbers of type dtype from `src`, `valid` of them there, the others zero
-__device__ __forceinline__ void eight_numbers(const char* src, int64_t valid, int dtype, float (&x)[8]) {
-  if (dtype == BRSVD_DTYPE_F32) {
-    const uint4 a = piece_of<4>(src, 4 * valid), b = piece_of<4>(src + 16, 4 * valid - 16);
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+// W numbers of a type as they lie in memory
+template <int DT, int W> struct Some {
+  static constexpr int kNumber = DT == BRSVD_DTYPE_F32 ? 4 : 2, kWords = W * kNumber / 4;
+  struct __attribute__((packed, aligned(1))) Words { uint32_t x[kWords]; };
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const char* src, int64_t valid) {       // valid of them are there, the others zero
+    if (valid >= W) {
+      const Words v = *(const Words*)src;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
-  } else {
-    const uint4 a = piece_of<2>(src, 2 * valid);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+      for (int i = 0; i < kWords; ++i) w[i] = v.x[i];
+    } else {
+      const uint4 v = piece_of<kNumber>(src, kNumber * valid);
+      const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint16_t h = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-      x[i] = dtype == BRSVD_DTYPE_BF16 ? from16<Bf16>(h) : from16<Fp16>(h);
+      for (int i = 0; i < kWords; ++i) w[i] = x[i];
     }
   }
-}
+  __device__ __forceinline__ float number(int i) const {
+    if (kNumber == 4) return __uint_as_float(w[i % kWords]);
+    const uint16_t h = (uint16_t)(w[(i >> 1) % kWords] >> (16 * (i & 1)));
+    return DT == BRSVD_DTYPE_BF16 ? from16<Bf16>(h) : from16<Fp16>(h);
+  }
+  static __device__ __forceinline__ void put(char* to, int64_t left, const float (&x)[W]) {
+    uint32_t v[kWords];
+    if (kNumber == 4) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) v[i] = __float_as_uint(x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i)
+        v[i] = DT == BRSVD_DTYPE_BF16 ? to16<Bf16>(x[2 * i % W]) | (uint32_t)to16<Bf16>(x[(2 * i + 1) % W]) << 16
+                                      : to16<Fp16>(x[2 * i % W]) | (uint32_t)to16<Fp16>(x[(2 * i + 1) % W]) << 16;
+    }
+    if (left >= W) {
+      Words o;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) o.x[i] = v[i];
+      *(Words*)to = o;
+    } else {
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        if (j < left) {
+          if (kNumber == 4) ((uint32_t*)to)[j] = v[j % kWords];
+          else ((uint16_t*)to)[j] = (uint16_t)(v[j / 2] >> (16 * (j & 1)));
+        }
+    }
+  }
+};
 
 // Which tensor a piece is of: the last one that begins at or before it
 __device__ __forceinline__ int tensor_of(const TensorList& l, uint32_t piece) {
@@ -56,20 +90,32 @@ __device__ __forceinline__ int tensor_of(const TensorList& l, uint32_t piece) {
   return __builtin_amdgcn_readfirstlane(at);
 }
 
-// Calls take(row, column, numbers of the row from there on, at most eight) for all eights of a piece; threads take neighbouring ones.
-template <class Take>
-__device__ __forceinline__ void eights_of(const TensorList& l, int i, uint32_t piece, Take take) {
+// Calls take(W numbers, row, column, numbers of the row from there on) for all of a piece; threads take neighbouring ones, 64 bytes a thread on their way.
+template <int DT, int W, class Take>
+__device__ __forceinline__ void all_of(const TensorList& l, int i, uint32_t piece, Take take) {
+  constexpr int EB = Some<DT, W>::kNumber, U = 64 / (W * EB), kStep = 256 * W;
   const uint32_t p = piece - l.first[i];
   const int64_t cols = l.cols[i];
+  Some<DT, W> x[U];
   if (l.rows_per[i] == 0) {
-    const uint32_t per = (uint32_t)((cols + kPiece - 1) / kPiece), row = p / per;
-    const int64_t c0 = (int64_t)(p - row * per) * kPiece, left = cols - c0 < kPiece ? cols - c0 : kPiece;
-    for (int c = 8 * threadIdx.x; c < left; c += 8 * 256) take((int64_t)row, c0 + c, left - c);
+    const uint32_t per = (uint32_t)((cols + l.piece - 1) / l.piece), row = p / per;
+    const int64_t c0 = (int64_t)(p - row * per) * l.piece, there = cols - c0 < l.piece ? cols - c0 : l.piece;
+    const char* from = l.x[i] + (row * l.ldx[i] + c0) * EB;
+    const int left = (int)there;
+    for (int c = W * threadIdx.x; c < left; c += kStep * U) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c + kStep * u < left) x[u].load(from + (int64_t)(c + kStep * u) * EB, left - c - kStep * u);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c + kStep * u < left) take(x[u], (int64_t)row, c0 + c + kStep * u, (int64_t)(left - c - kStep * u));
+    }
   } else {
-    const uint32_t eights = (uint32_t)((cols + 7) / 8), r0 = p * l.rows_per[i], rows = l.rows[i] - r0 < (uint32_t)l.rows_per[i] ? l.rows[i] - r0 : l.rows_per[i];
-    for (uint32_t e = threadIdx.x; e < rows * eights; e += 256) {
-      const uint32_t r = e / eights, c = 8 * (e - r * eights);
-      take((int64_t)(r0 + r), (int64_t)c, cols - c);
+    const uint32_t some = (uint32_t)((cols + W - 1) / W), r0 = p * l.rows_per[i], rows = l.rows[i] - r0 < (uint32_t)l.rows_per[i] ? l.rows[i] - r0 : l.rows_per[i];
+    for (uint32_t e = threadIdx.x; e < rows * some; e += 256) {
+      const uint32_t r = e / some, c = W * (e - r * some);
+      x[0].load(l.x[i] + ((int64_t)(r0 + r) * l.ldx[i] + c) * EB, cols - c);
+      take(x[0], (int64_t)(r0 + r), (int64_t)c, cols - c);
     }
   }
 }
@@ -84,18 +130,26 @@ __device__ __forceinline__ double sum_of_workgroup(double x, double* red) {
   return sum;
 }
 
+template <int DT>
+__device__ __forceinline__ double squares_of(const TensorList& l, int i, uint32_t piece) {
+  constexpr int W = DT == BRSVD_DTYPE_F32 ? 4 : 8;
+  double sum[2] = {0.0, 0.0};
+  all_of<DT, W>(l, i, piece, [&](const Some<DT, W>& x, int64_t, int64_t, int64_t) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      const double v = x.number(j);
+      sum[j & 1] = fma(v, v, sum[j & 1]);
+    }
+  });
+  return sum[0] + sum[1];
+}
+// Bound by memory.
 __global__ void __launch_bounds__(256)
 k_grad_squares(const TensorList l, double* __restrict__ sums) {
   __shared__ double red[4];
-  const int i = tensor_of(l, blockIdx.x);
-  const int dtype = l.tx[i], eb = dtype == BRSVD_DTYPE_F32 ? 4 : 2;
-  double sum = 0.0;
-  eights_of(l, i, blockIdx.x, [&](int64_t r, int64_t c, int64_t left) {
-    float x[8];
-    eight_numbers(l.x[i] + (r * l.ldx[i] + c) * eb, left, dtype, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum = fma((double)x[j], (double)x[j], sum);
-  });
+  const int i = tensor_of(l, blockIdx.x), dtype = l.tx[i];
+  double sum = dtype == BRSVD_DTYPE_F32 ? squares_of<BRSVD_DTYPE_F32>(l, i, blockIdx.x) : dtype == BRSVD_DTYPE_BF16 ? squares_of<BRSVD_DTYPE_BF16>(l, i, blockIdx.x)
+                                                                                                                   : squares_of<BRSVD_DTYPE_F16>(l, i, blockIdx.x);
   sum = sum_of_workgroup(sum, red);
   if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
@@ -104,14 +158,40 @@ __global__ void __launch_bounds__(1024)
 k_grad_norm(const double* __restrict__ sums, int64_t n, double scale, float* __restrict__ norm) {
   __shared__ double red[16];
   double sum = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) sum += sums[i];
+  int64_t i = threadIdx.x;
+  for (; i + 7 * 1024 < n; i += 8 * 1024) {
+    double x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = sums[i + 1024 * j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += x[j];
+  }
+  for (; i < n; i += 1024) sum += sums[i];
   sum = sum_of_workgroup(sum, red);
   if (threadIdx.x == 0) *norm = (float)(sqrt(sum) * scale);
 }
 
+template <int DT, int DY>
+__device__ __forceinline__ void clip_piece(const TensorList& l, int i, uint32_t piece, float f1, float f2) {
+  constexpr int W = DT == BRSVD_DTYPE_F32 || DY == BRSVD_DTYPE_F32 ? 4 : 8;        // 16 bytes of the wider type: lanes write next to each other
+  all_of<DT, W>(l, i, piece, [&](const Some<DT, W>& x, int64_t r, int64_t c, int64_t left) {
+    float y[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) y[j] = x.number(j) * f1 * f2;
+    Some<DY, W>::put(l.y[i] + (r * l.ldy[i] + c) * Some<DY, W>::kNumber, left, y);
+  });
+}
+template <int DT>
+__device__ __forceinline__ void clip_into(const TensorList& l, int i, uint32_t piece, float f1, float f2) {
+  const int ty = l.ty[i];
+  if (ty == BRSVD_DTYPE_F32) clip_piece<DT, BRSVD_DTYPE_F32>(l, i, piece, f1, f2);
+  else if (ty == BRSVD_DTYPE_BF16) clip_piece<DT, BRSVD_DTYPE_BF16>(l, i, piece, f1, f2);
+  else clip_piece<DT, BRSVD_DTYPE_F16>(l, i, piece, f1, f2);
+}
+// Bound by memory.  In place and with nothing to do it reads nothing.
 __global__ void __launch_bounds__(256)
 k_grad_clip(const TensorList l, const float* __restrict__ norm, double scale, double max_norm) {
-  const int i = tensor_of(l, blockIdx.x);
+  const int i = tensor_of(l, blockIdx.x), tx = l.tx[i];
   const double n = *norm;
   // a norm that is no finite number says nothing about how long the gradients are: they are scaled alone
   const double f = n > max_norm && n <= 3.402823466e38 ? scale * (max_norm / n) : scale;
@@ -119,35 +199,9 @@ k_grad_clip(const TensorList l, const float* __restrict__ norm, double scale, do
   // in two factors, so that neither leaves fp32's range where the product does not
   const double a = fabs(f) < 0x1p-100 ? f * 0x1p100 : fabs(f) > 0x1p100 ? f * 0x1p-100 : f;
   const float f1 = (float)a, f2 = fabs(f) < 0x1p-100 ? 0x1p-100f : fabs(f) > 0x1p100 ? 0x1p100f : 1.f;
-  const int tx = l.tx[i], ty = l.ty[i], ex = tx == BRSVD_DTYPE_F32 ? 4 : 2, ey = ty == BRSVD_DTYPE_F32 ? 4 : 2;
-  eights_of(l, i, blockIdx.x, [&](int64_t r, int64_t c, int64_t left) {
-    float x[8];
-    eight_numbers(l.x[i] + (r * l.ldx[i] + c) * ex, left, tx, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x[j] * f1 * f2;
-    char* to = l.y[i] + (r * l.ldy[i] + c) * ey;
-    if (ty == BRSVD_DTYPE_F32) {
-      if (left >= 8) {
-        *(Piece*)to = Piece{{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}};
-        *(Piece*)(to + 16) = Piece{{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])}};
-      } else {
-#pragma unroll
-        for (int j = 0; j < 7; ++j)
-          if (j < left) ((float*)to)[j] = x[j];
-      }
-    } else {
-      uint16_t h[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[j] = ty == BRSVD_DTYPE_BF16 ? to16<Bf16>(x[j]) : to16<Fp16>(x[j]);
-      if (left >= 8) {
-        *(Piece*)to = Piece{{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16}};
-      } else {
-#pragma unroll
-        for (int j = 0; j < 7; ++j)
-          if (j < left) ((uint16_t*)to)[j] = h[j];
-      }
-    }
-  });
+  if (tx == BRSVD_DTYPE_F32) clip_into<BRSVD_DTYPE_F32>(l, i, blockIdx.x, f1, f2);
+  else if (tx == BRSVD_DTYPE_BF16) clip_into<BRSVD_DTYPE_BF16>(l, i, blockIdx.x, f1, f2);
+  else clip_into<BRSVD_DTYPE_F16>(l, i, blockIdx.x, f1, f2);
 }
 
 // A tensor as kernels take it: rows next to each other are one long row.
@@ -156,35 +210,45 @@ struct Shape {
   int rows_per;
   int64_t pieces;
 };
-static Shape shape_of(const brsvd_tensor& x, const brsvd_tensor* y) {
+static Shape shape_of(const brsvd_tensor& x, const brsvd_tensor* y, int64_t piece) {
   Shape s{x.rows, x.cols, 0, 0};
   if (x.rows == 0 || x.cols == 0) return s;
   if (x.rows == 1 || (x.ld == x.cols && (!y || y->ld == y->cols))) s.cols = x.rows * x.cols, s.rows = 1;
-  if (s.rows > 1 && s.cols < kPiece) {
-    s.rows_per = (int)(kPiece / s.cols);
+  if (s.rows > 1 && s.cols < piece) {
+    s.rows_per = (int)(piece / s.cols);
     s.pieces = ceil_div(s.rows, s.rows_per);
   } else {
-    s.pieces = s.rows * ceil_div(s.cols, kPiece);
+    s.pieces = s.rows * ceil_div(s.cols, piece);
   }
   return s;
 }
-constexpr int64_t kMaxNumbers = (int64_t)1 << 44, kMaxPieces = (int64_t)1 << 24;
-// Number of pieces of all tensors, -1 where one is refused
-static int64_t check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count) {
-  if (count < 0 || (count > 0 && !x)) return -1;
-  int64_t pieces = 0;
+constexpr int64_t kMaxNumbers = (int64_t)1 << 44, kMaxPieces = ((int64_t)1 << 24) - 1;      // of a launch, 256 threads each
+// A list's pieces of up to `most` numbers, of more where there are too many for a launch.  pieces < 0: a tensor is refused
+struct Pieces {
+  int64_t piece, pieces;
+};
+static Pieces check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, int64_t most) {
+  const Pieces refused{0, -1};
+  if (count < 0 || (count > 0 && !x)) return refused;
+  int64_t numbers = 0;
   for (int64_t i = 0; i < count; ++i) {
     for (int k = 0; k < (y ? 2 : 1); ++k) {
       const brsvd_tensor& t = k ? y[i] : x[i];
-      if (!bytes_of((int)t.dtype) || t.dtype != (int)t.dtype || t.rows < 0 || t.cols < 0 || t.rows != x[i].rows || t.cols != x[i].cols) return -1;
+      if (t.dtype != (int)t.dtype || !bytes_of((int)t.dtype) || t.rows < 0 || t.cols < 0 || t.rows != x[i].rows || t.cols != x[i].cols) return refused;
       if (t.rows == 0 || t.cols == 0) continue;
-      if (!t.data || t.cols > kMaxNumbers || t.rows > kMaxNumbers / t.cols || t.rows > INT32_MAX) return -1;
-      if (t.rows > 1 && (t.ld < t.cols || t.ld > kMaxNumbers / t.rows)) return -1;
+      if (!t.data || t.cols > kMaxNumbers || t.rows > kMaxNumbers / t.cols || t.rows > INT32_MAX) return refused;
+      if (t.rows > 1 && (t.ld < t.cols || t.ld > kMaxNumbers / t.rows)) return refused;
     }
-    pieces += shape_of(x[i], y ? y + i : nullptr).pieces;
-    if (pieces > kMaxPieces) return -1;
+    numbers += x[i].rows * x[i].cols;
+    if (numbers > kMaxNumbers) return refused;
   }
-  return pieces;
+  Pieces p{kLeastPiece, 0};
+  while ((p.piece < most && numbers > 2048 * p.piece) || numbers > p.piece << 22) p.piece *= 2;
+  for (int64_t i = 0; i < count; ++i) {
+    p.pieces += shape_of(x[i], y ? y + i : nullptr, p.piece).pieces;
+    if (p.pieces > kMaxPieces) return refused;
+  }
+  return p;
 }
 // Whether numbers of one tensor are another's too: an address of `out` twice, or that of another tensor; and one that is its own tensor's has to be laid out like it.
 static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count) {
@@ -207,9 +271,10 @@ static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t co
 }
 // launch(list, workgroups) for as many tensors at a time as a list holds
 template <class Launch>
-static void in_lists(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, Launch launch) {
+static void in_lists(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, int64_t piece, Launch launch) {
   TensorList l;
   l.count = 0;
+  l.piece = (int)piece;
   uint32_t pieces = 0;
   auto flush = [&] {
     if (pieces == 0) return;
@@ -219,7 +284,7 @@ static void in_lists(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count
     pieces = 0;
   };
   for (int64_t i = 0; i < count; ++i) {
-    const Shape s = shape_of(x[i], y ? y + i : nullptr);
+    const Shape s = shape_of(x[i], y ? y + i : nullptr, piece);
     if (s.pieces == 0) continue;
     const int c = l.count++;
     l.x[c] = (const char*)x[i].data;
@@ -243,33 +308,33 @@ static void in_lists(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count
 using namespace brsvd;
 
 extern "C" uint64_t brsvd_grad_norm_workspace_bytes(const brsvd_tensor* tensors, int64_t count) {
-  const int64_t pieces = check_list(tensors, nullptr, count);
+  const int64_t pieces = check_list(tensors, nullptr, count, kNormPiece).pieces;
   return pieces < 0 ? 0 : (uint64_t)(pieces + 32) / 32 * 256;
 }
 
 extern "C" int brsvd_grad_norm(const brsvd_tensor* tensors, int64_t count, float scale, float* norm, void* workspace, uint64_t workspace_bytes, void* stream) {
-  const int64_t pieces = check_list(tensors, nullptr, count);
-  if (pieces < 0 || !norm || !(fabsf(scale) <= 3.402823466e38f)) return BRSVD_ERR_ARG;
+  const Pieces p = check_list(tensors, nullptr, count, kNormPiece);
+  if (p.pieces < 0 || !norm || !(fabsf(scale) <= 3.402823466e38f)) return BRSVD_ERR_ARG;
   if (!workspace || (uintptr_t)workspace % 256) return BRSVD_ERR_ARG;
-  if (workspace_bytes < (uint64_t)(pieces + 32) / 32 * 256) return BRSVD_ERR_BUDGET;
+  if (workspace_bytes < (uint64_t)(p.pieces + 32) / 32 * 256) return BRSVD_ERR_BUDGET;
   hipStream_t s = (hipStream_t)stream;
   double* sums = (double*)workspace;
-  in_lists(tensors, nullptr, count, [&](const TensorList& l, unsigned grid) {
+  in_lists(tensors, nullptr, count, p.piece, [&](const TensorList& l, unsigned grid) {
     hipLaunchKernelGGL(k_grad_squares, dim3(grid), dim3(256), 0, s, l, sums);
     sums += grid;
   });
-  hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(1024), 0, s, (const double*)workspace, pieces, fabs((double)scale), norm);
+  hipLaunchKernelGGL(k_grad_norm, dim3(1), dim3(1024), 0, s, (const double*)workspace, p.pieces, fabs((double)scale), norm);
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
 }
 
 extern "C" int brsvd_grad_clip(const brsvd_tensor* tensors, const brsvd_tensor* out, int64_t count, float scale, float max_norm, const float* norm, void* stream) {
-  const int64_t pieces = count > 0 && !out ? -1 : check_list(tensors, out, count);
-  if (pieces < 0 || !norm || !(fabsf(scale) <= 3.402823466e38f) || !(max_norm >= 0.f)) return BRSVD_ERR_ARG;
+  const Pieces p = count > 0 && !out ? Pieces{0, -1} : check_list(tensors, out, count, kClipPiece);
+  if (p.pieces < 0 || !norm || !(fabsf(scale) <= 3.402823466e38f) || !(max_norm >= 0.f)) return BRSVD_ERR_ARG;
   BRSVD_TRY(check_places(tensors, out, count));
-  if (pieces == 0) return BRSVD_OK;
+  if (p.pieces == 0) return BRSVD_OK;
   hipStream_t s = (hipStream_t)stream;
-  in_lists(tensors, out, count, [&](const TensorList& l, unsigned grid) {
+  in_lists(tensors, out, count, p.piece, [&](const TensorList& l, unsigned grid) {
     hipLaunchKernelGGL(k_grad_clip, dim3(grid), dim3(256), 0, s, l, norm, (double)scale, (double)max_norm);
   });
   BRSVD_HIP_TRY(hipGetLastError());
