@@ -125,13 +125,15 @@ k_tiles_e2m1(const E2m1Args g) {
   static_assert(T::kLds >= T::BQ * 512, "put_tile16");
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
-  const int64_t p0 = g.first + tp * T::BP, q0 = tq * T::BQ, k0 = blockIdx.y * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q * g.splits, 8, &tp, &tq)) return;
+  const int split = (int)((unsigned)tq / (unsigned)g.tiles_q);
+  tq -= split * g.tiles_q;
+  const int64_t p0 = g.first + tp * T::BP, q0 = tq * T::BQ, k0 = split * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
   floatx4 acc[T::NP][NQ];
   T::run(acc, g.W, p0, g.X, q0, k0, k1, lds);
   if (g.splits > 1) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % T::WP, wq = wave / T::WP;
-    float* C = (float*)g.C + (int64_t)blockIdx.y * g.X.n * g.cols;
+    float* C = (float*)g.C + (int64_t)split * g.X.n * g.cols;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const int64_t m = q0 + 16 * (wq * NQ + q) + (lane & 15);
@@ -160,33 +162,23 @@ void align_rows(const void* from, int64_t ld, int64_t rows, int64_t bytes, void*
 
 static uint64_t whole256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// A product of m rows and `cols` columns over a contraction of k.
 struct E2m1Plan {
   bool rows;                    // k_rows_e2m1
-  int nq;                       // rows of X in a tile, in 64, beside the large ones
-  int64_t large;                // columns in tiles of 256 rows, in 256
-  int splits;
-  int64_t per_split;
+  TilePlan tiles;
   uint64_t x, w, bytes;         // scratch: the parts at 0, X and W in aligned rows where they are laid out anew, all
 };
 // m rows of X, W n x k; aligned: rows of both begin at 16-byte addresses.
-static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k_, bool aligned, bool backward) {
-  const int64_t cols = backward ? k_ : n, k = backward ? n : k_;
+static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k, bool aligned, bool backward) {
+  static constexpr int kForward[3] = {62, 82, 150}, kBackward[3] = {85, 110, 165};      // 1/100 us a step, see tile_plan
+  const int64_t cols = backward ? k : n, in = backward ? n : k;
   E2m1Plan p;
   p.rows = !backward && m <= 64;
-  const int64_t tiles = ceil_div(cols, 256), steps = ceil_div(k, 64);
-  p.nq = m <= 64 ? 1 : 2;
-  p.large = m <= 128 ? 0 : large_tiles(tiles, ceil_div(m, 256), ceil_div(m, 128), steps);
-  const int64_t workgroups = p.large * ceil_div(m, 256) + (tiles - p.large) * ceil_div(m, 64 * p.nq);
-  int64_t s = p.rows ? 1 : 256 / workgroups;
-  if (s > steps / 8) s = steps / 8;
-  if (s > 16) s = 16;
-  if (s < 1) s = 1;
-  p.per_split = ceil_div(steps, s) * 64;
-  p.splits = (int)ceil_div(steps * 64, p.per_split);
-  p.x = p.splits > 1 ? whole256((uint64_t)p.splits * m * cols * 4) : 0;
-  p.w = p.x + (p.rows || aligned ? 0 : whole256((uint64_t)m * line_pitch(2 * k)));
-  p.bytes = p.w + (p.rows || aligned ? 0 : whole256((uint64_t)n * line_pitch((k_ + 1) / 2)));
+  p.tiles = tile_plan(ceil_div(cols, 256), m, ceil_div(in, 64), 1, m * cols, backward ? kBackward : kForward);
+  if (p.rows) p.tiles.splits = 1;
+  const bool laid = !p.rows && !aligned;
+  p.x = p.tiles.splits > 1 ? whole256((uint64_t)p.tiles.splits * m * cols * 4) : 0;
+  p.w = p.x + (laid ? whole256((uint64_t)m * line_pitch(2 * in)) : 0);
+  p.bytes = p.w + (laid ? whole256((uint64_t)n * line_pitch((k + 1) / 2)) : 0);
   return p;
 }
 
@@ -223,21 +215,20 @@ static void launch_rows(const E2m1Args& g, hipStream_t stream) {
 template <class El, int NQ, Order O>
 static void launch_tiles(E2m1Args g, hipStream_t stream) {
   g.tiles_q = ceil_div(g.X.n, 64 * NQ);
-  hipLaunchKernelGGL((k_tiles_e2m1<El, NQ, O>), dim3(tile_workgroups(g.tiles_p, g.tiles_q), (unsigned)g.splits), dim3(512), 0, stream, g);
+  hipLaunchKernelGGL((k_tiles_e2m1<El, NQ, O>), dim3(tile_workgroups(g.tiles_p, g.tiles_q * g.splits)), dim3(512), 0, stream, g);
 }
 template <class El, Order O>
-static void launch_tiles(E2m1Args g, const E2m1Plan& p, hipStream_t stream) {
-  const int64_t tiles = ceil_div(g.cols, 256);
+static void launch_tiles(E2m1Args g, const TilePlan& t, hipStream_t stream) {
   g.first = 0;
-  g.tiles_p = p.large;
-  if (p.large > 0) launch_tiles<El, 4, O>(g, stream);
-  g.first = 256 * p.large;
-  g.tiles_p = tiles - p.large;
-  if (g.tiles_p > 0) p.nq == 1 ? launch_tiles<El, 1, O>(g, stream) : launch_tiles<El, 2, O>(g, stream);
+  g.tiles_p = t.large;
+  if (t.large > 0) launch_tiles<El, 4, O>(g, stream);
+  g.first = 256 * t.large;
+  g.tiles_p = t.tiles - t.large;
+  if (g.tiles_p > 0) t.nq == 1 ? launch_tiles<El, 1, O>(g, stream) : launch_tiles<El, 2, O>(g, stream);
 }
 
 template <class El>
-static int product_e2m1(E2m1Args g, const E2m1Plan& p, int64_t wrows, int64_t wbytes, bool aligned, bool backward, char* scratch, int dtype, hipStream_t stream) {
+static int product_e2m1(E2m1Args g, const E2m1Plan& p, int64_t wrows, int64_t wbytes, bool backward, char* scratch, int dtype, hipStream_t stream) {
   void* C = g.C;
   const int64_t ldc = g.ldc;
   if (p.rows) {
@@ -246,20 +237,23 @@ static int product_e2m1(E2m1Args g, const E2m1Plan& p, int64_t wrows, int64_t wb
     else if (g.X.n <= 48) launch_rows<El, 3>(g, stream);
     else launch_rows<El, 4>(g, stream);
   } else {
-    if (!aligned) {
-      const int64_t px = line_pitch(2 * g.k), pw = line_pitch(wbytes);
-      align_rows(g.X.base, g.X.ld, g.X.n, 2 * g.k, scratch + p.x, px, stream);
-      align_rows(g.W.base, g.W.ld, wrows, wbytes, scratch + p.w, pw, stream);
+    if (!aligned_pieces(g.X.base, g.X.ld)) {
+      const int64_t pitch = line_pitch(2 * g.k);
+      align_rows(g.X.base, g.X.ld, g.X.n, 2 * g.k, scratch + p.x, pitch, stream);
       g.X.base = scratch + p.x;
-      g.X.ld = px;
-      g.W.base = (const uint8_t*)scratch + p.w;
-      g.W.ld = pw;
+      g.X.ld = pitch;
     }
-    g.splits = p.splits;
-    g.per_split = p.per_split;
-    if (p.splits > 1) g.C = scratch;
-    backward ? launch_tiles<El, kCols>(g, p, stream) : launch_tiles<El, kRows>(g, p, stream);
-    if (p.splits > 1) join_splits((const float*)scratch, p.splits, g.X.n, g.cols, C, ldc, dtype, stream);
+    if (!aligned_pieces(g.W.base, g.W.ld)) {
+      const int64_t pitch = line_pitch(wbytes);
+      align_rows(g.W.base, g.W.ld, wrows, wbytes, scratch + p.w, pitch, stream);
+      g.W.base = (const uint8_t*)scratch + p.w;
+      g.W.ld = pitch;
+    }
+    g.splits = p.tiles.splits;
+    g.per_split = p.tiles.per_split;
+    if (g.splits > 1) g.C = scratch;
+    backward ? launch_tiles<El, kCols>(g, p.tiles, stream) : launch_tiles<El, kRows>(g, p.tiles, stream);
+    if (g.splits > 1) join_splits((const float*)scratch, g.splits, g.X.n, g.cols, C, ldc, dtype, stream);
   }
   BRSVD_HIP_TRY(hipGetLastError());
   return BRSVD_OK;
@@ -302,8 +296,8 @@ static int call_e2m1(const void* X, int64_t ldx, int64_t in, int dtype, const ui
   g.C = Y;
   g.ldc = ldy;
   g.cols = out;
-  return dtype == BRSVD_DTYPE_BF16 ? product_e2m1<Bf16>(g, p, n, (k + 1) / 2, aligned, backward, (char*)scratch, dtype, s)
-                                   : product_e2m1<Fp16>(g, p, n, (k + 1) / 2, aligned, backward, (char*)scratch, dtype, s);
+  return dtype == BRSVD_DTYPE_BF16 ? product_e2m1<Bf16>(g, p, n, (k + 1) / 2, backward, (char*)scratch, dtype, s)
+                                   : product_e2m1<Fp16>(g, p, n, (k + 1) / 2, backward, (char*)scratch, dtype, s);
 }
 
 }  // namespace brsvd

@@ -140,8 +140,10 @@ k_glu_tiles(const GluArgs g) {
   using T = TileProduct<El, NQ, kRows, kRows, true, PairStager>;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
-  const int64_t f0 = g.first + 128 * tp, t0 = tq * T::BQ, k0 = blockIdx.y * g.per_split, k1 = k0 + g.per_split < g.dim ? k0 + g.per_split : g.dim;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q * g.splits, 8, &tp, &tq)) return;
+  const int split = (int)((unsigned)tq / (unsigned)g.tiles_q);
+  tq -= split * g.tiles_q;
+  const int64_t f0 = g.first + 128 * tp, t0 = tq * T::BQ, k0 = split * g.per_split, k1 = k0 + g.per_split < g.dim ? k0 + g.per_split : g.dim;
   floatx4 acc[T::NP][NQ];
   T::run(acc, g.W, 2 * f0, g.X, t0, k0, k1, lds);
   if (g.splits > 1) {
@@ -151,7 +153,7 @@ k_glu_tiles(const GluArgs g) {
     for (int q = 0; q < NQ; ++q) {
       const int64_t t = t0 + 16 * (wq * NQ + q) + (lane & 15);
       if (t >= g.X.n) continue;
-      const int64_t row = ((int64_t)blockIdx.y * g.X.n + t) * 2 * width;
+      const int64_t row = ((int64_t)split * g.X.n + t) * 2 * width;
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
         const int64_t f = f0 + 64 * wp + 16 * (p & 3) + 4 * (lane >> 4);
@@ -427,11 +429,11 @@ struct GradArgs {
 };
 
 template <class T, class El>
-__device__ __forceinline__ void leave_gradient(const GradArgs& g, floatx4 (&acc)[T::NP][T::NQ], char* lds, int which, int matrices, int64_t p0, int64_t q0) {
+__device__ __forceinline__ void leave_gradient(const GradArgs& g, floatx4 (&acc)[T::NP][T::NQ], char* lds, int split, int which, int matrices, int64_t p0, int64_t q0) {
   constexpr int NQ = T::NQ;
   if (g.splits > 1) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wp = wave % T::WP, wq = wave / T::WP;
-    float* part = g.part + ((int64_t)blockIdx.y * matrices + which) * g.rows * g.cols;
+    float* part = g.part + ((int64_t)split * matrices + which) * g.rows * g.cols;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       const int64_t r = q0 + 16 * (wq * NQ + q) + (lane & 15);
@@ -455,13 +457,15 @@ k_glu_dx(const GradArgs g) {
   using T = TileProduct<El, NQ, kCols, kRows, true, StackStager<El>>;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q, 8, &tp, &tq)) return;
-  const int64_t p0 = g.first + tp * kTileP, q0 = tq * T::BQ, k0 = blockIdx.y * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, g.tiles_q * g.splits, 8, &tp, &tq)) return;
+  const int split = (int)((unsigned)tq / (unsigned)g.tiles_q);
+  tq -= split * g.tiles_q;
+  const int64_t p0 = g.first + tp * kTileP, q0 = tq * T::BQ, k0 = split * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
   StackOperand W = g.W;
   W.end = k1;
   floatx4 acc[T::NP][NQ];
   T::run(acc, W, p0, g.D[0], q0, k0, k1, lds);
-  leave_gradient<T, El>(g, acc, lds, 0, 1, p0, q0);
+  leave_gradient<T, El>(g, acc, lds, split, 0, 1, p0, q0);
 }
 
 // dWg and dWu: both operands hold the tokens in their rows.
@@ -471,12 +475,13 @@ k_glu_dw(const GradArgs g) {
   using T = TileProduct<El, NQ, kCols, kCols, true>;
   __shared__ __attribute__((aligned(1024))) char lds[T::kLds];
   int64_t tp, tq;
-  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, 2 * g.tiles_q, 8, &tp, &tq)) return;
-  const int which = tq >= g.tiles_q;
-  const int64_t p0 = g.first + tp * kTileP, q0 = (which ? tq - g.tiles_q : tq) * T::BQ, k0 = blockIdx.y * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
+  if (!tile_of_workgroup(blockIdx.x, g.tiles_p, 2 * g.tiles_q * g.splits, 8, &tp, &tq)) return;
+  const int part = (int)((unsigned)tq / (unsigned)g.tiles_q), which = part & 1, split = part >> 1;
+  tq -= part * g.tiles_q;
+  const int64_t p0 = g.first + tp * kTileP, q0 = tq * T::BQ, k0 = split * g.per_split, k1 = k0 + g.per_split < g.k ? k0 + g.per_split : g.k;
   floatx4 acc[T::NP][NQ];
   T::run(acc, g.X, p0, g.D[which], q0, k0, k1, lds);
-  leave_gradient<T, El>(g, acc, lds, which, 2, p0, q0);
+  leave_gradient<T, El>(g, acc, lds, split, which, 2, p0, q0);
 }
 
 // Sums of the parts of a contraction that was cut, in their order; a thread four neighbouring columns of `matrices` x rows
@@ -502,27 +507,7 @@ k_glu_sum(const GradArgs g, int matrices, Divisor quads) {
 
 static uint64_t whole256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// A product of `p` columns (in tiles of `wide`) and `q` rows over `steps` steps of 64; `both` of them at once.
-struct TilePlan {
-  int nq;                    // rows of a tile, in 64, beside the large ones
-  int64_t tiles, large;      // along the columns: all, those in tiles of 256 rows
-  int splits;
-  int64_t per_split;
-};
-static TilePlan tile_plan(int64_t p, int64_t wide, int64_t q, int64_t steps, int both) {
-  TilePlan t;
-  t.tiles = ceil_div(p, wide);
-  t.nq = q <= 64 ? 1 : 2;
-  t.large = q <= 128 ? 0 : large_tiles(t.tiles, both * ceil_div(q, 256), both * ceil_div(q, 128), steps);
-  const int64_t workgroups = both * (t.large * ceil_div(q, 256) + (t.tiles - t.large) * ceil_div(q, 64 * t.nq));
-  int64_t s = 256 / workgroups;
-  if (s > steps / 8) s = steps / 8;
-  if (s > 16) s = 16;
-  if (s < 1) s = 1;
-  t.per_split = ceil_div(steps, s) * 64;
-  t.splits = (int)ceil_div(steps * 64, t.per_split);
-  return t;
-}
+static constexpr int kStep[3] = {60, 80, 147};        // 1/100 us a step, see tile_plan
 static bool few_tokens(int64_t tokens) { return tokens <= 64; }
 
 struct GluPlan {
@@ -533,9 +518,9 @@ struct GluPlan {
 };
 static GluPlan glu_plan(int64_t tokens, int64_t dim, int64_t width, bool aligned) {
   GluPlan p;
-  p.forward = tile_plan(width, 128, tokens, ceil_div(dim, 64), 1);
-  p.dx = tile_plan(dim, 256, tokens, 2 * ceil_div(width, 64), 1);
-  p.dw = tile_plan(dim, 256, width, ceil_div(tokens, 64), 2);
+  p.forward = tile_plan(ceil_div(width, 128), tokens, ceil_div(dim, 64), 1, 2 * tokens * width, kStep);
+  p.dx = tile_plan(ceil_div(dim, 256), tokens, 2 * ceil_div(width, 64), 1, tokens * dim, kStep);
+  p.dw = tile_plan(ceil_div(dim, 256), width, ceil_div(tokens, 64), 2, 2 * width * dim, kStep);
   p.pitch_x = line_pitch(2 * dim);
   p.pitch_w = p.pitch_x;
   p.half = 128 * ceil_div(width, 64);
@@ -608,13 +593,14 @@ static int glu_forward(const GluCall& c, const GluPlan& p, bool aligned, char* w
     auto launch = [&](int64_t tiles, int nq) {
       g.tiles_p = tiles;
       g.tiles_q = ceil_div(c.tokens, 64 * nq);
-      const dim3 grid(tile_workgroups(g.tiles_p, g.tiles_q), (unsigned)g.splits);
+      const dim3 grid(tile_workgroups(g.tiles_p, g.tiles_q * g.splits));
       if (nq == 4) hipLaunchKernelGGL((k_glu_tiles<El, 4>), grid, dim3(kTileThreads), 0, stream, g);
-      else hipLaunchKernelGGL((k_glu_tiles<El, 2>), grid, dim3(kTileThreads), 0, stream, g);
+      else if (nq == 2) hipLaunchKernelGGL((k_glu_tiles<El, 2>), grid, dim3(kTileThreads), 0, stream, g);
+      else hipLaunchKernelGGL((k_glu_tiles<El, 1>), grid, dim3(kTileThreads), 0, stream, g);
     };
     if (p.forward.large > 0) launch(p.forward.large, 4);
     g.first = 128 * p.forward.large;
-    if (p.forward.large < p.forward.tiles) launch(p.forward.tiles - p.forward.large, 2);
+    if (p.forward.large < p.forward.tiles) launch(p.forward.tiles - p.forward.large, p.forward.nq);
     if (g.splits > 1) {
       const int64_t quads = ceil_div(c.width, 4);
       hipLaunchKernelGGL(k_glu_join<El>, dim3((unsigned)ceil_div(c.tokens * quads, 256)), dim3(256), 0, stream, g, divisor((uint32_t)quads));
@@ -672,7 +658,7 @@ static int glu_backward(const GluCall& c, const GluPlan& p, bool aligned, char* 
     gradient<El>(g, p.dx, 1, [&](GradArgs g, int64_t tiles, int nq) {
       g.tiles_p = tiles;
       g.tiles_q = ceil_div(g.rows, 64 * nq);
-      const dim3 grid(tile_workgroups(g.tiles_p, g.tiles_q), (unsigned)g.splits);
+      const dim3 grid(tile_workgroups(g.tiles_p, g.tiles_q * g.splits));
       if (nq == 4) hipLaunchKernelGGL((k_glu_dx<El, 4>), grid, dim3(kTileThreads), 0, stream, g);
       else if (nq == 2) hipLaunchKernelGGL((k_glu_dx<El, 2>), grid, dim3(kTileThreads), 0, stream, g);
       else hipLaunchKernelGGL((k_glu_dx<El, 1>), grid, dim3(kTileThreads), 0, stream, g);
@@ -694,7 +680,7 @@ static int glu_backward(const GluCall& c, const GluPlan& p, bool aligned, char* 
     gradient<El>(g, p.dw, 2, [&](GradArgs g, int64_t tiles, int nq) {
       g.tiles_p = tiles;
       g.tiles_q = ceil_div(g.rows, 64 * nq);
-      const dim3 grid(tile_workgroups(g.tiles_p, 2 * g.tiles_q), (unsigned)g.splits);
+      const dim3 grid(tile_workgroups(g.tiles_p, 2 * g.tiles_q * g.splits));
       if (nq == 4) hipLaunchKernelGGL((k_glu_dw<El, 4>), grid, dim3(kTileThreads), 0, stream, g);
       else if (nq == 2) hipLaunchKernelGGL((k_glu_dw<El, 2>), grid, dim3(kTileThreads), 0, stream, g);
       else hipLaunchKernelGGL((k_glu_dw<El, 1>), grid, dim3(kTileThreads), 0, stream, g);
