@@ -307,7 +307,7 @@ int brsvd_dequantize_e2m1(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64
  * brsvd_dequantize_e2m1 rounds it: nothing is lost with BF16 from 2^-133 on and with F16 from 2^-24 on.  Products are exact, sums are fp32, the
  * result is rounded once.  Scales are any bytes.
  * scratch: brsvd_linear_e2m1_scratch_bytes of the same sizes; aligned = 1 where rows of X (dY) and W all begin at 16-byte
- * addresses (address and leading dimension), 0 is enough always.  0 bytes: NULL will do. */
+ * addresses (address and leading dimension), 0 is enough always.  0 bytes: NULL will do, as for up to 16 rows of X. */
 int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW,
                       int64_t m, int64_t n, int64_t k, void* Y, int64_t ldy, void* scratch,
                       uint64_t scratch_bytes, void* stream);

@@ -704,9 +704,10 @@ def _linear_e2m1(name, X, x_name, W, SW, k, backward, out):
         Y = out
         y, ldy = _rows(Y, X.dtype, width, "out", m)
     L = lib()
-    nbytes = L.brsvd_linear_e2m1_scratch_bytes(m, n, k, not ((x | w | ldw) & 15 or ldx & 7), backward)
+    # up to 16 rows of X take none
+    nbytes = L.brsvd_linear_e2m1_scratch_bytes(m, n, k, not ((x | w | ldw) & 15 or ldx & 7), backward) if m > 16 or backward else 0
     scr = _byte_scratch(nbytes, X.device) if nbytes else None
-    _check(getattr(L, name)(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes, _current(X.device)), name)
+    _check((L.brsvd_linear_e2m1_backward if backward else L.brsvd_linear_e2m1)(x, ldx, dt, w, ldw, sw, m, n, k, y, ldy, scr.data_ptr() if nbytes else None, nbytes, _current(X.device)), name)
     return Y
 
 

@@ -9,6 +9,8 @@
 
 namespace brsvd {
 
+constexpr int kChunk = 4 * kGroup;      // numbers of the contraction that a wave of k_rows_e2m1 takes at a time
+
 struct E2m1Args {
   E2m1Operand W;
   Operand X;               // rows: m; pitch in bytes
@@ -26,7 +28,6 @@ struct E2m1Args {
 template <class El, int MT, int NT, int U, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 k_rows_e2m1(const E2m1Args g) {
-  constexpr int kChunk = 4 * kGroup;
   struct __attribute__((packed, aligned(1))) Word {
     uint32_t x;
     __device__ operator uint32_t() const { return x; }
@@ -162,26 +163,6 @@ void align_rows(const void* from, int64_t ld, int64_t rows, int64_t bytes, void*
 
 static uint64_t whole256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-struct E2m1Plan {
-  bool rows;                    // k_rows_e2m1
-  TilePlan tiles;
-  uint64_t x, w, bytes;         // scratch: the parts at 0, X and W in aligned rows where they are laid out anew, all
-};
-// m rows of X, W n x k; aligned: rows of both begin at 16-byte addresses.
-static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k, bool aligned, bool backward) {
-  static constexpr int kForward[3] = {62, 82, 150}, kBackward[3] = {85, 110, 165};      // 1/100 us a step, see tile_plan
-  const int64_t cols = backward ? k : n, in = backward ? n : k;
-  E2m1Plan p;
-  p.rows = !backward && m <= 64;
-  p.tiles = tile_plan(ceil_div(cols, 256), m, ceil_div(in, 64), 1, m * cols, backward ? kBackward : kForward);
-  if (p.rows) p.tiles.splits = 1;
-  const bool laid = !p.rows && !aligned;
-  p.x = p.tiles.splits > 1 ? whole256((uint64_t)p.tiles.splits * m * cols * 4) : 0;
-  p.w = p.x + (laid ? whole256((uint64_t)m * line_pitch(2 * in)) : 0);
-  p.bytes = p.w + (laid ? whole256((uint64_t)n * line_pitch((k + 1) / 2)) : 0);
-  return p;
-}
-
 // Few rows of X: by the 16 rows of W in a wave (NT of them).  A CU takes a KiB of W in some time t, wherever it comes from, and the 16 rows of X that go with a chunk in 0.6 t;
 // with NT for which the workgroups fill rounds of 256 it has least to do: 16 x 12000 x 4096 11.3 us with three (250 workgroups), 16.5 with two (375), 18 with one (750);
 // 64 x 20000 x 5000 34, 43, 48 and 74 with five, three, two and one.  Up to eight rows the caches give X for less, and more than three are slower: 1 x 20000 x 5000 15.9 with
@@ -197,6 +178,29 @@ static int rows_in_wave(int64_t m, int64_t n) {
   }
   return best;
 }
+struct E2m1Plan {
+  bool rows;                    // k_rows_e2m1
+  TilePlan tiles;
+  uint64_t x, w, bytes;         // scratch: the parts at 0, X and W in aligned rows where they are laid out anew, all
+};
+// m rows of X, W n x k; aligned: rows of both begin at 16-byte addresses.
+static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k, bool aligned, bool backward) {
+  static constexpr int kForward[3] = {62, 82, 150}, kBackward[3] = {85, 110, 165};      // 1/100 us a step, see tile_plan
+  const int64_t cols = backward ? k : n, in = backward ? n : k;
+  E2m1Plan p;
+  p.tiles = tile_plan(ceil_div(cols, 256), m, ceil_div(in, 64), 1, m * cols, backward ? kBackward : kForward);
+  // Above 16 rows tiles are ahead where the contraction is long and W has few rows: 64 x 1000 x 8000 22 us, 31 in rows (a wave's chunk 0.35 us for 16 rows of W, 0.65 for 16 of X)
+  const int nt = rows_in_wave(m, n);
+  const double rows_us = 5.0 + (double)(ceil_div(ceil_div(k, kChunk), 8) * ceil_div(ceil_div(n, 16 * nt), 256)) * (0.35 * nt + 0.65 * ceil_div(m, 16));
+  p.rows = !backward && (m <= 16 || (m <= 64 && rows_us <= p.tiles.us));
+  if (p.rows) p.tiles.splits = 1;
+  const bool laid = !p.rows && !aligned;
+  p.x = p.tiles.splits > 1 ? whole256((uint64_t)p.tiles.splits * m * cols * 4) : 0;
+  p.w = p.x + (laid ? whole256((uint64_t)m * line_pitch(2 * in)) : 0);
+  p.bytes = p.w + (laid ? whole256((uint64_t)n * line_pitch((k + 1) / 2)) : 0);
+  return p;
+}
+
 template <class El, int MT, int NT, int U, int WAVES>
 static void launch_rows(const E2m1Args& g, hipStream_t stream) {
   hipLaunchKernelGGL((k_rows_e2m1<El, MT, NT, U, WAVES>), dim3((unsigned)ceil_div(g.W.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);

@@ -508,7 +508,9 @@ k_glu_sum(const GradArgs g, int matrices, Divisor quads) {
 static uint64_t whole256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 static constexpr int kStep[3] = {60, 80, 147};        // 1/100 us a step, see tile_plan
-static bool few_tokens(int64_t tokens) { return tokens <= 64; }
+// Tokens that go from memory to registers.  Above 32 the tiles are ahead unless they have little to do: 64 x 8000 x 4096 37 us in tiles and 49, 64 x 16000 x 4096 64 and 95, the other
+// way round 64 x 8000 x 1000 17.6 and 12.7; at 32 both are alike (8000 x 4096 33 and 33) or these are behind (4096 x 4096 22 and 17).
+static bool few_tokens(int64_t tokens, int64_t dim, int64_t width) { return tokens <= 32 || (tokens <= 64 && ceil_div(width, 16 * 256) * dim <= 3000); }
 
 struct GluPlan {
   TilePlan forward, dx, dw;
@@ -526,7 +528,7 @@ static GluPlan glu_plan(int64_t tokens, int64_t dim, int64_t width, bool aligned
   p.half = 128 * ceil_div(width, 64);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t here = at; at += whole256(bytes); return here; };
-  if (!few_tokens(tokens)) {
+  if (!few_tokens(tokens, dim, width)) {
     p.part = take(p.forward.splits > 1 ? (uint64_t)p.forward.splits * tokens * width * 8 : 0);
     p.x = take(aligned ? 0 : (uint64_t)tokens * p.pitch_x);
     p.wg = take(aligned ? 0 : (uint64_t)width * p.pitch_w);
@@ -576,7 +578,7 @@ template <class El>
 static int glu_forward(const GluCall& c, const GluPlan& p, bool aligned, char* ws, GluArgs g, hipStream_t stream) {
   g.dim = c.dim;
   g.act = c.act;
-  if (few_tokens(c.tokens)) {
+  if (few_tokens(c.tokens, c.dim, c.width)) {
     g.W = PairOperand{(const char*)c.Wg, (const char*)c.Wu, 2 * c.ldwg, 2 * c.ldwu, c.width};
     g.X = Operand{(const char*)c.X, 2 * c.ldx, c.tokens};
     const dim3 grid((unsigned)ceil_div(c.width, 16));

@@ -582,17 +582,17 @@ struct TilePlan {
   int64_t tiles, large;      // along the columns: all, those in tiles of 256 rows
   int splits;
   int64_t per_split;         // numbers of the contraction
+  double us;                 // what it is taken to last
 };
 inline TilePlan tile_plan(int64_t p_tiles, int64_t q, int64_t steps, int both, int64_t numbers, const int (&step)[3]) {
-  TilePlan best{1, p_tiles, 0, 1, 64 * steps};
-  double least = -1.0;
+  TilePlan best{1, p_tiles, 0, 1, 64 * steps, -1.0};
   auto rounds = [](int64_t workgroups) { return (double)(((workgroups + 7) / 8 + 31) / 32); };      // of 32 CUs in each of eight XCDs
   auto consider = [&](int nq, int64_t large, int splits) {
     const int64_t each = (steps + splits - 1) / splits, parts = (steps + each - 1) / each;
     double us = 5.0 + (parts > 1 ? 5.0 + (double)parts * numbers * 4 / 4.5e6 : 0.0);
     if (large > 0) us += rounds(large * both * parts * ((q + 255) / 256)) * (5.0 + 0.01 * step[2] * each);
     if (large < p_tiles) us += rounds((p_tiles - large) * both * parts * ((q + 64 * nq - 1) / (64 * nq))) * (5.0 + 0.01 * step[nq - 1] * each) + (large > 0 ? 2.0 : 0.0);
-    if (least < 0 || us < least) least = us, best = TilePlan{nq, p_tiles, large, (int)parts, 64 * each};
+    if (best.us < 0 || us < best.us) best = TilePlan{nq, p_tiles, large, (int)parts, 64 * each, us};
   };
   const int64_t wide = both * ((q + 255) / 256), full = p_tiles * wide / 256 * 256 / wide;      // columns in whole rounds of large tiles
   for (int s = 1; s <= 16 && (s == 1 || steps >= 3 * s); ++s) {

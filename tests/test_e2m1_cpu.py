@@ -60,7 +60,7 @@ def test_scratch(backward):
     assert linear(backward, **dict(wide, ldx=4097), bytes=need - 1) == BUDGET        # rows that begin at any address
     assert size(-1, 3, 3, 0, backward) == 0 and size(0, 3, 3, 0, backward) == 0 and size(5, 1 << 31, 3, 0, backward) == 0
     if not backward:
-        assert size(64, 512, 4096, 0, 0) == 0 and linear(m=64, scratch=None, bytes=1, X=None) == ARG
+        assert size(16, 512, 4096, 0, 0) == 0 and size(64, 4096, 4096, 0, 0) == 0 and linear(m=16, scratch=None, bytes=1, X=None) == ARG
 
 
 def test_operands_on_several_devices_are_refused(two_devices):  # noqa: F811
