@@ -5,30 +5,32 @@
 //
 // The tensors' addresses and sizes are arguments of the launches, as many tensors at a time as those hold: nothing is copied to the device, and a captured launch keeps them.
 #include <algorithm>
+#include <functional>
 #include <new>
 
 #include "tile.h"
 
 namespace brsvd {
 
-constexpr int kTensors = 64;                  // of a launch
+// Places in a launch's list.  What arguments a launch can have, 4 KB, is what there is: so a tensor without gaps takes one of 29 bytes, and one with strided rows two.
+constexpr int kPlaces = 128;
 // Numbers of a piece: so many that there are some 2000 pieces, within these bounds.  10 tensors of 155 000 numbers: squares 4.3 us in pieces of 2^12, 8.0 in pieces of 2^15.
 // 740 million bf16 numbers into fp32, 7 launches: pieces of 2^15 140 us a launch, 2^14 131, 2^13 125, as the last round of workgroups is a smaller part; the norm's sums
 // are added by one workgroup, which has 16 us to do for 2^13 and 10 for 2^14.
-constexpr int64_t kLeastPiece = 1 << 12, kNormPiece = 1 << 14, kClipPiece = 1 << 13;
+constexpr int kLeastPiece = 12, kNormPiece = 14, kClipPiece = 13;      // as powers of 2
 
-// Tensors of a launch, and which pieces are theirs: those of tensor i are first[i] to first[i + 1].
+// Tensors of a launch, and which pieces are theirs: those of the tensor at place i are first[i] up to the next tensor's.
 struct TensorList {
-  const char* x[kTensors];
-  char* y[kTensors];
-  int64_t cols[kTensors];      // numbers of a row
-  int64_t ldx[kTensors], ldy[kTensors];      // numbers
-  int32_t rows_per[kTensors];  // rows of a piece; 0: a row has several pieces
-  int32_t rows[kTensors];      // rows, where pieces have several
-  uint32_t first[kTensors + 1];
-  uint8_t tx[kTensors], ty[kTensors];
-  int count, piece;
+  const char* x[kPlaces];
+  char* y[kPlaces];
+  int64_t cols[kPlaces];       // numbers of a row
+  uint32_t first[kPlaces];
+  uint8_t types[kPlaces];      // x's, y's << 2; kStrided: the place behind a tensor that has several rows
+  int32_t count, piece;
+  // of such a place: x and y are the rows' distances in numbers, cols is rows_per << 32 | rows.  rows_per: rows of a piece, 0 where a row has several pieces
 };
+constexpr uint8_t kStrided = 0xff;
+static_assert(sizeof(TensorList) <= 3840 && BRSVD_DTYPE_F32 < 4 && BRSVD_DTYPE_BF16 < 4 && BRSVD_DTYPE_F16 < 4, "");
 
 static int bytes_of(int dtype) { return dtype == BRSVD_DTYPE_F32 ? 4 : dtype == BRSVD_DTYPE_BF16 || dtype == BRSVD_DTYPE_F16 ? 2 : 0; }
 
@@ -81,26 +83,40 @@ template <int DT, int W> struct Some {
   }
 };
 
-// Which tensor a piece is of: the last one that begins at or before it
-__device__ __forceinline__ int tensor_of(const TensorList& l, uint32_t piece) {
-  int at = 0;
+// The tensor that a piece is of, and its first piece
+struct Mine {
+  int at;
+  bool strided;
+  uint32_t first;
+};
+__device__ __forceinline__ Mine tensor_of(const TensorList& l, uint32_t piece) {
+  const int lane = threadIdx.x & 63;
+  int at = -1;
 #pragma unroll
-  for (int step = kTensors / 2; step > 0; step >>= 1)
-    if (at + step < l.count && l.first[at + step] <= piece) at += step;
-  return __builtin_amdgcn_readfirstlane(at);
+  for (int h = 0; h < kPlaces; h += 64) at += __popcll(__ballot(h + lane < l.count && l.first[h + lane] <= piece));      // a place of rows begins with its tensor
+  at = __builtin_amdgcn_readfirstlane(at);
+  const bool strided = l.types[at] == kStrided;
+  return {at - (strided ? 1 : 0), strided, l.first[at]};
 }
 
 // Calls take(W numbers, row, column, numbers of the row from there on) for all of a piece; threads take neighbouring ones, 64 bytes a thread on their way.
 template <int DT, int W, class Take>
-__device__ __forceinline__ void all_of(const TensorList& l, int i, uint32_t piece, Take take) {
+__device__ __forceinline__ void all_of(const TensorList& l, Mine mine, Take take) {
   constexpr int EB = Some<DT, W>::kNumber, U = 64 / (W * EB), kStep = 256 * W;
-  const uint32_t p = piece - l.first[i];
-  const int64_t cols = l.cols[i];
+  const int i = mine.at;
+  const uint32_t p = blockIdx.x - mine.first;
+  const int64_t cols = l.cols[i], ld = mine.strided ? (int64_t)l.x[i + 1] : 0, shape = mine.strided ? l.cols[i + 1] : 0;
+  const uint32_t rows_per = (uint32_t)(shape >> 32), all_rows = (uint32_t)shape;
   Some<DT, W> x[U];
-  if (l.rows_per[i] == 0) {
-    const uint32_t per = (uint32_t)((cols + l.piece - 1) / l.piece), row = p / per;
-    const int64_t c0 = (int64_t)(p - row * per) * l.piece, there = cols - c0 < l.piece ? cols - c0 : l.piece;
-    const char* from = l.x[i] + (row * l.ldx[i] + c0) * EB;
+  if (rows_per == 0) {
+    uint32_t row = 0, part = p;
+    if (mine.strided) {
+      const uint32_t per = (uint32_t)((cols + l.piece - 1) / l.piece);
+      row = p / per;
+      part = p - row * per;
+    }
+    const int64_t c0 = (int64_t)part * l.piece, there = cols - c0 < l.piece ? cols - c0 : l.piece;
+    const char* from = l.x[i] + (row * ld + c0) * EB;
     const int left = (int)there;
     for (int c = W * threadIdx.x; c < left; c += kStep * U) {
 #pragma unroll
@@ -111,10 +127,10 @@ __device__ __forceinline__ void all_of(const TensorList& l, int i, uint32_t piec
         if (c + kStep * u < left) take(x[u], (int64_t)row, c0 + c + kStep * u, (int64_t)(left - c - kStep * u));
     }
   } else {
-    const uint32_t some = (uint32_t)((cols + W - 1) / W), r0 = p * l.rows_per[i], rows = l.rows[i] - r0 < (uint32_t)l.rows_per[i] ? l.rows[i] - r0 : l.rows_per[i];
+    const uint32_t some = (uint32_t)((cols + W - 1) / W), r0 = p * rows_per, rows = all_rows - r0 < rows_per ? all_rows - r0 : rows_per;
     for (uint32_t e = threadIdx.x; e < rows * some; e += 256) {
       const uint32_t r = e / some, c = W * (e - r * some);
-      x[0].load(l.x[i] + ((int64_t)(r0 + r) * l.ldx[i] + c) * EB, cols - c);
+      x[0].load(l.x[i] + ((int64_t)(r0 + r) * ld + c) * EB, cols - c);
       take(x[0], (int64_t)(r0 + r), (int64_t)c, cols - c);
     }
   }
@@ -131,10 +147,10 @@ __device__ __forceinline__ double sum_of_workgroup(double x, double* red) {
 }
 
 template <int DT>
-__device__ __forceinline__ double squares_of(const TensorList& l, int i, uint32_t piece) {
+__device__ __forceinline__ double squares_of(const TensorList& l, Mine mine) {
   constexpr int W = DT == BRSVD_DTYPE_F32 ? 4 : 8;
   double sum[2] = {0.0, 0.0};
-  all_of<DT, W>(l, i, piece, [&](const Some<DT, W>& x, int64_t, int64_t, int64_t) {
+  all_of<DT, W>(l, mine, [&](const Some<DT, W>& x, int64_t, int64_t, int64_t) {
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const double v = x.number(j);
@@ -147,9 +163,10 @@ __device__ __forceinline__ double squares_of(const TensorList& l, int i, uint32_
 __global__ void __launch_bounds__(256)
 k_grad_squares(const TensorList l, double* __restrict__ sums) {
   __shared__ double red[4];
-  const int i = tensor_of(l, blockIdx.x), dtype = l.tx[i];
-  double sum = dtype == BRSVD_DTYPE_F32 ? squares_of<BRSVD_DTYPE_F32>(l, i, blockIdx.x) : dtype == BRSVD_DTYPE_BF16 ? squares_of<BRSVD_DTYPE_BF16>(l, i, blockIdx.x)
-                                                                                                                   : squares_of<BRSVD_DTYPE_F16>(l, i, blockIdx.x);
+  const Mine mine = tensor_of(l, blockIdx.x);
+  const int dtype = l.types[mine.at] & 3;
+  double sum = dtype == BRSVD_DTYPE_F32 ? squares_of<BRSVD_DTYPE_F32>(l, mine) : dtype == BRSVD_DTYPE_BF16 ? squares_of<BRSVD_DTYPE_BF16>(l, mine)
+                                                                                                           : squares_of<BRSVD_DTYPE_F16>(l, mine);
   sum = sum_of_workgroup(sum, red);
   if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
@@ -172,36 +189,39 @@ k_grad_norm(const double* __restrict__ sums, int64_t n, double scale, float* __r
 }
 
 template <int DT, int DY>
-__device__ __forceinline__ void clip_piece(const TensorList& l, int i, uint32_t piece, float f1, float f2) {
+__device__ __forceinline__ void clip_piece(const TensorList& l, Mine mine, float f1, float f2) {
   constexpr int W = DT == BRSVD_DTYPE_F32 || DY == BRSVD_DTYPE_F32 ? 4 : 8;        // 16 bytes of the wider type: lanes write next to each other
-  all_of<DT, W>(l, i, piece, [&](const Some<DT, W>& x, int64_t r, int64_t c, int64_t left) {
+  char* y0 = l.y[mine.at];
+  const int64_t ld = mine.strided ? (int64_t)l.y[mine.at + 1] : 0;
+  all_of<DT, W>(l, mine, [&](const Some<DT, W>& x, int64_t r, int64_t c, int64_t left) {
     float y[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) y[j] = x.number(j) * f1 * f2;
-    Some<DY, W>::put(l.y[i] + (r * l.ldy[i] + c) * Some<DY, W>::kNumber, left, y);
+    Some<DY, W>::put(y0 + (r * ld + c) * Some<DY, W>::kNumber, left, y);
   });
 }
 template <int DT>
-__device__ __forceinline__ void clip_into(const TensorList& l, int i, uint32_t piece, float f1, float f2) {
-  const int ty = l.ty[i];
-  if (ty == BRSVD_DTYPE_F32) clip_piece<DT, BRSVD_DTYPE_F32>(l, i, piece, f1, f2);
-  else if (ty == BRSVD_DTYPE_BF16) clip_piece<DT, BRSVD_DTYPE_BF16>(l, i, piece, f1, f2);
-  else clip_piece<DT, BRSVD_DTYPE_F16>(l, i, piece, f1, f2);
+__device__ __forceinline__ void clip_into(const TensorList& l, Mine mine, float f1, float f2) {
+  const int ty = l.types[mine.at] >> 2;
+  if (ty == BRSVD_DTYPE_F32) clip_piece<DT, BRSVD_DTYPE_F32>(l, mine, f1, f2);
+  else if (ty == BRSVD_DTYPE_BF16) clip_piece<DT, BRSVD_DTYPE_BF16>(l, mine, f1, f2);
+  else clip_piece<DT, BRSVD_DTYPE_F16>(l, mine, f1, f2);
 }
 // Bound by memory.  In place and with nothing to do it reads nothing.
 __global__ void __launch_bounds__(256)
 k_grad_clip(const TensorList l, const float* __restrict__ norm, double scale, double max_norm) {
-  const int i = tensor_of(l, blockIdx.x), tx = l.tx[i];
+  const Mine mine = tensor_of(l, blockIdx.x);
+  const int tx = l.types[mine.at] & 3;
   const double n = *norm;
   // a norm that is no finite number says nothing about how long the gradients are: they are scaled alone
   const double f = n > max_norm && n <= 3.402823466e38 ? scale * (max_norm / n) : scale;
-  if (f == 1.0 && l.x[i] == l.y[i]) return;
+  if (f == 1.0 && l.x[mine.at] == l.y[mine.at]) return;
   // in two factors, so that neither leaves fp32's range where the product does not
   const double a = fabs(f) < 0x1p-100 ? f * 0x1p100 : fabs(f) > 0x1p100 ? f * 0x1p-100 : f;
   const float f1 = (float)a, f2 = fabs(f) < 0x1p-100 ? 0x1p-100f : fabs(f) > 0x1p100 ? 0x1p100f : 1.f;
-  if (tx == BRSVD_DTYPE_F32) clip_into<BRSVD_DTYPE_F32>(l, i, blockIdx.x, f1, f2);
-  else if (tx == BRSVD_DTYPE_BF16) clip_into<BRSVD_DTYPE_BF16>(l, i, blockIdx.x, f1, f2);
-  else clip_into<BRSVD_DTYPE_F16>(l, i, blockIdx.x, f1, f2);
+  if (tx == BRSVD_DTYPE_F32) clip_into<BRSVD_DTYPE_F32>(l, mine, f1, f2);
+  else if (tx == BRSVD_DTYPE_BF16) clip_into<BRSVD_DTYPE_BF16>(l, mine, f1, f2);
+  else clip_into<BRSVD_DTYPE_F16>(l, mine, f1, f2);
 }
 
 // A tensor as kernels take it: rows next to each other are one long row.
@@ -210,7 +230,8 @@ struct Shape {
   int rows_per;
   int64_t pieces;
 };
-static Shape shape_of(const brsvd_tensor& x, const brsvd_tensor* y, int64_t piece) {
+static Shape shape_of(const brsvd_tensor& x, const brsvd_tensor* y, int log_piece) {
+  const int64_t piece = (int64_t)1 << log_piece;
   Shape s{x.rows, x.cols, 0, 0};
   if (x.rows == 0 || x.cols == 0) return s;
   if (x.rows == 1 || (x.ld == x.cols && (!y || y->ld == y->cols))) s.cols = x.rows * x.cols, s.rows = 1;
@@ -218,16 +239,17 @@ static Shape shape_of(const brsvd_tensor& x, const brsvd_tensor* y, int64_t piec
     s.rows_per = (int)(piece / s.cols);
     s.pieces = ceil_div(s.rows, s.rows_per);
   } else {
-    s.pieces = s.rows * ceil_div(s.cols, piece);
+    s.pieces = s.rows * ((s.cols + piece - 1) >> log_piece);
   }
   return s;
 }
 constexpr int64_t kMaxNumbers = (int64_t)1 << 44, kMaxPieces = ((int64_t)1 << 24) - 1;      // of a launch, 256 threads each
 // A list's pieces of up to `most` numbers, of more where there are too many for a launch.  pieces < 0: a tensor is refused
 struct Pieces {
-  int64_t piece, pieces;
+  int log_piece;
+  int64_t pieces;
 };
-static Pieces check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, int64_t most) {
+static Pieces check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, int most) {
   const Pieces refused{0, -1};
   if (count < 0 || (count > 0 && !x)) return refused;
   int64_t numbers = 0;
@@ -236,16 +258,17 @@ static Pieces check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t c
       const brsvd_tensor& t = k ? y[i] : x[i];
       if (t.dtype != (int)t.dtype || !bytes_of((int)t.dtype) || t.rows < 0 || t.cols < 0 || t.rows != x[i].rows || t.cols != x[i].cols) return refused;
       if (t.rows == 0 || t.cols == 0) continue;
-      if (!t.data || t.cols > kMaxNumbers || t.rows > kMaxNumbers / t.cols || t.rows > INT32_MAX) return refused;
-      if (t.rows > 1 && (t.ld < t.cols || t.ld > kMaxNumbers / t.rows)) return refused;
+      int64_t all = 0;
+      if (!t.data || t.rows > INT32_MAX || __builtin_mul_overflow(t.rows, t.cols, &all) || all > kMaxNumbers) return refused;
+      if (t.rows > 1 && (t.ld < t.cols || __builtin_mul_overflow(t.rows, t.ld, &all) || all > kMaxNumbers)) return refused;
     }
     numbers += x[i].rows * x[i].cols;
     if (numbers > kMaxNumbers) return refused;
   }
   Pieces p{kLeastPiece, 0};
-  while ((p.piece < most && numbers > 2048 * p.piece) || numbers > p.piece << 22) p.piece *= 2;
+  while ((p.log_piece < most && numbers >> p.log_piece > 2048) || numbers >> p.log_piece > 1 << 22) ++p.log_piece;
   for (int64_t i = 0; i < count; ++i) {
-    p.pieces += shape_of(x[i], y ? y + i : nullptr, p.piece).pieces;
+    p.pieces += shape_of(x[i], y ? y + i : nullptr, p.log_piece).pieces;
     if (p.pieces > kMaxPieces) return refused;
   }
   return p;
@@ -253,52 +276,56 @@ static Pieces check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t c
 // Whether numbers of one tensor are another's too: an address of `out` twice, or that of another tensor; and one that is its own tensor's has to be laid out like it.
 static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count) {
   if (count == 0) return BRSVD_OK;
-  const void** places = new (std::nothrow) const void*[count];
+  const void** places = new (std::nothrow) const void*[2 * count];
   if (!places) return BRSVD_ERR_ALLOC;
-  int64_t n = 0;
+  const void** others = places + count;
+  int64_t n = 0, m = 0;
   bool good = true;
   for (int64_t i = 0; i < count; ++i)
     if (x[i].rows > 0 && x[i].cols > 0) {
       places[n++] = y[i].data;
-      good &= y[i].data != x[i].data || (y[i].dtype == x[i].dtype && (x[i].rows == 1 || y[i].ld == x[i].ld));
+      if (y[i].data != x[i].data) others[m++] = x[i].data;
+      else good &= y[i].dtype == x[i].dtype && (x[i].rows == 1 || y[i].ld == x[i].ld);
     }
   if (!std::is_sorted(places, places + n)) std::sort(places, places + n);
+  if (!std::is_sorted(others, others + m)) std::sort(others, others + m);
   for (int64_t i = 1; i < n; ++i) good &= places[i] != places[i - 1];
-  for (int64_t i = 0; i < count && good; ++i)
-    if (x[i].rows > 0 && x[i].cols > 0 && x[i].data != y[i].data) good &= !std::binary_search(places, places + n, (const void*)x[i].data);
+  for (int64_t i = 0, j = 0; i < n && j < m && good;) {
+    good = places[i] != others[j];
+    if (std::less<const void*>()(places[i], others[j])) ++i;
+    else ++j;
+  }
   delete[] places;
   return good ? BRSVD_OK : BRSVD_ERR_ARG;
 }
 // launch(list, workgroups) for as many tensors at a time as a list holds
 template <class Launch>
-static void in_lists(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, int64_t piece, Launch launch) {
+static void in_lists(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, int log_piece, Launch launch) {
   TensorList l;
   l.count = 0;
-  l.piece = (int)piece;
+  l.piece = 1 << log_piece;
   uint32_t pieces = 0;
   auto flush = [&] {
     if (pieces == 0) return;
-    l.first[l.count] = pieces;
     launch(l, pieces);
     l.count = 0;
     pieces = 0;
   };
-  for (int64_t i = 0; i < count; ++i) {
-    const Shape s = shape_of(x[i], y ? y + i : nullptr, piece);
-    if (s.pieces == 0) continue;
+  auto put = [&](const void* a, void* b, int64_t cols, int types) {
     const int c = l.count++;
-    l.x[c] = (const char*)x[i].data;
-    l.ldx[c] = x[i].ld;
-    l.tx[c] = (uint8_t)x[i].dtype;
-    l.y[c] = y ? (char*)y[i].data : nullptr;
-    l.ldy[c] = y ? y[i].ld : 0;
-    l.ty[c] = y ? (uint8_t)y[i].dtype : 0;
-    l.cols[c] = s.cols;
-    l.rows[c] = (int32_t)s.rows;
-    l.rows_per[c] = s.rows_per;
+    l.x[c] = (const char*)a;
+    l.y[c] = (char*)b;
+    l.cols[c] = cols;
     l.first[c] = pieces;
+    l.types[c] = (uint8_t)types;
+  };
+  for (int64_t i = 0; i < count; ++i) {
+    const Shape s = shape_of(x[i], y ? y + i : nullptr, log_piece);
+    if (s.pieces == 0) continue;
+    if (l.count + (s.rows > 1 ? 2 : 1) > kPlaces) flush();
+    put(x[i].data, y ? y[i].data : nullptr, s.cols, (int)x[i].dtype | (y ? (int)y[i].dtype << 2 : 0));
+    if (s.rows > 1) put((const void*)x[i].ld, y ? (void*)y[i].ld : nullptr, (int64_t)s.rows_per << 32 | s.rows, kStrided);
     pieces += (uint32_t)s.pieces;
-    if (l.count == kTensors) flush();
   }
   flush();
 }
@@ -319,7 +346,7 @@ extern "C" int brsvd_grad_norm(const brsvd_tensor* tensors, int64_t count, float
   if (workspace_bytes < (uint64_t)(p.pieces + 32) / 32 * 256) return BRSVD_ERR_BUDGET;
   hipStream_t s = (hipStream_t)stream;
   double* sums = (double*)workspace;
-  in_lists(tensors, nullptr, count, p.piece, [&](const TensorList& l, unsigned grid) {
+  in_lists(tensors, nullptr, count, p.log_piece, [&](const TensorList& l, unsigned grid) {
     hipLaunchKernelGGL(k_grad_squares, dim3(grid), dim3(256), 0, s, l, sums);
     sums += grid;
   });
@@ -334,7 +361,7 @@ extern "C" int brsvd_grad_clip(const brsvd_tensor* tensors, const brsvd_tensor* 
   BRSVD_TRY(check_places(tensors, out, count));
   if (p.pieces == 0) return BRSVD_OK;
   hipStream_t s = (hipStream_t)stream;
-  in_lists(tensors, out, count, p.piece, [&](const TensorList& l, unsigned grid) {
+  in_lists(tensors, out, count, p.log_piece, [&](const TensorList& l, unsigned grid) {
     hipLaunchKernelGGL(k_grad_clip, dim3(grid), dim3(256), 0, s, l, norm, (double)scale, (double)max_norm);
   });
   BRSVD_HIP_TRY(hipGetLastError());
