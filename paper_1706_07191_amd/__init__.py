@@ -7,7 +7,6 @@ library has not been built (python -m paper_1706_07191_amd.build) importing `lib
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
 import operator
 import os
@@ -786,90 +785,28 @@ def brsvd_glu_backward(X, Wg, Wu, G, U, dH, act="silu", need_dX=True, need_dW=Tr
     return dX, dWg, dWu
 
 
-_grad_types = {}
-_dtype_of, _shape_of, _is_cuda = map(operator.attrgetter, ("dtype", "shape", "is_cuda"))
+_tables = None
 
 
-def _dense_order(t):
-    """Strides of a tensor whose numbers fill their memory without gaps in some order of its dimensions (0 for a dimension of one), else None."""
-    expected = 1
-    for size, step in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda x: (x[1], x[0])):
-        if step != expected:
-            return None
-        expected *= size
-    return tuple(s if n != 1 else 0 for n, s in zip(t.shape, t.stride()))
-
-
-def _plain_lists(lists):
-    """Lists of CUDA tensors of the same shapes, each without a gap in the order of its sizes, as arrays of brsvd_tensor; None for others.  Lists are long, and each of
-    these steps goes through one without a step of Python for a tensor."""
-    T, n = torch.Tensor, len(lists[0])
-    try:
-        if not all(all(map(T.is_contiguous, v)) and all(map(_is_cuda, v)) for v in lists):
-            return None
-        if len(lists) == 2 and lists[1] is not lists[0] and list(map(_shape_of, lists[0])) != list(map(_shape_of, lists[1])):
-            return None
-        one = array.array("q", [1]) * n
-        sizes, tables = array.array("q", list(map(T.numel, lists[0]))), []
-        for v in lists:
-            types = list(map(_dtype_of, v))
-            table = array.array("q", bytes(40 * n))
-            table[0::5] = array.array("q", list(map(T.data_ptr, v)))
-            table[1::5] = one
-            table[2::5] = table[3::5] = sizes
-            table[4::5] = (array.array("q", [_grad_types[types[0]]]) * n if types.count(types[0]) == n else
-                           array.array("q", list(map(_grad_types.__getitem__, types))))
-            tables.append(table)
-        return tables
-    except (TypeError, KeyError, AttributeError, RuntimeError):
-        return None
-
-
-def _tensors(tensors, name, out=None):
+def _tensors(*lists):
     """A list of tensors as an array of brsvd_tensor; two lists, whose numbers have to be in the same order, as two."""
-    if not _grad_types:
-        _grad_types.update({torch.float32: BRSVD_DTYPE_F32, torch.bfloat16: BRSVD_DTYPE_BF16, torch.float16: BRSVD_DTYPE_F16})
-    lists = [tensors] if out is None else [tensors, out]
-    if not all(isinstance(v, (list, tuple)) for v in lists):
-        raise TypeError(f"{name if len(lists) == 1 else name + ' and out'} must be lists of CUDA tensors")
-    if len(lists[0]) != len(lists[-1]):
-        raise ValueError(f"out has {len(out)} tensors, expected {len(tensors)}")
-    if not tensors:
-        return [array.array("q") for _ in lists]
-    plain = _plain_lists(lists)
-    if plain is not None:
-        return plain
-    tables = [array.array("q", bytes(40 * len(tensors))) for _ in lists]
-    for i, pair in enumerate(zip(*lists)):
-        for t, what in zip(pair, (name, "out")):
-            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided or t.dtype not in _grad_types:
-                raise TypeError(f"{what}[{i}] must be a CUDA tensor of dtype torch.float32, torch.bfloat16 or torch.float16")
-            if t.shape != pair[0].shape:
-                raise TypeError(f"{what}[{i}] has shape {tuple(t.shape)}, expected {tuple(pair[0].shape)}")
-        t, numbers = pair[0], pair[0].numel()
-        rows, cols, strided = 1, numbers, False
-        if numbers and not all(x.is_contiguous() for x in pair):
-            if t.dim() == 2 and all(x.stride(1) == 1 and x.stride(0) >= x.shape[1] for x in pair):
-                (rows, cols), strided = t.shape, True
-            elif _dense_order(t) is None or any(_dense_order(x) != _dense_order(t) for x in pair):
-                raise TypeError(f"{name}[{i}] must be dense, or a matrix with unit column stride" + ("" if out is None else ", and laid out as out's"))
-        for table, x in zip(tables, pair):
-            table[5 * i:5 * i + 5] = array.array("q", [x.data_ptr(), rows, cols, x.stride(0) if strided else cols, _grad_types[x.dtype]])
-    return tables
+    global _tables
+    if _tables is None:
+        from ._lists import tables as _tables          # needs torch
+    return _tables(*lists)
 
 
 @_scoped
 def brsvd_grad_norm(tensors, scale=1.0):
     """|scale| times the 2-norm over all numbers of a list of CUDA tensors (fp32, bf16 or fp16, mixed; dense or matrices with strided rows), as a
     tensor of one fp32 number.  Sums are fp64.  scale: what the gradients are to be multiplied by, such as one over a loss's factor."""
-    table, = _tensors(tensors, "tensors")
+    table, = _tensors(tensors)
     count = len(tensors)
     device = tensors[0].device if count else torch.device("cuda", torch.cuda.current_device())
     norm = torch.empty(1, dtype=torch.float32, device=device)
-    at = table.buffer_info()[0] if count else None
-    nbytes = lib().brsvd_grad_norm_workspace_bytes(at, count)
+    nbytes = lib().brsvd_grad_norm_workspace_bytes(table, count)
     ws = _byte_scratch(nbytes, device)
-    _check(lib().brsvd_grad_norm(at, count, scale, norm.data_ptr(), ws.data_ptr(), nbytes, _current(device)), "brsvd_grad_norm")
+    _check(lib().brsvd_grad_norm(table, count, scale, norm.data_ptr(), ws.data_ptr(), nbytes, _current(device)), "brsvd_grad_norm")
     return norm
 
 
@@ -881,9 +818,8 @@ def brsvd_grad_clip(tensors, norm, max_norm, scale=1.0, out=None):
     if not isinstance(norm, torch.Tensor) or norm.numel() != 1:
         raise TypeError("norm must be a CUDA tensor of one fp32 number")
     n = _dev(norm, torch.float32, "norm")
-    tables = _tensors(tensors, "tensors", None if out is tensors else out)
-    at = [t.buffer_info()[0] for t in tables]
-    _check(lib().brsvd_grad_clip(at[0] if len(tensors) else None, at[-1], len(tensors), scale, max_norm, n, _current(norm.device)), "brsvd_grad_clip")
+    tables = _tensors(tensors) if out is None or out is tensors else _tensors(tensors, out)
+    _check(lib().brsvd_grad_clip(tables[0], tables[-1], len(tensors), scale, max_norm, n, _current(norm.device)), "brsvd_grad_clip")
     return tensors if out is None else out
 
 

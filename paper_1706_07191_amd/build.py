@@ -1,8 +1,8 @@
-"""Builds libbrsvd.so (hand-written HIP for gfx950) in-tree with hipcc.
+"""Builds libbrsvd.so (hand-written HIP for gfx950) in-tree with hipcc, and the Python module _lists.so with the host's compiler.
 
 Usage: python -m paper_1706_07191_amd.build [--force]
        python -m paper_1706_07191_amd.build --host-asan
-The shared library is written next to this file; object files go to csrc/_build/.
+The shared libraries are written next to this file; object files go to csrc/_build/.
 --host-asan builds csrc/_build_asan/host_checks instead: the same sources with their HOST code instrumented by
 the address and undefined-behaviour sanitizers (the device code is compiled as usual and never runs), linked
 with csrc/host_checks.cpp, which exercises argument checks, working-set sizing, the launch planners and the
@@ -22,6 +22,7 @@ OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libbrsvd.so")
 SOURCES = ["gemm_half.hip", "gemm_split.hip", "gemm_thin.hip", "orth.hip", "tsqr.hip", "small_svd.hip", "rpca.hip", "philox.hip", "probe.hip",
            "quantize.hip", "gemm_e4m3.hip", "quantize_e2m1.hip", "gemm_e2m1.hip", "glu.hip", "grads.hip", "head_loss.hip", "brsvd.hip"]
+LISTS = os.path.join(HERE, "_lists.so")        # reads lists of torch tensors: host code against torch's headers, which libbrsvd.so knows nothing of
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
@@ -54,6 +55,17 @@ def _headers():
             + [os.path.join(ROOT, "include", h) for h in ("brsvd.h", "brsvd_steps.h")])
 
 
+def _lists_command():
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+            "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"), os.path.join(CSRC, "lists.cpp"), "-o", LISTS,
+            "-L" + os.path.join(home, "lib"), "-ltorch_python", "-lc10"]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     hipcc = _hipcc()
@@ -66,8 +78,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(o)
         if force or _stale(o, [s] + headers):
             jobs.append([hipcc] + FLAGS + ["-c", s, "-o", o])
-    with ThreadPoolExecutor(max_workers=min(6, max(1, len(jobs)))) as ex:
-        for out in ex.map(_run, jobs):
+    lists = [_lists_command()] if force or _stale(LISTS, [os.path.join(CSRC, "lists.cpp"), os.path.join(ROOT, "include", "brsvd.h")]) else []
+    with ThreadPoolExecutor(max_workers=min(6, max(1, len(jobs + lists)))) as ex:
+        for out in ex.map(_run, jobs + lists):
             if verbose and out.strip():
                 print(out)
     if force or jobs or _stale(LIB, objs):

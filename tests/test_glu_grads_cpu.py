@@ -119,3 +119,16 @@ def test_operands_on_several_devices_are_refused(two_devices):  # noqa: F811
     seen = []
     B._scoped(lambda tensors: seen.append(two_devices[0]))([on(1, 4), on(1, 5)])
     assert seen == [1] and two_devices == [0]
+
+
+@pytest.mark.parametrize("lists,error,text", [
+    (([torch.ones(3)],), TypeError, r"tensors\[0\] must be a CUDA tensor"), (([None],), TypeError, r"tensors\[0\]"), ((torch.ones(3),), TypeError, "tensors must be a list"),
+    (([], torch.ones(3)), TypeError, "out must be a list"), (([], [torch.ones(3)]), ValueError, "out has 1 tensors, expected 0"), (((torch.ones(3).to_sparse(),),), TypeError, r"tensors\[0\]"),
+    ((), TypeError, "one list or two"), (([], [], []), TypeError, "one list or two")])
+def test_lists_refuse(lists, error, text):
+    with pytest.raises(error, match=text):
+        B._tensors(*lists)
+
+
+def test_empty_lists():
+    assert B._tensors([]) == (b"",) and B._tensors((), []) == (b"", b"")
