@@ -16,6 +16,7 @@
 #include "brsvd_steps.h"
 #include "common.h"
 #include "split.h"
+#include "tile.h"
 
 static int g_checks = 0, g_failed = 0;
 #define CHECK(cond)                                                             \
@@ -328,6 +329,74 @@ int main() {
   CHECK(brsvd_dequantize_e4m3((const uint8_t*)0x10000, INT64_MAX, (const float*)0x10000, INT64_MAX, INT64_MAX, 1, BRSVD_DTYPE_F32, (void*)0x10000, INT64_MAX, nullptr) ==
         BRSVD_ERR_ARG);
   CHECK(brsvd_dequantize_e4m3(nullptr, 0, nullptr, INT64_MAX, INT64_MAX, 128, BRSVD_DTYPE_F32, nullptr, 0, nullptr) == BRSVD_ERR_ARG);
+
+  // ---- plans of tiles over a contraction in parts: all of it once, in launches that there are ----
+  for (int i = 0; i < 20000; ++i) {
+    const int64_t big[] = {1, 3, 20, 300, 5000, 100000, 2000000};
+    const int64_t np = uniform(1, big[next_u64() % 6]), q = uniform(1, big[next_u64() % 7]), steps = uniform(1, big[next_u64() % 6]);
+    const int both = 1 + (int)(next_u64() & 1);
+    if (!brsvd::tiles_fit(np, both * ((q + 63) / 64), 512)) continue;
+    const int step[3] = {60, 80, 147};
+    const brsvd::TilePlan t = brsvd::tile_plan(np, q, steps, both, both * np * 256 * q, step);
+    const int64_t per = t.per_split / 64;
+    bool good = (t.nq == 1 || t.nq == 2) && t.tiles == np && t.large >= 0 && t.large <= np && t.splits >= 1 && t.splits <= 16 && t.per_split % 64 == 0 && per >= 1 && t.us > 0;
+    good = good && (t.splits - 1) * per < steps && t.splits * per >= steps;
+    good = good && brsvd::tiles_fit(t.large, both * t.splits * ((q + 255) / 256), 512) && brsvd::tiles_fit(np - t.large, both * t.splits * ((q + 64 * t.nq - 1) / (64 * t.nq)), 512);
+    CHECK(good);
+  }
+
+  // ---- 4-bit weights, gated blocks: sizes over their whole range, refusals before any GPU call ----
+  for (int i = 0; i < 20000; ++i) {
+    const int64_t big[] = {1, 7, 64, 300, 5000, 100000, 3000000, (int64_t)1 << 29, (int64_t)1 << 31, (int64_t)1 << 40, INT64_MAX / 2};
+    const int64_t m = uniform(-1, big[next_u64() % 11]), n = uniform(-1, big[next_u64() % 11]), k = uniform(-1, big[next_u64() % 11]);
+    const int32_t aligned = (int32_t)(next_u64() & 1);
+    uint8_t* at = (uint8_t*)0x10000;
+    for (int back = 0; back < 2; ++back) {
+      const uint64_t some = brsvd_linear_e2m1_scratch_bytes(m, n, k, aligned, back), all = brsvd_linear_e2m1_scratch_bytes(m, n, k, 0, back);
+      CHECK(some % 256 == 0 && some <= all && (back || m > 16 || all == 0));
+      auto call = back ? brsvd_linear_e2m1_backward : brsvd_linear_e2m1;
+      const int64_t ldx = back ? n : k, ldy = back ? k : n;
+      if (all) {
+        CHECK(call(at + 2, ldx, BRSVD_DTYPE_F16, at + 1, (k + 1) / 2, at, m, n, k, at, ldy, at, all - 1, nullptr) == BRSVD_ERR_BUDGET);
+        CHECK(call(at + 2, ldx, BRSVD_DTYPE_BF16, at + 1, (k + 1) / 2, at, m, n, k, at, ldy, at + 1, all, nullptr) == BRSVD_ERR_ARG);
+      }
+      if (m > 0 && n > 0 && k > 0) {
+        CHECK(call(at, ldx - 1, BRSVD_DTYPE_BF16, at, (k + 1) / 2, at, m, n, k, at, ldy, at, UINT64_MAX, nullptr) == BRSVD_ERR_ARG);
+        CHECK(call(at, ldx, BRSVD_DTYPE_BF16, at, (k + 1) / 2 - 1, at, m, n, k, at, ldy, at, UINT64_MAX, nullptr) == BRSVD_ERR_ARG);
+        CHECK(call(at, ldx, BRSVD_DTYPE_BF16, at, (k + 1) / 2, at, m, n, k, at, ldy - 1, at, UINT64_MAX, nullptr) == BRSVD_ERR_ARG);
+      }
+      const uint64_t glu = brsvd_glu_workspace_bytes(m, k, n, aligned, back), whole = brsvd_glu_workspace_bytes(m, k, n, 0, back);
+      CHECK(glu % 256 == 0 && glu <= whole);
+      if (whole && !back) {
+        CHECK(brsvd_glu_forward(at + 2, k, at, k, at, k, m, k, n, BRSVD_DTYPE_F16, BRSVD_ACT_GELU, at, n, nullptr, 0, nullptr, 0, at, whole - 1, nullptr) == BRSVD_ERR_BUDGET);
+      }
+      if (whole && back && m > 0 && n > 0 && k > 0)
+        CHECK(brsvd_glu_backward(at + 2, k, at, k, at, k, at, n, at, n, at, n, m, k, n, BRSVD_DTYPE_F16, BRSVD_ACT_SILU, at, k, at, k, at, k, at, whole - 1, nullptr) == BRSVD_ERR_BUDGET);
+    }
+    CHECK(brsvd_quantize_e2m1(at, k, m, k, BRSVD_DTYPE_F64, at, k, at, nullptr) == BRSVD_ERR_ARG);
+    if (m > 0 && k > 0) CHECK(brsvd_dequantize_e2m1(at, k / 2 - (k & 1 ? 0 : 1), at, m, k, BRSVD_DTYPE_F32, at, k, nullptr) == BRSVD_ERR_ARG);
+  }
+
+  // ---- lists of tensors ----
+  for (int i = 0; i < 2000; ++i) {
+    std::vector<brsvd_tensor> x((size_t)uniform(0, 300));
+    for (size_t j = 0; j < x.size(); ++j) {
+      const int64_t rows = uniform(0, next_u64() % 9 ? 40 : (int64_t)1 << 33), cols = uniform(0, next_u64() % 9 ? 5000 : (int64_t)1 << 43);
+      x[j] = brsvd_tensor{(void*)((j + 1) << 20), rows, cols, cols + uniform(0, 2), next_u64() % 50 ? BRSVD_DTYPE_BF16 : uniform(-1, 4)};
+    }
+    const uint64_t bytes = brsvd_grad_norm_workspace_bytes(x.data(), (int64_t)x.size());
+    CHECK(bytes % 256 == 0);
+    float norm = 0;
+    if (bytes) CHECK(brsvd_grad_norm(x.data(), (int64_t)x.size(), 1.f, &norm, (void*)0x10000, bytes - 256, nullptr) == BRSVD_ERR_BUDGET || bytes == 256);
+    else CHECK(brsvd_grad_norm(x.data(), (int64_t)x.size(), 1.f, &norm, (void*)0x10000, UINT64_MAX, nullptr) == BRSVD_ERR_ARG);
+    if (x.size() > 1 && x[0].rows > 0 && x[0].cols > 0) {
+      std::vector<brsvd_tensor> y = x;
+      y.back() = y[0];
+      CHECK(brsvd_grad_clip(x.data(), y.data(), (int64_t)x.size(), 1.f, 1.f, &norm, nullptr) == BRSVD_ERR_ARG);
+      x.back() = x[0];
+      CHECK(brsvd_grad_clip(x.data(), x.data(), (int64_t)x.size(), 1.f, 1.f, &norm, nullptr) == BRSVD_ERR_ARG);
+    }
+  }
 
   std::printf("host checks: %d run, %d failed\n", g_checks, g_failed);
   std::fflush(stdout);
