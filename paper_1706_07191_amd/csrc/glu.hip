@@ -17,26 +17,28 @@ struct Slope {
 // a(g) = g p(g) and its derivative.  Exponentials and reciprocals are the hardware's, good to 2^-22, where results keep eleven bits at most.
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * x)); }
 constexpr float kTanhA = 1.59576912f /* 2 sqrt(2 / pi) */, kTanhB = 0.044715f;
-// Beyond 30 either way p is 0 or 1: cubes and squares stay finite.  NaN stays NaN.
-__device__ __forceinline__ float within30(float g) { return fabsf(g) > 30.f ? copysignf(30.f, g) : g; }
+// Beyond 100 either way p is 0 or 1 in fp32, beyond 30 where its exponent is a square or a cube: g is taken as that there, so that powers stay finite and an infinity, which G may
+// be once it is rounded, has its limit.  NaN stays NaN.
+__device__ __forceinline__ float within(float g, float most) { return fabsf(g) > most ? copysignf(most, g) : g; }
+__device__ __forceinline__ float above(float g) { return g < -100.f ? -100.f : g; }
 __device__ __forceinline__ float activation(float g, int act) {
-  if (act == BRSVD_ACT_SILU) return g * logistic(g);
-  if (act == BRSVD_ACT_GELU) return g * (0.5f * erfcf(-0.707106781f * g));
-  const float c = within30(g);
-  return g * logistic(kTanhA * (c + kTanhB * c * c * c));
+  if (act == BRSVD_ACT_SILU) return above(g) * logistic(g);
+  if (act == BRSVD_ACT_GELU) return above(g) * (0.5f * erfcf(-0.707106781f * g));
+  const float c = within(g, 30.f);
+  return above(g) * logistic(kTanhA * (c + kTanhB * c * c * c));
 }
 __device__ __forceinline__ Slope activation_slope(float g, int act) {
   if (act == BRSVD_ACT_SILU) {
     const float p = logistic(g);
-    return Slope{g * p, p * (1.f + g * (1.f - p))};
+    return Slope{above(g) * p, p * (1.f + within(g, 100.f) * (1.f - p))};
   }
-  const float c = within30(g);
+  const float c = within(g, 30.f);
   if (act == BRSVD_ACT_GELU) {
     const float p = 0.5f * erfcf(-0.707106781f * g);
-    return Slope{g * p, p + c * (0.398942280f * __builtin_amdgcn_exp2f(-0.721347520f * c * c))};
+    return Slope{above(g) * p, p + c * (0.398942280f * __builtin_amdgcn_exp2f(-0.721347520f * c * c))};
   }
   const float p = logistic(kTanhA * (c + kTanhB * c * c * c));
-  return Slope{g * p, p * (1.f + c * (1.f - p) * (kTanhA * (1.f + 3.f * kTanhB * c * c)))};
+  return Slope{above(g) * p, p * (1.f + c * (1.f - p) * (kTanhA * (1.f + 3.f * kTanhB * c * c)))};
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------------

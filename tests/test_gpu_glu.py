@@ -192,6 +192,27 @@ def test_nan_and_infinity_stay_in_their_rows(t, dtype):
     assert torch.equal(got[keep], clean[keep])
 
 
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("act", ACTS)
+def test_infinite_gates(act, dtype):
+    """G that was rounded to an infinity: a and its slope have limits there, a(-inf) = 0, a'(inf) = 1, a'(-inf) = 0, and gradients are finite where those are."""
+    dev = need_gpu()
+    inf = float("inf")
+    G = torch.tensor([[inf, -inf, -inf, 1.0, float("nan")]], dtype=dtype, device=dev).t().contiguous()
+    U, dH = torch.tensor([[2.0, 3.0, -1.0, 0.0, 1.0]], dtype=dtype, device=dev).t().contiguous(), torch.full((5, 1), 0.5, dtype=dtype, device=dev)
+    X, one = torch.ones(5, 1, dtype=dtype, device=dev), torch.ones(1, 1, dtype=dtype, device=dev)
+    by_gate = B.brsvd_glu_backward(X, one, one * 0, G, U, dH, act=act, need_dW=False)[0][:, 0]        # dG, and 0 dU
+    assert by_gate[1:3].tolist() == [0.0, 0.0] and bool(torch.isnan(by_gate[4])) and by_gate[3] == 0.0
+    dWg, dWu = B.brsvd_glu_backward(X[:1], one, one, G[:1], U[:1], dH[:1], act=act, need_dX=False)[1:]
+    assert dWg.item() == 1.0 and dWu.item() == inf                                                     # dH U a'(inf), dH a(inf)
+    dWg, dWu = B.brsvd_glu_backward(X[1:4], one, one, G[1:4], U[1:4], dH[1:4], act=act, need_dX=False)[1:]
+    a = float(act_of(torch.tensor(1.0).double(), act)[0])
+    assert dWg.item() == 0.0 and abs(dWu.item() - 0.5 * a) <= (3 * ROUND[dtype] + 2.0 ** -20) * a      # dU and dWu rounded
+    X = torch.tensor([[1.0, 1.0]], dtype=dtype, device=dev).t().contiguous()
+    H = B.brsvd_glu_forward(X, torch.full((3, 1), -inf, dtype=dtype, device=dev), torch.full((3, 1), 2.0, dtype=dtype, device=dev), act=act)
+    assert bool((H == 0).all())
+
+
 @pytest.mark.parametrize("scale", [2.0 ** -24, 2.0 ** -12, 1.0, 2.0 ** 8])
 def test_fp16_gradients_of_any_size(scale):
     """dH from fp16's finest numbers to large ones: dG and dU keep eleven bits, as one power of two takes them into fp16's range."""
