@@ -5,7 +5,6 @@
 //
 // The tensors' addresses and sizes are arguments of the launches, as many tensors at a time as those hold: nothing is copied to the device, and a captured launch keeps them.
 #include <algorithm>
-#include <functional>
 #include <new>
 
 #include "tile.h"
@@ -273,28 +272,49 @@ static Pieces check_list(const brsvd_tensor* x, const brsvd_tensor* y, int64_t c
   }
   return p;
 }
-// Whether numbers of one tensor are another's too: an address of `out` twice, or that of another tensor; and one that is its own tensor's has to be laid out like it.
+// Where a tensor's numbers lie: `rows` times `width` bytes from `lo` on, `ld` bytes apart
+struct Place {
+  uintptr_t lo, hi;
+  int64_t width, ld;         // ld = 0: one row
+  bool written;
+};
+static Place place_of(const brsvd_tensor& t, bool written) {
+  const int64_t eb = bytes_of((int)t.dtype);
+  const bool one = t.rows == 1 || t.ld == t.cols;
+  const uintptr_t lo = (uintptr_t)t.data;
+  return Place{lo, lo + (uintptr_t)(((t.rows - 1) * (one ? t.cols : t.ld) + t.cols) * eb), (one ? t.rows * t.cols : t.cols) * eb, one ? 0 : t.ld * eb, written};
+}
+// Of places of which b begins in a's extent: whether they share no number, as columns of one matrix do not
+static bool apart(const Place& a, const Place& b) {
+  const int64_t ld = a.ld ? a.ld : b.ld;
+  if (ld == 0 || (a.ld && b.ld && a.ld != b.ld)) return false;
+  const int64_t d = (int64_t)((b.lo - a.lo) % (uintptr_t)ld);
+  return d >= a.width && d + b.width <= ld;
+}
+// Whether a number that one tensor is written to is another's too, whichever of its list; a tensor may be written to its own place.
 static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count) {
   if (count == 0) return BRSVD_OK;
-  const void** places = new (std::nothrow) const void*[2 * count];
+  Place* places = new (std::nothrow) Place[2 * count];
   if (!places) return BRSVD_ERR_ALLOC;
-  const void** others = places + count;
-  int64_t n = 0, m = 0;
+  int64_t n = 0;
   bool good = true;
-  for (int64_t i = 0; i < count; ++i)
-    if (x[i].rows > 0 && x[i].cols > 0) {
-      places[n++] = y[i].data;
-      if (y[i].data != x[i].data) others[m++] = x[i].data;
-      else good &= y[i].dtype == x[i].dtype && (x[i].rows == 1 || y[i].ld == x[i].ld);
+  for (int list = 0; list < 2; ++list) {
+    const int64_t first = n;
+    for (int64_t i = 0; i < count; ++i) {
+      if (x[i].rows == 0 || x[i].cols == 0) continue;
+      if (list == 0) {
+        places[n++] = place_of(y[i], true);
+        good &= y[i].data != x[i].data || (y[i].dtype == x[i].dtype && (x[i].rows == 1 || y[i].ld == x[i].ld));
+      } else if (y[i].data != x[i].data) {
+        places[n++] = place_of(x[i], false);
+      }
     }
-  if (!std::is_sorted(places, places + n)) std::sort(places, places + n);
-  if (!std::is_sorted(others, others + m)) std::sort(others, others + m);
-  for (int64_t i = 1; i < n; ++i) good &= places[i] != places[i - 1];
-  for (int64_t i = 0, j = 0; i < n && j < m && good;) {
-    good = places[i] != others[j];
-    if (std::less<const void*>()(places[i], others[j])) ++i;
-    else ++j;
+    auto before = [](const Place& a, const Place& b) { return a.lo < b.lo; };
+    if (!std::is_sorted(places + first, places + n, before)) std::sort(places + first, places + n, before);
+    if (list == 1) std::inplace_merge(places, places + first, places + n, before);
   }
+  for (int64_t i = 0; i < n; ++i)
+    for (int64_t j = i + 1; j < n && places[j].lo < places[i].hi && good; ++j) good = (!places[i].written && !places[j].written) || apart(places[i], places[j]);
   delete[] places;
   return good ? BRSVD_OK : BRSVD_ERR_ARG;
 }

@@ -132,3 +132,23 @@ def test_lists_refuse(lists, error, text):
 
 def test_empty_lists():
     assert B._tensors([]) == (b"",) and B._tensors((), []) == (b"", b"")
+
+
+def wrote(*pairs):
+    """What clip says to tensors that are read and written; a sound list would go on to the GPU, so a refused one behind it says so."""
+    return clip([a for a, _ in pairs], [b for _, b in pairs])
+
+
+def test_clip_refuses_parts_of_others():
+    whole, part = tensor(), tensor(data=4096 + 400, rows=1, cols=100, ld=100)
+    other, far = tensor(data=65536), tensor(data=131072, rows=1, cols=100, ld=100)
+    assert wrote((whole, whole), (part, part)) == ARG and wrote((part, part), (whole, whole)) == ARG            # a matrix and its lower half, in place
+    assert wrote((other, whole), (far, part)) == ARG and wrote((whole, other), (far, part)) == ARG and wrote((part, far), (other, whole)) == ARG
+    assert wrote((whole, tensor(data=4096 + 4))) == ARG                                                          # one tensor, shifted
+    small = tensor(data=4096, dtype=BF16)
+    assert wrote((other, small), (far, tensor(data=4096 + 398, rows=1, cols=100, ld=100))) == ARG
+    left, right = tensor(rows=10, cols=20, ld=64), tensor(data=4096 + 4 * 19, rows=10, cols=20, ld=64)
+    assert wrote((left, left), (right, right)) == ARG and wrote((left, left), (tensor(data=4096 + 4 * 50, ld=64), tensor(data=4096 + 4 * 50, ld=64))) == ARG
+    assert wrote((left, left), (tensor(data=4096 + 80, ld=63), tensor(data=4096 + 80, ld=63))) == ARG
+    long = tensor(rows=1, cols=1000, ld=1000)
+    assert wrote((long, long), (other, other), (tensor(data=8092, rows=1, cols=1, ld=1), far)) == ARG            # its last number, read

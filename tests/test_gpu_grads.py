@@ -6,6 +6,7 @@ import torch
 
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
+from tests.test_gpu_e4m3 import randn
 
 pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
@@ -220,3 +221,23 @@ def test_refusals():
             call()
     assert bool((x == 1).all() and (y == 1).all())
     assert float(B.brsvd_grad_norm([x, x])) == 4.0
+
+
+def test_columns_of_one_matrix():
+    """Tensors that lie between each other's rows share no number; in place, and one into the gaps of another."""
+    dev = need_gpu()
+    m = randn(3, 40, 300).float().to(dev)
+    parts = [m[:, :100], m[:, 100:101], m[:, 101:290]]
+    want, norm = m.clone(), B.brsvd_grad_norm(parts)
+    exact = math.sqrt(float(m[:, :290].double().square().sum()))
+    assert abs(float(norm) - exact) <= exact * 2.0 ** -23
+    B.brsvd_grad_clip(parts, norm, float("inf"), scale=0.5)
+    want[:, :290] *= 0.5
+    assert torch.equal(m, want)
+    B.brsvd_grad_clip([m[:, :100]], norm, float("inf"), out=[m[:, 150:250]])
+    want[:, 150:250] = want[:, :100]
+    assert torch.equal(m, want)
+    for bad in ([m, m[:, 3:5]], [m[:, :100], m[:, 99:120]], [m.view(-1)[:1000], m.view(-1)[999:]]):
+        with pytest.raises(B.BrsvdError):
+            B.brsvd_grad_clip(bad, norm, 1.0)
+    assert torch.equal(m, want)
