@@ -3,10 +3,10 @@
     python examples/compress_output_matrix.py [--vocab 32768 --dim 1024 --rank 128 --tokens 4096 --steps 40]
 
 W (vocab x dim), as in a trained model with a spectrum that falls off, is factored by the block randomized SVD, W ~ U S V^T,
-and what the factors leave is kept in 8 bits with a scale for each 128 x 128 block.  The loss of the model's logits H W^T is
-worked out without them: for W, for the factors alone (hidden states H V S of width rank, output matrix U) and for the factors
-with the 8-bit remainder.  Then U is repaired by distillation from the stored top logits of W: gradient steps on the
-divergence, whose effect the cross entropy shows.  Inputs are synthetic."""
+and what the factors leave is kept in 8 bits with a scale for each 128 x 128 block, or in 4 bits with a scale for each 32
+numbers of a row.  The loss of the model's logits H W^T is worked out without them: for W, for the factors alone (hidden states
+H V S of width rank, output matrix U) and for the factors with the remainder.  Then U is repaired by distillation from the
+stored top logits of W: clipped gradient steps on the divergence, whose effect the cross entropy shows.  Inputs are synthetic."""
 import argparse
 import math
 import os
@@ -77,17 +77,26 @@ def main(argv=None):
     served = B.brsvd_linear_e4m3(H[:4], Q, scales) + narrow[:4] @ U.t()
     said["logits of four tokens off by"] = float((served - H[:4] @ W.t()).norm() / (H[:4] @ W.t()).norm())
 
+    # and in 4 bits
+    Q, scales = B.brsvd_quantize_e2m1(W - (U * S) @ Vt)
+    said["factors and 4-bit remainder"] = mean_loss(H, (U * S) @ Vt + B.brsvd_dequantize_e2m1(Q, scales, cols=a.dim), words)
+    served = B.brsvd_linear_e2m1(H[:4].bfloat16(), Q, scales).float() + narrow[:4] @ U.t()
+    said["4 bits: logits off by"] = float((served - H[:4] @ W.t()).norm() / (H[:4] @ W.t()).norm())
+
     # distillation of the narrow model: its output matrix moves, the hidden states stay
     h, tau = narrow.bfloat16(), a.temperature
     weight = torch.full((1,), 1.0 / a.tokens, device=dev)
-    M, moment, square = U.clone(), torch.zeros_like(U), torch.zeros_like(U)
+    M, moment, square, g = U.clone(), torch.zeros_like(U), torch.zeros_like(U), torch.empty_like(U)
     for step in range(a.steps):
         w = M.bfloat16()
         loss, lse, z = B.brsvd_distill_forward(h, w, ids, top, tau)
         if step == 0:
             said["divergence before"] = float(loss.mean())
         _, dW = B.brsvd_distill_backward(h, w, ids, top, tau, lse, z, weight, need_dH=False)
-        g = dW.float()
+        norm = B.brsvd_grad_norm([dW])
+        if step == 0:
+            most = float(norm)                                  # later gradients are smaller unless something is wrong
+        B.brsvd_grad_clip([dW], norm, most, out=[g])
         moment.lerp_(g, 0.1)
         square.lerp_(g * g, 0.02)
         M -= 0.02 * float(U.pow(2).mean().sqrt()) * (moment / (1 - 0.9 ** (step + 1))) / ((square / (1 - 0.98 ** (step + 1))).sqrt() + 1e-12)

@@ -1,6 +1,8 @@
 """The operators of a compressed layer together, as a repair step and a server run them: a gated feed-forward block whose second matrix is factors and a remainder in 4 bits,
 the loss of the output matrix behind it, gradients of everything that is not frozen, clipped by their norm; eagerly, as a captured graph, and token by token."""
+import importlib.util
 import math
+import os
 
 import pytest
 import torch
@@ -10,6 +12,7 @@ from tests.gpu_util import need_gpu
 from tests.test_gpu_e4m3 import randn
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 T, D, F, V, R = 300, 136, 400, 1000, 24
 
 
@@ -147,3 +150,13 @@ def test_token_by_token(dtype):
     for got in (one, some):
         assert bool(((got.double() - whole.double()).abs() <= bound).all())
         assert float((got != whole).float().mean()) < 0.2
+
+
+def test_example_keeps_the_remainder_in_4_bits():
+    need_gpu()
+    spec = importlib.util.spec_from_file_location("compress_output_matrix", os.path.join(ROOT, "examples", "compress_output_matrix.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    said = example.main(["--vocab", "2000", "--dim", "151", "--rank", "30", "--tokens", "300", "--steps", "3"])
+    assert all(math.isfinite(v) for v in said.values())
+    assert 0 < said["4 bits: logits off by"] < 1 and said["factors and 4-bit remainder"] > 0
