@@ -330,16 +330,10 @@ k_tiles_e4m3(const E4m3Args g) {
 
 // C (m x n, type dtype) = sum of the splits' parts, in their order
 __global__ void __launch_bounds__(256)
-k_join_splits(const float* __restrict__ part, int splits, int64_t m, int64_t n, void* __restrict__ C, int64_t ldc, int dtype, unsigned first_wg) {
-  const int64_t quads = (n + 3) / 4, i = ((int64_t)first_wg + blockIdx.x) * 256 + threadIdx.x;
-  if (i >= m * quads) return;
-  const int64_t row = i / quads, col = (i - row * quads) * 4, at = row * n + col;
-  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (col + r < n) sum[r] += part[s * m * n + at + r];
-  put_four(C, row * ldc + col, n - col, dtype, sum);
+k_join_splits(const float* __restrict__ part, int splits, int64_t stride, int64_t m, int64_t n, Divisor quads, void* __restrict__ C, int64_t ldc, int dtype) {
+  uint32_t c;
+  const int64_t row = divide(blockIdx.x * 256 + threadIdx.x, quads, &c), col = 4 * (int64_t)c;
+  if (row < m) put_four(C, row * ldc + col, n - col, dtype, sum_of_parts(part + row * n + col, stride, splits, n - col));
 }
 
 // Up to 16 MT rows of A.  The WAVES waves of a workgroup share 16 NT rows of B and take the blocks of the contraction in turn; their sums are added through
@@ -479,8 +473,10 @@ k_rows_e4m3(const E4m3Args g) {
 }
 
 void join_splits(const float* part, int splits, int64_t m, int64_t n, void* C, int64_t ldc, int dtype, hipStream_t stream) {
-  in_launches(ceil_div(m * ceil_div(n, 4), 256), 256, [&](unsigned first, dim3 grid) {
-    hipLaunchKernelGGL(k_join_splits, grid, dim3(256), 0, stream, part, splits, m, n, C, ldc, dtype, first);
+  const int64_t quads = ceil_div(n, 4);
+  by_rows(m, quads, 256, [&](int64_t r, int64_t rows, dim3 grid) {
+    hipLaunchKernelGGL(k_join_splits, grid, dim3(256), 0, stream, part ? part + r * n : nullptr, splits, m * n, rows, n, divisor((uint32_t)quads),
+                       (char*)C + r * ldc * (dtype == BRSVD_DTYPE_F32 ? 4 : 2), ldc, dtype);
   });
 }
 

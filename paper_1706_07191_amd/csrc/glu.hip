@@ -182,16 +182,8 @@ k_glu_join(const GluArgs g, Divisor quads) {
   uint32_t c;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, t = divide((uint32_t)i, quads, &c), f = 4 * (int64_t)c;
   if (t >= tokens) return;
-  floatx4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-  for (int s = 0; s < g.splits; ++s) {
-    const float* row = g.part + ((int64_t)s * tokens + t) * 2 * width + f;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (f + r < width) {
-        a[r] += row[r];
-        b[r] += row[width + r];
-      }
-  }
+  const float* row = g.part + t * 2 * width + f;
+  const floatx4 a = sum_of_parts(row, 2 * tokens * width, g.splits, width - f), b = sum_of_parts(row + width, 2 * tokens * width, g.splits, width - f);
   floatx4 h;
 #pragma unroll
   for (int r = 0; r < 4; ++r) h[r] = activation(a[r], g.act) * b[r];
@@ -324,17 +316,20 @@ __global__ void __launch_bounds__(256)
 k_glu_tops(const SlopeArgs g) {
   __shared__ float red[4];
   float top = 0.f;
-  const int64_t all = g.tokens * g.pieces.d;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)kTops * 256) {
+  uint32_t c, dc;
+  const uint32_t dt = divide(kTops * 256, g.pieces, &dc);
+  for (int64_t t = divide(blockIdx.x * 256 + threadIdx.x, g.pieces, &c); t < g.tokens;) {
     float a[8], b[8];
-    const int64_t t = i / g.pieces.d;
-    slopes_of<Fp16>(g, t, 8 * (i - t * g.pieces.d), a, b);
+    slopes_of<Fp16>(g, t, 8 * (int64_t)c, a, b);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float m = fabsf(a[j]), n = fabsf(b[j]);
       if (m <= 3.402823466e38f) top = fmaxf(top, m);
       if (n <= 3.402823466e38f) top = fmaxf(top, n);
     }
+    t += dt;
+    c += dc;
+    if (c >= g.pieces.d) c -= g.pieces.d, ++t;
   }
   top = max_of_workgroup(top, red);
   if (threadIdx.x == 0) g.tops[blockIdx.x] = top;
@@ -494,13 +489,7 @@ k_glu_sum(const GradArgs g, int matrices, Divisor quads) {
   const int64_t row = divide(blockIdx.x * 256 + threadIdx.x, quads, &c), col = 4 * (int64_t)c;
   if (row >= matrices * g.rows) return;
   const int which = row >= g.rows;
-  floatx4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < g.splits; ++s) {
-    const float* from = g.part + ((int64_t)s * matrices * g.rows + row) * g.cols + col;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (col + r < g.cols) x[r] += from[r];
-  }
+  floatx4 x = sum_of_parts(g.part + row * g.cols + col, matrices * g.rows * g.cols, g.splits, g.cols - col);
   if (g.down) x *= *g.down;
   put_four(g.out[which], (row - which * g.rows) * g.ldo[which] + col, g.cols - col, __is_same(El, Bf16) ? BRSVD_DTYPE_BF16 : BRSVD_DTYPE_F16, x);
 }

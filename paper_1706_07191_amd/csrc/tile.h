@@ -482,6 +482,29 @@ __device__ __forceinline__ void put_four(void* C, int64_t at, int64_t left, int 
   }
 }
 
+// The sum of four neighbouring numbers (of `left` that the row still has) over `parts` parts, `stride` numbers apart, in their order; four parts on their way
+__device__ __forceinline__ floatx4 sum_of_parts(const float* __restrict__ from, int64_t stride, int parts, int64_t left) {
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (left >= 4) {
+    auto part = [&](int s) { return __builtin_bit_cast(floatx4, *(const Piece*)(from + s * stride)); };
+    int s = 0;
+    for (; s + 4 <= parts; s += 4) {
+      floatx4 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = part(s + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += x[i];
+    }
+    for (; s < parts; ++s) sum += part(s);
+  } else {
+    for (int s = 0; s < parts; ++s)
+#pragma unroll
+      for (int r = 0; r < 3; ++r)
+        if (r < left) sum[r] += from[s * stride + r];
+  }
+  return sum;
+}
+
 // A workgroup's tile D (of sums, a wave has 8 x NQ tiles of it) to memory as 16-bit numbers: row j of `out` (pitch ldo numbers) gets column j of D, of which
 // `rows` and `cols` are there.  A lane's four numbers of a row go through LDS, so that a row's 256 leave as one piece of memory, 16 bytes a lane at any
 // alignment: stored from where they are, 32 bytes of a row at a time, an 8192 x 8192 result took 33 us.  Eight bytes u of row j lie at
