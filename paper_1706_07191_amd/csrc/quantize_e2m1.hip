@@ -19,7 +19,8 @@ __device__ __forceinline__ uint32_t max_of_group(uint32_t x) {
   return x;
 }
 
-// A thread has 16 bytes of a group, U groups of them on their way.  Bound by memory.
+// A thread has 16 bytes of a group, so that lanes read next to each other, and U such pieces on their way; the group's largest number goes between four or eight lanes in registers.
+// Bound by memory: 20000 x 20000 fp32 373 us (1.81 GB, 4.9 TB/s).
 template <int DT, int U>
 __global__ void __launch_bounds__(256)
 k_quantize_e2m1(const char* __restrict__ X, int64_t ldx_bytes, int64_t rows, int64_t cols, Divisor groups, uint8_t* __restrict__ Q, int64_t ldq, uint8_t* __restrict__ S) {
@@ -83,7 +84,7 @@ k_quantize_e2m1(const char* __restrict__ X, int64_t ldx_bytes, int64_t rows, int
   }
 }
 
-// A thread writes 16 bytes.  Bound by memory.
+// A thread writes 16 bytes, and has U such pieces on their way.  Bound by memory: 20000 x 20000 to fp32 300 us (1.81 GB, 6.0 TB/s).
 template <int DT, int U>
 __global__ void __launch_bounds__(256)
 k_dequantize_e2m1(const uint8_t* __restrict__ Q, int64_t ldq, const uint8_t* __restrict__ S, int64_t rows, int64_t cols, Divisor pieces, int64_t groups,
