@@ -359,3 +359,18 @@ def test_refusals():
     for call in (lambda: B.brsvd_dequantize_e2m1(Q, S, cols=254), lambda: B.brsvd_dequantize_e2m1(Q, S, cols=257), lambda: B.brsvd_linear_e2m1_backward(X[:, :4], Q, S, cols=12)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("m,n,k", [(530001, 64, 4099), (70001, 33000, 64)])
+def test_products_of_more_than_4_gib(m, n, k):
+    """Operands and results whose bytes, and results whose numbers, pass 32 bits: rows at both ends and where they pass."""
+    dev = need_gpu()
+    W, S, w = four_bits(m, n, k, dev)
+    X = randn(m, 997, k).bfloat16().to(dev).repeat(-(-m // 997), 1)[:m]
+    Y = B.brsvd_linear_e2m1(X, W, S)
+    dX = B.brsvd_linear_e2m1_backward(Y, W, S, cols=k)
+    widest = max(n, k)
+    for first in (0, 2 ** 31 // widest - 20, 2 ** 32 // (2 * widest) + 1, m - 60):
+        at = slice(min(first, m - 60), min(first, m - 60) + 60)
+        check_product(Y[at], X[at].double().cpu(), w.t())
+        check_product(dX[at], Y[at].double().cpu(), w)

@@ -324,3 +324,26 @@ def test_refusals():
     for call in (lambda: B.brsvd_glu_forward(X, Wg, Wu, act="relu"), lambda: B.brsvd_glu_backward(X, Wg, Wu, G, U, H, need_dX=False, need_dW=False)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_more_than_4_gib():
+    """X, G, U, H, dG and dU whose bytes and numbers pass 32 bits: rows at both ends and where they pass; the tokens repeat, so that the weights' gradients are known."""
+    dev = need_gpu()
+    t, d, f, period = 140000, 64, 16008, 1000
+    X, Wg, Wu = problem(period, d, f, torch.bfloat16, dev)
+    dH = randn(8, period, f).bfloat16().to(dev)
+    some = B.brsvd_glu_forward(X, Wg, Wu, keep=True)
+    some_back = B.brsvd_glu_backward(X, Wg, Wu, *some[1:], dH)
+    many = X.repeat(t // period, 1)
+    H, G, U = B.brsvd_glu_forward(many, Wg, Wu, keep=True)
+    dX, dWg, dWu = B.brsvd_glu_backward(many, Wg, Wu, G, U, dH.repeat(t // period, 1))
+    for first in (0, 2 ** 31 // (2 * f) // period * period, 2 ** 31 // f // period * period, t - period):
+        at = slice(first, first + period)
+        for a, b in ((H, some[0]), (G, some[1]), (U, some[2])):
+            assert torch.equal(a[at], b)                      # a contraction of one step, in whatever tiles
+        # 16 bits of the same sum in other parts
+        assert float((dX[at].double() - some_back[0].double()).norm() / some_back[0].double().norm()) <= 2 * ROUND[torch.bfloat16]
+    # the sum over a period comes back t / period times, so that what is added up to is the result at most, and each of t additions cuts off a step of that
+    for a, b in ((dWg, some_back[1]), (dWu, some_back[2])):
+        b = b.double() * (t // period)
+        assert float((a.double() - b).norm() / b.norm()) <= 2 * ROUND[torch.bfloat16] + 2 * STEP * t

@@ -110,6 +110,24 @@ def test_lists_of_any_length(count):
     check_clipped(out, tensors, float(norm), 0.25, -0.5)
 
 
+@pytest.mark.parametrize("count", [63, 64, 65, 85, 86, 126, 127, 128, 129, 300])
+@pytest.mark.parametrize("every", [1, 2, 3])
+def test_matrices_with_strided_rows_at_any_place(count, every):
+    """They take two places in a launch's list: the list ends before, between and behind them."""
+    dev = need_gpu()
+    tensors = drawn(count, [(2 + i % 5, 1 + i * 7 % 40) for i in range(count)], dev)
+    for i in range(0, count, every):
+        wide = torch.full((tensors[i].shape[0], tensors[i].shape[1] + 3), 7.0, dtype=tensors[i].dtype, device=dev)
+        wide[:, 1:-2] = tensors[i]
+        tensors[i] = wide[:, 1:-2]
+    norm = B.brsvd_grad_norm(tensors)
+    check_norm(norm, tensors, 1.0)
+    out = [torch.full((t.shape[0], t.shape[1] + i % 2), 9.0, device=dev)[:, :t.shape[1]] for i, t in enumerate(tensors)]
+    B.brsvd_grad_clip(tensors, norm, 0.25, out=out)
+    check_clipped(out, tensors, float(norm), 0.25)
+    assert all(bool((o._base[:, -1] == 9).all()) for i, o in enumerate(out) if i % 2)
+
+
 def test_no_tensors_and_empty_ones():
     dev = need_gpu()
     assert float(B.brsvd_grad_norm([])) == 0
