@@ -23,18 +23,21 @@ struct E2m1Args {
 };
 
 // Up to 16 MT rows of X.  The WAVES waves of a workgroup share 16 NT rows of W and take chunks of 128 numbers of the contraction in turn; their sums are added
-// through LDS in wave order.  A lane reads one group of a chunk, 16 bytes, and the four scales of its row; lanes then exchange words, so that an instruction takes one
+// through LDS in wave order.  A lane reads one group of a chunk, 16 bytes; lanes then exchange words, so that an instruction takes one
 // group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  The U chunks that a wave takes next are on their way.
+// The scales of the workgroup's rows come first, whole rows of them, into LDS (where a contraction has more than there is room for, for as many chunks at a time): four bytes of 16
+// rows for each chunk, as they are used, take as many lines as W itself.
 // Bound by what a CU can have on its way: 1 x 4096 x 4096 5.5 us (8.9 MB; a launch is four), 24 x 20000 x 5000 23 us (58 MB fetched, 2.5 TB/s; 10.4 at a copy's rate): the 24
 // rows of X take three fifths of what a wave loads.  With X kept in registers while W streams past 27 us.
 template <class El, int MT, int NT, int U, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES)
 k_rows_e2m1(const E2m1Args g) {
-  struct __attribute__((packed, aligned(1))) Word {
-    uint32_t x;
-    __device__ operator uint32_t() const { return x; }
-  };
-  __shared__ floatx4 parts[WAVES][MT * NT][64];
+  struct __attribute__((packed, aligned(1))) Word { uint32_t x; };
+  constexpr int kRoom = 24576, kChunks = kRoom / (64 * NT) - 1, kMine = 16 * NT / WAVES;      // bytes for scales; chunks whose scales they hold; rows of them that a wave brings
+  constexpr int kParts = WAVES * MT * NT * 64 * 16;
+  __shared__ __attribute__((aligned(16))) char lds[kParts > kRoom ? kParts : kRoom];
+  uint32_t* scales = (uint32_t*)lds;
+  auto parts = [&](int w, int i) -> floatx4& { return ((floatx4*)lds)[(w * MT * NT + i) * 64 + (threadIdx.x & 63)]; };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = lane & 15, group = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16 * NT;
   floatx4 acc[MT][NT];
@@ -42,12 +45,11 @@ k_rows_e2m1(const E2m1Args g) {
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int u = 0; u < NT; ++u) acc[t][u] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const uint8_t *rw[NT], *rs[NT];
+  const uint8_t* rw[NT];
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     const int64_t n = n0 + 16 * u + row, in = n < g.W.n ? n : g.W.n - 1;
     rw[u] = g.W.base + in * g.W.ld + 16 * group;
-    rs[u] = g.W.scales + in * g.W.groups;
   }
   const char* rx[MT];
 #pragma unroll
@@ -55,66 +57,95 @@ k_rows_e2m1(const E2m1Args g) {
     const int64_t m = 16 * t + row < g.X.n ? 16 * t + row : g.X.n - 1;
     rx[t] = g.X.base + m * g.X.ld + 16 * group;
   }
-  struct Chunk {
-    uint4 w[NT], x[MT][4];
-    uint32_t s[NT];
-  };
+  struct Chunk { uint4 w[NT], x[MT][4]; };
   auto fetch = [&](Chunk& c, int at, bool whole, int64_t left) {       // left: numbers of the row from the chunk on
 #pragma unroll
-    for (int u = 0; u < NT; ++u) {
-      c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left - kGroup * group);
-      const uint8_t* s = rs[u] + (int64_t)at * 4;
-      if (whole) c.s[u] = *(const Word*)s;
-      else {
-        c.s[u] = 0x7f7f7f7fu;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (left > kGroup * j) c.s[u] += (uint32_t)(s[j] - 127) << (8 * j);
-      }
-    }
+    for (int u = 0; u < NT; ++u) c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left - kGroup * group);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) c.x[t][j] = piece_of<2>(rx[t] + (int64_t)at * 256 + 64 * j, whole ? 16 : 2 * (left - kGroup * j - 8 * group));
   };
-  auto multiply = [&](const Chunk& c) {
+  auto multiply = [&](const Chunk& c, const uint32_t* four, int pitch, uint32_t there, uint32_t missing) {       // four: scales of the chunk, of this lane's first row
+    uint32_t four_of[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) four_of[u] = four[16 * u * pitch];
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
+      const uint32_t s = (four_of[u] & there) | missing;
       uint32_t w[4] = {c.w[u].x, c.w[u].y, c.w[u].z, c.w[u].w};
       turn_groups(w);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int4v p = __builtin_bit_cast(int4v, eight_e2m1<El>(w[j], scale_e8m0(c.s[u] >> (8 * j) & 255)));
+        const int4v p = __builtin_bit_cast(int4v, eight_e2m1<El>(w[j], scale_e8m0(s >> (8 * j) & 255)));
 #pragma unroll
         for (int t = 0; t < MT; ++t) acc[t][u] = mfma16<El>(p, __builtin_bit_cast(int4v, c.x[t][j]), acc[t][u]);
       }
+      if (MT > 2) __builtin_amdgcn_sched_barrier(0);        // numbers of one tile at a time: the registers are taken
     }
   };
-  const int whole = (int)(g.k / kChunk);
-  Chunk c[U];
+  // Four scales of row r of the workgroup's from chunk `at` on, behind those of the row's end any bytes; `last`: the array may end here
+  auto four_scales = [&](int r, int at, bool last) {
+    const int64_t n = n0 + r < g.W.n ? n0 + r : g.W.n - 1, left = last ? (g.W.n - n) * g.W.groups - 4 * (int64_t)at : 4;       // bytes that are there
+    const uint8_t* from = g.W.scales + n * g.W.groups + 4 * (int64_t)at;
+    if (left >= 4) return ((const Word*)from)->x;
+    uint32_t x = 0;
 #pragma unroll
-  for (int i = 0; i < U; ++i)
-    if (wave + WAVES * i < whole) fetch(c[i], wave + WAVES * i, true, 0);
-  for (int b = wave; b < whole; b += WAVES * U) {
+    for (int j = 0; j < 3; ++j)
+      if (j < left) x |= (uint32_t)from[j] << (8 * j);
+    return x;
+  };
+  const int whole = (int)(g.k / kChunk), all = (int)((g.k + kChunk - 1) / kChunk);
+  const bool last = (g.W.n - n0 - 16 * NT) * g.W.groups < 4;
+  const uint32_t* four = scales;       // of this lane's first row, at chunk 0
+  int pitch = 0;
+  for (int first = 0; first < all; first += kChunks) {
+    const int count = all - first < kChunks ? all - first : kChunks, end = first + count < whole ? first + count : whole;
+    pitch = count | 1;                 // odd: rows in different banks
+    if (first > 0) __syncthreads();
+    for (int j = lane; j < count; j += 64) {
+      uint32_t x[kMine];
+      if (last) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (b + WAVES * i < whole) multiply(c[i]);
-      if (b + WAVES * (i + U) < whole) fetch(c[i], b + WAVES * (i + U), true, 0);
+        for (int i = 0; i < kMine; ++i) x[i] = four_scales(kMine * wave + i, first + j, true);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) x[i] = four_scales(kMine * wave + i, first + j, false);
+      }
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) scales[(kMine * wave + i) * pitch + j] = x[i];
+    }
+    Chunk c[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (first + wave + WAVES * i < end) fetch(c[i], first + wave + WAVES * i, true, 0);
+    meet_but<63>();              // what has been fetched may be on its way
+    four = scales + row * pitch - first;
+    for (int b = first + wave; b < end; b += WAVES * U) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (b + WAVES * i < end) multiply(c[i], four + b + WAVES * i, pitch, ~0u, 0);
+        if (b + WAVES * (i + U) < end) fetch(c[i], b + WAVES * (i + U), true, 0);
+      }
     }
   }
-  if (g.k % kChunk != 0 && whole % WAVES == wave) {          // the contraction's end, after the wave's other chunks
-    fetch(c[0], whole, false, g.k - (int64_t)whole * kChunk);
-    multiply(c[0]);
+  if (whole < all && whole % WAVES == wave) {          // the contraction's end, after the wave's other chunks
+    const int64_t left = g.k - (int64_t)whole * kChunk;
+    const uint32_t there = left > 3 * kGroup ? ~0u : left > 2 * kGroup ? 0xffffffu : left > kGroup ? 0xffffu : 0xffu;      // scales of the row; other groups are zeros, times 1
+    Chunk c;
+    fetch(c, whole, false, left);
+    multiply(c, four + whole, pitch, there, 0x7f7f7f7fu & ~there);
   }
+  __syncthreads();               // the scales have been read
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int u = 0; u < NT; ++u) parts[wave][t * NT + u][lane] = acc[t][u];
+    for (int u = 0; u < NT; ++u) parts(wave, t * NT + u) = acc[t][u];
   __syncthreads();
   for (int i = wave; i < MT * NT; i += WAVES) {
-    floatx4 sum = parts[0][i][lane];
+    floatx4 sum = parts(0, i);
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) sum += parts[w][i][lane];
+    for (int w = 1; w < WAVES; ++w) sum += parts(w, i);
     const int64_t m = 16 * (i / NT) + row, n = n0 + 16 * (i % NT) + 4 * group;
     if (m < g.X.n && n < g.W.n) put_four(g.C, m * g.ldc + n, g.W.n - n, __is_same(El, Bf16) ? BRSVD_DTYPE_BF16 : BRSVD_DTYPE_F16, sum);
   }

@@ -374,3 +374,18 @@ def test_products_of_more_than_4_gib(m, n, k):
         at = slice(min(first, m - 60), min(first, m - 60) + 60)
         check_product(Y[at], X[at].double().cpu(), w.t())
         check_product(dX[at], Y[at].double().cpu(), w)
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 49153 + 100), (16, 33, 98437), (5, 17, 49024), (9, 4112, 24448 + 33), (20, 12000, 9600 * 2 + 64)])
+def test_more_scales_than_a_workgroup_holds(m, n, k):
+    """Few rows and a long contraction: the scales of a workgroup's rows of W come in parts.  The first and the last of W's rows against 64 bits."""
+    dev = need_gpu()
+    g = torch.Generator(device=dev).manual_seed(k)
+    W = torch.randint(0, 256, (n, (k + 1) // 2), generator=g, device=dev).to(torch.uint8)
+    S = torch.randint(124, 131, (n, -(-k // 32)), generator=g, device=dev).to(torch.uint8)
+    X = randn(m, m, k).bfloat16().to(dev)
+    Y = B.brsvd_linear_e2m1(X, W.view(torch.float4_e2m1fn_x2), S.view(torch.float8_e8m0fnu))
+    for at in (slice(0, 20), slice(max(n - 90, 0), n)):
+        b = W[at].long().cpu()
+        w = values(torch.stack([b & 15, b >> 4], dim=2).view(b.shape[0], -1)[:, :k], S[at].long().cpu())
+        check_product(Y[:, at], X.double().cpu(), w.t())
