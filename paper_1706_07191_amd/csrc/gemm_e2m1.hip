@@ -22,18 +22,18 @@ struct E2m1Args {
   int64_t tiles_p, tiles_q, first;     // tiles along W and along X; column that the first tile begins with
 };
 
-// Up to 16 MT rows of X.  The WAVES waves of a workgroup share 16 NT rows of W and take chunks of 128 numbers of the contraction in turn; their sums are added
+// Up to 16 MT rows of X.  The eight waves of a workgroup share 16 NT rows of W and take chunks of 128 numbers of the contraction in turn; their sums are added
 // through LDS in wave order.  A lane reads one group of a chunk, 16 bytes; lanes then exchange words, so that an instruction takes one
-// group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  The U chunks that a wave takes next are on their way.
+// group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  A wave's next chunk is on its way while it multiplies one.
 // The scales of the workgroup's rows come first, whole rows of them, into LDS (where a contraction has more than there is room for, for as many chunks at a time): four bytes of 16
 // rows for each chunk, as they are used, take as many lines as W itself.
 // Bound by what a CU can have on its way: 1 x 4096 x 4096 5.5 us (8.9 MB; a launch is four), 24 x 20000 x 5000 23 us (58 MB fetched, 2.5 TB/s; 10.4 at a copy's rate): the 24
 // rows of X take three fifths of what a wave loads.  With X kept in registers while W streams past 27 us.
-template <class El, int MT, int NT, int U, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES)
+template <class El, int MT, int NT>
+__global__ void __launch_bounds__(512)
 k_rows_e2m1(const E2m1Args g) {
   struct __attribute__((packed, aligned(1))) Word { uint32_t x; };
-  constexpr int kRoom = 24576, kChunks = kRoom / (64 * NT) - 1, kMine = 16 * NT / WAVES;      // bytes for scales; chunks whose scales they hold; rows of them that a wave brings
+  constexpr int WAVES = 8, kRoom = 24576, kChunks = kRoom / (64 * NT) - 1, kMine = 16 * NT / WAVES;      // bytes for scales; chunks whose scales they hold; rows of them that a wave brings
   constexpr int kParts = WAVES * MT * NT * 64 * 16;
   __shared__ __attribute__((aligned(16))) char lds[kParts > kRoom ? kParts : kRoom];
   uint32_t* scales = (uint32_t*)lds;
@@ -115,18 +115,14 @@ k_rows_e2m1(const E2m1Args g) {
 #pragma unroll
       for (int i = 0; i < kMine; ++i) scales[(kMine * wave + i) * pitch + j] = x[i];
     }
-    Chunk c[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (first + wave + WAVES * i < end) fetch(c[i], first + wave + WAVES * i, true, 0);
+    Chunk c;
+    int at = first + wave;
+    if (at < end) fetch(c, at, true, 0);
     meet_but<63>();              // what has been fetched may be on its way
     four = scales + row * pitch - first;
-    for (int b = first + wave; b < end; b += WAVES * U) {
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (b + WAVES * i < end) multiply(c[i], four + b + WAVES * i, pitch, ~0u, 0);
-        if (b + WAVES * (i + U) < end) fetch(c[i], b + WAVES * (i + U), true, 0);
-      }
+    for (; at < end; at += WAVES) {
+      multiply(c, four + at, pitch, ~0u, 0);
+      if (at + WAVES < end) fetch(c, at + WAVES, true, 0);
     }
   }
   if (whole < all && whole % WAVES == wave) {          // the contraction's end, after the wave's other chunks
@@ -198,17 +194,14 @@ void align_rows(const void* from, int64_t ld, int64_t rows, int64_t bytes, void*
 
 static uint64_t whole256(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Few rows of X: by the 16 rows of W in a wave (NT of them).  A CU takes a KiB of W in some time t, wherever it comes from, and the 16 rows of X that go with a chunk in 0.6 t;
-// with NT for which the workgroups fill rounds of 256 it has least to do: 16 x 12000 x 4096 11.3 us with three (250 workgroups), 16.5 with two (375), 18 with one (750);
-// 64 x 20000 x 5000 34, 43, 48 and 74 with five, three, two and one.  Up to eight rows the caches give X for less, and more than three are slower: 1 x 20000 x 5000 15.9 with
-// one, 17.9 with five.
+// Few rows of X: by the 16 rows of W in a wave (NT of them).  A round of 256 workgroups takes some time for what they read of W and of X, and all of them a start, which rounds share; with NT
+// for which the workgroups fill rounds there is least to do.  In units of 0.08 us at 4096 columns: 16 x 12000 x 4096 10.2 us with three (250 workgroups), 14.1 with two (375), 16.3 with
+// one (750); 16 x 20000 x 4096 12.7, 16.7, 19.6 and 24.8 with five, three, two and one; 1 x 20000 x 4096 10.8 and 12.6 with five and one.  Of 60 sizes the best is met or missed by 8 % at most.
 static int rows_in_wave(int64_t m, int64_t n) {
-  const int64_t tiles = ceil_div(n, 16), x = m <= 8 ? 3 : 6 * ceil_div(m, 16);
   int best = 1;
   int64_t least = 0;
   for (int nt : {1, 2, 3, 5}) {
-    if (nt == 5 && m <= 8) continue;
-    const int64_t cost = ceil_div(ceil_div(tiles, nt), 256) * (10 * nt + x);
+    const int64_t cost = ceil_div(ceil_div(n, 16 * nt), 256) * (16 + 10 * nt + 2 * m) + 10 * nt;
     if (nt == 1 || cost < least) least = cost, best = nt;
   }
   return best;
@@ -224,9 +217,10 @@ static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k, bool aligned, bool ba
   const int64_t cols = backward ? k : n, in = backward ? n : k;
   E2m1Plan p;
   p.tiles = tile_plan(ceil_div(cols, 256), m, ceil_div(in, 64), 1, m * cols, backward ? kBackward : kForward);
-  // Above 16 rows tiles are ahead where the contraction is long and W has few rows: 64 x 1000 x 8000 22 us, 31 in rows (a wave's chunk 0.35 us for 16 rows of W, 0.65 for 16 of X)
+  // Above 16 rows tiles are ahead where the contraction is long and W has few rows: 48 x 4096 x 10240 21 us, 31 in rows; the other way round 48 x 12000 x 4096 22 and 18.  Eight chunks of a
+  // wave each take 0.35 us for 16 rows of W and 0.05 for a row of X.
   const int nt = rows_in_wave(m, n);
-  const double rows_us = 5.0 + (double)(ceil_div(ceil_div(k, kChunk), 8) * ceil_div(ceil_div(n, 16 * nt), 256)) * (0.35 * nt + 0.65 * ceil_div(m, 16));
+  const double rows_us = 3.5 + (double)(ceil_div(ceil_div(k, kChunk), 8) * ceil_div(ceil_div(n, 16 * nt), 256)) * (0.35 * nt + 0.05 * m);
   p.rows = !backward && (m <= 16 || (m <= 64 && rows_us <= p.tiles.us));
   if (p.rows) p.tiles.splits = 1;
   const bool laid = !p.rows && !aligned;
@@ -236,19 +230,17 @@ static E2m1Plan e2m1_plan(int64_t m, int64_t n, int64_t k, bool aligned, bool ba
   return p;
 }
 
-template <class El, int MT, int NT, int U, int WAVES>
+template <class El, int MT, int NT>
 static void launch_rows(const E2m1Args& g, hipStream_t stream) {
-  hipLaunchKernelGGL((k_rows_e2m1<El, MT, NT, U, WAVES>), dim3((unsigned)ceil_div(g.W.n, 16 * NT)), dim3(64 * WAVES), 0, stream, g);
+  hipLaunchKernelGGL((k_rows_e2m1<El, MT, NT>), dim3((unsigned)ceil_div(g.W.n, 16 * NT)), dim3(512), 0, stream, g);
 }
-// Chunks on their way as registers allow: two in each of four waves or one in each of eight, two in each of eight where a wave has one tile.
 template <class El, int MT>
 static void launch_rows(const E2m1Args& g, hipStream_t stream) {
-  constexpr int U = MT <= 2 ? 2 : 1, WAVES = MT <= 2 ? 4 : 8;
   switch (rows_in_wave(g.X.n, g.W.n)) {
-    case 1: return launch_rows<El, MT, 1, U, 8>(g, stream);
-    case 2: return launch_rows<El, MT, 2, U, WAVES>(g, stream);
-    case 3: return launch_rows<El, MT, 3, U, WAVES>(g, stream);
-    default: return launch_rows<El, MT, 5, U, WAVES>(g, stream);
+    case 1: return launch_rows<El, MT, 1>(g, stream);
+    case 2: return launch_rows<El, MT, 2>(g, stream);
+    case 3: return launch_rows<El, MT, 3>(g, stream);
+    default: return launch_rows<El, MT, 5>(g, stream);
   }
 }
 template <class El, int NQ, Order O>

@@ -597,7 +597,7 @@ inline int64_t large_tiles(int64_t np, int64_t q256, int64_t q128, int64_t steps
 }
 
 // How a product of `q` rows and p_tiles tiles of 256 columns, `both` times, over `steps` steps is cut into tiles and parts of its contraction: by what a tile of 64, 128 or
-// 256 rows takes for a step on a CU of its own (`step`, in 1/100 us), 5 us for a tile's start and end and for a launch, and 4.5 TB/s for the parts and their join.  244 plans of 26
+// 256 rows takes for a step on a CU of its own (`step`, in 1/100 us), 5 us for a tile's start and end and for a launch, 3 and 4.5 TB/s for the parts and their join.  244 plans of 26
 // products of 4-bit weights, from one tile to 500, meet this within 7 % on average.  So a contraction is cut where CUs would have nothing to do: 300 x 2000 over 8192 39 us in
 // 8 parts, 124 in one; and tiles are small where they are few: 300 x 8192 over 2000 32 us in tiles of 64, 36 in 128 and two parts.
 struct TilePlan {
@@ -612,7 +612,7 @@ inline TilePlan tile_plan(int64_t p_tiles, int64_t q, int64_t steps, int both, i
   auto rounds = [](int64_t workgroups) { return (double)(((workgroups + 7) / 8 + 31) / 32); };      // of 32 CUs in each of eight XCDs
   auto consider = [&](int nq, int64_t large, int splits) {
     const int64_t each = (steps + splits - 1) / splits, parts = (steps + each - 1) / each;
-    double us = 5.0 + (parts > 1 ? 5.0 + (double)parts * numbers * 4 / 4.5e6 : 0.0);
+    double us = 5.0 + (parts > 1 ? 3.0 + (double)parts * numbers * 4 / 4.5e6 : 0.0);
     if (large > 0) us += rounds(large * both * parts * ((q + 255) / 256)) * (5.0 + 0.01 * step[2] * each);
     if (large < p_tiles) us += rounds((p_tiles - large) * both * parts * ((q + 64 * nq - 1) / (64 * nq))) * (5.0 + 0.01 * step[nq - 1] * each) + (large > 0 ? 2.0 : 0.0);
     if (best.us < 0 || us < best.us) best = TilePlan{nq, p_tiles, large, (int)parts, 64 * each, us};
