@@ -32,13 +32,27 @@ __device__ __forceinline__ uint4 eight_e2m1(uint32_t w, float scale) {
   return make_uint4(two_e2m1<El, 0>(w, scale), two_e2m1<El, 1>(w, scale), two_e2m1<El, 2>(w, scale), two_e2m1<El, 3>(w, scale));
 }
 
-// 16 bytes from `src`, the numbers of a group, of which the first `valid` are there; the others are zero.
-__device__ __forceinline__ uint4 group_of(const uint8_t* src, int64_t valid) {
+// 16 bytes from `src`, of which the first `have` are there and the others zero; `before` bytes of the row are in front of them.  One load, of the row's last 16 bytes: put together
+// number by number, each waiting for the one before, the end of a contraction took as long as ten of its steps.
+__device__ __forceinline__ uint4 piece_at_end(const uint8_t* src, int64_t have, int64_t before) {
+  if (have <= 0) return make_uint4(0u, 0u, 0u, 0u);
+  if (have < 16 && before + have < 16) return piece_of<1>((const char*)src, have);
+  const int back = have < 16 ? 16 - (int)have : 0;
+  const Piece v = *(const Piece*)(src - back);
+  uint64_t lo = v.x[0] | (uint64_t)v.x[1] << 32, hi = v.x[2] | (uint64_t)v.x[3] << 32;
+  const int s = 8 * back;
+  if (s >= 64) lo = hi >> (s - 64), hi = 0;
+  else if (s > 0) lo = lo >> s | hi << (64 - s), hi >>= s;
+  return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+// 16 bytes from `src`, the numbers of a group, of which the first `valid` are there; the others are zero.  `before`: the row's bytes in front of them
+__device__ __forceinline__ uint4 group_of(const uint8_t* src, int64_t valid, int64_t before) {
   if (valid >= kGroup) {
     const Piece v = *(const Piece*)src;
     return make_uint4(v.x[0], v.x[1], v.x[2], v.x[3]);
   }
-  uint4 v = piece_of<1>((const char*)src, valid > 0 ? (valid + 1) / 2 : 0);
+  uint4 v = piece_at_end(src, valid > 0 ? (valid + 1) / 2 : 0, before);
   if (valid > 0 && (valid & 1)) {            // the upper half of the last byte is no number of the row
     uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -94,6 +108,7 @@ struct E2m1Feed {
   uint32_t off, scale_off;
   int64_t step, scale_step;
   int32_t valid;                     // kCols: the group's columns that are there
+  int32_t front;                     // bytes of the row that are in front of the first step's group at least
   bool ragged;                       // kCols: the columns end inside the tile's last group
 
   struct Group {
@@ -114,6 +129,7 @@ struct E2m1Feed {
       scale_off = (uint32_t)(r * op.groups + (tid & 1));
       ragged = false;
       valid = kGroup;
+      front = 16 * (tid & 1);
     } else {
       const int row = tid >> 3, c = kGroup * (tid & 7) < left ? tid & 7 : 0;      // a group beyond the end: some other one, nothing of it is stored
       at = op.base + k0 * op.ld + first / 2;
@@ -122,6 +138,7 @@ struct E2m1Feed {
       scale_step = 64 * op.groups;
       ragged = left < 256 && left % kGroup != 0;
       valid = (int32_t)(left - kGroup * c < kGroup ? left - kGroup * c : kGroup);
+      front = 16 * c;
       off = (uint32_t)(row * op.ld + 16 * c);
       scale_off = (uint32_t)(row * op.groups + c);
     }
@@ -141,7 +158,7 @@ struct E2m1Feed {
     const int64_t left = k - (int64_t)t * 64;
     const int there = O == kRows ? (int)(left < 64 ? left : 64) - kGroup * (threadIdx.x & 1) : (int)threadIdx.x >> 3 < left ? valid : 0;
     Group x;
-    x.w = group_of(at + off, there);
+    x.w = group_of(at + off, there, front + (O == kRows ? (int64_t)t * 32 : 0));
     x.s = there > 0 ? scale_at[scale_off] : 127;
     at += step;
     scale_at += scale_step;

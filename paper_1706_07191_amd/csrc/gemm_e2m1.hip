@@ -60,11 +60,14 @@ k_rows_e2m1(const E2m1Args g) {
   struct Chunk { uint4 w[NT], x[MT][4]; };
   auto fetch = [&](Chunk& c, int at, bool whole, int64_t left) {       // left: numbers of the row from the chunk on
 #pragma unroll
-    for (int u = 0; u < NT; ++u) c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left - kGroup * group);
+    for (int u = 0; u < NT; ++u) c.w[u] = group_of(rw[u] + (int64_t)at * 64, whole ? kGroup : left - kGroup * group, (int64_t)at * 64 + 16 * group);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c.x[t][j] = piece_of<2>(rx[t] + (int64_t)at * 256 + 64 * j, whole ? 16 : 2 * (left - kGroup * j - 8 * group));
+      for (int j = 0; j < 4; ++j) {
+        const char* from = rx[t] + (int64_t)at * 256 + 64 * j;
+        c.x[t][j] = whole ? piece_of<2>(from, 16) : piece_at_end((const uint8_t*)from, 2 * (left - kGroup * j - 8 * group), (int64_t)at * 256 + 64 * j + 16 * group);
+      }
   };
   auto multiply = [&](const Chunk& c, const uint32_t* four, int pitch, uint32_t there, uint32_t missing) {       // four: scales of the chunk, of this lane's first row
     uint32_t four_of[NT];

@@ -389,3 +389,20 @@ def test_more_scales_than_a_workgroup_holds(m, n, k):
         b = W[at].long().cpu()
         w = values(torch.stack([b & 15, b >> 4], dim=2).view(b.shape[0], -1)[:, :k], S[at].long().cpu())
         check_product(Y[:, at], X.double().cpu(), w.t())
+
+
+@pytest.mark.parametrize("m", [1, 3, 20, 100, 300])
+@pytest.mark.parametrize("n,k", [(5, 1), (40, 2), (33, 9), (70, 29), (70, 30), (70, 31), (70, 33), (300, 61), (300, 95), (40, 127), (40, 129), (40, 135), (300, 257), (300, 259), (20, 286), (20, 287), (64, 2001)])
+def test_rows_that_end_anywhere(m, n, k):
+    """The last piece of a row comes from in front of its end where the row has so much; nothing in front of a short row is read (NaN there would show)."""
+    dev = need_gpu()
+    store = torch.full((n * ((k + 1) // 2) + 64,), 0xff, dtype=torch.uint8, device=dev)
+    W, S, w = four_bits(m + n + k, n, k, dev)
+    flat = store[48:48 + n * ((k + 1) // 2)].view(n, (k + 1) // 2)
+    flat.copy_(W.view(torch.uint8))
+    x = torch.full((m * k + 64,), float("nan"), dtype=torch.bfloat16, device=dev)
+    X = x[24:24 + m * k].view(m, k)
+    X.copy_(randn(k + m, m, k))
+    check_product(B.brsvd_linear_e2m1(X, flat.view(torch.float4_e2m1fn_x2), S), X.double().cpu(), w.t())
+    dY = randn(m, m, n).bfloat16().to(dev)
+    check_product(B.brsvd_linear_e2m1_backward(dY, flat.view(torch.float4_e2m1fn_x2), S, cols=k), dY.double().cpu(), w)
