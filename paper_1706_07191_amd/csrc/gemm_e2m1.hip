@@ -27,8 +27,8 @@ struct E2m1Args {
 // group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  A wave's next chunk is on its way while it multiplies one.
 // The scales of the workgroup's rows come first, whole rows of them, into LDS (where a contraction has more than there is room for, for as many chunks at a time): four bytes of 16
 // rows for each chunk, as they are used, take as many lines as W itself.
-// Bound by what a CU can have on its way: 1 x 4096 x 4096 5.5 us (8.9 MB; a launch is four), 24 x 20000 x 5000 23 us (58 MB fetched, 2.5 TB/s; 10.4 at a copy's rate): the 24
-// rows of X take three fifths of what a wave loads.  With X kept in registers while W streams past 27 us.
+// Bound by what a CU can have on its way: 1 x 4096 x 4096 5.0 us (8.9 MB; a launch is four), 1 x 20000 x 4096 10.8 us (43.5 MB, 4.0 TB/s), 24 x 20000 x 5000 19.5 us (58 MB fetched,
+// 3.0 TB/s; 10.4 at a copy's rate): the 24 rows of X, from the caches, are three fifths of what a wave loads.  Scales read where they are used: 22.6 us; X kept in registers while W streams past: 27.
 template <class El, int MT, int NT>
 __global__ void __launch_bounds__(512)
 k_rows_e2m1(const E2m1Args g) {
