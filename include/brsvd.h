@@ -393,7 +393,7 @@ uint64_t brsvd_head_workspace_bytes(int64_t tokens, int64_t vocab, int64_t dim, 
  *   brsvd_grad_clip:  y = x scale min(1, max_norm / *norm), rounded to out's dtype; max_norm >= 0
  * scale: what the gradients are to be multiplied by, such as one over the factor of a loss.  A *norm that is infinite or NaN clips
  * nothing: y = x scale.  out[i] has the shape of tensors[i], any dtype, and either its memory, type and ld or no number of any tensor's or
- * other result's; what shares one is refused.  A number that two of a list share counts twice in the norm.
+ * other result's, and no part of *norm; what shares one is refused.  A number that two of a list share counts twice in the norm.
  * workspace: at least brsvd_grad_norm_workspace_bytes of the same list. */
 typedef struct brsvd_tensor {
   void* data;

@@ -814,8 +814,8 @@ def brsvd_grad_norm(tensors, scale=1.0):
 def brsvd_grad_clip(tensors, norm, max_norm, scale=1.0, out=None):
     """Multiplies every tensor of a list by scale min(1, max_norm / norm), norm being that of brsvd_grad_norm with the same scale (one fp32 number on
     the device).  out: tensors of the same shapes, of any of the three types, that the results are written to instead of the tensors
-    themselves.  A norm that is infinite or NaN clips nothing.  Results that share memory with each other or with another
-    tensor are refused.  Returns the tensors written."""
+    themselves.  A norm that is infinite or NaN clips nothing.  Results that share memory with each other, with another
+    tensor or with norm are refused.  Returns the tensors written."""
     if not isinstance(norm, torch.Tensor) or norm.numel() != 1:
         raise TypeError("norm must be a CUDA tensor of one fp32 number")
     n = _dev(norm, torch.float32, "norm")

@@ -291,10 +291,10 @@ static bool apart(const Place& a, const Place& b) {
   const int64_t d = (int64_t)((b.lo - a.lo) % (uintptr_t)ld);
   return d >= a.width && d + b.width <= ld;
 }
-// Whether a number that one tensor is written to is another's too, whichever of its list; a tensor may be written to its own place.
-static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count) {
+// Whether a number that one tensor is written to is another's too, whichever of its list, or part of the norm, which all workgroups read; a tensor may be written to its own place.
+static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t count, const float* norm) {
   if (count == 0) return BRSVD_OK;
-  Place* places = new (std::nothrow) Place[2 * count];
+  Place* places = new (std::nothrow) Place[2 * count + 1];
   if (!places) return BRSVD_ERR_ALLOC;
   int64_t n = 0;
   bool good = true;
@@ -309,6 +309,7 @@ static int check_places(const brsvd_tensor* x, const brsvd_tensor* y, int64_t co
         places[n++] = place_of(x[i], false);
       }
     }
+    if (list == 1) places[n++] = Place{(uintptr_t)norm, (uintptr_t)norm + sizeof(float), sizeof(float), 0, false};
     auto before = [](const Place& a, const Place& b) { return a.lo < b.lo; };
     if (!std::is_sorted(places + first, places + n, before)) std::sort(places + first, places + n, before);
     if (list == 1) std::inplace_merge(places, places + first, places + n, before);
@@ -378,7 +379,7 @@ extern "C" int brsvd_grad_norm(const brsvd_tensor* tensors, int64_t count, float
 extern "C" int brsvd_grad_clip(const brsvd_tensor* tensors, const brsvd_tensor* out, int64_t count, float scale, float max_norm, const float* norm, void* stream) {
   const Pieces p = count > 0 && !out ? Pieces{0, -1} : check_list(tensors, out, count, kClipPiece);
   if (p.pieces < 0 || !norm || !(fabsf(scale) <= 3.402823466e38f) || !(max_norm >= 0.f)) return BRSVD_ERR_ARG;
-  BRSVD_TRY(check_places(tensors, out, count));
+  BRSVD_TRY(check_places(tensors, out, count, norm));
   if (p.pieces == 0) return BRSVD_OK;
   hipStream_t s = (hipStream_t)stream;
   in_lists(tensors, out, count, p.log_piece, [&](const TensorList& l, unsigned grid) {

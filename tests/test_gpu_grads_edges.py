@@ -1,0 +1,35 @@
+"""Clipping at the ends of what it takes: a norm beside, in front of and behind the memory that is written."""
+import pytest
+import torch
+
+import paper_1706_07191_amd as B
+from tests.gpu_util import need_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+def test_norm_beside_what_is_written():
+    """In the gaps of a matrix, in front of and behind a tensor, in one that is read only: taken, and none of them changes; inside a result: refused, and nothing is written."""
+    dev = need_gpu()
+    base = torch.full((10, 50), 4.0, device=dev)
+    part = base[:, 5:25]
+    flat = base.view(-1)
+    for where in (0, 4, 25, 49, 9 * 50 + 25):
+        base.fill_(4.0)
+        flat[where] = 8.0
+        assert B.brsvd_grad_clip([part], flat[where:where + 1], 2.0)[0] is part
+        want = torch.full((10, 50), 4.0, device=dev)
+        want[:, 5:25] = 1.0
+        want.view(-1)[where] = 8.0
+        assert torch.equal(base, want), where
+    x, y = torch.full((100,), 4.0, device=dev), torch.zeros(100, device=dev)
+    x[99] = 8.0
+    B.brsvd_grad_clip([x], x[99:], 2.0, out=[y])
+    assert bool((y[:99] == 1).all()) and y[99] == 2
+    for where in (0, 50, 99):
+        for kw in ({}, {"out": [x]}):
+            with pytest.raises(B.BrsvdError):
+                B.brsvd_grad_clip([y if kw else x], x[where:where + 1], 2.0, **kw)
+    with pytest.raises(B.BrsvdError):
+        B.brsvd_grad_clip([part], flat[5:6], 2.0)
+    assert bool((x[:99] == 4).all()) and x[99] == 8
