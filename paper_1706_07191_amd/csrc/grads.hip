@@ -215,12 +215,13 @@ k_grad_clip(const TensorList l, const float* __restrict__ norm, double scale, do
   // a norm that is no finite number says nothing about how long the gradients are: they are scaled alone
   const double f = n > max_norm && n <= 3.402823466e38 ? scale * (max_norm / n) : scale;
   if (f == 1.0 && l.x[mine.at] == l.y[mine.at]) return;
-  // in two factors, so that neither leaves fp32's range where the product does not
-  const double a = fabs(f) < 0x1p-100 ? f * 0x1p100 : fabs(f) > 0x1p100 ? f * 0x1p-100 : f;
-  const float f1 = (float)a, f2 = fabs(f) < 0x1p-100 ? 0x1p-100f : fabs(f) > 0x1p100 ? 0x1p100f : 1.f;
-  if (tx == BRSVD_DTYPE_F32) clip_into<BRSVD_DTYPE_F32>(l, mine, f1, f2);
-  else if (tx == BRSVD_DTYPE_BF16) clip_into<BRSVD_DTYPE_BF16>(l, mine, f1, f2);
-  else clip_into<BRSVD_DTYPE_F16>(l, mine, f1, f2);
+  // In two factors, so that neither leaves fp32's range where the product does not.  The second is a power of two.  The first is rounded to 24 bits as a normal number where
+  // a result is one: f below 2^-275 leaves fewer than three bits of the largest x.
+  const double size = fabs(f), f2 = size < 0x1p-200 ? 0x1p-149 : size < 0x1p-100 ? 0x1p-100 : size > 0x1p100 ? 0x1p100 : 1.0;
+  const float a = (float)(f / f2), b = (float)f2;
+  if (tx == BRSVD_DTYPE_F32) clip_into<BRSVD_DTYPE_F32>(l, mine, a, b);
+  else if (tx == BRSVD_DTYPE_BF16) clip_into<BRSVD_DTYPE_BF16>(l, mine, a, b);
+  else clip_into<BRSVD_DTYPE_F16>(l, mine, a, b);
 }
 
 // A tensor as kernels take it: rows next to each other are one long row.

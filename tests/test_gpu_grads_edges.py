@@ -4,6 +4,7 @@ import torch
 
 import paper_1706_07191_amd as B
 from tests.gpu_util import need_gpu
+from tests.test_gpu_grads import check_clipped
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +34,22 @@ def test_norm_beside_what_is_written():
     with pytest.raises(B.BrsvdError):
         B.brsvd_grad_clip([part], flat[5:6], 2.0)
     assert bool((x[:99] == 4).all()) and x[99] == 8
+
+
+@pytest.mark.parametrize("power_scale,power_most", [(-126, -110), (-120, -100), (-100, -126), (-126, -126), (-140, -130), (-149, -149), (-99, 0), (-101, 0), (-100, -1), (110, 3), (0, -110)])
+def test_factors_of_any_size(power_scale, power_most):
+    """scale max_norm / norm from 2^-400 to 2^110, on numbers whose results are normal ones where there are such: the factor keeps its 24 bits."""
+    dev = need_gpu()
+    scale, most = 1.375 * 2.0 ** power_scale if power_scale > -149 else 2.0 ** -149, 1.5 * 2.0 ** power_most if power_most > -149 else 2.0 ** -149
+    x = (1 + torch.rand(1000, generator=torch.Generator().manual_seed(1))) * 2.0 ** (-130 if power_scale > 0 else 110)
+    x[::7] = 1.75 * 2.0 ** (-149 if power_scale > 0 else 127)
+    tensors = [x.to(dev), x.bfloat16().to(dev)]
+    out = [torch.empty(1000, device=dev) for _ in tensors]
+    norm = B.brsvd_grad_norm(tensors, scale=scale)
+    B.brsvd_grad_clip(tensors, norm, most, scale=scale, out=out)
+    check_clipped(out, tensors, float(norm), most, scale)
+    # and with a norm that has nothing to do with them
+    for power in (-60, 0, 120):
+        norm = torch.full((1,), 1.25 * 2.0 ** power, device=dev)
+        B.brsvd_grad_clip(tensors, norm, most, scale=scale, out=out)
+        check_clipped(out, tensors, float(norm), most, scale)
