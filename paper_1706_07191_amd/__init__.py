@@ -792,7 +792,12 @@ def _tensors(*lists):
     """A list of tensors as an array of brsvd_tensor; two lists, whose numbers have to be in the same order, as two."""
     global _tables
     if _tables is None:
-        from ._lists import tables as _tables          # needs torch
+        import torch
+
+        from . import _lists               # needs torch
+        if _lists.torch_version != torch.__version__:
+            raise ImportError(f"_lists.so was built for torch {_lists.torch_version}, this is {torch.__version__}: python -m paper_1706_07191_amd.build")
+        _tables = _lists.tables
     return _tables(*lists)
 
 

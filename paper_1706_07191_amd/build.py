@@ -56,14 +56,36 @@ def _headers():
 
 
 def _lists_command():
+    """The command that builds the reader of lists, and what of torch its result is bound to."""
     import sysconfig
 
     import torch
     home = os.path.dirname(torch.__file__)
-    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
-            "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
-            "-isystem", sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"), os.path.join(CSRC, "lists.cpp"), "-o", LISTS,
-            "-L" + os.path.join(home, "lib"), "-ltorch_python", "-lc10"]
+    abi = int(torch.compiled_with_cxx11_abi())
+    command = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % abi, '-DBRSVD_TORCH_VERSION="%s"' % torch.__version__,
+               "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               "-isystem", sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"), os.path.join(CSRC, "lists.cpp"), "-o", LISTS,
+               "-L" + os.path.join(home, "lib"), "-ltorch_python", "-lc10"]
+    return command, "torch %s, C++11 ABI %d" % (torch.__version__, abi)
+
+
+def _build_lists(force: bool) -> str:
+    """Builds _lists.so where it is missing, older than its sources or bound to another torch, which the file beside the objects says.  Without torch there are no lists to read."""
+    try:
+        command, bound = _lists_command()
+    except ImportError:
+        return "torch cannot be imported: _lists.so, which the calls on lists of tensors need, is not built"
+    stamp = os.path.join(OBJ, "_lists.torch")
+    if not force and os.path.exists(stamp) and not _stale(LISTS, [os.path.join(CSRC, "lists.cpp"), os.path.join(ROOT, "include", "brsvd.h")]):
+        with open(stamp) as f:
+            if f.read() == bound:
+                return ""
+    if os.path.exists(stamp):
+        os.remove(stamp)
+    out = _run(command)
+    with open(stamp, "w") as f:
+        f.write(bound)
+    return out
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -78,15 +100,17 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(o)
         if force or _stale(o, [s] + headers):
             jobs.append([hipcc] + FLAGS + ["-c", s, "-o", o])
-    lists = [_lists_command()] if force or _stale(LISTS, [os.path.join(CSRC, "lists.cpp"), os.path.join(ROOT, "include", "brsvd.h")]) else []
-    with ThreadPoolExecutor(max_workers=min(6, max(1, len(jobs + lists)))) as ex:
-        for out in ex.map(_run, jobs + lists):
+    with ThreadPoolExecutor(max_workers=min(6, max(1, len(jobs)))) as ex:
+        for out in ex.map(_run, jobs):
             if verbose and out.strip():
                 print(out)
     if force or jobs or _stale(LIB, objs):
         out = _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs)
         if verbose and out.strip():
             print(out)
+    out = _build_lists(force)            # the library is there whatever becomes of it
+    if out.startswith("torch cannot") or verbose and out.strip():
+        print(out)
     return LIB
 
 

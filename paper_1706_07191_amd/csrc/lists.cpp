@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <array>
+#include <cstring>
 #include <exception>
 
 #include "brsvd.h"
@@ -106,4 +107,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods, nul
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__lists() { return PyModule_Create(&module); }
+// torch_version: the torch whose objects it reads; another one's may be laid out differently.
+PyMODINIT_FUNC PyInit__lists() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", BRSVD_TORCH_VERSION) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
