@@ -294,8 +294,8 @@ uint64_t brsvd_linear_e4m3_scratch_bytes(int64_t m, int64_t n, int64_t k, int32_
  * ceil(cols/32), dense.  Behind a row's last number the upper half of a byte is no part of it: written as zero, never read as a number.
  *
  * brsvd_quantize_e2m1: Q = round(X / S), S the least power of two >= 2^-126 for which no number of the group exceeds 6 S (1 for a
- * group of zeros), to nearest, ties to an even code.  A group with an infinity or a NaN gets the scale NaN.  X: rows x cols of
- * dtype BRSVD_DTYPE_F32, _BF16 or _F16.
+ * group of zeros), to nearest, ties to an even code.  A group with an infinity or a NaN gets the scale NaN.  Finite numbers from 3.5 * 2^126 on become
+ * 4 S = 2^128, the nearest that there is, which comes back as infinity and enters products as one.  X: rows x cols of dtype BRSVD_DTYPE_F32, _BF16 or _F16.
  * brsvd_dequantize_e2m1: X = Q S, rounded to dtype (a group of scale NaN: NaN). */
 int brsvd_quantize_e2m1(const void* X, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype, uint8_t* Q,
                         int64_t ldq, uint8_t* S, void* stream);
@@ -304,8 +304,9 @@ int brsvd_dequantize_e2m1(const uint8_t* Q, int64_t ldq, const uint8_t* S, int64
 
 /* Y (m x n) = X W^T with X m x k of dtype BF16 or F16 (Y has the same type) and W n x k in 4 bits, as brsvd_quantize_e2m1
  * lays it out; and the gradient of X, dX (m x k) = dY W.  X is taken as it is.  A number of W times its scale is taken in X's type, as
- * brsvd_dequantize_e2m1 rounds it: nothing is lost with BF16 from 2^-133 on and with F16 from 2^-24 on.  Products are exact, sums are fp32, the
- * result is rounded once.  Scales are any bytes.
+ * brsvd_dequantize_e2m1 rounds it.  BF16 holds every one, from 2^-128 to 1.5 * 2^127; from 2^128 on they are infinite.  F16 holds those from 2^-23 to
+ * 49152; smaller ones are rounded to multiples of 2^-24, from 2^16 on they are infinite.  Products are exact, sums are fp32, the result is rounded once.
+ * Scales are any bytes.
  * scratch: brsvd_linear_e2m1_scratch_bytes of the same sizes; aligned = 1 where rows of X (dY) and W all begin at 16-byte
  * addresses (address and leading dimension), 0 is enough always.  0 bytes: NULL will do, as for up to 16 rows of X. */
 int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW,

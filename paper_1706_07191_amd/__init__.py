@@ -672,7 +672,7 @@ def _columns(Q, cols):
 def brsvd_quantize_e2m1(X):
     """X (rows, cols) CUDA, fp32, bf16 or fp16, as e2m1 numbers Q (float4_e2m1fn_x2, (rows, ceil(cols/2)): two in a byte, the first in its
     lower half; rows 16- or 128-byte aligned) and power-of-two scales S (float8_e8m0fnu), one for each 32 numbers of a row.  A group with an
-    infinity or a NaN becomes NaN.  Returns (Q, S)."""
+    infinity or a NaN becomes NaN; finite numbers from 3.5 * 2^126 on stand for 2^128 and come back infinite.  Returns (Q, S)."""
     dt = _model_dtype(X.dtype, "X")
     x, ldx = _rows(X, X.dtype, None, "X")
     rows, cols = X.shape

@@ -20,7 +20,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
-// The two numbers of byte B of w times the scale, rounded to the type (bf16 holds all of them from 2^-127 to 6 * 2^125)
+// The two numbers of byte B of w times the scale, rounded to the type: bf16 holds all of them, from 2^-128 to 1.5 * 2^127, fp16 those from 2^-23 to 49152; from 2^128 and 2^16 on
+// they are infinite
 template <class El, int B>
 __device__ __forceinline__ uint32_t two_e2m1(uint32_t w, float scale) {
   if constexpr (__is_same(El, Bf16)) return __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));

@@ -1,10 +1,11 @@
 // Products with a matrix W (n x k) in 4 bits with a scale for each 32 numbers of a row, and 16-bit activations:
 //   Y = X W^T (X m x k),    dX = dY W (dY m x n)
-// A number of W times its scale is a number of the activations' type (bf16 holds every one, fp16 those from 2^-24 to 65504), so the 16-bit matrix cores multiply
+// A number of W times its scale is a number of the activations' type (bf16 holds every one, fp16 those from 2^-23 to 49152), so the 16-bit matrix cores multiply
 // exactly and add in fp32; Y is rounded once.  The conversion takes the scale with it: two numbers an instruction.  W is the instruction's first operand, a
 // lane has four neighbouring columns of Y for one row of X.
 //
-// k_rows_e2m1: for few rows of X, bound by the read of W.  k_tiles_e2m1: for many, bound by the matrix cores; W's numbers are made on their way into LDS.
+// k_rows_e2m1: for few rows of X, bound by the read of W.  k_tiles_e2m1: for many, bound by the matrix cores; for Y, W's numbers are made where they are multiplied, for dX on
+// their way into the tile that they are multiplied from.
 #include "e2m1.h"
 
 namespace brsvd {
