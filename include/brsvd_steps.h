@@ -93,6 +93,15 @@ int brsvd_gemm_is_split(int32_t which, const void* A, int64_t lda, int64_t rows,
  * matrix products for one in fp32) or, for long contractions, two scaled fp16 ones (three).  Host-only. */
 int brsvd_gemm_split_parts(int32_t which, int64_t rows, int64_t n, int32_t l);
 
+/* How a product with 4-bit weights (brsvd_linear_e2m1 and, with backward = 1, its gradient) and the products of a gated feed-forward
+ * block (which = 0: brsvd_glu_forward, 1: dX, 2: dWg and dWu) go to the GPU, whatever their type and alignment (host-only, no GPU call):
+ * for checking that every way there is has a test, and for reading profiles.  out8 (HOST, 8 ints) = {1 for few rows, which
+ * go from memory to registers, 0 for tiles; of few rows: 16-row tiles of X in a wave, and 16-row tiles of W (of each of Wg and Wu); of tiles: those along the columns (256 wide, of
+ * the forward gated block 128), how many of these are 256 rows high, the others' rows / 64 (the two sizes are launches of their own), parts that the contraction is cut into,
+ * 64-number steps of a part}; what does not apply is 0.  BRSVD_ERR_ARG for sizes that the calls refuse or that have no numbers. */
+int brsvd_linear_e2m1_plan(int64_t m, int64_t n, int64_t k, int32_t backward, int32_t* out8);
+int brsvd_glu_plan(int32_t which, int64_t tokens, int64_t dim, int64_t width, int32_t* out8);
+
 /* Measurement helper, not a step of the method: measured peaks of the device, to put next to the
  * published ones in roofline figures.  One timed launch after one warm-up launch; synchronous.
  *   kind 0: streaming read of `amount` bytes from buf (at least `amount` bytes);

@@ -82,7 +82,7 @@ EXPORTS = ["brsvd_workspace_bytes", "brsvd_create", "brsvd_run", "brsvd_run_f64"
            "brsvd_destroy", "brsvd_status_string"]
 STEP_EXPORTS = ["brsvd_gemm_an", "brsvd_gemm_at", "brsvd_gemm_scratch_bytes", "brsvd_gemm_an_f64",
                 "brsvd_gemm_at_f64", "brsvd_gemm_scratch_bytes_f64", "brsvd_orth", "brsvd_orth_scratch_bytes",
-                "brsvd_small_svd", "brsvd_small_svd_scratch_bytes", "brsvd_small_svd_static", "brsvd_gemm_plan",
+                "brsvd_small_svd", "brsvd_small_svd_scratch_bytes", "brsvd_small_svd_static", "brsvd_gemm_plan", "brsvd_linear_e2m1_plan", "brsvd_glu_plan",
                 "brsvd_gemm_is_split", "brsvd_gemm_split_parts", "brsvd_probe"]
 
 _lib = None
@@ -122,6 +122,8 @@ def lib() -> C.CDLL:
     L.brsvd_philox_normal_f64.argtypes = L.brsvd_philox_normal.argtypes
     L.brsvd_probe.argtypes = [i32, vp, u64, C.POINTER(dbl), C.POINTER(dbl), vp]
     L.brsvd_gemm_plan.argtypes = [i32, i64, i64, i32, i64, i32, C.POINTER(i32)]
+    L.brsvd_linear_e2m1_plan.argtypes = [i64, i64, i64, i32, C.POINTER(i32)]
+    L.brsvd_glu_plan.argtypes = [i32, i64, i64, i64, C.POINTER(i32)]
     L.brsvd_gemm_is_split.argtypes = [i32, vp, i64, i64, i64, i32, i32]
     L.brsvd_gemm_split_parts.argtypes = [i32, i64, i64, i32]
     L.brsvd_destroy.argtypes = [vp]
@@ -285,6 +287,20 @@ def brsvd_gemm_plan(which, rows, n, l, block_rows=0, dtype=BRSVD_DTYPE_F32):
     """The launch plan of gemm_an (which = 0) or gemm_at (which = 1) as a list of 12 ints (see brsvd.h)."""
     out = (C.c_int32 * 12)()
     _check(lib().brsvd_gemm_plan(which, rows, n, l, block_rows, dtype, out), "brsvd_gemm_plan")
+    return list(out)
+
+
+def brsvd_linear_e2m1_plan(m, n, k, backward=False):
+    """How X W^T (or its gradient) with X m x k and W n x k in 4 bits goes to the GPU, as a list of 8 ints (see brsvd_steps.h)."""
+    out = (C.c_int32 * 8)()
+    _check(lib().brsvd_linear_e2m1_plan(m, n, k, backward, out), "brsvd_linear_e2m1_plan")
+    return list(out)
+
+
+def brsvd_glu_plan(which, tokens, dim, width):
+    """How a gated block's products (which = 0: forward, 1: dX, 2: dWg and dWu) go to the GPU, as a list of 8 ints (see brsvd_steps.h)."""
+    out = (C.c_int32 * 8)()
+    _check(lib().brsvd_glu_plan(which, tokens, dim, width, out), "brsvd_glu_plan")
     return list(out)
 
 

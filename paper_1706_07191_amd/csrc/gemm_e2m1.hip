@@ -6,6 +6,7 @@
 //
 // k_rows_e2m1: for few rows of X, bound by the read of W.  k_tiles_e2m1: for many, bound by the matrix cores; for Y, W's numbers are made where they are multiplied, for dX on
 // their way into the tile that they are multiplied from.
+#include "brsvd_steps.h"
 #include "e2m1.h"
 
 namespace brsvd {
@@ -210,6 +211,8 @@ static int rows_in_wave(int64_t m, int64_t n) {
   }
   return best;
 }
+// 16-row tiles of X
+static int row_tiles(int64_t m) { return (int)ceil_div(m, 16); }
 struct E2m1Plan {
   bool rows;                    // k_rows_e2m1
   TilePlan tiles;
@@ -267,10 +270,12 @@ static int product_e2m1(E2m1Args g, const E2m1Plan& p, int64_t wrows, int64_t wb
   void* C = g.C;
   const int64_t ldc = g.ldc;
   if (p.rows) {
-    if (g.X.n <= 16) launch_rows<El, 1>(g, stream);
-    else if (g.X.n <= 32) launch_rows<El, 2>(g, stream);
-    else if (g.X.n <= 48) launch_rows<El, 3>(g, stream);
-    else launch_rows<El, 4>(g, stream);
+    switch (row_tiles(g.X.n)) {
+      case 1: launch_rows<El, 1>(g, stream); break;
+      case 2: launch_rows<El, 2>(g, stream); break;
+      case 3: launch_rows<El, 3>(g, stream); break;
+      default: launch_rows<El, 4>(g, stream);
+    }
   } else {
     if (!aligned_pieces(g.X.base, g.X.ld)) {
       const int64_t pitch = line_pitch(2 * g.k);
@@ -352,4 +357,11 @@ extern "C" int brsvd_linear_e2m1(const void* X, int64_t ldx, int32_t dtype, cons
 extern "C" int brsvd_linear_e2m1_backward(const void* dY, int64_t lddy, int32_t dtype, const uint8_t* W, int64_t ldw, const uint8_t* SW, int64_t m, int64_t n, int64_t k,
                                           void* dX, int64_t lddx, void* scratch, uint64_t scratch_bytes, void* stream) {
   return call_e2m1(dY, lddy, n, dtype, W, ldw, SW, m, n, k, dX, lddx, k, true, scratch, scratch_bytes, (hipStream_t)stream);
+}
+
+extern "C" int brsvd_linear_e2m1_plan(int64_t m, int64_t n, int64_t k, int32_t backward, int32_t* out8) {
+  if (!out8 || !e2m1_sizes(m, n, k, backward != 0) || m == 0 || n == 0 || k == 0) return BRSVD_ERR_ARG;
+  const E2m1Plan p = e2m1_plan(m, n, k, true, backward != 0);
+  p.rows ? describe_rows(row_tiles(m), rows_in_wave(m, n), out8) : describe_plan(p.tiles, out8);
+  return BRSVD_OK;
 }

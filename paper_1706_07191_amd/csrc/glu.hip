@@ -3,6 +3,7 @@
 //   dG = dH U a'(G),  dU = dH a(G),   dX = dG Wg + dU Wu,   dWg = dG^T X,  dWu = dU^T X
 // Forward: one kernel.  A tile has 128 columns of G and the same of U, 64 of each in a wave, so that a lane holds both numbers of a product; sums are fp32 until H (and G, U
 // where they are kept for the backward pass) is rounded.  Backward: dG and dU are formed once, in 16 bits, and multiplied: dX is one sum over both.
+#include "brsvd_steps.h"
 #include "tile.h"
 
 namespace brsvd {
@@ -505,6 +506,9 @@ static constexpr int kStep[3] = {60, 80, 147};        // 1/100 us a step, see ti
 // way round 64 x 8000 x 1000 17.6 and 12.7; at 32 both are alike (8000 x 4096 33 and 33) or these are behind (4096 x 4096 22 and 17).
 static bool few_tokens(int64_t tokens, int64_t dim, int64_t width) { return tokens <= 32 || (tokens <= 64 && ceil_div(width, 16 * 256) * dim <= 3000); }
 
+// 16-row tiles of X that a wave has of few tokens
+static int token_tiles(int64_t tokens) { return tokens <= 16 ? 1 : tokens <= 32 ? 2 : 4; }
+
 struct GluPlan {
   TilePlan forward, dx, dw;
   int64_t pitch_x, pitch_w, half;                                            // bytes; half: of a row of dG or dU
@@ -575,8 +579,9 @@ static int glu_forward(const GluCall& c, const GluPlan& p, bool aligned, char* w
     g.W = PairOperand{(const char*)c.Wg, (const char*)c.Wu, 2 * c.ldwg, 2 * c.ldwu, c.width};
     g.X = Operand{(const char*)c.X, 2 * c.ldx, c.tokens};
     const dim3 grid((unsigned)ceil_div(c.width, 16));
-    if (c.tokens <= 16) hipLaunchKernelGGL((k_glu_rows<El, 1, 4, 8>), grid, dim3(512), 0, stream, g);
-    else if (c.tokens <= 32) hipLaunchKernelGGL((k_glu_rows<El, 2, 2, 8>), grid, dim3(512), 0, stream, g);
+    const int mt = token_tiles(c.tokens);
+    if (mt == 1) hipLaunchKernelGGL((k_glu_rows<El, 1, 4, 8>), grid, dim3(512), 0, stream, g);
+    else if (mt == 2) hipLaunchKernelGGL((k_glu_rows<El, 2, 2, 8>), grid, dim3(512), 0, stream, g);
     else hipLaunchKernelGGL((k_glu_rows<El, 4, 2, 8>), grid, dim3(512), 0, stream, g);
   } else {
     g.X = laid_out(c.X, c.ldx, c.tokens, c.dim, aligned, ws + p.x, p.pitch_x, stream);
@@ -765,4 +770,12 @@ extern "C" int brsvd_glu_backward(const void* X, int64_t ldx, const void* Wg, in
   char* ws = (char*)workspace;
   return dtype == BRSVD_DTYPE_BF16 ? glu_backward<Bf16>(c, p, aligned, ws, a, dX, lddx, dWg, lddwg, dWu, lddwu, s)
                                    : glu_backward<Fp16>(c, p, aligned, ws, a, dX, lddx, dWg, lddwg, dWu, lddwu, s);
+}
+
+extern "C" int brsvd_glu_plan(int32_t which, int64_t tokens, int64_t dim, int64_t width, int32_t* out8) {
+  if (!out8 || which < 0 || which > 2 || !glu_sizes(tokens, dim, width) || tokens == 0 || dim == 0 || width == 0) return BRSVD_ERR_ARG;
+  const GluPlan p = glu_plan(tokens, dim, width, true);
+  if (which == 0 && few_tokens(tokens, dim, width)) describe_rows(token_tiles(tokens), 1, out8);
+  else describe_plan(which == 0 ? p.forward : which == 1 ? p.dx : p.dw, out8);
+  return BRSVD_OK;
 }

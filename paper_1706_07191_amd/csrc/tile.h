@@ -627,4 +627,14 @@ inline TilePlan tile_plan(int64_t p_tiles, int64_t q, int64_t steps, int both, i
   return best;
 }
 
+// What the plan queries say of it
+inline void describe_plan(const TilePlan& t, int32_t* out8) {
+  const int32_t all = (int32_t)t.tiles, large = (int32_t)t.large, nq = t.large < t.tiles ? t.nq : 0;
+  const int32_t plan[8] = {0, 0, 0, all, large, nq, t.splits, (int32_t)(t.per_split / 64)};
+  for (int i = 0; i < 8; ++i) out8[i] = plan[i];
+}
+inline void describe_rows(int mt, int nt, int32_t* out8) {
+  for (int i = 0; i < 8; ++i) out8[i] = i == 0 ? 1 : i == 1 ? mt : i == 2 ? nt : 0;
+}
+
 }  // namespace brsvd
