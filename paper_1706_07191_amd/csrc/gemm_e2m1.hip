@@ -26,11 +26,12 @@ struct E2m1Args {
 
 // Up to 16 MT rows of X.  The eight waves of a workgroup share 16 NT rows of W and take chunks of 128 numbers of the contraction in turn; their sums are added
 // through LDS in wave order.  A lane reads one group of a chunk, 16 bytes; lanes then exchange words, so that an instruction takes one
-// group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  A wave's next chunk is on its way while it multiplies one.
+// group of all rows.  X, which all workgroups read and the caches hold, comes in pieces of 64 bytes of a row.  While a wave multiplies a chunk, those of the other seven are on their way.
 // The scales of the workgroup's rows come first, whole rows of them, into LDS (where a contraction has more than there is room for, for as many chunks at a time): four bytes of 16
 // rows for each chunk, as they are used, take as many lines as W itself.
-// Bound by what a CU can have on its way: 1 x 4096 x 4096 5.0 us (8.9 MB; a launch is four), 1 x 20000 x 4096 10.8 us (43.5 MB, 4.0 TB/s), 24 x 20000 x 5000 19.5 us (58 MB fetched,
-// 3.0 TB/s; 10.4 at a copy's rate): the 24 rows of X, from the caches, are three fifths of what a wave loads.  Scales read where they are used: 22.6 us; X kept in registers while W streams past: 27.
+// Bound by the pace of a wave's loads, the next chunk's being sent once the last one is multiplied: 1 x 4096 x 4096 5.0 us (8.9 MB; a launch is four), 1 x 20000 x 4096 10.8 us (43.5 MB,
+// 4.0 TB/s), 24 x 20000 x 5000 19.5 us (58 MB fetched, 3.0 TB/s; 10.4 at a copy's rate): the 24 rows of X, which come from the caches with each 80 rows of W, are three fifths of what a wave
+// loads, 12 bytes a clock and CU in all.  Scales read where they are used: 22.6 us; X kept in registers while W streams past: 27.
 template <class El, int MT, int NT>
 __global__ void __launch_bounds__(512)
 k_rows_e2m1(const E2m1Args g) {

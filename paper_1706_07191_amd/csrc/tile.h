@@ -599,7 +599,7 @@ inline int64_t large_tiles(int64_t np, int64_t q256, int64_t q128, int64_t steps
 // How a product of `q` rows and p_tiles tiles of 256 columns, `both` times, over `steps` steps is cut into tiles and parts of its contraction: by what a tile of 64, 128 or
 // 256 rows takes for a step on a CU of its own (`step`, in 1/100 us), 5 us for a tile's start and end and for a launch, 3 and 4.5 TB/s for the parts and their join.  244 plans of 26
 // products of 4-bit weights, from one tile to 500, meet this within 7 % on average.  So a contraction is cut where CUs would have nothing to do: 300 x 2000 over 8192 31 us in
-// 8 parts, 124 in one; and tiles are small where they are few: 300 x 8192 over 2000 32 us in tiles of 64, 36 in 128 and two parts.
+// ten parts, 124 in one; and tiles are small where they are few: 300 x 8192 over 2000 32 us in tiles of 64, 36 in 128 and two parts.
 struct TilePlan {
   int nq;                    // rows of a tile, in 64, beside the large ones
   int64_t tiles, large;      // along the columns: all, those in tiles of 256 rows
